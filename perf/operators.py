@@ -299,7 +299,7 @@ def _run_plan(c, s):
     fits = need <= s["table"].shape[1]
     new = torch.where(live & fits, (need - held).clamp(min=0), 0)
     upto = torch.cumsum(new, 0)
-    given = live & fits & (upto <= ends[1] - ends[0])
+    given = live & fits & ((new == 0) | (upto <= ends[1] - ends[0]))
     new = torch.where(given, new, 0)
     back = torch.where(live, 0, held)
     j = torch.arange(s["table"].shape[1], device="cuda")
