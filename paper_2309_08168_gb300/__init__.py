@@ -2,8 +2,8 @@
 
 Argument marshalling only: every step of the decode path runs in the CUDA
 library (csrc/, built for sm_103a by build.py).  The functions keep the C
-ABI's names (include/ssd.h).  Importing this module fails loudly when the
-library has not been built; there is no fallback path.
+ABI's names (include/ssd.h, include/ssd_ops.h).  Importing this module fails
+loudly when the library has not been built; there is no fallback path.
 """
 from __future__ import annotations
 
@@ -29,6 +29,13 @@ SSD_SAMPLE = 1
 EXPORTS = ("ssd_create", "ssd_set_skip", "ssd_set_sampling", "ssd_set_draft_exit", "ssd_prefill", "ssd_generate",
            "ssd_debug_forward", "ssd_debug_spec_accept", "ssd_debug_time_forward", "ssd_destroy",
            "ssd_last_error", "ssd_linear_noalloc", "ssd_debug_trace_forward", "ssd_debug_stall_barrier")
+
+# every symbol include/ssd_ops.h declares
+OPERATOR_EXPORTS = ("ssd_tree_plan", "ssd_rope_init", "ssd_rope_kv", "ssd_tree_attention",
+                    "ssd_tree_attention_workspace", "ssd_tree_commit")
+SSD_F32, SSD_F16, SSD_BF16 = 0, 1, 2
+SSD_STATUS_PAGES, SSD_STATUS_TABLE, SSD_STATUS_PARENT, SSD_STATUS_TIMEOUT = 1, 2, 4, 8
+SSD_ROPE_PLAIN, SSD_ROPE_LINEAR, SSD_ROPE_BY_PARTS = 0, 1, 2
 
 
 class ssd_config(ctypes.Structure):
@@ -58,6 +65,22 @@ class ssd_stats(ctypes.Structure):
                 "emitted": self.emitted, "accept_rate": self.accept_rate, "hist": list(self.hist),
                 "draft_ms": self.draft_ms, "verify_ms": self.verify_ms, "total_ms": self.total_ms,
                 "kernel_launches": self.kernel_launches, "gamma": self.gamma}
+
+
+class ssd_pages(ctypes.Structure):
+    _fields_ = [("k", _VP), ("v", _VP)] + \
+               [(n, ctypes.c_int) for n in ("dtype", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim")] + \
+               [(n, ctypes.c_int64) for n in ("layer_stride", "page_stride", "head_stride", "pos_stride")]
+
+
+class ssd_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_requests", "n_rows", "max_rows", "max_blocks")] + \
+               [("row_start", _VP), ("lens", _VP), ("block_table", _VP)]
+
+
+class ssd_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_float),
+                ("turns", ctypes.c_uint64 * 64)]
 
 
 class SSDError(RuntimeError):
@@ -90,6 +113,15 @@ def _load():
     lib.ssd_debug_stall_barrier.restype = ctypes.c_int
     lib.ssd_linear_noalloc.argtypes = [_VP, _VP, _VP, ctypes.c_int, ctypes.c_int, ctypes.c_int, _VP]
     lib.ssd_linear_noalloc.restype = ctypes.c_int
+    I, L, BP, PP, RP = ctypes.c_int, ctypes.c_int64, ctypes.POINTER(ssd_batch), ctypes.POINTER(ssd_pages), ctypes.POINTER(ssd_rope)
+    lib.ssd_tree_plan.argtypes = [BP, I, I] + [_VP] * 9 + [I, _VP, _VP]
+    lib.ssd_rope_init.argtypes = [I, I, I] + [ctypes.c_double] * 6 + [RP]
+    lib.ssd_rope_kv.argtypes = [PP, I, RP, I, I, I, _VP, L, _VP, L, _VP, L, _VP, _VP, _VP, L, _VP]
+    lib.ssd_tree_attention.argtypes = [BP, PP, I, I, I, _VP, L, _VP, I, ctypes.c_float, _VP, L, _VP, ctypes.c_size_t, _VP, _VP]
+    lib.ssd_tree_attention_workspace.argtypes = [I, ctypes.POINTER(ctypes.c_size_t)]
+    lib.ssd_tree_commit.argtypes = [BP, PP] + [_VP] * 9
+    for n in OPERATOR_EXPORTS:
+        getattr(lib, n).restype = ctypes.c_int
     lib.ssd_destroy.argtypes = [H]
     lib.ssd_destroy.restype = None
     lib.ssd_last_error.argtypes = []
@@ -221,6 +253,137 @@ def ssd_debug_trace_forward(h: int, draft: bool, rows: int, detail_op: int = -1)
                                        ct.ctypes.data if detail else None, max_ctas, ctypes.addressof(n_ctas)))
     ops = [(OP_NAMES[ty[i]], float(us[i])) for i in range(n.value)]
     return (ops, ut, ct[:n_ctas.value]) if detail else ops
+
+
+# -- operators on the caller's device tensors (include/ssd_ops.h) -------------
+
+_ROW_TYPES = {"torch.float32": SSD_F32, "torch.float16": SSD_F16, "torch.bfloat16": SSD_BF16}
+
+
+def _refuse(what: str):
+    raise SSDError(SSD_ERR_INVALID_ARG, what)
+
+
+def _dev(t, what: str, dtype: str, device, shape=None):
+    """Address of a contiguous CUDA tensor of this type (and shape) on `device`, or None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device != device or str(t.dtype) != dtype or not t.is_contiguous():
+        _refuse(f"{what}: a contiguous {dtype} tensor on {device} is wanted")
+    if shape is not None and tuple(t.shape) != shape:
+        _refuse(f"{what}: shape {tuple(t.shape)}, {shape} is wanted")
+    return t.data_ptr()
+
+
+def _rows(t, what: str, device, dtype, n_rows: int, heads: int | None, hd: int):
+    """(address, row stride) of rows [row][head][dim] whose heads lie behind one another."""
+    if not t.is_cuda or t.device != device or (dtype is not None and t.dtype != dtype) or str(t.dtype) not in _ROW_TYPES:
+        _refuse(f"{what}: fp32, fp16 or bf16 rows on {device} are wanted, all of one type")
+    if t.dim() != 3 or t.shape[0] != n_rows or t.shape[2] != hd or (heads is not None and t.shape[1] != heads):
+        _refuse(f"{what}: shape {tuple(t.shape)}, ({n_rows}, {heads if heads is not None else 'heads'}, {hd}) is wanted")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != hd):
+        _refuse(f"{what}: the heads of a row must lie behind one another")
+    return t.data_ptr(), t.stride(0) if n_rows > 1 else t.shape[1] * hd
+
+
+class PagedKV:
+    """A paged cache: k and v are fp16 or bf16 CUDA tensors indexed [layer][page][kv_head][position in page][dim],
+    of equal shape and strides (any memory order in which dims are adjacent).  Keeps the tensors."""
+
+    def __init__(self, k, v):
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device or not k.is_cuda:
+            _refuse("k and v: CUDA tensors [layer][page][kv_head][position][dim] of one shape, type and memory order are wanted")
+        if str(k.dtype) not in ("torch.float16", "torch.bfloat16") or k.stride(4) != 1:
+            _refuse("k and v: fp16 or bf16 with adjacent dims are wanted")
+        self.k, self.v, self.device = k, v, k.device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.struct = ssd_pages(k.data_ptr(), v.data_ptr(), _ROW_TYPES[str(k.dtype)], *(k.shape[i] for i in (0, 1, 2, 3, 4)), *k.stride()[:4])
+
+
+class TreeBatch:
+    """A round's rows: row_start int32 [n + 1], lens int32 [n] and block_table int32 [n][max_blocks] on one device.
+    Keeps the tensors; their contents may change between calls."""
+
+    def __init__(self, row_start, lens, block_table, n_rows: int, max_rows: int):
+        n, self.device = lens.numel(), lens.device
+        if block_table.dim() != 2:
+            _refuse("block_table: [request][block] is wanted")
+        self.keep = (row_start, lens, block_table)
+        self.n_requests, self.n_rows, self.max_rows, self.max_blocks = n, n_rows, max_rows, block_table.shape[1]
+        self.struct = ssd_batch(n, n_rows, max_rows, self.max_blocks, _dev(row_start, "row_start", "torch.int32", lens.device, (n + 1,)),
+                                _dev(lens, "lens", "torch.int32", lens.device, (n,)),
+                                _dev(block_table, "block_table", "torch.int32", lens.device, (n, self.max_blocks)))
+
+
+def ssd_tree_plan(batch: TreeBatch, page_size: int, n_pages: int, parents, held, held_out, ring, ends, ends_out, slots,
+                  positions, masks=None, status=None, cuda_stream: int | None = None) -> None:
+    """Pages, slots, positions and ancestor masks of a round.  parents int32 [n_rows] or None (chains); held, held_out
+    int32 [n]; ring int32 [n_pages]; ends, ends_out int64 [2]; slots, positions int32 [n_rows]; masks int64 [n_rows][words]
+    (bit patterns) with parents; status int32 [1] or None."""
+    d, n, r, i32 = batch.device, batch.n_requests, batch.n_rows, "torch.int32"
+    words = masks.shape[1] if masks is not None and masks.dim() == 2 else 0
+    _check(lib.ssd_tree_plan(batch.struct, page_size, n_pages, _dev(parents, "parents", i32, d, (r,)), _dev(held, "held", i32, d, (n,)),
+                             _dev(held_out, "held_out", i32, d, (n,)), _dev(ring, "ring", i32, d, (n_pages,)),
+                             _dev(ends, "ends", "torch.int64", d, (2,)), _dev(ends_out, "ends_out", "torch.int64", d, (2,)),
+                             _dev(slots, "slots", i32, d, (r,)), _dev(positions, "positions", i32, d, (r,)),
+                             _dev(masks, "masks", "torch.int64", d, (r, words)), words, _dev(status, "status", i32, d, (1,)),
+                             cuda_stream))
+
+
+def ssd_rope_init(rot_dim: int, theta: float = 1e4, interleaved: bool = False, scaling: int = SSD_ROPE_PLAIN, factor: float = 1.0,
+                  original_len: float = 0.0, slow: float = 1.0, fast: float = 32.0, amplitude: float = 1.0) -> ssd_rope:
+    out = ssd_rope()
+    _check(lib.ssd_rope_init(rot_dim, int(bool(interleaved)), scaling, theta, factor, original_len, slow, fast, amplitude, out))
+    return out
+
+
+def ssd_rope_kv(cache: PagedKV, layer: int, rope: ssd_rope, q, k, v, positions, slots, q_out,
+                cuda_stream: int | None = None) -> None:
+    """Turns q [n][heads][hd] and k [n][kv_heads][hd] to positions int32 [n]; q to q_out, k and v [n][kv_heads][hd] to
+    rows slots int32 [n] of the cache's layer."""
+    d, n, hd = cache.device, q.shape[0], cache.head_dim
+    rows = [x for t, what, heads in ((q, "q", None), (k, "k", cache.n_kv_heads), (v, "v", cache.n_kv_heads))
+            for x in _rows(t, what, d, q.dtype, n, heads, hd)]
+    _check(lib.ssd_rope_kv(cache.struct, layer, rope, _ROW_TYPES[str(q.dtype)], n, q.shape[1], *rows,
+                           _dev(positions, "positions", "torch.int32", d, (n,)), _dev(slots, "slots", "torch.int32", d, (n,)),
+                           *_rows(q_out, "q_out", d, q.dtype, n, q.shape[1], hd), cuda_stream))
+
+
+def ssd_tree_attention_workspace(cache: PagedKV) -> int:
+    """Bytes of workspace that ssd_tree_attention wants for this cache."""
+    n = ctypes.c_size_t()
+    _check(lib.ssd_tree_attention_workspace(cache.head_dim, n))
+    return n.value
+
+
+def ssd_tree_attention(batch: TreeBatch, cache: PagedKV, layer: int, q, masks, scale: float, out, workspace, status=None,
+                       cuda_stream: int | None = None) -> None:
+    """out [n_rows][heads][hd] = attention of q over the requests' cached positions and the nodes that masks
+    int64 [n_rows][words] show (None: chains).  workspace: a contiguous uint8 tensor."""
+    d, n = cache.device, batch.n_rows
+    if batch.device != d:
+        _refuse("the batch and the cache are on different devices")
+    qp, qs = _rows(q, "q", d, None, n, None, cache.head_dim)
+    op, os_ = _rows(out, "out", d, q.dtype, n, q.shape[1], cache.head_dim)
+    words = masks.shape[1] if masks is not None and masks.dim() == 2 else 0
+    _check(lib.ssd_tree_attention(batch.struct, cache.struct, layer, _ROW_TYPES[str(q.dtype)], q.shape[1], qp, qs,
+                                  _dev(masks, "masks", "torch.int64", d, (n, words)), words, scale, op, os_,
+                                  _dev(workspace, "workspace", "torch.uint8", d), workspace.numel(),
+                                  _dev(status, "status", "torch.int32", d, (1,)), cuda_stream))
+
+
+def ssd_tree_commit(batch: TreeBatch, cache: PagedKV | None, parents, tokens, target, accepted, next_token, lens_out, path,
+                    emitted, cuda_stream: int | None = None) -> None:
+    """Walks every tree along target int32 [n_rows]: accepted, next_token, lens_out int32 [n]; path, emitted int32
+    [n_rows]; moves the accepted rows of every layer of the cache (None: tokens only).  parents None: chains."""
+    d, n, r, i32 = batch.device, batch.n_requests, batch.n_rows, "torch.int32"
+    if cache is not None and cache.device != d:
+        _refuse("the batch and the cache are on different devices")
+    _check(lib.ssd_tree_commit(batch.struct, cache.struct if cache is not None else None, _dev(parents, "parents", i32, d, (r,)),
+                               _dev(tokens, "tokens", i32, d, (r,)), _dev(target, "target", i32, d, (r,)),
+                               _dev(accepted, "accepted", i32, d, (n,)), _dev(next_token, "next_token", i32, d, (n,)),
+                               _dev(lens_out, "lens_out", i32, d, (n,)), _dev(path, "path", i32, d, (r,)),
+                               _dev(emitted, "emitted", i32, d, (r,)), cuda_stream))
 
 
 def ssd_destroy(h: int) -> None:

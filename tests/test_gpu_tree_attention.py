@@ -1,0 +1,387 @@
+"""ssd_tree_attention on the GPU against plain numpy in 64 bits
+(tests/tree_reference.py), and a round of all the tree operators.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import tree_reference as ref
+from test_gpu_tree_ops import TYPES, dev, ints, random_parents
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ssd():
+    import paper_2309_08168_gb300 as m
+    return m
+
+
+class Case:
+    """A batch over a paged cache.  What no row may see is NaN: positions behind a request's last, pages of nobody."""
+
+    def __init__(self, rng, kind, heads, kv, hd, page, lens, counts, masks="tree", words=None, apart=False, q_scale=1.5, extra_rows=2, layers=1):
+        self.heads, self.kv, self.hd, self.page, self.kind = heads, kv, hd, page, kind
+        self.lens, counts = np.array(lens, np.int32), np.array(counts)
+        self.row_start = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        self.n_rows, self.max_rows = int(self.row_start[-1]) + extra_rows, int(counts.max())
+        total = np.maximum(self.lens, 0).astype(np.int64) + counts
+        need = -(-total // page)
+        width = int(max(1, need.max())) + 1
+        n_pages = int(need.sum()) + 2
+        perm, at = rng.permutation(n_pages), 0
+        self.table = np.full((len(lens), width), -1, np.int32)
+        for b in range(len(lens)):
+            self.table[b, :need[b]] = perm[at:at + need[b]]
+            at += need[b]
+        t = torch.float16 if kind == "f32" else TYPES[kind]
+        shape = (layers, n_pages, page, kv, hd) if apart else (layers, n_pages, kv, page, hd)
+        self.k, self.v = (torch.full(shape, float("nan"), dtype=t, device="cuda") for _ in range(2))
+        if apart:
+            self.k, self.v = self.k.transpose(2, 3), self.v.transpose(2, 3)
+        for b in range(len(lens)):
+            x = np.arange(total[b])
+            p, o = (torch.from_numpy(i).cuda() for i in (self.table[b, x // page].astype(np.int64), x % page))
+            for c in (self.k, self.v):
+                c[layers - 1, p, :, o] = torch.from_numpy(rng.standard_normal((len(x), kv, hd)).astype(np.float32)).cuda().to(t)
+        self.q = torch.from_numpy((q_scale * rng.standard_normal((self.n_rows, heads, hd))).astype(np.float32)).cuda().to(TYPES[kind])
+        self.masks = None
+        if masks is not None:
+            self.words = words or -(-max(1, self.max_rows) // 64)
+            parents = random_parents(rng, counts, masks)
+            m = np.zeros((self.n_rows, self.words), np.uint64)
+            for b, n in enumerate(counts):
+                seen = []
+                for i in range(n):
+                    p = parents[self.row_start[b] + i]
+                    seen.append((1 << i) | (seen[p] if p >= 0 else 0))
+                    for w in range(self.words):
+                        m[self.row_start[b] + i, w] = (seen[i] >> (64 * w)) & (2**64 - 1)
+            self.masks = m.view(np.int64)
+
+    def run(self, ssd, scale=None, status=None, workspace=None, stream=None, layer=None, out=None):
+        kv = ssd.PagedKV(self.k, self.v)
+        b = ssd.TreeBatch(dev(self.row_start), dev(self.lens), dev(self.table), self.n_rows, self.max_rows)
+        if out is None:
+            out = torch.full(self.q.shape, 77.0, dtype=self.q.dtype, device="cuda")
+        if workspace is None:
+            workspace = torch.full((ssd.ssd_tree_attention_workspace(kv),), 255, dtype=torch.uint8, device="cuda")
+        layer = self.k.shape[0] - 1 if layer is None else layer
+        ssd.ssd_tree_attention(b, kv, layer, self.q, dev(self.masks) if self.masks is not None else None, scale or 1 / math.sqrt(self.hd), out, workspace, status,
+                               torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return out
+
+    def want(self, scale=None):
+        k, v = (c[-1].float().cpu().numpy() for c in (self.k, self.v))
+        return ref.attention(self.q.double().cpu().numpy(), k, v, self.row_start, self.lens, self.table, self.page, self.masks, scale or 1 / math.sqrt(self.hd))
+
+    def check(self, out, scale=None):
+        want, written, (vmax, smax, count) = self.want(scale)
+        got = out.double().cpu().numpy()
+        assert (got[~written] == 77).all()
+        # a score's products enter with 2^-22 (fp32 rows: fp16 pairs of q) and are summed in fp32 in hd / 16 + 4 steps that
+        # round or truncate (2^-22 each, of the sum of |products|); the exponential adds 2^-20; a weight enters the second
+        # product with 2^-21 (fp32 rows, pairs) or half a step of its type, the sums of weights and outputs in steps of 2^-22
+        # for every 16 positions, and 16 for joining parts; then one rounding to the rows' type
+        d = smax * (2.0**-22 * (self.hd / 16 + 4 + 1)) + 2.0**-20
+        p = {"f32": 2.0**-21, "f16": 2.0**-11, "bf16": 2.0**-8}[self.kind]
+        tol = vmax * (2 * np.expm1(d) + 2 * p + 2 * 2.0**-22 * (count / 16 + 20))
+        tol = tol[..., None] + np.abs(want) * {"f32": 2.0**-24, "f16": 2.0**-11, "bf16": 2.0**-8}[self.kind] * 1.01 + (2.0**-25 if self.kind == "f16" else 0)
+        err = np.where(written[:, None, None], np.abs(got - want), 0)
+        assert np.isfinite(got).all()
+        assert (err <= tol).all(), ((err / tol).max(), np.unravel_index(np.argmax(err / tol), err.shape))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads,kv,page,lens,counts,masks,apart", [
+    (4, 4, 16, [37], [5], "tree", False),
+    (1, 1, 16, [0], [1], "tree", False),  # nothing cached: a root sees itself
+    (2, 1, 16, [0, 1, 63, 64, 65], [1, 1, 1, 1, 1], None, False),  # single tokens around a tile
+    (3, 3, 48, [127, 128, 129, 0], [4, 64, 65, 2], "tree", True),
+    (8, 1, 64, [300, -1, 5, 70], [9, 3, 0, 17], "tree", False),  # ended, empty
+    (10, 2, 80, [200, 90], [33, 7], "chain", True),  # groups of 5
+    (14, 2, 16, [515], [37], "star", False),  # groups of 7: rows end inside a tile
+    (6, 6, 256, [1000, 3], [16, 17], "tree", False),
+    (4, 2, 32, [40, 700], [130, 100], "tree", False),  # three mask words
+    (2, 2, 16, [100, 33], [200, 300], None, False),  # prompt chunks
+    (64, 1, 16, [77], [3], "tree", False),  # one KV head for all
+])
+def test_attention(ssd, kind, hd, heads, kv, page, lens, counts, masks, apart):
+    c = Case(np.random.default_rng(heads * 100 + page), kind, heads, kv, hd, page, lens, counts, masks, apart=apart)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = c.run(ssd, status=status)
+    torch.cuda.synchronize()
+    c.check(out)
+    assert int(status) == 0
+    assert torch.equal(out, c.run(ssd))  # the same bits again
+
+
+@pytest.mark.parametrize("kind,heads,kv,lens,counts", [("f32", 2, 2, [6000], [1]), ("f16", 8, 1, [20001], [3]), ("bf16", 4, 2, [3000, 9, 7000], [20, 1, 64]),
+                                                       ("f32", 4, 4, [2500] + [20] * 40, [3] * 41)])
+def test_attention_along_a_long_cache(ssd, kind, heads, kv, lens, counts):
+    c = Case(np.random.default_rng(len(lens) + heads), kind, heads, kv, 128, 64, lens, counts)
+    c.check(c.run(ssd))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_rows_that_see_nothing_are_zero(ssd, kind):
+    c = Case(np.random.default_rng(1), kind, 4, 2, 64, 16, [0, 30], [7, 70])
+    c.masks[2] = c.masks[5] = 0  # of the request with nothing cached
+    c.masks[10] = 0              # of the other one: its cached positions only
+    out = c.run(ssd)
+    c.check(out)
+    assert (out[[2, 5]] == 0).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,kv,counts", [(4, 4, [9, 5]), (16, 2, [40, 30])])
+def test_what_a_row_does_not_see_does_not_matter(ssd, kind, heads, kv, counts):
+    """NaN and infinities in the keys and values of single nodes reach the rows that see them, and no others."""
+    c = Case(np.random.default_rng(2), kind, heads, kv, 128, 16, [50, 70], counts, "star")
+    clean = c.run(ssd)
+    bad = {0: (3, float("nan"), None), 1: (4, None, float("inf"))}
+    for b, (node, knew, vnew) in bad.items():
+        x = int(c.lens[b]) + node
+        page, at = int(c.table[b, x // 16]), x % 16
+        if knew is not None:
+            c.k[0, page, :, at] = knew
+            c.v[0, page, :, at, ::2] = knew
+        if vnew is not None:
+            c.v[0, page, :, at, 5] = vnew
+    out = c.run(ssd)
+    hit = [int(c.row_start[b]) + node for b, (node, _, _) in bad.items()]
+    rest = [r for r in range(int(c.row_start[-1])) if r not in hit]
+    assert torch.equal(out[rest], clean[rest])
+    assert out[hit[0]].isnan().all()
+    assert (out[hit[1], :, 5] == float("inf")).all()
+    keep = [d for d in range(128) if d != 5]
+    assert torch.equal(out[hit[1]][:, keep], clean[hit[1]][:, keep])
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_scores_of_minus_infinity_have_no_weight(ssd, kind, rows):
+    """Keys of -inf in one dim, against positive queries there; a row all of whose scores are -inf is zero."""
+    c = Case(np.random.default_rng(3), kind, 4, 2, 64, 16, [0, 0], [rows, rows], None)
+    c.q[:, :, 7] = c.q[:, :, 7].abs() + 0.5
+    for b in (0, 1):
+        for x in ([0, 2] if b == 0 else [0, 1]):  # request 1: the first two rows see only such keys
+            c.k[0, int(c.table[b, 0]), :, x, 7] = -float("inf")
+    out = c.run(ssd)
+    first = int(c.row_start[1])
+    assert (out[0] == 0).all() and (out[first:first + 2] == 0).all()
+    c.check(out)
+
+
+def test_large_scores_and_values(ssd):
+    """Peaked rows (one position has all the weight), fp32 queries far outside fp16's range and far below it."""
+    for q_scale, scale in ((40.0, None), (1e6, 1e-6), (1e-9, 1e9), (1e-3, None)):
+        c = Case(np.random.default_rng(4), "f32", 4, 2, 64, 16, [200, 3], [6, 40], q_scale=q_scale)
+        c.check(c.run(ssd, scale), scale)
+
+
+def test_pages_outside_the_cache_read_as_zeros(ssd):
+    c = Case(np.random.default_rng(5), "f16", 4, 2, 64, 16, [100], [20])
+    c.table[0, 2], c.table[0, 4] = -1, 10**6
+    c.check(c.run(ssd))
+
+
+def test_table_too_narrow(ssd):
+    """Positions that the table does not hold are not seen; the call says so."""
+    for rows in (3, 30):
+        c = Case(np.random.default_rng(6), "f32", 4, 2, 64, 16, [60], [rows])
+        c.table = np.ascontiguousarray(c.table[:, :2])
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = c.run(ssd, status=status)
+        c.check(out)
+        assert int(status) == ssd.SSD_STATUS_TABLE
+
+
+def test_broken_row_starts_stay_inside(ssd):
+    for rows in (2, 60):
+        c = Case(np.random.default_rng(7), "f16", 4, 2, 64, 16, [60, 20], [rows, rows], extra_rows=0)
+        c.row_start = np.array([-4, 2 * rows + 90, 1], np.int32)
+        guard = torch.full((c.n_rows + 64, 4, 64), 77.0, dtype=torch.float16, device="cuda")
+        c.masks[:] = -1
+        c.run(ssd, out=guard[32:32 + c.n_rows])
+        torch.cuda.synchronize()
+        assert (guard[:32] == 77).all() and (guard[32 + c.n_rows:] == 77).all()
+
+
+def test_layers_and_strided_rows(ssd):
+    """The layer asked for is read; q and out may be parts of wider rows."""
+    c = Case(np.random.default_rng(8), "bf16", 4, 2, 128, 48, [90, 10], [30, 4], layers=3, apart=True)
+    n, w = c.n_rows, 4 * 128
+    wide, res = torch.zeros(n, w + 64, dtype=torch.bfloat16, device="cuda"), torch.full((n, w + 8), 77.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 64:] = c.q.reshape(n, w)
+    c.q = wide[:, 64:].unflatten(1, (4, 128))
+    out = c.run(ssd, out=res[:, :w].unflatten(1, (4, 128)))
+    c.check(out)
+    assert (res[:, w:] == 77).all()
+
+
+def test_on_another_stream_and_in_graphs_that_share_a_workspace(ssd):
+    a = Case(np.random.default_rng(9), "f32", 8, 2, 128, 16, [900, 40], [9, 3])
+    b = Case(np.random.default_rng(10), "f16", 16, 2, 64, 16, [500, 700], [60, 64])
+    want = [a.run(ssd), b.run(ssd)]
+    ws = torch.full((ssd.ssd_tree_attention_workspace(ssd.PagedKV(a.k, a.v)),), 255, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = a.run(ssd, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(out, want[0])
+    graphs, outs = [], []
+    for c in (a, b):
+        kv, o = ssd.PagedKV(c.k, c.v), torch.full(c.q.shape, 77.0, dtype=c.q.dtype, device="cuda")
+        bt, m = ssd.TreeBatch(dev(c.row_start), dev(c.lens), dev(c.table), c.n_rows, c.max_rows), dev(c.masks)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            ssd.ssd_tree_attention(bt, kv, 0, c.q, m, 1 / math.sqrt(c.hd), o, ws, None, torch.cuda.current_stream().cuda_stream)
+        graphs.append((g, bt, m, kv))
+        outs.append(o)
+    for _ in range(3):
+        for (g, *_), o in zip(graphs, outs):
+            o.fill_(77.0)
+            g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_a_captured_call_follows_the_lengths(ssd):
+    """Lengths, starts and tables are read when the graph runs."""
+    c = Case(np.random.default_rng(11), "f32", 4, 2, 64, 16, [900, 800], [9, 3])
+    kv, ws = ssd.PagedKV(c.k, c.v), torch.empty(ssd.ssd_tree_attention_workspace(ssd.PagedKV(c.k, c.v)), dtype=torch.uint8, device="cuda")
+    lens, m = dev(c.lens), dev(c.masks)
+    bt, o = ssd.TreeBatch(dev(c.row_start), lens, dev(c.table), c.n_rows, c.max_rows), torch.full(c.q.shape, 77.0, device="cuda")
+    c.run(ssd)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ssd.ssd_tree_attention(bt, kv, 0, c.q, m, 0.125, o, ws, None, torch.cuda.current_stream().cuda_stream)
+    for new in ([900, 800], [3, 500], [0, 64], [-1, 1]):
+        c.lens = np.array(new, np.int32)
+        lens.copy_(torch.from_numpy(c.lens))
+        o.fill_(77.0)
+        g.replay()
+        c.check(o, 0.125)
+
+
+def test_tensors_elsewhere_are_refused(ssd):
+    c = Case(np.random.default_rng(12), "f32", 2, 2, 64, 16, [9], [2])
+    c.q = c.q.cpu()
+    with pytest.raises(ssd.SSDError):
+        c.run(ssd)
+    with pytest.raises(ssd.SSDError):
+        ssd.PagedKV(c.k.cpu(), c.v.cpu())
+    host = torch.zeros(64, dtype=torch.int32)
+    b = ssd.ssd_batch(1, 1, 1, 1, host.data_ptr(), host.data_ptr(), host.data_ptr())
+    assert ssd.lib.ssd_tree_plan(b, 16, 10, None, *[host.data_ptr() + 16 * i for i in range(7)], None, 0, None, None) == ssd.SSD_ERR_INVALID_ARG
+    assert "current device" in ssd.ssd_last_error()
+
+
+# -- a round of all of them ---------------------------------------------------
+
+@pytest.mark.parametrize("kind,heads,kv,hd,page,tree", [("f32", 4, 2, 64, 16, True), ("f16", 8, 1, 128, 48, True), ("bf16", 4, 4, 64, 16, False)])
+def test_rounds_of_a_batch(ssd, kind, heads, kv, hd, page, tree):
+    """Prompts, then rounds of drafted trees: plan, rope, attention, commit.  q, k and v of a token follow from the token
+    alone; after every round the cache of each request holds its sequence, and the rows' attention is what the
+    sequence through their ancestors gives.  Requests end and their pages serve others."""
+    rng = np.random.default_rng(13)
+    t, ct, n, vocab = TYPES[kind], torch.float16 if kind == "f32" else TYPES[kind], 3, 50
+    emb = [torch.from_numpy(rng.standard_normal((vocab, h, hd)).astype(np.float32)).cuda().to(t) for h in (heads, kv, kv)]
+    n_pages, width = 3 * (-(-130 // page)) , -(-130 // page)
+    kc, vc = (torch.full((1, n_pages, kv, page, hd), float("nan"), dtype=ct, device="cuda") for _ in range(2))
+    cache, rope = ssd.PagedKV(kc, vc), ssd.ssd_rope_init(hd, 1e4)
+    f = ref.frequencies(hd)
+    ring = torch.arange(n_pages, dtype=torch.int32, device="cuda")
+    ends, held, table = torch.tensor([0, n_pages], device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), ints(n, width)
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ws = torch.empty(ssd.ssd_tree_attention_workspace(cache), dtype=torch.uint8, device="cuda")
+    seqs = [rng.integers(0, vocab, int(k)).tolist() for k in (33, 1, 20)]  # the last token of each is not cached
+    s = torch.cuda.current_stream().cuda_stream
+    for step in range(9):
+        prompt = step == 0
+        if step == 5:  # request 1 ends; the next round starts another one in its place
+            lens[1] = -1
+        counts, parents, tokens = [], [], []
+        for b in range(n):
+            if int(lens[b]) < 0:
+                counts.append(0)
+                continue
+            c = len(seqs[b]) if prompt or int(lens[b]) == 0 else int(rng.integers(1, 13))
+            counts.append(c)
+            if prompt or int(lens[b]) == 0 or not tree:
+                parents += range(-1, c - 1)
+            else:
+                parents += [-1] + [int(rng.integers(0, i)) for i in range(1, c)]
+            tokens += seqs[b] if prompt or int(lens[b]) == 0 else [seqs[b][-1]] + rng.integers(0, 3, c - 1).tolist()
+        row_start = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        rows = int(row_start[-1])
+        words = -(-max(counts) // 64) if tree else 0
+        pt, tk = dev(np.array(parents, np.int32)) if tree else None, dev(np.array(tokens, np.int32))
+        bt = ssd.TreeBatch(dev(row_start), lens, table, rows, max(counts))
+        held2, ends2, slots, pos = ints(n), torch.zeros_like(ends), ints(rows), ints(rows)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        masks = torch.zeros(rows, words, dtype=torch.int64, device="cuda") if tree else None
+        ssd.ssd_tree_plan(bt, page, n_pages, pt, held, held2, ring, ends, ends2, slots, pos, masks, status, s)
+        q, k, v = (e[tk.long()] for e in emb)
+        turned, out = torch.empty_like(q), torch.empty_like(q)
+        ssd.ssd_rope_kv(cache, 0, rope, q, k, v, pos, slots, turned, s)
+        ssd.ssd_tree_attention(bt, cache, 0, turned, masks, hd**-0.5, out, ws, status, s)
+        # what each row's own sequence gives
+        assert int(status) == 0
+        for b in range(n):
+            for i in range(counts[b]):
+                r = int(row_start[b]) + i
+                line, x = [], i
+                while x >= 0:
+                    line.insert(0, tokens[row_start[b] + x])
+                    x = parents[row_start[b] + x]
+                line = (seqs[b][:int(lens[b])] if not prompt else []) + line
+                assert int(pos[r]) == len(line) - 1
+                kk = torch.from_numpy(ref.rope(emb[1][line].double().cpu().numpy(), np.arange(len(line)), f, False)).to(ct).double().numpy()
+                vv = emb[2][line].to(ct).double().cpu().numpy()
+                qq = ref.rope(emb[0][line[-1:]].double().cpu().numpy(), [len(line) - 1], f, False)[0]
+                g = heads // kv
+                sc = np.einsum("hd,phd->hp", qq, np.repeat(kk, g, 1)) * hd**-0.5
+                w = np.exp(sc - sc.max(1, keepdims=True))
+                o = np.einsum("hp,phd->hd", w / w.sum(1, keepdims=True), np.repeat(vv, g, 1))
+                # keys (and in 16 bits queries, weights, outputs) rounded to their type
+                tol = {"f32": 8 * 2.0**-11, "f16": 12 * 2.0**-11, "bf16": 12 * 2.0**-8}[kind] * np.abs(vv).max()
+                assert np.abs(out[r].double().cpu().numpy() - o).max() <= tol
+        # the target's choices: the drafts mostly, then something else
+        target = rng.integers(0, 3, rows).astype(np.int32)
+        acc, nxt, new = ints(n), ints(n), ints(n)
+        path, emitted = ints(rows), ints(rows)
+        if prompt or any(counts[b] and int(lens[b]) == 0 for b in range(n)):  # prompts are taken whole
+            target = np.concatenate([np.array(tokens[1:] + [2], np.int32)])
+            for b in range(n):
+                if counts[b]:
+                    target[row_start[b + 1] - 1] = 2
+        ssd.ssd_tree_commit(bt, cache, pt, tk, dev(target), acc, nxt, new, path, emitted, s)
+        torch.cuda.synchronize()
+        for b in range(n):
+            if not counts[b]:
+                continue
+            a = int(acc[b])
+            got = emitted[int(row_start[b]):int(row_start[b]) + a + 1].cpu().tolist()
+            if prompt or int(lens[b]) == 0:
+                seqs[b] = seqs[b] + got[len(seqs[b]) - 1:] if a >= len(seqs[b]) - 1 else seqs[b][:a + 1] + got[-1:]
+            else:
+                seqs[b] += got
+            assert int(new[b]) == len(seqs[b]) - 1 and got[-1] == int(nxt[b])
+            x = np.arange(int(new[b]))
+            tb = table[b].cpu().numpy()
+            have = kc[0][torch.from_numpy(tb[x // page].astype(np.int64)), :, torch.from_numpy(x % page)].double().cpu().numpy()
+            line = seqs[b][:-1]
+            full = ref.rope(emb[1][line].double().cpu().numpy(), x, f, False)
+            assert np.abs(have - full).max() <= {"f32": 1.01 * 2.0**-11, "f16": 1.01 * 2.0**-11, "bf16": 1.01 * 2.0**-8}[kind] * 2 * np.abs(full).max() + 1e-5
+        held, ends = held2, ends2
+        lens.copy_(new)
+        if step == 5:
+            assert int(held[1]) == 0
+            lens[1] = 0
+            seqs[1] = rng.integers(0, vocab, 7).tolist()
+    assert int(ends[1]) > n_pages  # pages came back
