@@ -1,0 +1,137 @@
+// tree_sched.cuh - how ssd_tree_attention's work is spread over its CTAs.
+//
+// An item is a tile of query rows of one request against one KV head; a unit is
+// 64 positions of its cache.  Items stand in a row - request by request, KV head
+// by KV head, tile by tile - and the units of all of them are cut into
+// equal ranges, one per CTA: whatever the lengths are, every CTA has the same number of
+// units, give or take one.  An item that lies in one CTA's range is finished there;
+// one that a range end cuts leaves a partial sum per CTA, joined afterwards in
+// the order of the CTAs.  A CTA has at most two of those: the item that its range
+// starts in and the one that it ends in.
+//
+// Row r of a request and KV head is node r / group, query head r % group of the
+// head's group.
+#pragma once
+
+#include <stdint.h>
+
+#include "ssd_internal.cuh"
+
+namespace ssd {
+namespace tree {
+
+constexpr int kUnit = 64;  // positions
+constexpr int kMinUnits = 1;  // a CTA gets at least (so few units are not spread thinner)
+
+struct Shape {
+    int n_requests, n_rows, max_blocks, page_size, n_kv_heads, group, chain;
+    const int32_t *row_start, *lens;
+};
+__host__ __device__ __forceinline__ int sched_load(const int32_t* p) {
+#ifdef __CUDA_ARCH__
+    return __ldcg(p);
+#else
+    return *p;
+#endif
+}
+
+// A request; rows stay inside [0, n_rows) whatever row_start holds.
+struct Req {
+    int r0, n, len;  // first row, rows (0: nothing to do), cached positions
+    int total;       // positions that its rows may see
+    int clipped;     // some are not in the table
+};
+__host__ __device__ __forceinline__ Req req_of(const Shape& s, int b) {
+    Req q;
+    int e = sched_load(s.row_start + b + 1);
+    q.r0 = sched_load(s.row_start + b);
+    q.len = sched_load(s.lens + b);
+    q.r0 = q.r0 < 0 ? 0 : q.r0 > s.n_rows ? s.n_rows : q.r0;
+    e = e < q.r0 ? q.r0 : e > s.n_rows ? s.n_rows : e;
+    q.n = q.len < 0 ? 0 : e - q.r0;
+    const long long most = (1ll << 31) - 2 * kUnit, cap = (long long)s.max_blocks * s.page_size;
+    const long long room = cap < most ? cap : most, want = (long long)q.len + q.n;
+    q.clipped = want > room;
+    q.total = (int)(want < room ? want : room);
+    return q;
+}
+__host__ __device__ __forceinline__ int tiles_of(const Shape& s, const Req& q, int tile) {
+    return (q.n * s.group + tile - 1) / tile;
+}
+// units of a tile: of a chain, up to the position of its last row
+__host__ __device__ __forceinline__ int units_of(const Shape& s, const Req& q, int tile, int mt) {
+    int keys = q.total;
+    if (s.chain) {
+        const int last = ((mt + 1) * tile - 1) / s.group;  // the tile's last node
+        const long long seen = (long long)q.len + (last < q.n - 1 ? last : q.n - 1) + 1;
+        if (seen < keys) keys = (int)seen;
+    }
+    return (keys + kUnit - 1) / kUnit;
+}
+// units of one KV head of a request
+__host__ __device__ __forceinline__ long long head_units(const Shape& s, const Req& q, int tile) {
+    const int n = tiles_of(s, q, tile);
+    if (!s.chain) return (long long)n * (n ? units_of(s, q, tile, 0) : 0);
+    long long u = 0;
+    for (int mt = 0; mt < n; ++mt) u += units_of(s, q, tile, mt);
+    return u;
+}
+
+// CTAs that take part, the first unit of a CTA's range, the CTA that a unit belongs to
+__host__ __device__ __forceinline__ int ctas_of(long long units, int grid) {
+    const long long most = units / kMinUnits;
+    return most < 1 ? 1 : most < grid ? (int)most : grid;
+}
+__host__ __device__ __forceinline__ long long range_start(long long units, int ctas, int c) { return units * c / ctas; }
+__host__ __device__ __forceinline__ int cta_of(long long units, int ctas, long long u) {
+    return (int)(((u + 1) * ctas - 1) / units);
+}
+
+// One CTA's share of an item: units [u0, u1) of n.
+struct Seg {
+    int b, kvh, mt, u0, u1, n;
+    Req q;
+};
+// A walk through a CTA's range.
+struct Walk {
+    int b, kvh, mt, u;
+    long long left;
+    Req q;
+};
+// `off`: units of request b before the range
+__host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int tile, int b, long long off, long long left) {
+    w.left = left;
+    if (left <= 0) return;
+    w.b = b;
+    w.q = req_of(s, b);
+    const long long per = head_units(s, w.q, tile);
+    w.kvh = (int)(off / per);
+    off -= w.kvh * per;
+    w.mt = 0;
+    for (int n; off >= (n = units_of(s, w.q, tile, w.mt)); ++w.mt) off -= n;
+    w.u = (int)off;
+}
+__host__ __device__ __forceinline__ bool walk_next(Walk& w, const Shape& s, int tile, Seg& g) {
+    if (w.left <= 0) return false;
+    g.b = w.b;
+    g.kvh = w.kvh;
+    g.mt = w.mt;
+    g.q = w.q;
+    g.n = units_of(s, w.q, tile, w.mt);
+    g.u0 = w.u;
+    g.u1 = g.n - w.u < w.left ? g.n : w.u + (int)w.left;
+    w.left -= g.u1 - g.u0;
+    w.u = 0;
+    if (w.left > 0 && ++w.mt == tiles_of(s, w.q, tile)) {
+        w.mt = 0;
+        if (++w.kvh == s.n_kv_heads) {
+            w.kvh = 0;
+            do w.q = req_of(s, ++w.b);
+            while (w.q.n == 0);  // (units are left, so there is one)
+        }
+    }
+    return true;
+}
+
+}  // namespace tree
+}  // namespace ssd
