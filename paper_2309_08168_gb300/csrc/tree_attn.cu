@@ -9,17 +9,20 @@
 // 4 hd bytes and 4 hd R flops.  Up to some 250 rows the bound is HBM, beyond it the
 // tensor cores and the exponentials.
 //
-// A CTA walks its range of units (tree_sched.cuh), 64 positions at a time:
-//   warp TILE / 32     : TMA producer: K and V of a unit, 16 to 64 rows of a page per
-//                        copy, into a ring;
-//   warp TILE / 32 + 1 : MMA issuer: S = q K^T (tcgen05.mma, 128 x 64 x 16, TMEM
-//                        accumulators) a unit ahead of O += P V (P in TMEM over the
-//                        columns of S, V as it lies in the cache, MN-major);
-//   warps 0 ..         : softmax, a row per thread: S from TMEM, P back to it, running
-//                        maximum and sum; at an item's end O / sum, or O, maximum
-//                        and sum to the workspace if other CTAs hold parts of the item.
-// The tile has 128 rows or, for requests of up to 32 rows, 32 (the other lanes
-// of the MMA are not read).  join_kernel adds the parts of cut items.
+// A CTA (one per SM) walks its range of units (tree_sched.cuh), 128 positions at a time:
+//   warps 8, 9 : TMA producers of K and of V, a lane per copy of 16 to 64 rows of a page,
+//                into a ring each (K in slots of 64 dims, free once multiplied; V in
+//                slots of 64 positions);
+//   warp 10    : issues S = q K^T (tcgen05.mma, 128 x 128 x 16, TMEM accumulators);
+//   warp 11    : issues O += P V (P in TMEM over the columns of S, V as it lies in the
+//                cache, MN-major, N = hd);
+//   warps 0-3, 4-7 : softmax of the even and of the odd units, a row per thread: S from
+//                TMEM, P back to it, running maximum and sum, with an accumulator O of
+//                its own each.  At an item's end the two are joined (half of the dims
+//                each): O / sum, or O, maximum and sum to the workspace if other CTAs
+//                hold parts of the item.  join_kernel adds those.
+// The tile has 128 rows; 32 where no request has more, which leaves the ring the
+// shared memory of the other rows' q (their lanes then hold what no one reads).
 //
 // O is rescaled only when a row's maximum has grown by more than kSlack (log2)
 // over the one its weights are relative to (the running softmax of Milakov and
@@ -54,8 +57,11 @@ namespace {
 
 constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp16
 constexpr unsigned long long kWaitNs = 2000000000ull;
-constexpr int kTmem = 256;  // columns: O 0 .. hd, S / P of even units at 128, of odd ones at 192
-constexpr int kJoinThreads = 128;
+constexpr int kTile = 128;  // rows: the TMEM lanes
+constexpr int kThreads = 384;
+constexpr int kTmem = 512;  // columns: O of even units at 0, of odd ones at 128, S / P at 256 and 384
+constexpr int kMaxSlots = 12;
+constexpr int kJoinThreads = 256, kJoinLines = 4;
 
 // what a CTA whose range ends inside an item leaves for join_kernel
 struct alignas(16) Cut {
@@ -80,9 +86,12 @@ struct AttnOpArgs {
     int box_shift;  // positions per copy, log2: 16 .. 64 of them, which divide page_size
     int at_pos, at_head, at_page;  // which coordinate (1 .. 3) of the tensor maps is which
     float scale2;  // log2(e) * scale
+    int tile;      // rows: 32 or 128
+    unsigned nk, nv;    // slots of the rings
+    uint64_t group_inv;  // ceil(2^32 / group)
     Cut* cuts;     // [grid]
-    float* stats;  // [grid][2][2][TILE]: maximum, sum
-    float4* part;  // [grid][2][HD / 4][TILE]
+    float* stats;  // [grid][2][2][kTile]: maximum, sum
+    float4* part;  // [grid][2][HD / 4][kTile]
     int32_t* status;
 };
 
@@ -97,21 +106,27 @@ struct Types<float> {
     static constexpr int PARTS = 2;
 };
 
-template <typename T, int HD, int TILE>
+template <typename T, int HD>
 struct Lay {
     static constexpr int PARTS = Types<T>::PARTS, BOXES = HD / 64;
-    static constexpr int QB = TILE * 128;             // bytes of 64 dims of the tile's q, one part
-    static constexpr int Q = PARTS * BOXES * QB;
-    static constexpr int KB = kUnit * 128;            // bytes of 64 dims of a unit of K or V
-    static constexpr int STAGE = 2 * BOXES * KB;      // K boxes, then V boxes
-    // two CTAs an SM, except for fp32 rows in tiles of 128 at hd 128, whose q takes 64 KB
-    static constexpr int CTAS = Q > 32 * 1024 ? 1 : 2;
-    static constexpr int FIT = ((CTAS == 1 ? 220 : 110) * 1024 - Q) / STAGE;
-    static constexpr int STAGES = FIT > 6 ? 6 : FIT;
-    // (the MMA reads 128 rows of q whatever TILE is: what lies behind has to be shared memory of the CTA)
-    static constexpr size_t BYTES = 1024 + (size_t)Q + (size_t)STAGES * STAGE;
-    static constexpr int THREADS = TILE + 64;
-    static_assert(STAGES >= 2 && Q + STAGES * STAGE >= Q - QB + 128 * 128, "");
+    static constexpr int KSLOT = kUnit * 128;         // 64 dims of a unit's K
+    static constexpr int VBOX = 64 * 128;             // 64 dims of 64 positions of V
+    static constexpr int VSLOT = BOXES * VBOX;
+    static constexpr int RING = 219 * 1024;           // shared memory for q and the rings
+    static __host__ __device__ constexpr int q_bytes(int tile) { return PARTS * BOXES * tile * 128; }
+    // slots: the same bytes of K and V in flight, and V's wait for the softmax
+    static constexpr int nk(int tile) {
+        const int n = (RING - q_bytes(tile)) * 9 / 20 / KSLOT;
+        return n < kMaxSlots ? n : kMaxSlots;
+    }
+    static constexpr int nv(int tile) {
+        const int n = (RING - q_bytes(tile) - nk(tile) * KSLOT) / VSLOT;
+        return n < kMaxSlots ? n : kMaxSlots;
+    }
+    static_assert(nk(128) >= 2 * BOXES && nv(128) >= 4, "a unit of K and two of V");
+    // (the MMA reads 128 rows of q whatever the tile is: what lies behind is shared memory of the ring)
+    static_assert(q_bytes(32) - 32 * 128 + 128 * 128 <= RING, "");
+    static constexpr size_t BYTES = 1024 + (size_t)RING;
 };
 
 __device__ __forceinline__ void tma4d(void* dst, const CUtensorMap* map, int x, int c1, int c2, int c3, uint64_t* bar) {
@@ -120,11 +135,11 @@ __device__ __forceinline__ void tma4d(void* dst, const CUtensorMap* map, int x, 
         ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar))
         : "memory");
 }
-// kind::f16, A = B = fp16 or bf16, D = fp32, M = 128, N = 64; B K-major or (V) MN-major
+// kind::f16, A = B = fp16 or bf16, D = fp32, M = 128, N = n; B K-major or (V) MN-major
 template <typename C>
-__device__ __forceinline__ constexpr uint32_t idesc(bool b_mn) {
+__device__ __forceinline__ constexpr uint32_t idesc(int n, bool b_mn) {
     return (1u << 4) | (sizeof(C) == 2 && std::is_same<C, bf16>::value ? (1u << 7) | (1u << 10) : 0u) | (b_mn ? 1u << 16 : 0u) |
-           ((64u >> 3) << 17) | ((128u >> 4) << 24);
+           ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t ad, uint64_t bd, uint32_t id, uint32_t acc) {
     asm volatile(
@@ -161,8 +176,19 @@ __device__ __forceinline__ void st32(uint32_t t, const uint32_t (&r)[32]) {
         ::SSD_I8(r, 0), SSD_I8(r, 8), SSD_I8(r, 16), SSD_I8(r, 24), "r"(t)
         : "memory");
 }
+// 16 columns
+__device__ __forceinline__ void st16(uint32_t t, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::SSD_I8(r, 0), SSD_I8(r, 8), "r"(t)
+                 : "memory");
+}
 #undef SSD_R8
 #undef SSD_I8
+// 2^x; below 2^-126: 0
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -200,7 +226,7 @@ __device__ __forceinline__ void split_rn(float a, float b, uint32_t& hi, uint32_
 }
 
 // which of the positions p0 .. p0 + 63 node `node` (mask words m) sees, as bits
-__device__ __forceinline__ uint64_t visible(const Req& q, int chain, int words, const uint64_t (&m)[4], int node, int p0) {
+__device__ __forceinline__ uint64_t visible(const Req& q, int chain, const uint64_t (&m)[4], int node, int p0) {
     const int end = q.total - p0;  // the unit's positions below it exist
     uint64_t v;
     if (chain) {
@@ -225,39 +251,48 @@ __device__ __forceinline__ uint64_t visible(const Req& q, int chain, int words, 
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, f16) { return ((u & 0x7c00u) == 0x7c00u) | ((u & 0x7c000000u) == 0x7c000000u) << 1; }
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, bf16) { return ((u & 0x7f80u) == 0x7f80u) | ((u & 0x7f800000u) == 0x7f800000u) << 1; }
 
-template <typename T, int HD, int TILE>
-__global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::CTAS)
+template <typename T, int HD>
+__global__ void __launch_bounds__(kThreads, 1)
     attn_kernel(const __grid_constant__ AttnOpArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
-    using L = Lay<T, HD, TILE>;
+    using L = Lay<T, HD>;
     using C = typename Types<T>::C;
-    constexpr int BOXES = L::BOXES, PARTS = L::PARTS, NW = TILE / 32, S = L::STAGES;
+    constexpr int BOXES = L::BOXES, PARTS = L::PARTS;
+    const int tile = a.tile;
+    const unsigned nk = a.nk, nv = a.nv;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    unsigned char* kv = smem + L::Q;
-    __shared__ __align__(8) uint64_t k_full[S], v_full[S], kv_empty[S], q_ready, s_full[2], p_ready[2], pv_done[2];
+    unsigned char *ks = smem + L::q_bytes(tile), *vs = ks + nk * L::KSLOT;
+    __shared__ __align__(8) uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
+    __shared__ __align__(8) uint64_t q_ready, ends_ready, o_free, s_full[2], p_ready[2], pv_done[2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
-    __shared__ long long s_sum[L::THREADS / 32], s_off;
+    __shared__ long long s_sum[kThreads / 32], s_off;
     __shared__ int s_b;
+    __shared__ Req s_req;  // the request that the range starts in
+    __shared__ float s_scale[2][kTile];     // [segment & 1]: power of two that a row of q was divided by
+    __shared__ float2 s_end[2][2][kTile];   // [segment & 1][group]: a row's maximum and sum
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         s_fail = s_odd = 0;
         s_b = -1;
-        for (int s = 0; s < S; ++s) {
-            tc::mb_init(k_full + s, 1);
-            tc::mb_init(v_full + s, 1);
-            tc::mb_init(kv_empty + s, 1);
+        for (int i = 0; i < kMaxSlots; ++i) {
+            tc::mb_init(k_full + i, 1);
+            tc::mb_init(k_empty + i, 1);
+            tc::mb_init(v_full + i, 1);
+            tc::mb_init(v_empty + i, 1);
         }
-        tc::mb_init(&q_ready, NW);
+        tc::mb_init(&q_ready, 8);
+        tc::mb_init(&ends_ready, 8);
+        tc::mb_init(&o_free, 8);
         for (int i = 0; i < 2; ++i) {
             tc::mb_init(s_full + i, 1);
-            tc::mb_init(p_ready + i, NW);
+            tc::mb_init(p_ready + i, 4);
             tc::mb_init(pv_done + i, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == NW) {
+    if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -267,13 +302,14 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
 
     // this CTA's range: units of all requests, a run of requests per thread
     const Shape& sh = a.shape;
-    const int per = (sh.n_requests + L::THREADS - 1) / L::THREADS;
+    const int per = (sh.n_requests + kThreads - 1) / kThreads;
     const int b0 = min(tid * per, sh.n_requests), b1 = min(b0 + per, sh.n_requests);
     long long mine = 0;
+    Req last{};
     for (int b = b0; b < b1; ++b) {
-        const Req q = req_of(sh, b);
-        if (q.clipped && q.n && blockIdx.x == 0) say(a.status, SSD_STATUS_TABLE);
-        mine += head_units(sh, q, TILE) * sh.n_kv_heads;
+        last = req_of(sh, b);
+        if (last.clipped && last.n && blockIdx.x == 0) say(a.status, SSD_STATUS_TABLE);
+        mine += head_units(sh, last, tile) * sh.n_kv_heads;
     }
     long long before = mine;
 #pragma unroll
@@ -285,7 +321,7 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
     __syncthreads();
     before -= mine;
     long long units = 0;
-    for (int w = 0; w < L::THREADS / 32; ++w) {
+    for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) before += s_sum[w];
         units += s_sum[w];
     }
@@ -294,9 +330,11 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
     if (before <= lo && lo < before + mine) {
         long long off = lo - before;
         for (int b = b0; b < b1; ++b) {
-            const long long n = head_units(sh, req_of(sh, b), TILE) * sh.n_kv_heads;
+            const Req q = per == 1 ? last : req_of(sh, b);
+            const long long n = head_units(sh, q, tile) * sh.n_kv_heads;
             if (off < n) {
                 s_b = b;
+                s_req = q;
                 s_off = off;
                 break;
             }
@@ -308,16 +346,30 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
     tc::fence_after();
     const uint32_t tmem = s_tmem;
     Walk walk;
-    walk_init(walk, sh, TILE, s_b, s_off, hi - lo);
+    walk_init(walk, sh, tile, s_b, s_req, s_off, hi - lo);
     Seg g;
     bool ok = true;
+    auto wait = [&](uint64_t* b, unsigned phase) {
+        ok = ok && __all_sync(0xffffffffu, mb_wait(b, phase & 1u, &s_fail));
+        return ok;
+    };
 
-    if (warp == NW) {
-        // page ids are asked for 32 copies ahead, one per lane
+    if (warp == 8 || warp == 9) {
+        // page ids are asked for 32 copies (of one 64-dim half) ahead, one per lane
         asm volatile("fence.proxy.async.global;" ::: "memory");  // K / V rows that the previous kernel wrote
-        const int n_box = kUnit >> a.box_shift, batch = 32 << a.box_shift;  // copies per unit, positions per 32 copies
-        unsigned j = 0;
-        while (ok && walk_next(walk, sh, TILE, g)) {
+        const bool is_v = warp == 9;
+        const unsigned n_slots = is_v ? nv : nk;
+        unsigned char* ring = is_v ? vs : ks;
+        uint64_t *full = is_v ? v_full : k_full, *empty = is_v ? v_empty : k_empty;
+        const CUtensorMap* map = is_v ? &tm_v : &tm_k;
+        const int batch = 32 << a.box_shift;  // positions of 32 copies
+        // a slot: V 64 positions x BOXES halves, K 128 positions x one half
+        const int slot_rows = is_v ? 64 : kUnit, copies = slot_rows >> a.box_shift;
+        const int my_box = is_v ? lane % copies : lane, my_half = is_v ? lane / copies : 0;
+        const bool mine_too = lane < (is_v ? copies * BOXES : copies);
+        const unsigned bytes = is_v ? L::VSLOT : L::KSLOT;
+        unsigned slot = 0, phase = 1;
+        while (ok && walk_next(walk, sh, tile, g)) {
             const int32_t* table = a.block_table + (size_t)g.b * sh.max_blocks;
             auto fetch = [&](long long x) {  // page of this lane's copy of the 32 from x on; -1: outside, reads as zeros
                 x += lane << a.box_shift;
@@ -325,310 +377,348 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
                 if (x < g.q.total) page = __ldcg(table + (int)x / sh.page_size);
                 return page >= 0 && page < a.n_pages ? page : -1;
             };
-            int x0 = g.u0 * kUnit, got = fetch(x0), ahead = fetch((long long)x0 + batch);
-            for (int u = g.u0; u < g.u1 && ok; ++u, ++j) {
-                if (u * kUnit - x0 >= batch) {
+            const int n = (g.u1 - g.u0) * (is_v ? 2 : BOXES);  // slots of the segment
+            long long x0 = (long long)g.u0 * kUnit;
+            int got = fetch(x0), ahead = fetch(x0 + batch);
+            for (int i = 0; i < n; ++i) {
+                const long long x = (long long)g.u0 * kUnit + (is_v ? i * 64 : i / BOXES * kUnit);  // the slot's first position
+                if (x - x0 >= batch) {
                     x0 += batch;
                     got = ahead;
-                    ahead = fetch((long long)x0 + batch);
+                    ahead = fetch(x0 + batch);
                 }
-                const int s = j % S;
-                ok = __all_sync(0xffffffffu, mb_wait(kv_empty + s, (j / S + 1) & 1u, &s_fail));
-                if (!ok) break;
-                unsigned char* st = kv + s * L::STAGE;
-                const bool one = elect_one();
-                if (one) {
-                    tc::mb_arrive_tx(k_full + s, (unsigned)(BOXES * L::KB));
-                    tc::mb_arrive_tx(v_full + s, (unsigned)(BOXES * L::KB));
-                }
-#pragma unroll
-                for (int kvp = 0; kvp < 2; ++kvp)
-                    for (int i = 0; i < n_box; ++i) {
-                        const int page = __shfl_sync(0xffffffffu, got, ((u * kUnit - x0) >> a.box_shift) + i);
-                        if (one) {
-                            const int in_page = (u * kUnit + (i << a.box_shift)) % sh.page_size;
-                            const int c1 = a.at_pos == 1 ? in_page : a.at_head == 1 ? g.kvh : page;
-                            const int c2 = a.at_pos == 2 ? in_page : a.at_head == 2 ? g.kvh : page;
-                            const int c3 = a.at_pos == 3 ? in_page : a.at_head == 3 ? g.kvh : page;
-#pragma unroll
-                            for (int b = 0; b < BOXES; ++b)
-                                tma4d(st + (kvp * BOXES + b) * L::KB + (i << a.box_shift) * 128, kvp ? &tm_v : &tm_k, b * 64, c1, c2, c3, (kvp ? v_full : k_full) + s);
-                        }
-                    }
+                const int page = __shfl_sync(0xffffffffu, got, ((int)(x - x0) >> a.box_shift) + my_box);
+                const int in_page = (int)((unsigned)(x + (my_box << a.box_shift)) % (unsigned)sh.page_size);
+                if (!wait(empty + slot, phase)) break;
+                if (elect_one()) tc::mb_arrive_tx(full + slot, bytes);
                 __syncwarp();
+                if (mine_too) {
+                    const int c1 = a.at_pos == 1 ? in_page : a.at_head == 1 ? g.kvh : page;
+                    const int c2 = a.at_pos == 2 ? in_page : a.at_head == 2 ? g.kvh : page;
+                    const int c3 = a.at_pos == 3 ? in_page : a.at_head == 3 ? g.kvh : page;
+                    const int half = is_v ? my_half : i % BOXES;
+                    tma4d(ring + slot * bytes + my_half * L::VBOX + (my_box << a.box_shift) * 128, map, half * 64, c1, c2, c3, full + slot);
+                }
+                __syncwarp();
+                if (++slot == n_slots) slot = 0, phase ^= 1u;
             }
         }
-    } else if (warp == NW + 1) {
-        const uint64_t q0 = tc::sdesc(smem_u32(smem)), kv0 = tc::sdesc(smem_u32(kv));
-        auto wait = [&](uint64_t* b, unsigned phase) {
-            ok = ok && __all_sync(0xffffffffu, mb_wait(b, phase & 1u, &s_fail));
-            return ok;
-        };
-        // S of unit j; its K has landed and P of unit j - 2, which held these columns, is used up
-        auto scores = [&](unsigned j) {
-            if (!wait(k_full + j % S, j / S)) return;
-            if (j >= 2 && !wait(pv_done + (j & 1), (j - 2) >> 1)) return;
-            tc::fence_after();
-            if (elect_one()) {
-                const uint64_t k0 = kv0 + (uint64_t)((j % S) * (L::STAGE >> 4));
-                const uint32_t d = tmem + 128u + 64u * (j & 1);
-#pragma unroll
-                for (int h = 0; h < PARTS; ++h)
-#pragma unroll
-                    for (int b = 0; b < BOXES; ++b)
-#pragma unroll
-                        for (int ks = 0; ks < 4; ++ks)
-                            mma_ss(d, q0 + (uint64_t)(((h * BOXES + b) * L::QB + ks * 32) >> 4), k0 + (uint64_t)((b * L::KB + ks * 32) >> 4),
-                                   idesc<C>(false), (h | b | ks) ? 1u : 0u);
-                commit(s_full + (j & 1));
-            }
-            __syncwarp();
-        };
-        unsigned j = 0, n_seg = 0;
-        while (ok && walk_next(walk, sh, TILE, g)) {
-            if (!wait(&q_ready, n_seg++)) break;
-            scores(j);
+    } else if (warp == 10) {
+        const uint64_t q0 = tc::sdesc(smem_u32(smem)), k0 = tc::sdesc(smem_u32(ks));
+        const uint32_t qb = (uint32_t)tile * 128;  // 64 dims of the tile's q
+        unsigned j = 0, slot = 0, phase = 0;
+        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+            if (!wait(&q_ready, n_seg)) break;
             for (int u = g.u0; u < g.u1 && ok; ++u, ++j) {
-                if (u + 1 < g.u1) scores(j + 1);
-                if (!ok || !wait(p_ready + (j & 1), j >> 1) || !wait(v_full + j % S, j / S)) break;
-                tc::fence_after();
-                if (elect_one()) {
-                    // V: 64 dims (MN) x 16 positions (K) per MMA; 8 positions are 1024 bytes apart
-                    const uint64_t v0 = kv0 + (uint64_t)(((j % S) * L::STAGE + BOXES * L::KB) >> 4);
-                    const uint64_t mn = (uint64_t)((1024 >> 4) - 1) << 16;  // leading byte offset 1024 too
-                    const uint32_t p = tmem + 128u + 64u * (j & 1);
+                // P of unit j - 2, which held these columns, is used up
+                if (j >= 2 && !wait(pv_done + (j & 1), (j - 2) >> 1)) break;
 #pragma unroll
-                    for (int b = 0; b < BOXES; ++b)
+                for (int b = 0; b < BOXES; ++b) {
+                    if (!wait(k_full + slot, phase)) break;
+                    tc::fence_after();
+                    if (elect_one()) {
+                        const uint32_t d = tmem + 256u + 128u * (j & 1);
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks)
+                        for (int h = 0; h < PARTS; ++h)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                mma_ss(d, q0 + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
+                                       idesc<C>(kUnit, false), (b | h | k) ? 1u : 0u);
+                        commit(k_empty + slot);
+                        if (b == BOXES - 1) commit(s_full + (j & 1));
+                    }
+                    __syncwarp();
+                    if (++slot == nk) slot = 0, phase ^= 1u;
+                }
+            }
+        }
+    } else if (warp == 11) {
+        // V: hd dims (MN) x 16 positions (K) per MMA; 8 positions are 1024 bytes apart, 64 dims a box
+        const uint64_t v0 = tc::sdesc(smem_u32(vs)) + ((uint64_t)((L::VBOX >> 4) - 1) << 16);
+        unsigned j = 0, slot = 0, phase = 0;
+        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+            for (int u = g.u0; u < g.u1 && ok; ++u, ++j) {
+                if (!wait(p_ready + (j & 1), j >> 1)) break;
+                const bool fresh = u - g.u0 < 2;  // the group's first unit of the segment
+                if (fresh && n_seg && !wait(&o_free, n_seg - 1)) break;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (!wait(v_full + slot, phase)) break;
+                    tc::fence_after();
+                    if (elect_one()) {
+                        const uint32_t p = tmem + 256u + 128u * (j & 1) + 64u * half, o = tmem + 128u * (j & 1);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
 #pragma unroll
                             for (int h = 0; h < PARTS; ++h)
-                                mma_ts(tmem + 64u * b, p + 32u * h + 8u * ks, v0 + mn + (uint64_t)((b * L::KB + ks * 2048) >> 4), idesc<C>(true),
-                                       (u > g.u0 || ks || h) ? 1u : 0u);
-                    commit(kv_empty + j % S);
-                    commit(pv_done + (j & 1));
+                                mma_ts(o, p + 32u * (k >> 1) + 16u * h + 8u * (k & 1), v0 + (uint64_t)((slot * L::VSLOT + k * 2048) >> 4), idesc<C>(HD, true),
+                                       (!fresh || half || k || h) ? 1u : 0u);
+                        commit(v_empty + slot);
+                        if (half) commit(pv_done + (j & 1));
+                    }
+                    __syncwarp();
+                    if (++slot == nv) slot = 0, phase ^= 1u;
                 }
-                __syncwarp();
             }
         }
     } else {
-        const uint32_t tl = tmem + ((uint32_t)(warp * 32) << 16);
+        const int grp = warp >> 2, quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
+        const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16), ts = tl + 256u + 128u * grp;
+        // node and query head of row `row` of a tile whose first row is `rem` heads into its first node
+        auto node_of = [&](int rem, int row) { return (int)(((uint64_t)(unsigned)(rem + row) * a.group_inv) >> 32); };
         // q of the segment's rows (K-major, 128-byte swizzle: row r of 64 dims at r * 128, 16-byte
-        // chunk c at (c ^ (r & 7)) * 16), a few rows of this warp's 32 at a time; returns the power
-        // of two that this thread's row was divided by
-        float q_scale = 1.f;
-        auto load_q = [&](const Seg& s) {
-            constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR, N = 8;  // lanes per row, rows per step, steps at once
-            const int rows = s.q.n * sh.group;
-            float mult = 1.f;
-            for (int i0 = 0; i0 < 32; i0 += N * RPI) {
+        // chunk c at (c ^ (r & 7)) * 16), a few rows a step, steps over the eight warps.  Rows that do not
+        // exist keep what lies there: no one reads their lanes.
+        auto load_q = [&](const Seg& s, int parity) {
+            constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR, N = 4;  // lanes per row, rows per step, steps at once
+            const int start = s.mt * tile, rows = min(s.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
+            const int e = (lane % LPR) * V;
+            for (int i0 = warp * RPI; i0 < rows; i0 += 8 * N * RPI) {
                 uint4 x[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int r = s.mt * TILE + warp * 32 + i0 + i * RPI + lane / LPR, e = (lane % LPR) * V;
+                    const int r = i0 + i * 8 * RPI + lane / LPR;
                     x[i] = make_uint4(0, 0, 0, 0);
                     if (r < rows) {
-                        const int node = r / sh.group, head = s.kvh * sh.group + r - node * sh.group;
-                        x[i] = __ldcg(reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(s.q.r0 + node) * a.q_stride + head * HD + e));
+                        const int node = node_of(rem, r), head = s.kvh * sh.group + rem + r - node * sh.group;
+                        x[i] = __ldcg(reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(s.q.r0 + node0 + node) * a.q_stride + head * HD + e));
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int r = warp * 32 + i0 + i * RPI + lane / LPR, e = (lane % LPR) * V;
-                    unsigned char* at = smem + (e >> 6) * L::QB + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4) + (e & 7) * 2;
+                    const int r = i0 + i * 8 * RPI + lane / LPR;
+                    if (i0 + i * 8 * RPI >= rows) break;
+                    unsigned char* at = smem + (e >> 6) * tile * 128 + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4) + (e & 7) * 2;
                     if constexpr (PARTS == 1) {
-                        *reinterpret_cast<uint4*>(at) = x[i];
+                        if (r < rows) *reinterpret_cast<uint4*>(at) = x[i];
                     } else {
                         float f[4];
                         Vec<float>::get(x[i], f);
                         float m = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
 #pragma unroll
                         for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                        // 2^e with the row's largest value at 2^9 .. 2^10 (rows of zeros, infinities and subnormals: as if 2^-126 or 2^127)
+                        // 2^e2 with the row's largest value at 2^9 .. 2^10 of it (zeros and the smallest values: as if that were 2^-117)
                         const int e2 = min(max((int)(__float_as_uint(m) >> 23), 10), 254) - 127 - 9;
                         const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
                         uint2 h, l;
                         split_away(f[0] * down, f[1] * down, h.x, l.x);
                         split_away(f[2] * down, f[3] * down, h.y, l.y);
-                        *reinterpret_cast<uint2*>(at) = h;
-                        *reinterpret_cast<uint2*>(at + BOXES * L::QB) = l;
-                        const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
-                        // lane i0 + i RPI + (row in step) holds that row
-#pragma unroll
-                        for (int k = 0; k < RPI; ++k) {
-                            const float v = __shfl_sync(0xffffffffu, up, k * LPR);
-                            if (lane == i0 + i * RPI + k) mult = v;
+                        if (r < rows) {
+                            *reinterpret_cast<uint2*>(at) = h;
+                            *reinterpret_cast<uint2*>(at + BOXES * tile * 128) = l;
+                            if (lane % LPR == 0) s_scale[parity][r] = __uint_as_float((uint32_t)(127 + e2) << 23);
                         }
                     }
                 }
             }
-            q_scale = mult;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) arrive(&q_ready);
         };
 
-        unsigned j = 0;
-        bool more = walk_next(walk, sh, TILE, g);
-        if (more) load_q(g);
+        unsigned j = 0;  // of the segment's first unit
+        bool more = walk_next(walk, sh, tile, g);
+        if (more) load_q(g, 0);
         long long at = lo;  // global unit of the segment's start
-        bool first_seg = true;
-        while (more && ok) {
-            const int rows = g.q.n * sh.group - g.mt * TILE;     // of the tile that exist
-            const bool active = warp * 32 < rows;                // some row of the warp
-            const int r = g.mt * TILE + warp * 32 + lane, node = min(r / sh.group, g.q.n - 1), head = g.kvh * sh.group + r % sh.group;
-            const bool valid = warp * 32 + lane < rows;
-            const float sc = a.scale2 * q_scale;
+        for (unsigned n_seg = 0; more && ok; ++n_seg) {
+            const Seg cur = g;
+            const int n = cur.u1 - cur.u0, start = cur.mt * tile, rows = min(cur.q.n * sh.group - start, tile);  // units; rows that exist
+            const bool active = quarter * 32 < rows, valid = mine32 < rows;
+            const int node0 = start / sh.group, rem = start - node0 * sh.group, row = min(mine32, rows - 1);
+            const int node = node0 + node_of(rem, row), head = cur.kvh * sh.group + rem + row - (node - node0) * sh.group;
             uint64_t m[4] = {0, 0, 0, 0};
             if (!sh.chain && valid)
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
-                    if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(g.q.r0 + node) * a.words + w);
-            const int all_seen = sh.chain ? g.q.len + min(g.mt * TILE / sh.group, g.q.n - 1) + 1 : g.q.len;  // positions below it are seen by every row
-            float mx = 0.f, l = 0.f;  // maximum that the weights are relative to, their sum
-            for (int u = g.u0; u < g.u1; ++u, ++j) {
-                const int p0 = u * kUnit;
-                const uint32_t ts = tl + 128u + 64u * (j & 1);
-                ok = __all_sync(0xffffffffu, mb_wait(s_full + (j & 1), (j >> 1) & 1u, &s_fail));
-                if (!ok) break;
+                    if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(cur.q.r0 + node) * a.words + w);
+            // positions below it are seen by every row of the tile
+            const int all_seen = min(sh.chain ? cur.q.len + node0 + 1 : cur.q.len, cur.q.total);
+            const int first = (int)((j ^ (unsigned)grp) & 1u);  // this group's first unit of the segment
+            const unsigned j_last = j + (unsigned)n - 1;
+            float mx = -INFINITY, l = 0.f, sc = a.scale2;  // maximum that the weights are relative to, their sum
+            // the next rows' q, once all scores of this segment are there: before the softmax of the
+            // segment's last unit (the other group: after its own last one), so that the next scores are not late
+            auto next_q = [&] {
+                more = walk_next(walk, sh, tile, g);
+                if (more) load_q(g, (int)((n_seg + 1) & 1));
+            };
+            for (int i = first; i < n; i += 2) {
+                const unsigned ju = j + (unsigned)i;
+                const int p0 = (cur.u0 + i) * kUnit;
+                if (!wait(s_full + grp, ju >> 1)) break;
                 tc::fence_after();
-                const bool tail = p0 + kUnit > min(all_seen, g.q.total);
+                if constexpr (PARTS == 2)
+                    if (i == first) sc = a.scale2 * s_scale[n_seg & 1][mine32];
+                if (i == n - 1) next_q();
+                const bool tail = p0 + kUnit > all_seen;
                 if (tail) {  // V of positions that not every row sees
-                    ok = __all_sync(0xffffffffu, mb_wait(v_full + j % S, (j / S) & 1u, &s_fail));
-                    if (!ok) break;
-                    unsigned char* vs = kv + (j % S) * L::STAGE + BOXES * L::KB;
-                    for (int i = tid; i < BOXES * kUnit * 8; i += TILE) {
-                        const int x = p0 + ((i >> 3) & 63);
-                        if (x < g.q.len && x < g.q.total) continue;
-                        uint4* v = reinterpret_cast<uint4*>(vs + i * 16);
-                        if (x >= g.q.total) {
-                            *v = make_uint4(0, 0, 0, 0);
-                            continue;
-                        }
-                        uint32_t w[4] = {v->x, v->y, v->z, v->w}, odd = 0;
+                    for (int half = 0; half < 2; ++half) {
+                        const unsigned s = 2 * ju + half;
+                        const int x0 = p0 + 64 * half, lo_row = max(min(cur.q.len, cur.q.total) - x0, 0);
+                        // (copies that begin behind the last position have brought zeros)
+                        const int hi_row = min((max(cur.q.total - x0, 0) + (1 << a.box_shift) - 1) >> a.box_shift << a.box_shift, 64);
+                        if (lo_row >= hi_row) continue;
+                        if (!wait(v_full + s % nv, s / nv)) break;
+                        unsigned char* v8 = vs + s % nv * L::VSLOT;
+                        for (int c = tid & (kTile - 1); c < (hi_row - lo_row) * 8 * BOXES; c += kTile) {
+                            const int r = lo_row + (BOXES == 2 ? c >> 4 : c >> 3);
+                            uint4* v = reinterpret_cast<uint4*>(v8 + (BOXES == 2 ? (c >> 3 & 1) * L::VBOX : 0) + r * 128 + (c & 7) * 16);
+                            if (x0 + r >= cur.q.total) {
+                                *v = make_uint4(0, 0, 0, 0);
+                                continue;
+                            }
+                            uint32_t w[4] = {v->x, v->y, v->z, v->w}, odd = 0;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) odd |= exps_all_ones(w[k], C()) << (2 * k);
-                        if (odd) {
+                            for (int k = 0; k < 4; ++k) odd |= exps_all_ones(w[k], C()) << (2 * k);
+                            if (odd) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) w[k] &= (odd >> (2 * k) & 1 ? 0u : 0xffffu) | (odd >> (2 * k) & 2 ? 0u : 0xffff0000u);
-                            *v = make_uint4(w[0], w[1], w[2], w[3]);
-                            *(volatile int*)&s_odd = 1;
+                                for (int k = 0; k < 4; ++k) w[k] &= (odd >> (2 * k) & 1 ? 0u : 0xffffu) | (odd >> (2 * k) & 2 ? 0u : 0xffff0000u);
+                                *v = make_uint4(w[0], w[1], w[2], w[3]);
+                                *(volatile int*)&s_odd = 1;
+                            }
                         }
                     }
+                    if (!ok) break;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 if (active) {
-                    uint32_t u0[32], u1[32];
-                    ld32(ts, u0);
-                    ld32(ts + 32, u1);
-                    wait_ld();
-                    if (tail) {
-                        const uint64_t v = visible(g.q, sh.chain, a.words, m, node, p0);
-                        const uint32_t v0 = (uint32_t)v, v1 = (uint32_t)(v >> 32);
+                    uint64_t seen[2] = {~0ull, ~0ull};
+                    if (tail)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (!(v0 >> i & 1u)) u0[i] = 0xff800000u;
-                            if (!(v1 >> i & 1u)) u1[i] = 0xff800000u;
+                        for (int h = 0; h < 2; ++h) seen[h] = visible(cur.q, sh.chain, m, node, p0 + 64 * h);
+                    uint32_t x0[32], x1[32];
+                    auto load = [&](int h) {  // scores of half of the unit
+                        ld32(ts + 64 * h, x0);
+                        ld32(ts + 64 * h + 32, x1);
+                        wait_ld();
+                        if (tail) {
+                            const uint32_t v0 = (uint32_t)seen[h], v1 = (uint32_t)(seen[h] >> 32);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                if (!(v0 >> k & 1u)) x0[k] = 0xff800000u;
+                                if (!(v1 >> k & 1u)) x1[k] = 0xff800000u;
+                            }
                         }
-                    }
+                    };
                     float bm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) bm4[i & 3] = fmaxf(bm4[i & 3], fmaxf(__uint_as_float(u0[i]), __uint_as_float(u1[i])));
+                    for (int h = 0; h < 2; ++h) {
+                        load(h);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) bm4[k & 3] = fmaxf(bm4[k & 3], fmaxf(__uint_as_float(x0[k]), __uint_as_float(x1[k])));
+                    }
                     const float bm = fmaxf(fmaxf(bm4[0], bm4[1]), fmaxf(bm4[2], bm4[3])) * sc;
-                    if (u == g.u0) {
+                    if (i == first) {
                         mx = bm;
                     } else if (__any_sync(0xffffffffu, bm > mx + kSlack)) {
-                        // O and the sum move to the new maximum (all rows of the warp)
-                        ok = __all_sync(0xffffffffu, mb_wait(pv_done + ((j - 1) & 1), ((j - 1) >> 1) & 1u, &s_fail));
-                        if (!ok) break;
-                        tc::fence_after();
-                        const float nm = fmaxf(mx, bm), f = nm == -INFINITY ? 1.f : exp2f(mx - nm);
+                        // O and the sum move to the new maximum (all rows of the warp; the group's last unit
+                        // is in O, as the scores took its place)
+                        const float nm = fmaxf(mx, bm), f = nm == -INFINITY ? 1.f : ex2(mx - nm);
                         for (int c = 0; c < HD; c += 32) {
                             uint32_t o[32];
-                            ld32(tl + c, o);
+                            ld32(tl + 128u * grp + c, o);
                             wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            st32(tl + c, o);
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            st32(tl + 128u * grp + c, o);
                         }
                         l *= f;
                         mx = nm;
+                        load(1);  // (not kept through the above)
                     }
                     // (a row that has seen nothing yet, or only scores of -inf: weights 0)
                     const float ref = (mx == -INFINITY ? 0.f : mx) - kShift;
                     float l4[4] = {0.f, 0.f, 0.f, 0.f};
-                    uint32_t ph[32], pl[32];
+                    // 32 weights in the place of their scores: 16 columns of pairs (hi), 16 of lo
+                    auto weights = [&](const uint32_t (&x)[32], uint32_t t) {
+                        uint32_t ph[16], pl[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float p0f = exp2f(fmaf(__uint_as_float(u0[2 * i]), sc, -ref)), p1f = exp2f(fmaf(__uint_as_float(u0[2 * i + 1]), sc, -ref));
-                        const float p2f = exp2f(fmaf(__uint_as_float(u1[2 * i]), sc, -ref)), p3f = exp2f(fmaf(__uint_as_float(u1[2 * i + 1]), sc, -ref));
-                        l4[i & 3] += (p0f + p1f) + (p2f + p3f);
-                        if constexpr (PARTS == 2) {
-                            split_rn(p0f, p1f, ph[i], pl[i]);
-                            split_rn(p2f, p3f, ph[i + 16], pl[i + 16]);
-                        } else {
-                            ph[i] = pack2(p0f, p1f, C());
-                            ph[i + 16] = pack2(p2f, p3f, C());
+                        for (int k = 0; k < 16; ++k) {
+                            const float e0 = ex2(fmaf(__uint_as_float(x[2 * k]), sc, -ref)), e1 = ex2(fmaf(__uint_as_float(x[2 * k + 1]), sc, -ref));
+                            l4[k & 3] += e0 + e1;
+                            if constexpr (PARTS == 2) split_rn(e0, e1, ph[k], pl[k]);
+                            else ph[k] = pack2(e0, e1, C());
                         }
-                    }
+                        st16(t, ph);
+                        if constexpr (PARTS == 2) st16(t + 16, pl);
+                    };
+                    weights(x0, ts + 64);
+                    weights(x1, ts + 96);
+                    load(0);
+                    weights(x0, ts);
+                    weights(x1, ts + 32);
                     l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-                    st32(ts, ph);
-                    if constexpr (PARTS == 2) st32(ts + 32, pl);
                     wait_st();
                 }
                 tc::fence_before();
                 __syncwarp();
-                if (lane == 0) arrive(p_ready + (j & 1));
+                if (lane == 0) arrive(p_ready + grp);
             }
             if (!ok) break;
-            const Seg done = g;
-            const bool whole = done.u0 == 0 && done.u1 == done.n;
-            const long long item = at - done.u0;  // global unit of the item's start
-            const int slot = first_seg ? 0 : 1;
-            at += done.u1 - done.u0;
-            first_seg = false;
-            // the next rows' q while the last products run (all scores of this segment are done)
-            more = walk_next(walk, sh, TILE, g);
-            if (more) load_q(g);
-            if (tid == 0 && done.u1 < done.n) {
+            s_end[n_seg & 1][grp][mine32] = make_float2(mx == -INFINITY ? mx : mx - kShift, l);
+            __syncwarp();
+            if (lane == 0) arrive(&ends_ready);
+            if ((j_last & 1u) != (unsigned)grp) {
+                if (!wait(s_full + (j_last & 1), j_last >> 1)) break;
+                next_q();
+            }
+            const bool whole = cur.u0 == 0 && cur.u1 == cur.n;
+            const int slot = n_seg ? 1 : 0;
+            if (tid == 0 && cur.u1 < cur.n) {
+                const long long item = at - cur.u0;  // global unit of the item's start
                 Cut c;
                 c.first = cta_of(units, ctas, item);
-                c.last = cta_of(units, ctas, item + done.n - 1);
+                c.last = cta_of(units, ctas, item + cur.n - 1);
                 c.first_slot = range_start(units, ctas, c.first) == item ? 0 : 1;
-                c.row0 = done.mt * TILE;
-                c.rows = min(rows, TILE);
-                c.r0 = done.q.r0;
-                c.kvh = done.kvh;
+                c.row0 = start;
+                c.rows = rows;
+                c.r0 = cur.q.r0;
+                c.kvh = cur.kvh;
                 c.pad = 0;
                 a.cuts[cta] = c;
             }
-            ok = __all_sync(0xffffffffu, mb_wait(pv_done + ((j - 1) & 1), ((j - 1) >> 1) & 1u, &s_fail));
-            if (!ok) break;
+            at += n;
+            // both accumulators: this group writes half of the dims of their sum
+            if (!wait(&ends_ready, n_seg) || !wait(pv_done + (j_last & 1), j_last >> 1)) break;
+            const bool both = n > 1;  // else only the group of the one unit has an accumulator
+            if (both && !wait(pv_done + ((j_last - 1) & 1), (j_last - 1) >> 1)) break;
             tc::fence_after();
             if (active) {
+                const int g0 = (int)(j & 1u);  // group of the first unit
+                const float2 e0 = s_end[n_seg & 1][g0][mine32], e1 = s_end[n_seg & 1][g0 ^ 1][mine32];
+                const float top = both ? fmaxf(e0.x, e1.x) : e0.x;
+                const float f0 = e0.x == -INFINITY ? 0.f : ex2(e0.x - top), f1 = !both || e1.x == -INFINITY ? 0.f : ex2(e1.x - top);
+                const float sum = both ? fmaf(e0.y, f0, e1.y * f1) : e0.y;
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 const bool odd = *(volatile int*)&s_odd;
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                if (!whole && valid) {
-                    float* st = a.stats + (size_t)(cta * 2 + slot) * 2 * TILE + warp * 32 + lane;
-                    st[0] = mx == -INFINITY ? mx : mx - kShift;
-                    st[TILE] = l;
+                if (!whole && valid && grp == 0) {
+                    float* st = a.stats + (size_t)(cta * 2 + slot) * 2 * kTile + mine32;
+                    st[0] = top;
+                    st[kTile] = sum;
                 }
-                for (int c = 0; c < HD; c += 32) {
+                for (int c = grp * (HD / 2); c < (grp + 1) * (HD / 2); c += 32) {
                     uint32_t o[32];
-                    ld32(tl + c, o);
-                    wait_ld();
+                    ld32(tl + 128u * g0 + c, o);
+                    if (both) {
+                        uint32_t o1[32];
+                        ld32(tl + 128u * (g0 ^ 1) + c, o1);
+                        wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o[k]), f0, __uint_as_float(o1[k]) * f1));
+                    } else {
+                        wait_ld();
+                    }
                     if (!valid) continue;
                     if (odd) {  // values that are not finite, of nodes that this row sees
-                        for (int u = done.u0; u < done.u1; ++u) {
+                        for (int u = cur.u0; u < cur.u1; ++u) {
                             const int p0 = u * kUnit;
-                            if (p0 + kUnit <= done.q.len) continue;
-                            const uint64_t v = visible(done.q, sh.chain, a.words, m, node, p0);
+                            if (p0 + kUnit <= cur.q.len) continue;
                             for (int k = 0; k < kUnit; ++k) {
                                 const int x = p0 + k;
-                                if (x < done.q.len || !(v >> k & 1)) continue;
-                                const int page = __ldcg(a.block_table + (size_t)done.b * sh.max_blocks + x / sh.page_size);
+                                if (x < cur.q.len || !(visible(cur.q, sh.chain, m, node, x) & 1)) continue;
+                                const int page = __ldcg(a.block_table + (size_t)cur.b * sh.max_blocks + x / sh.page_size);
                                 if (page < 0 || page >= a.n_pages) continue;
-                                const C* vr = (const C*)a.vc + page * a.page_stride + done.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + c;
+                                const C* vr = (const C*)a.vc + page * a.page_stride + cur.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + c;
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) {
                                     const float f = (float)vr[i];
@@ -638,7 +728,7 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
                         }
                     }
                     if (whole) {
-                        T* to = (T*)a.out + (int64_t)(done.q.r0 + node) * a.out_stride + head * HD + c;
+                        T* to = (T*)a.out + (int64_t)(cur.q.r0 + node) * a.out_stride + head * HD + c;
                         constexpr int V = Vec<T>::N;
 #pragma unroll
                         for (int i = 0; i < 32; i += V) {
@@ -648,13 +738,17 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
                             *reinterpret_cast<uint4*>(to + i) = Vec<T>::put(f);
                         }
                     } else {
-                        float4* to = a.part + ((size_t)(cta * 2 + slot) * (HD / 4) + c / 4) * TILE + warp * 32 + lane;
+                        float4* to = a.part + ((size_t)(cta * 2 + slot) * (HD / 4) + c / 4) * kTile + mine32;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
-                            to[(i / 4) * TILE] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+                            to[(i / 4) * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
                     }
                 }
             }
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(&o_free);
+            j += (unsigned)n;
         }
     }
     if (!ok) s_fail = 1;
@@ -667,65 +761,73 @@ __global__ void __launch_bounds__(Lay<T, HD, TILE>::THREADS, Lay<T, HD, TILE>::C
         while (tc::gtime() - t0 < 2000000ull) __nanosleep(1000);
     }
     __syncthreads();
-    if (warp == NW) {
+    if (warp == 8) {
         tc::fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmem) : "memory");
     }
 }
 
-
 // Joins the parts of the items that range ends cut.  CTA c of the attention left a
-// Cut if its range ends inside an item; with n such ends in an item, n CTAs share
-// it here: a warp takes 32 rows (a lane each) and 4 dims at a time, first the
-// largest maximum of the parts, then the weighted sums, in the order of the parts.
-template <typename T, int HD, int TILE>
+// Cut if its range ends inside an item; with n such ends in an item, n lines of CTAs
+// (gridDim.y each) share it here: a warp takes 32 rows (a lane each) and 16 dims at a
+// time, first the largest maximum of the parts, then the weighted sums, in the order
+// of the parts.  Bound by L2 latency: all loads of a few parts are under way at once.
+template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnOpArgs a) {
+    constexpr int W = kJoinThreads / 32, D = 16;
     pdl_launch_dependents();
     pdl_wait();
     const int cta = blockIdx.x, lane = threadIdx.x & 31;
     const int4 c0 = __ldcg(reinterpret_cast<const int4*>(a.cuts + cta)), c1 = __ldcg(reinterpret_cast<const int4*>(a.cuts + cta) + 1);
     const int first = c0.x, last = c0.y, slot = c0.z, row0 = c0.w, rows = c1.x, r0 = c1.y, kvh = c1.z;
     if (last < 0) return;
-    const int warps = (last - first) * (kJoinThreads / 32), items = (rows + 31) / 32 * (HD / 4);
-    for (int w = (cta - first) * (kJoinThreads / 32) + (threadIdx.x >> 5); w < items; w += warps) {
-        const int chunk = w % (HD / 4), row = w / (HD / 4) * 32 + lane;
+    const int warps = (last - first) * (int)gridDim.y * W, items = (rows + 31) / 32 * (HD / D);
+    for (int w = ((cta - first) * (int)gridDim.y + blockIdx.y) * W + (threadIdx.x >> 5); w < items; w += warps) {
+        const int chunk = w % (HD / D), row = w / (HD / D) * 32 + lane;
         if (row >= rows) continue;
         auto part_of = [&](int p) { return (size_t)(p * 2 + (p == first ? slot : 0)); };
         float top = -INFINITY;
 #pragma unroll 8
-        for (int p = first; p <= last; ++p) top = fmaxf(top, __ldcg(a.stats + part_of(p) * 2 * TILE + row));
-        float l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = first; p <= last; ++p) top = fmaxf(top, __ldcg(a.stats + part_of(p) * 2 * kTile + row));
+        float l = 0.f, o[D];
+#pragma unroll
+        for (int i = 0; i < D; ++i) o[i] = 0.f;
 #pragma unroll 4
         for (int p = first; p <= last; ++p) {
-            const float* st = a.stats + part_of(p) * 2 * TILE + row;
-            const float m = __ldcg(st), lp = __ldcg(st + TILE);
-            const float4 x = __ldcg(a.part + (part_of(p) * (HD / 4) + chunk) * TILE + row);
-            const float f = m == -INFINITY ? 0.f : exp2f(m - top);  // (0 x NaN stays NaN)
+            const float* st = a.stats + part_of(p) * 2 * kTile + row;
+            const float m = __ldcg(st), lp = __ldcg(st + kTile);
+            float4 x[D / 4];
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) x[i] = __ldcg(a.part + (part_of(p) * (HD / 4) + chunk * (D / 4) + i) * kTile + row);
+            const float f = m == -INFINITY ? 0.f : ex2(m - top);  // (0 x NaN stays NaN)
             l = fmaf(lp, f, l);
-            o.x = fmaf(x.x, f, o.x);
-            o.y = fmaf(x.y, f, o.y);
-            o.z = fmaf(x.z, f, o.z);
-            o.w = fmaf(x.w, f, o.w);
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) {
+                o[4 * i] = fmaf(x[i].x, f, o[4 * i]);
+                o[4 * i + 1] = fmaf(x[i].y, f, o[4 * i + 1]);
+                o[4 * i + 2] = fmaf(x[i].z, f, o[4 * i + 2]);
+                o[4 * i + 3] = fmaf(x[i].w, f, o[4 * i + 3]);
+            }
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int r = row0 + row, node = r / a.shape.group, head = kvh * a.shape.group + r - node * a.shape.group;
-        T* to = (T*)a.out + (int64_t)(r0 + node) * a.out_stride + head * HD + chunk * 4;
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        } else {
-            *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o.x * inv, o.y * inv, T()), pack2(o.z * inv, o.w * inv, T()));
+        T* to = (T*)a.out + (int64_t)(r0 + node) * a.out_stride + head * HD + chunk * D;
+        constexpr int V = Vec<T>::N;
+#pragma unroll
+        for (int i = 0; i < D; i += V) {
+            float f[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) f[k] = o[i + k] * inv;
+            *reinterpret_cast<uint4*>(to + i) = Vec<T>::put(f);
         }
     }
 }
 
 // -- host ----------------------------------------------------------------------
 
-// the workspace: cuts, statistics and parts of the largest grid (two CTAs an SM) and tile
-constexpr int kMaxTile = 128, kMaxCtas = 2;
+// the workspace: cuts, parts and statistics of a grid of one CTA an SM
 size_t workspace_need(int n_sms, int hd) {
-    const size_t grid = (size_t)kMaxCtas * n_sms;
-    return grid * (sizeof(Cut) + 2 * 2 * kMaxTile * sizeof(float) + 2 * (size_t)kMaxTile * hd * sizeof(float));
+    return (size_t)n_sms * (sizeof(Cut) + 2 * 2 * kTile * sizeof(float) + 2 * (size_t)kTile * hd * sizeof(float));
 }
 
 // Per device, once: kernel attributes and the SM count.
@@ -738,16 +840,10 @@ AttnDevice g_attn_dev[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 std::mutex g_attn_mu;
 
-template <typename T, int HD, int TILE>
-cudaError_t set_up_one() {
-    return cudaFuncSetAttribute(attn_kernel<T, HD, TILE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Lay<T, HD, TILE>::BYTES);
-}
 template <typename T>
 cudaError_t set_up_type() {
-    cudaError_t e = set_up_one<T, 64, 32>();
-    if (e == cudaSuccess) e = set_up_one<T, 64, 128>();
-    if (e == cudaSuccess) e = set_up_one<T, 128, 32>();
-    if (e == cudaSuccess) e = set_up_one<T, 128, 128>();
+    cudaError_t e = cudaFuncSetAttribute(attn_kernel<T, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Lay<T, 64>::BYTES);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_kernel<T, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Lay<T, 128>::BYTES);
     return e;
 }
 int set_up(const char* call, int* n_sms) {
@@ -797,24 +893,23 @@ int encode(const char* call, CUtensorMap* m, const void* base, const ssd_pages* 
     return r == CUDA_SUCCESS ? SSD_OK : refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-template <typename T, int HD, int TILE>
-int run_tile(const char* call, AttnOpArgs& a, const CUtensorMap& k, const CUtensorMap& v, int n_sms, void* workspace, void* stream) {
-    using L = Lay<T, HD, TILE>;
-    a.grid = L::CTAS * n_sms;
+template <typename T, int HD>
+int run_hd(const char* call, AttnOpArgs& a, const CUtensorMap& k, const CUtensorMap& v, int n_sms, void* workspace, void* stream) {
+    using L = Lay<T, HD>;
+    a.grid = n_sms;
+    a.nk = (unsigned)L::nk(a.tile);
+    a.nv = (unsigned)L::nv(a.tile);
     a.cuts = (Cut*)workspace;
     a.part = (float4*)(a.cuts + a.grid);
-    a.stats = (float*)(a.part + (size_t)a.grid * 2 * (HD / 4) * TILE);
-    if (int rc = launch(call, attn_kernel<T, HD, TILE>, dim3((unsigned)a.grid), L::THREADS, L::BYTES, stream, a, k, v)) return rc;
+    a.stats = (float*)(a.part + (size_t)a.grid * 2 * (HD / 4) * kTile);
+    if (int rc = launch(call, attn_kernel<T, HD>, dim3((unsigned)a.grid), kThreads, L::BYTES, stream, a, k, v)) return rc;
     // an item of one unit is never cut
-    if ((long long)a.shape.max_blocks * a.shape.page_size <= kUnit) return SSD_OK;
-    return launch(call, join_kernel<T, HD, TILE>, dim3((unsigned)(a.grid - 1)), kJoinThreads, 0, stream, a);
+    if ((long long)a.shape.max_blocks * a.shape.page_size <= kUnit || a.grid == 1) return SSD_OK;
+    return launch(call, join_kernel<T, HD>, dim3((unsigned)(a.grid - 1), kJoinLines), kJoinThreads, 0, stream, a);
 }
-// Tiles of 32 rows where every request has at most that many per KV head.
 template <typename T>
-int run(const char* call, AttnOpArgs& a, int hd, int max_rows, const CUtensorMap& k, const CUtensorMap& v, int n_sms, void* ws, void* stream) {
-    const bool small = (long long)max_rows * a.shape.group <= 32;
-    if (hd == 64) return small ? run_tile<T, 64, 32>(call, a, k, v, n_sms, ws, stream) : run_tile<T, 64, 128>(call, a, k, v, n_sms, ws, stream);
-    return small ? run_tile<T, 128, 32>(call, a, k, v, n_sms, ws, stream) : run_tile<T, 128, 128>(call, a, k, v, n_sms, ws, stream);
+int run(const char* call, AttnOpArgs& a, int hd, const CUtensorMap& k, const CUtensorMap& v, int n_sms, void* ws, void* stream) {
+    return hd == 64 ? run_hd<T, 64>(call, a, k, v, n_sms, ws, stream) : run_hd<T, 128>(call, a, k, v, n_sms, ws, stream);
 }
 
 }  // namespace
@@ -888,11 +983,13 @@ extern "C" int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache
     a.box_shift = cache->page_size % 64 == 0 ? 6 : cache->page_size % 32 == 0 ? 5 : 4;
     a.scale2 = (float)(1.4426950408889634 * scale);
     a.status = status;
+    a.tile = (long long)batch->max_rows * group <= 32 ? 32 : kTile;
+    a.group_inv = ((1ull << 32) + group - 1) / group;
     CUtensorMap k, v;
     if (int rc = encode(call, &k, (const char*)cache->k + 2 * layer * cache->layer_stride, cache, a)) return rc;
     if (int rc = encode(call, &v, a.vc, cache, a)) return rc;
-    const int hd = cache->head_dim, rows = batch->max_rows;
-    if (dtype == SSD_F32) return run<float>(call, a, hd, rows, k, v, n_sms, workspace, cuda_stream);
-    if (dtype == SSD_F16) return run<f16>(call, a, hd, rows, k, v, n_sms, workspace, cuda_stream);
-    return run<bf16>(call, a, hd, rows, k, v, n_sms, workspace, cuda_stream);
+    const int hd = cache->head_dim;
+    if (dtype == SSD_F32) return run<float>(call, a, hd, k, v, n_sms, workspace, cuda_stream);
+    if (dtype == SSD_F16) return run<f16>(call, a, hd, k, v, n_sms, workspace, cuda_stream);
+    return run<bf16>(call, a, hd, k, v, n_sms, workspace, cuda_stream);
 }

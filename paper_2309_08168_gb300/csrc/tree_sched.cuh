@@ -1,7 +1,7 @@
 // tree_sched.cuh - how ssd_tree_attention's work is spread over its CTAs.
 //
 // An item is a tile of query rows of one request against one KV head; a unit is
-// 64 positions of its cache.  Items stand in a row - request by request, KV head
+// kUnit positions of its cache.  Items stand in a row - request by request, KV head
 // by KV head, tile by tile - and the units of all of them are cut into
 // equal ranges, one per CTA: whatever the lengths are, every CTA has the same number of
 // units, give or take one.  An item that lies in one CTA's range is finished there;
@@ -20,8 +20,7 @@
 namespace ssd {
 namespace tree {
 
-constexpr int kUnit = 64;  // positions
-constexpr int kMinUnits = 1;  // a CTA gets at least (so few units are not spread thinner)
+constexpr int kUnit = 128;  // positions
 
 struct Shape {
     int n_requests, n_rows, max_blocks, page_size, n_kv_heads, group, chain;
@@ -79,8 +78,7 @@ __host__ __device__ __forceinline__ long long head_units(const Shape& s, const R
 
 // CTAs that take part, the first unit of a CTA's range, the CTA that a unit belongs to
 __host__ __device__ __forceinline__ int ctas_of(long long units, int grid) {
-    const long long most = units / kMinUnits;
-    return most < 1 ? 1 : most < grid ? (int)most : grid;
+    return units < 1 ? 1 : units < grid ? (int)units : grid;
 }
 __host__ __device__ __forceinline__ long long range_start(long long units, int ctas, int c) { return units * c / ctas; }
 __host__ __device__ __forceinline__ int cta_of(long long units, int ctas, long long u) {
@@ -98,12 +96,12 @@ struct Walk {
     long long left;
     Req q;
 };
-// `off`: units of request b before the range
-__host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int tile, int b, long long off, long long left) {
+// `off`: units of request b (q) before the range
+__host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int tile, int b, const Req& q, long long off, long long left) {
     w.left = left;
     if (left <= 0) return;
     w.b = b;
-    w.q = req_of(s, b);
+    w.q = q;
     const long long per = head_units(s, w.q, tile);
     w.kvh = (int)(off / per);
     off -= w.kvh * per;

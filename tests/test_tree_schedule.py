@@ -56,7 +56,7 @@ int main(int argc, char** argv) {
             for (int mt = 0; mt < tiles_of(s, q, tile); ++mt) {
                 const int last = std::min(q.n - 1, ((mt + 1) * tile - 1) / s.group);
                 const int keys = s.chain ? std::min(q.total, lens[b] + last + 1) : q.total;
-                if (units_of(s, q, tile, mt) != (keys + 63) / 64) return bad("units", it);
+                if (units_of(s, q, tile, mt) != (keys + 127) / 128) return bad("units", it);
             }
             before[b + 1] = before[b] + head_units(s, q, tile) * s.n_kv_heads;
         }
@@ -74,7 +74,7 @@ int main(int argc, char** argv) {
             int b = 0;
             while (!(before[b] <= lo && lo < before[b + 1])) ++b;
             Walk w;
-            walk_init(w, s, tile, b, lo - before[b], hi - lo);
+            walk_init(w, s, tile, b, req_of(s, b), lo - before[b], hi - lo);
             Seg g;
             long long at = lo;
             int n_parts = 0;
