@@ -113,19 +113,21 @@ struct Lay {
     static constexpr int VBOX = 64 * 128;             // 64 dims of 64 positions of V
     static constexpr int VSLOT = BOXES * VBOX;
     static constexpr int RING = 219 * 1024;           // shared memory for q and the rings
+    // two buffers of a tile of 32 rows, one of 128
     static __host__ __device__ constexpr int q_bytes(int tile) { return PARTS * BOXES * tile * 128; }
+    static __host__ __device__ constexpr int q_all(int tile) { return q_bytes(tile) * (tile == 32 ? 2 : 1); }
     // slots: the same bytes of K and V in flight, and V's wait for the softmax
     static constexpr int nk(int tile) {
-        const int n = (RING - q_bytes(tile)) * 9 / 20 / KSLOT;
+        const int n = (RING - q_all(tile)) * 9 / 20 / KSLOT;
         return n < kMaxSlots ? n : kMaxSlots;
     }
     static constexpr int nv(int tile) {
-        const int n = (RING - q_bytes(tile) - nk(tile) * KSLOT) / VSLOT;
+        const int n = (RING - q_all(tile) - nk(tile) * KSLOT) / VSLOT;
         return n < kMaxSlots ? n : kMaxSlots;
     }
     static_assert(nk(128) >= 2 * BOXES && nv(128) >= 4, "a unit of K and two of V");
     // (the MMA reads 128 rows of q whatever the tile is: what lies behind is shared memory of the ring)
-    static_assert(q_bytes(32) - 32 * 128 + 128 * 128 <= RING, "");
+    static_assert(q_all(32) - 32 * 128 + 128 * 128 <= RING, "");
     static constexpr size_t BYTES = 1024 + (size_t)RING;
 };
 
@@ -217,12 +219,11 @@ __device__ __forceinline__ void split_away(float a, float b, uint32_t& hi, uint3
     if ((lo & 0x7fffu) == 0 && a != 0.f) lo = (lo & 0xffff0000u) | (hi & 0x8000u) | 1u;
     if ((lo & 0x7fff0000u) == 0 && b != 0.f) lo = (lo & 0xffffu) | (hi & 0x80000000u) | 0x10000u;
 }
-// hi = rn(a, b), lo = rn((a, b) - hi), packed
-__device__ __forceinline__ void split_rn(float a, float b, uint32_t& hi, uint32_t& lo) {
-    const __half2 h = __floats2half2_rn(a, b);
-    const float2 f = __half22float2(h);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = pack2(a - f.x, b - f.y, f16());
+// weights as fp16 pairs: hi the upper 11 bits, lo the rest, packed
+__device__ __forceinline__ void split_bits(float a, float b, uint32_t& hi, uint32_t& lo) {
+    const float ha = __uint_as_float(__float_as_uint(a) & 0xffffe000u), hb = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
+    hi = pack2(ha, hb, f16());
+    lo = pack2(a - ha, b - hb, f16());
 }
 
 // which of the positions p0 .. p0 + 63 node `node` (mask words m) sees, as bits
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const unsigned nk = a.nk, nv = a.nv;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    unsigned char *ks = smem + L::q_bytes(tile), *vs = ks + nk * L::KSLOT;
+    unsigned char *ks = smem + L::q_all(tile), *vs = ks + nk * L::KSLOT;
     __shared__ __align__(8) uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
     __shared__ __align__(8) uint64_t q_ready, ends_ready, o_free, s_full[2], p_ready[2], pv_done[2];
     __shared__ uint32_t s_tmem;
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mb_init(v_full + i, 1);
             tc::mb_init(v_empty + i, 1);
         }
-        tc::mb_init(&q_ready, 8);
+        tc::mb_init(&q_ready, a.tile == 32 ? 6 : 8);
         tc::mb_init(&ends_ready, 8);
         tc::mb_init(&o_free, 8);
         for (int i = 0; i < 2; ++i) {
@@ -409,6 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         unsigned j = 0, slot = 0, phase = 0;
         for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
             if (!wait(&q_ready, n_seg)) break;
+            const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
             for (int u = g.u0; u < g.u1 && ok; ++u, ++j) {
                 // P of unit j - 2, which held these columns, is used up
                 if (j >= 2 && !wait(pv_done + (j & 1), (j - 2) >> 1)) break;
@@ -422,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int h = 0; h < PARTS; ++h)
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
-                                mma_ss(d, q0 + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
+                                mma_ss(d, qs + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
                                        idesc<C>(kUnit, false), (b | h | k) ? 1u : 0u);
                         commit(k_empty + slot);
                         if (b == BOXES - 1) commit(s_full + (j & 1));
@@ -467,17 +469,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         // node and query head of row `row` of a tile whose first row is `rem` heads into its first node
         auto node_of = [&](int rem, int row) { return (int)(((uint64_t)(unsigned)(rem + row) * a.group_inv) >> 32); };
         // q of the segment's rows (K-major, 128-byte swizzle: row r of 64 dims at r * 128, 16-byte
-        // chunk c at (c ^ (r & 7)) * 16), a few rows a step, steps over the eight warps.  Rows that do not
-        // exist keep what lies there: no one reads their lanes.
+        // chunk c at (c ^ (r & 7)) * 16), a few rows a step, steps over the loading warps: all of them,
+        // or for tiles of 32 rows those that have no row of the softmax.  Rows that do not exist keep
+        // what lies there: no one reads their lanes.
+        const int loader = tile == 32 ? (quarter ? grp * 3 + quarter - 1 : -1) : warp, loaders = tile == 32 ? 6 : 8;
         auto load_q = [&](const Seg& s, int parity) {
-            constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR, N = 4;  // lanes per row, rows per step, steps at once
+            if (loader < 0) return;
+            constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR, N = 8;  // lanes per row, rows per step, steps at once
             const int start = s.mt * tile, rows = min(s.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
-            const int e = (lane % LPR) * V;
-            for (int i0 = warp * RPI; i0 < rows; i0 += 8 * N * RPI) {
+            const int e = (lane % LPR) * V, stride = loaders * RPI;
+            unsigned char* to = smem + (tile == 32 ? parity * L::q_bytes(32) : 0) + (e >> 6) * tile * 128 + (e & 7) * 2;
+            for (int i0 = loader * RPI; i0 < rows; i0 += N * stride) {
                 uint4 x[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int r = i0 + i * 8 * RPI + lane / LPR;
+                    const int r = i0 + i * stride + lane / LPR;
                     x[i] = make_uint4(0, 0, 0, 0);
                     if (r < rows) {
                         const int node = node_of(rem, r), head = s.kvh * sh.group + rem + r - node * sh.group;
@@ -486,9 +492,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int r = i0 + i * 8 * RPI + lane / LPR;
-                    if (i0 + i * 8 * RPI >= rows) break;
-                    unsigned char* at = smem + (e >> 6) * tile * 128 + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4) + (e & 7) * 2;
+                    const int r = i0 + i * stride + lane / LPR;
+                    if (i0 + i * stride >= rows) break;
+                    unsigned char* at = to + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4);
                     if constexpr (PARTS == 1) {
                         if (r < rows) *reinterpret_cast<uint4*>(at) = x[i];
                     } else {
@@ -536,12 +542,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int first = (int)((j ^ (unsigned)grp) & 1u);  // this group's first unit of the segment
             const unsigned j_last = j + (unsigned)n - 1;
             float mx = -INFINITY, l = 0.f, sc = a.scale2;  // maximum that the weights are relative to, their sum
-            // the next rows' q, once all scores of this segment are there: before the softmax of the
-            // segment's last unit (the other group: after its own last one), so that the next scores are not late
+            // The next rows' q.  Tiles of 32 rows: now, into the other buffer.  Of 128: once all scores of this
+            // segment are there, before the softmax of its last unit (the other group: after its own
+            // last one), so that the next scores are not late.
             auto next_q = [&] {
                 more = walk_next(walk, sh, tile, g);
                 if (more) load_q(g, (int)((n_seg + 1) & 1));
             };
+            if (tile == 32) next_q();
             for (int i = first; i < n; i += 2) {
                 const unsigned ju = j + (unsigned)i;
                 const int p0 = (cur.u0 + i) * kUnit;
@@ -549,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::fence_after();
                 if constexpr (PARTS == 2)
                     if (i == first) sc = a.scale2 * s_scale[n_seg & 1][mine32];
-                if (i == n - 1) next_q();
+                if (i == n - 1 && tile != 32) next_q();
                 const bool tail = p0 + kUnit > all_seen;
                 if (tail) {  // V of positions that not every row sees
                     for (int half = 0; half < 2; ++half) {
@@ -586,68 +594,66 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (tail)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) seen[h] = visible(cur.q, sh.chain, m, node, p0 + 64 * h);
-                    uint32_t x0[32], x1[32];
-                    auto load = [&](int h) {  // scores of half of the unit
-                        ld32(ts + 64 * h, x0);
-                        ld32(ts + 64 * h + 32, x1);
+                    // 32 scores of the unit.  (Twice, once for the maximum and once for the weights, in loops that are not
+                    // unrolled: the code of a unit then is an eighth, and a kernel that has just started waits
+                    // for its instructions, 2 to 4 us with all of it unrolled.)
+                    uint32_t x[32];
+                    auto load = [&](int c) {
+                        ld32(ts + 32 * c, x);
                         wait_ld();
                         if (tail) {
-                            const uint32_t v0 = (uint32_t)seen[h], v1 = (uint32_t)(seen[h] >> 32);
+                            const uint32_t v = (uint32_t)((c & 2 ? seen[1] : seen[0]) >> (c & 1 ? 32 : 0));
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) {
-                                if (!(v0 >> k & 1u)) x0[k] = 0xff800000u;
-                                if (!(v1 >> k & 1u)) x1[k] = 0xff800000u;
-                            }
+                            for (int k = 0; k < 32; ++k)
+                                if (!(v >> k & 1u)) x[k] = 0xff800000u;
                         }
                     };
-                    float bm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float bm = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < kUnit / 32; ++c) {
+                        load(c);
+                        float bm4[4] = {bm, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        load(h);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) bm4[k & 3] = fmaxf(bm4[k & 3], fmaxf(__uint_as_float(x0[k]), __uint_as_float(x1[k])));
+                        for (int k = 0; k < 32; ++k) bm4[k & 3] = fmaxf(bm4[k & 3], __uint_as_float(x[k]));
+                        bm = fmaxf(fmaxf(bm4[0], bm4[1]), fmaxf(bm4[2], bm4[3]));
                     }
-                    const float bm = fmaxf(fmaxf(bm4[0], bm4[1]), fmaxf(bm4[2], bm4[3])) * sc;
+                    bm *= sc;
                     if (i == first) {
                         mx = bm;
                     } else if (__any_sync(0xffffffffu, bm > mx + kSlack)) {
                         // O and the sum move to the new maximum (all rows of the warp; the group's last unit
                         // is in O, as the scores took its place)
                         const float nm = fmaxf(mx, bm), f = nm == -INFINITY ? 1.f : ex2(mx - nm);
+#pragma unroll 1
                         for (int c = 0; c < HD; c += 32) {
-                            uint32_t o[32];
-                            ld32(tl + 128u * grp + c, o);
+                            ld32(tl + 128u * grp + c, x);
                             wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            st32(tl + 128u * grp + c, o);
+                            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+                            st32(tl + 128u * grp + c, x);
                         }
                         l *= f;
                         mx = nm;
-                        load(1);  // (not kept through the above)
                     }
                     // (a row that has seen nothing yet, or only scores of -inf: weights 0)
                     const float ref = (mx == -INFINITY ? 0.f : mx) - kShift;
-                    float l4[4] = {0.f, 0.f, 0.f, 0.f};
-                    // 32 weights in the place of their scores: 16 columns of pairs (hi), 16 of lo
-                    auto weights = [&](const uint32_t (&x)[32], uint32_t t) {
+#pragma unroll 1
+                    for (int c = 0; c < kUnit / 32; ++c) {
+                        load(c);
+                        float l4[4] = {0.f, 0.f, 0.f, 0.f};
+                        // 32 weights in the place of their scores: 16 columns of pairs (hi), 16 of lo
                         uint32_t ph[16], pl[16];
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             const float e0 = ex2(fmaf(__uint_as_float(x[2 * k]), sc, -ref)), e1 = ex2(fmaf(__uint_as_float(x[2 * k + 1]), sc, -ref));
                             l4[k & 3] += e0 + e1;
-                            if constexpr (PARTS == 2) split_rn(e0, e1, ph[k], pl[k]);
+                            if constexpr (PARTS == 2) split_bits(e0, e1, ph[k], pl[k]);
                             else ph[k] = pack2(e0, e1, C());
                         }
-                        st16(t, ph);
-                        if constexpr (PARTS == 2) st16(t + 16, pl);
-                    };
-                    weights(x0, ts + 64);
-                    weights(x1, ts + 96);
-                    load(0);
-                    weights(x0, ts);
-                    weights(x1, ts + 32);
-                    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                        st16(ts + 32 * c, ph);
+                        if constexpr (PARTS == 2) st16(ts + 32 * c + 16, pl);
+                        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                    }
                     wait_st();
                 }
                 tc::fence_before();
@@ -658,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             s_end[n_seg & 1][grp][mine32] = make_float2(mx == -INFINITY ? mx : mx - kShift, l);
             __syncwarp();
             if (lane == 0) arrive(&ends_ready);
-            if ((j_last & 1u) != (unsigned)grp) {
+            if (tile != 32 && (j_last & 1u) != (unsigned)grp) {
                 if (!wait(s_full + (j_last & 1), j_last >> 1)) break;
                 next_q();
             }
@@ -696,6 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     st[0] = top;
                     st[kTile] = sum;
                 }
+#pragma unroll 1
                 for (int c = grp * (HD / 2); c < (grp + 1) * (HD / 2); c += 32) {
                     uint32_t o[32];
                     ld32(tl + 128u * g0 + c, o);

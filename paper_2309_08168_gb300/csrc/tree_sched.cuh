@@ -80,9 +80,14 @@ __host__ __device__ __forceinline__ long long head_units(const Shape& s, const R
 __host__ __device__ __forceinline__ int ctas_of(long long units, int grid) {
     return units < 1 ? 1 : units < grid ? (int)units : grid;
 }
-__host__ __device__ __forceinline__ long long range_start(long long units, int ctas, int c) { return units * c / ctas; }
+// (in 32 bits where that is enough: a 64-bit division is some 100 instructions)
+__host__ __device__ __forceinline__ long long range_start(long long units, int ctas, int c) {
+    const long long x = units * c;
+    return x >> 32 ? x / ctas : (long long)((uint32_t)x / (uint32_t)ctas);
+}
 __host__ __device__ __forceinline__ int cta_of(long long units, int ctas, long long u) {
-    return (int)(((u + 1) * ctas - 1) / units);
+    const long long x = (u + 1) * ctas - 1;
+    return x >> 32 ? (int)(x / units) : (int)((uint32_t)x / (uint32_t)units);
 }
 
 // One CTA's share of an item: units [u0, u1) of n.
@@ -103,7 +108,7 @@ __host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int 
     w.b = b;
     w.q = q;
     const long long per = head_units(s, w.q, tile);
-    w.kvh = (int)(off / per);
+    w.kvh = (off | per) >> 32 ? (int)(off / per) : (int)((uint32_t)off / (uint32_t)per);
     off -= w.kvh * per;
     w.mt = 0;
     for (int n; off >= (n = units_of(s, w.q, tile, w.mt)); ++w.mt) off -= n;
