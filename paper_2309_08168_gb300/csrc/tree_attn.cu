@@ -17,10 +17,14 @@
 //   warp 11    : issues O += P V (P in TMEM over the columns of S, V as it lies in the
 //                cache, MN-major, N = hd);
 //   warps 0-3, 4-7 : softmax of the even and of the odd units, a row per thread: S from
-//                TMEM, P back to it, running maximum and sum, with an accumulator O of
-//                its own each.  At an item's end the two are joined (half of the dims
-//                each): O / sum, or O, maximum and sum to the workspace if other CTAs
-//                hold parts of the item.  join_kernel adds those.
+//                TMEM, P back to it.  Three units' S and P have a place, so that the tensor
+//                cores multiply for two while both groups work; there is one
+//                accumulator, and the maximum that weights are relative to goes from unit
+//                to unit, from a group's warp to the other's (before its weights are
+//                computed, so that the groups overlap).
+//   warps 12-15 : q of the next item to shared memory; at an item's end O / sum, or O,
+//                maximum and sum to the workspace if other CTAs hold parts of the
+//                item, while the others are at the next item.  join_kernel adds those.
 // The tile has 128 rows; 32 where no request has more, which leaves the ring the
 // shared memory of the other rows' q (their lanes then hold what no one reads).
 //
@@ -58,8 +62,8 @@ namespace {
 constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp16
 constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr int kTile = 128;  // rows: the TMEM lanes
-constexpr int kThreads = 384;
-constexpr int kTmem = 512;  // columns: O of even units at 0, of odd ones at 128, S / P at 256 and 384
+constexpr int kThreads = 512;
+constexpr int kTmem = 512;  // columns: O at 0, S / P of unit j at 128 + 128 (j mod 3)
 constexpr int kMaxSlots = 12;
 constexpr int kJoinThreads = 256, kJoinLines = 4;
 
@@ -112,7 +116,7 @@ struct Lay {
     static constexpr int KSLOT = kUnit * 128;         // 64 dims of a unit's K
     static constexpr int VBOX = 64 * 128;             // 64 dims of 64 positions of V
     static constexpr int VSLOT = BOXES * VBOX;
-    static constexpr int RING = 219 * 1024;           // shared memory for q and the rings
+    static constexpr int RING = 213 * 1024;           // shared memory for q and the rings
     // two buffers of a tile of 32 rows, one of 128
     static __host__ __device__ constexpr int q_bytes(int tile) { return PARTS * BOXES * tile * 128; }
     static __host__ __device__ constexpr int q_all(int tile) { return q_bytes(tile) * (tile == 32 ? 2 : 1); }
@@ -194,6 +198,35 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// two fp32 values in one register pair: fma, add and mul of both in one instruction
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 two(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void of_two(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // bounded wait; false after kWaitNs, or once another thread of the CTA has given up
 __device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail) {
     if (tc::mb_try(b, parity)) return true;
@@ -208,26 +241,30 @@ __device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile i
     return true;
 }
 
-// fp16 pair of x: hi towards zero, lo the rest, of the same sign and not 0 unless x is
-__device__ __forceinline__ void split_away(float a, float b, uint32_t& hi, uint32_t& lo) {
-    const __half2 h = __halves2half2(__float2half_rz(a), __float2half_rz(b));
-    const float2 f = __half22float2(h);
-    const float la = a - f.x, lb = b - f.y;
-    __half2 l = __floats2half2_rn(la, lb);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
-    if ((lo & 0x7fffu) == 0 && a != 0.f) lo = (lo & 0xffff0000u) | (hi & 0x8000u) | 1u;
-    if ((lo & 0x7fff0000u) == 0 && b != 0.f) lo = (lo & 0xffffu) | (hi & 0x80000000u) | 0x10000u;
+// the upper 11 bits of two values, and the rest
+__device__ __forceinline__ f32x2 upper(f32x2 v) { return v & 0xffffe000ffffe000ull; }
+__device__ __forceinline__ f32x2 rest(f32x2 v, f32x2 hi) { return fma2(hi, two(-1.f, -1.f), v); }
+__device__ __forceinline__ uint32_t half2_of(f32x2 v) {
+    float a, b;
+    of_two(v, a, b);
+    return pack2(a, b, f16());
 }
-// weights as fp16 pairs: hi the upper 11 bits, lo the rest, packed
-__device__ __forceinline__ void split_bits(float a, float b, uint32_t& hi, uint32_t& lo) {
-    const float ha = __uint_as_float(__float_as_uint(a) & 0xffffe000u), hb = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
-    hi = pack2(ha, hb, f16());
-    lo = pack2(a - ha, b - hb, f16());
+// fp16 pairs of two values of q: hi towards zero, lo the rest and 2^-24 of the value, so that it has
+// the value's sign and (down to 2^-16 of the row's largest value) is not 0
+__device__ __forceinline__ void split_away(f32x2 v, uint32_t& hi, uint32_t& lo) {
+    const f32x2 h = upper(v);
+    hi = half2_of(h);
+    lo = half2_of(fma2(v, two(0x1p-24f, 0x1p-24f), rest(v, h)));
+}
+// weights as fp16 pairs: hi the upper 11 bits, lo the rest
+__device__ __forceinline__ void split_bits(f32x2 v, uint32_t& hi, uint32_t& lo) {
+    const f32x2 h = upper(v);
+    hi = half2_of(h);
+    lo = half2_of(rest(v, h));
 }
 
 // which of the positions p0 .. p0 + 63 node `node` (mask words m) sees, as bits
-__device__ __forceinline__ uint64_t visible(const Req& q, int chain, const uint64_t (&m)[4], int node, int p0) {
+__device__ __noinline__ uint64_t visible(const Req& q, int chain, const uint64_t (&m)[4], int node, int p0) {
     const int end = q.total - p0;  // the unit's positions below it exist
     uint64_t v;
     if (chain) {
@@ -249,8 +286,72 @@ __device__ __forceinline__ uint64_t visible(const Req& q, int chain, const uint6
     return end >= 64 ? v : end <= 0 ? 0ull : v & ((1ull << end) - 1ull);
 }
 
+// (one copy for all roles)
+__device__ __noinline__ bool next_seg(Walk& w, const Shape& s, int tile, Seg& g) { return walk_next(w, s, tile, g); }
+
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, f16) { return ((u & 0x7c00u) == 0x7c00u) | ((u & 0x7c000000u) == 0x7c000000u) << 1; }
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, bf16) { return ((u & 0x7f80u) == 0x7f80u) | ((u & 0x7f800000u) == 0x7f800000u) << 1; }
+
+// 0 if both values are finite, else a NaN in some half
+__device__ __forceinline__ uint32_t finite2(uint32_t u, uint32_t acc, f16) {
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&u), __float2half2_rn(0.f), *reinterpret_cast<const __half2*>(&acc));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t finite2(uint32_t u, uint32_t acc, bf16) {
+    const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&u), __float2bfloat162_rn(0.f), *reinterpret_cast<const __nv_bfloat162*>(&acc));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Rows lo .. hi - 1 of 64 positions of V in shared memory, of which those from end on
+// do not exist: zeros there, and in the place of values that are not finite.  By 128 threads.
+template <typename C, int HD>
+__device__ __noinline__ void clean_v(unsigned char* v8, int lo, int end, int hi, int t, int* odd_seen) {
+    constexpr int PER_ROW = HD / 8;  // 16-byte pieces
+    auto piece = [&](int c) {
+        const int r = lo + c / PER_ROW, k = c % PER_ROW;
+        return reinterpret_cast<uint4*>(v8 + (k >> 3) * (64 * 128) + r * 128 + (k & 7) * 16);
+    };
+    const int n = (max(end - lo, 0)) * PER_ROW, all = (hi - lo) * PER_ROW;
+#pragma unroll 1
+    for (int c = t; c < all; c += kTile) {
+        uint4* v = piece(c);
+        if (c >= n) {
+            *v = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        uint32_t w[4] = {v->x, v->y, v->z, v->w};
+        if (!exps_all_ones(finite2(w[0], finite2(w[1], finite2(w[2], finite2(w[3], 0, C()), C()), C()), C()), C())) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t odd = exps_all_ones(w[k], C());
+            w[k] &= (odd & 1 ? 0u : 0xffffu) | (odd & 2 ? 0u : 0xffff0000u);
+        }
+        *v = make_uint4(w[0], w[1], w[2], w[3]);
+        *(volatile int*)odd_seen = 1;
+    }
+}
+
+// Adds to 32 dims from c on of a row's sums the values that are not finite, of the
+// segment's nodes that the row sees (they were left out of the products).
+template <typename C>
+__device__ __noinline__ void add_odd(const AttnOpArgs& a, const Seg& g, int node, int c, uint32_t (&o)[32]) {
+    const Shape& sh = a.shape;
+    uint64_t m[4] = {0, 0, 0, 0};
+    if (!sh.chain)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(g.q.r0 + node) * a.words + w);
+    for (int x = max(g.u0 * kUnit, g.q.len); x < min(g.u1 * kUnit, g.q.total); ++x) {
+        if (!(visible(g.q, sh.chain, m, node, x) & 1)) continue;
+        const int page = __ldcg(a.block_table + (size_t)g.b * sh.max_blocks + x / sh.page_size);
+        if (page < 0 || page >= a.n_pages) continue;
+        const C* v = (const C*)a.vc + page * a.page_stride + g.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + c;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float f = (float)v[i];
+            if (!isfinite(f)) o[i] = __float_as_uint(__uint_as_float(o[i]) + f);
+        }
+    }
+}
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -264,14 +365,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *ks = smem + L::q_all(tile), *vs = ks + nk * L::KSLOT;
     __shared__ __align__(8) uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
-    __shared__ __align__(8) uint64_t q_ready, ends_ready, o_free, s_full[2], p_ready[2], pv_done[2];
+    __shared__ __align__(8) uint64_t q_ready, q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
     __shared__ long long s_sum[kThreads / 32], s_off;
     __shared__ int s_b;
     __shared__ Req s_req;  // the request that the range starts in
-    __shared__ float s_scale[2][kTile];     // [segment & 1]: power of two that a row of q was divided by
-    __shared__ float2 s_end[2][2][kTile];   // [segment & 1][group]: a row's maximum and sum
+    // (four segments: scores are at most three units ahead of the accumulator)
+    __shared__ float s_scale[4][kTile];    // [segment & 3]: power of two that a row of q was divided by
+    __shared__ float2 s_end[4][2][kTile];  // [segment & 3][group]: what a row's weights are relative to, and their sum
+    __shared__ float s_ref[2][kTile];      // [group]: the same after the group's last unit
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         s_fail = s_odd = 0;
@@ -282,13 +385,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mb_init(v_full + i, 1);
             tc::mb_init(v_empty + i, 1);
         }
-        tc::mb_init(&q_ready, a.tile == 32 ? 6 : 8);
-        tc::mb_init(&ends_ready, 8);
-        tc::mb_init(&o_free, 8);
-        for (int i = 0; i < 2; ++i) {
+        tc::mb_init(&q_ready, 4);
+        tc::mb_init(&q_free, 1);
+        tc::mb_init(&o_free, 4);
+        for (int i = 0; i < 3; ++i) {
             tc::mb_init(s_full + i, 1);
-            tc::mb_init(p_ready + i, 4);
+            tc::mb_init(&p_ready[i][0], 4);
+            tc::mb_init(&p_ready[i][1], 4);
             tc::mb_init(pv_done + i, 1);
+        }
+        for (int i = 0; i < 4; ++i) {
+            tc::mb_init(ends_ready + i, 8);
+            tc::mb_init(&ref_ready[0][i], 1);
+            tc::mb_init(&ref_ready[1][i], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -347,13 +456,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::fence_after();
     const uint32_t tmem = s_tmem;
     Walk walk;
-    walk_init(walk, sh, tile, s_b, s_req, s_off, hi - lo);
+    walk_init(walk, sh, tile, s_b, s_req, s_off, lo, hi - lo);
     Seg g;
     bool ok = true;
     auto wait = [&](uint64_t* b, unsigned phase) {
         ok = ok && __all_sync(0xffffffffu, mb_wait(b, phase & 1u, &s_fail));
         return ok;
     };
+
+    // node of row `row` of a tile whose first row is `rem` heads into its first node, from that node on
+    auto node_of = [&](int rem, int row) { return (int)(((uint64_t)(unsigned)(rem + row) * a.group_inv) >> 32); };
 
     if (warp == 8 || warp == 9) {
         // page ids are asked for 32 copies (of one 64-dim half) ahead, one per lane
@@ -370,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool mine_too = lane < (is_v ? copies * BOXES : copies);
         const unsigned bytes = is_v ? L::VSLOT : L::KSLOT;
         unsigned slot = 0, phase = 1;
-        while (ok && walk_next(walk, sh, tile, g)) {
+        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
             const int32_t* table = a.block_table + (size_t)g.b * sh.max_blocks;
             auto fetch = [&](long long x) {  // page of this lane's copy of the 32 from x on; -1: outside, reads as zeros
                 x += lane << a.box_shift;
@@ -402,24 +514,32 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 __syncwarp();
                 if (++slot == n_slots) slot = 0, phase ^= 1u;
+                if (!is_v && n_seg && i == BOXES) {  // the rows of q that will be asked for at the end of the segment before, into L2
+                    const int start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
+                    for (int r = lane; r < rows; r += 32) {
+                        const int node = node_of(rem, r), head = g.kvh * sh.group + rem + r - node * sh.group;
+                        const T* row = (const T*)a.q + (int64_t)(g.q.r0 + node0 + node) * a.q_stride + head * HD;
+                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "n"(HD * sizeof(T)) : "memory");
+                    }
+                }
             }
         }
     } else if (warp == 10) {
         const uint64_t q0 = tc::sdesc(smem_u32(smem)), k0 = tc::sdesc(smem_u32(ks));
         const uint32_t qb = (uint32_t)tile * 128;  // 64 dims of the tile's q
-        unsigned j = 0, slot = 0, phase = 0;
-        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+        unsigned slot = 0, phase = 0, buf = 0, turn = 0;  // unit 3 turn + buf
+        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
             if (!wait(&q_ready, n_seg)) break;
             const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
-            for (int u = g.u0; u < g.u1 && ok; ++u, ++j) {
-                // P of unit j - 2, which held these columns, is used up
-                if (j >= 2 && !wait(pv_done + (j & 1), (j - 2) >> 1)) break;
+            for (int u = g.u0; u < g.u1 && ok; ++u) {
+                // P of unit j - 3, which held these columns, is used up
+                if (turn && !wait(pv_done + buf, turn - 1)) break;
 #pragma unroll
                 for (int b = 0; b < BOXES; ++b) {
                     if (!wait(k_full + slot, phase)) break;
                     tc::fence_after();
                     if (elect_one()) {
-                        const uint32_t d = tmem + 256u + 128u * (j & 1);
+                        const uint32_t d = tmem + 128u + 128u * buf;
 #pragma unroll
                         for (int h = 0; h < PARTS; ++h)
 #pragma unroll
@@ -427,92 +547,100 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 mma_ss(d, qs + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
                                        idesc<C>(kUnit, false), (b | h | k) ? 1u : 0u);
                         commit(k_empty + slot);
-                        if (b == BOXES - 1) commit(s_full + (j & 1));
+                        if (b == BOXES - 1) {
+                            commit(s_full + buf);
+                            if (u == g.u1 - 1) commit(&q_free);
+                        }
                     }
                     __syncwarp();
                     if (++slot == nk) slot = 0, phase ^= 1u;
                 }
+                if (++buf == 3) buf = 0, ++turn;
             }
         }
     } else if (warp == 11) {
         // V: hd dims (MN) x 16 positions (K) per MMA; 8 positions are 1024 bytes apart, 64 dims a box
         const uint64_t v0 = tc::sdesc(smem_u32(vs)) + ((uint64_t)((L::VBOX >> 4) - 1) << 16);
-        unsigned j = 0, slot = 0, phase = 0;
-        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
-            for (int u = g.u0; u < g.u1 && ok; ++u, ++j) {
-                if (!wait(p_ready + (j & 1), j >> 1)) break;
-                const bool fresh = u - g.u0 < 2;  // the group's first unit of the segment
+        unsigned slot = 0, phase = 0, buf = 0, turn = 0;
+        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+            for (int u = g.u0; u < g.u1 && ok; ++u) {
+                const bool fresh = u == g.u0;
                 if (fresh && n_seg && !wait(&o_free, n_seg - 1)) break;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    if (!wait(v_full + slot, phase)) break;
+                    if (!wait(&p_ready[buf][half], turn) || !wait(v_full + slot, phase)) break;
                     tc::fence_after();
                     if (elect_one()) {
-                        const uint32_t p = tmem + 256u + 128u * (j & 1) + 64u * half, o = tmem + 128u * (j & 1);
+                        const uint32_t p = tmem + 128u + 128u * buf + 64u * half;
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
 #pragma unroll
                             for (int h = 0; h < PARTS; ++h)
-                                mma_ts(o, p + 32u * (k >> 1) + 16u * h + 8u * (k & 1), v0 + (uint64_t)((slot * L::VSLOT + k * 2048) >> 4), idesc<C>(HD, true),
+                                mma_ts(tmem, p + 32u * (k >> 1) + 16u * h + 8u * (k & 1), v0 + (uint64_t)((slot * L::VSLOT + k * 2048) >> 4), idesc<C>(HD, true),
                                        (!fresh || half || k || h) ? 1u : 0u);
                         commit(v_empty + slot);
-                        if (half) commit(pv_done + (j & 1));
+                        if (half) commit(pv_done + buf);
                     }
                     __syncwarp();
                     if (++slot == nv) slot = 0, phase ^= 1u;
                 }
+                if (++buf == 3) buf = 0, ++turn;
             }
         }
-    } else {
-        const int grp = warp >> 2, quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
-        const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16), ts = tl + 256u + 128u * grp;
-        // node and query head of row `row` of a tile whose first row is `rem` heads into its first node
-        auto node_of = [&](int rem, int row) { return (int)(((uint64_t)(unsigned)(rem + row) * a.group_inv) >> 32); };
+    } else if (warp >= 12) {
+        const int quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
+        const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16);
         // q of the segment's rows (K-major, 128-byte swizzle: row r of 64 dims at r * 128, 16-byte
-        // chunk c at (c ^ (r & 7)) * 16), a few rows a step, steps over the loading warps: all of them,
-        // or for tiles of 32 rows those that have no row of the softmax.  Rows that do not exist keep
-        // what lies there: no one reads their lanes.
-        const int loader = tile == 32 ? (quarter ? grp * 3 + quarter - 1 : -1) : warp, loaders = tile == 32 ? 6 : 8;
-        auto load_q = [&](const Seg& s, int parity) {
-            if (loader < 0) return;
-            constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR, N = 8;  // lanes per row, rows per step, steps at once
+        // chunk c at (c ^ (r & 7)) * 16), a few rows a step, steps over the four warps.  Rows that do not
+        // exist keep what lies there: no one reads their lanes.
+        // fp32 rows come as they are into the place of their pairs - a row has 16 bytes of each for 16 bytes of dims -
+        // and are converted there.
+        auto load_q = [&](const Seg& s, unsigned n_seg) {
+            constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR;  // lanes per row, rows per step
             const int start = s.mt * tile, rows = min(s.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
-            const int e = (lane % LPR) * V, stride = loaders * RPI;
-            unsigned char* to = smem + (tile == 32 ? parity * L::q_bytes(32) : 0) + (e >> 6) * tile * 128 + (e & 7) * 2;
-            for (int i0 = loader * RPI; i0 < rows; i0 += N * stride) {
-                uint4 x[N];
+            const int piece = lane % LPR;
+            const uint32_t box = (uint32_t)tile * 128;
+            unsigned char* to = smem + (tile == 32 ? (n_seg & 1) * L::q_bytes(32) : 0) + (piece >> 3) * box;
+#pragma unroll 1
+            for (int r = quarter * RPI + lane / LPR; r < rows; r += 4 * RPI) {
+                const int node = node_of(rem, r), head = s.kvh * sh.group + rem + r - node * sh.group;
+                const T* from = (const T*)a.q + (int64_t)(s.q.r0 + node0 + node) * a.q_stride + head * HD + piece * V;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4))), "l"(from) : "memory");
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+            if constexpr (PARTS == 2) {
+                constexpr int N = 4;  // steps at once
+                const int e = piece * V;
+                unsigned char* hi = smem + (tile == 32 ? (n_seg & 1) * L::q_bytes(32) : 0) + (e >> 6) * box + (e & 7) * 2;
+#pragma unroll 1
+                for (int i0 = quarter * RPI + lane / LPR; i0 - lane / LPR < rows; i0 += N * 4 * RPI) {
+                    uint4 x[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int r = i0 + i * stride + lane / LPR;
-                    x[i] = make_uint4(0, 0, 0, 0);
-                    if (r < rows) {
-                        const int node = node_of(rem, r), head = s.kvh * sh.group + rem + r - node * sh.group;
-                        x[i] = __ldcg(reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(s.q.r0 + node0 + node) * a.q_stride + head * HD + e));
+                    for (int i = 0; i < N; ++i) {
+                        const int r = min(i0 + i * 4 * RPI, tile - 1);
+                        x[i] = *reinterpret_cast<const uint4*>(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
                     }
-                }
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int r = i0 + i * stride + lane / LPR;
-                    if (i0 + i * stride >= rows) break;
-                    unsigned char* at = to + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4);
-                    if constexpr (PARTS == 1) {
-                        if (r < rows) *reinterpret_cast<uint4*>(at) = x[i];
-                    } else {
+                    for (int i = 0; i < N; ++i) {
+                        const int r = i0 + i * 4 * RPI;
                         float f[4];
                         Vec<float>::get(x[i], f);
-                        float m = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
-#pragma unroll
-                        for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                        // 2^e2 with the row's largest value at 2^9 .. 2^10 of it (zeros and the smallest values: as if that were 2^-117)
-                        const int e2 = min(max((int)(__float_as_uint(m) >> 23), 10), 254) - 127 - 9;
+                        // the row's largest absolute value (as bits: their order is the same, NaN above all)
+                        const float m = fmaxf(max3(fabsf(f[0]), fabsf(f[1]), fabsf(f[2])), fabsf(f[3]));
+                        const uint32_t top = __reduce_max_sync(LPR == 32 ? 0xffffffffu : lane < 16 ? 0xffffu : 0xffff0000u, __float_as_uint(m));
+                        // 2^e2 with that at 2^14 .. 2^15 of it (zeros and the smallest values: as if it were 2^-111)
+                        const int e2 = min(max((int)(top >> 23), 16), 254) - 127 - 14;
                         const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
                         uint2 h, l;
-                        split_away(f[0] * down, f[1] * down, h.x, l.x);
-                        split_away(f[2] * down, f[3] * down, h.y, l.y);
+                        split_away(mul2(two(f[0], f[1]), two(down, down)), h.x, l.x);
+                        split_away(mul2(two(f[2], f[3]), two(down, down)), h.y, l.y);
                         if (r < rows) {
+                            unsigned char* at = hi + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4);
                             *reinterpret_cast<uint2*>(at) = h;
-                            *reinterpret_cast<uint2*>(at + BOXES * tile * 128) = l;
-                            if (lane % LPR == 0) s_scale[parity][r] = __uint_as_float((uint32_t)(127 + e2) << 23);
+                            *reinterpret_cast<uint2*>(at + BOXES * box) = l;
+                            if (piece == 0) s_scale[n_seg & 3][r] = __uint_as_float((uint32_t)(127 + e2) << 23);
                         }
                     }
                 }
@@ -521,161 +649,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             if (lane == 0) arrive(&q_ready);
         };
-
-        unsigned j = 0;  // of the segment's first unit
-        bool more = walk_next(walk, sh, tile, g);
+        bool more = next_seg(walk, sh, tile, g);
         if (more) load_q(g, 0);
-        long long at = lo;  // global unit of the segment's start
+        unsigned j_end = 0;  // units of the CTA up to the segment's end
         for (unsigned n_seg = 0; more && ok; ++n_seg) {
             const Seg cur = g;
-            const int n = cur.u1 - cur.u0, start = cur.mt * tile, rows = min(cur.q.n * sh.group - start, tile);  // units; rows that exist
-            const bool active = quarter * 32 < rows, valid = mine32 < rows;
-            const int node0 = start / sh.group, rem = start - node0 * sh.group, row = min(mine32, rows - 1);
-            const int node = node0 + node_of(rem, row), head = cur.kvh * sh.group + rem + row - (node - node0) * sh.group;
-            uint64_t m[4] = {0, 0, 0, 0};
-            if (!sh.chain && valid)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(cur.q.r0 + node) * a.words + w);
-            // positions below it are seen by every row of the tile
-            const int all_seen = min(sh.chain ? cur.q.len + node0 + 1 : cur.q.len, cur.q.total);
-            const int first = (int)((j ^ (unsigned)grp) & 1u);  // this group's first unit of the segment
-            const unsigned j_last = j + (unsigned)n - 1;
-            float mx = -INFINITY, l = 0.f, sc = a.scale2;  // maximum that the weights are relative to, their sum
-            // The next rows' q.  Tiles of 32 rows: now, into the other buffer.  Of 128: once all scores of this
-            // segment are there, before the softmax of its last unit (the other group: after its own
-            // last one), so that the next scores are not late.
-            auto next_q = [&] {
-                more = walk_next(walk, sh, tile, g);
-                if (more) load_q(g, (int)((n_seg + 1) & 1));
-            };
-            if (tile == 32) next_q();
-            for (int i = first; i < n; i += 2) {
-                const unsigned ju = j + (unsigned)i;
-                const int p0 = (cur.u0 + i) * kUnit;
-                if (!wait(s_full + grp, ju >> 1)) break;
-                tc::fence_after();
-                if constexpr (PARTS == 2)
-                    if (i == first) sc = a.scale2 * s_scale[n_seg & 1][mine32];
-                if (i == n - 1 && tile != 32) next_q();
-                const bool tail = p0 + kUnit > all_seen;
-                if (tail) {  // V of positions that not every row sees
-                    for (int half = 0; half < 2; ++half) {
-                        const unsigned s = 2 * ju + half;
-                        const int x0 = p0 + 64 * half, lo_row = max(min(cur.q.len, cur.q.total) - x0, 0);
-                        // (copies that begin behind the last position have brought zeros)
-                        const int hi_row = min((max(cur.q.total - x0, 0) + (1 << a.box_shift) - 1) >> a.box_shift << a.box_shift, 64);
-                        if (lo_row >= hi_row) continue;
-                        if (!wait(v_full + s % nv, s / nv)) break;
-                        unsigned char* v8 = vs + s % nv * L::VSLOT;
-                        for (int c = tid & (kTile - 1); c < (hi_row - lo_row) * 8 * BOXES; c += kTile) {
-                            const int r = lo_row + (BOXES == 2 ? c >> 4 : c >> 3);
-                            uint4* v = reinterpret_cast<uint4*>(v8 + (BOXES == 2 ? (c >> 3 & 1) * L::VBOX : 0) + r * 128 + (c & 7) * 16);
-                            if (x0 + r >= cur.q.total) {
-                                *v = make_uint4(0, 0, 0, 0);
-                                continue;
-                            }
-                            uint32_t w[4] = {v->x, v->y, v->z, v->w}, odd = 0;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) odd |= exps_all_ones(w[k], C()) << (2 * k);
-                            if (odd) {
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) w[k] &= (odd >> (2 * k) & 1 ? 0u : 0xffffu) | (odd >> (2 * k) & 2 ? 0u : 0xffff0000u);
-                                *v = make_uint4(w[0], w[1], w[2], w[3]);
-                                *(volatile int*)&s_odd = 1;
-                            }
-                        }
-                    }
-                    if (!ok) break;
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
-                if (active) {
-                    uint64_t seen[2] = {~0ull, ~0ull};
-                    if (tail)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) seen[h] = visible(cur.q, sh.chain, m, node, p0 + 64 * h);
-                    // 32 scores of the unit.  (Twice, once for the maximum and once for the weights, in loops that are not
-                    // unrolled: the code of a unit then is an eighth, and a kernel that has just started waits
-                    // for its instructions, 2 to 4 us with all of it unrolled.)
-                    uint32_t x[32];
-                    auto load = [&](int c) {
-                        ld32(ts + 32 * c, x);
-                        wait_ld();
-                        if (tail) {
-                            const uint32_t v = (uint32_t)((c & 2 ? seen[1] : seen[0]) >> (c & 1 ? 32 : 0));
-#pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (!(v >> k & 1u)) x[k] = 0xff800000u;
-                        }
-                    };
-                    float bm = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < kUnit / 32; ++c) {
-                        load(c);
-                        float bm4[4] = {bm, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) bm4[k & 3] = fmaxf(bm4[k & 3], __uint_as_float(x[k]));
-                        bm = fmaxf(fmaxf(bm4[0], bm4[1]), fmaxf(bm4[2], bm4[3]));
-                    }
-                    bm *= sc;
-                    if (i == first) {
-                        mx = bm;
-                    } else if (__any_sync(0xffffffffu, bm > mx + kSlack)) {
-                        // O and the sum move to the new maximum (all rows of the warp; the group's last unit
-                        // is in O, as the scores took its place)
-                        const float nm = fmaxf(mx, bm), f = nm == -INFINITY ? 1.f : ex2(mx - nm);
-#pragma unroll 1
-                        for (int c = 0; c < HD; c += 32) {
-                            ld32(tl + 128u * grp + c, x);
-                            wait_ld();
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-                            st32(tl + 128u * grp + c, x);
-                        }
-                        l *= f;
-                        mx = nm;
-                    }
-                    // (a row that has seen nothing yet, or only scores of -inf: weights 0)
-                    const float ref = (mx == -INFINITY ? 0.f : mx) - kShift;
-#pragma unroll 1
-                    for (int c = 0; c < kUnit / 32; ++c) {
-                        load(c);
-                        float l4[4] = {0.f, 0.f, 0.f, 0.f};
-                        // 32 weights in the place of their scores: 16 columns of pairs (hi), 16 of lo
-                        uint32_t ph[16], pl[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float e0 = ex2(fmaf(__uint_as_float(x[2 * k]), sc, -ref)), e1 = ex2(fmaf(__uint_as_float(x[2 * k + 1]), sc, -ref));
-                            l4[k & 3] += e0 + e1;
-                            if constexpr (PARTS == 2) split_bits(e0, e1, ph[k], pl[k]);
-                            else ph[k] = pack2(e0, e1, C());
-                        }
-                        st16(ts + 32 * c, ph);
-                        if constexpr (PARTS == 2) st16(ts + 32 * c + 16, pl);
-                        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-                    }
-                    wait_st();
-                }
-                tc::fence_before();
-                __syncwarp();
-                if (lane == 0) arrive(p_ready + grp);
+            const int start = cur.mt * tile, rows = min(cur.q.n * sh.group - start, tile);
+            const bool valid = mine32 < rows, whole = cur.u0 == 0 && cur.u1 == cur.n;
+            j_end += (unsigned)(cur.u1 - cur.u0);
+            const unsigned buf = (j_end - 1) % 3, turn = (j_end - 1) / 3;  // of the segment's last unit
+            // The next rows' q: into the other buffer (the last segment but this one is finished), or, with
+            // one buffer, once all scores of this segment are there
+            more = next_seg(walk, sh, tile, g);
+            if (more) {
+                if (tile != 32 && !wait(&q_free, n_seg)) break;
+                load_q(g, n_seg + 1);
             }
-            if (!ok) break;
-            s_end[n_seg & 1][grp][mine32] = make_float2(mx == -INFINITY ? mx : mx - kShift, l);
-            __syncwarp();
-            if (lane == 0) arrive(&ends_ready);
-            if (tile != 32 && (j_last & 1u) != (unsigned)grp) {
-                if (!wait(s_full + (j_last & 1), j_last >> 1)) break;
-                next_q();
-            }
-            const bool whole = cur.u0 == 0 && cur.u1 == cur.n;
             const int slot = n_seg ? 1 : 0;
-            if (tid == 0 && cur.u1 < cur.n) {
-                const long long item = at - cur.u0;  // global unit of the item's start
+            if (tid == 12 * 32 && cur.u1 < cur.n) {
                 Cut c;
-                c.first = cta_of(units, ctas, item);
-                c.last = cta_of(units, ctas, item + cur.n - 1);
-                c.first_slot = range_start(units, ctas, c.first) == item ? 0 : 1;
+                holders(cur, units, ctas, c.first, c.last, c.first_slot);
                 c.row0 = start;
                 c.rows = rows;
                 c.r0 = cur.q.r0;
@@ -683,57 +676,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                 c.pad = 0;
                 a.cuts[cta] = c;
             }
-            at += n;
-            // both accumulators: this group writes half of the dims of their sum
-            if (!wait(&ends_ready, n_seg) || !wait(pv_done + (j_last & 1), j_last >> 1)) break;
-            const bool both = n > 1;  // else only the group of the one unit has an accumulator
-            if (both && !wait(pv_done + ((j_last - 1) & 1), (j_last - 1) >> 1)) break;
+            const int node0 = start / sh.group, rem = start - node0 * sh.group, row = min(mine32, rows - 1);
+            const int node = node0 + node_of(rem, row), head = cur.kvh * sh.group + rem + row - (node - node0) * sh.group;
+            if (!wait(ends_ready + (n_seg & 3), n_seg >> 2) || !wait(pv_done + buf, turn)) break;
             tc::fence_after();
-            if (active) {
-                const int g0 = (int)(j & 1u);  // group of the first unit
-                const float2 e0 = s_end[n_seg & 1][g0][mine32], e1 = s_end[n_seg & 1][g0 ^ 1][mine32];
-                const float top = both ? fmaxf(e0.x, e1.x) : e0.x;
-                const float f0 = e0.x == -INFINITY ? 0.f : ex2(e0.x - top), f1 = !both || e1.x == -INFINITY ? 0.f : ex2(e1.x - top);
-                const float sum = both ? fmaf(e0.y, f0, e1.y * f1) : e0.y;
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            if (quarter * 32 < rows) {
+                // the last unit's group has what the accumulator is relative to now
+                const int last = (int)((j_end - 1) & 1u);
+                const float2 e = s_end[n_seg & 3][last][mine32], f = s_end[n_seg & 3][last ^ 1][mine32];
+                const float sum = e.y + f.y * (f.x == -INFINITY ? 0.f : ex2(f.x - e.x)), inv = sum == 0.f ? 0.f : 1.f / sum;
                 const bool odd = *(volatile int*)&s_odd;
-                if (!whole && valid && grp == 0) {
+                if (!whole && valid) {
                     float* st = a.stats + (size_t)(cta * 2 + slot) * 2 * kTile + mine32;
-                    st[0] = top;
+                    st[0] = e.x;
                     st[kTile] = sum;
                 }
 #pragma unroll 1
-                for (int c = grp * (HD / 2); c < (grp + 1) * (HD / 2); c += 32) {
+                for (int c = 0; c < HD; c += 32) {
                     uint32_t o[32];
-                    ld32(tl + 128u * g0 + c, o);
-                    if (both) {
-                        uint32_t o1[32];
-                        ld32(tl + 128u * (g0 ^ 1) + c, o1);
-                        wait_ld();
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o[k]), f0, __uint_as_float(o1[k]) * f1));
-                    } else {
-                        wait_ld();
-                    }
+                    ld32(tl + c, o);
+                    wait_ld();
                     if (!valid) continue;
-                    if (odd) {  // values that are not finite, of nodes that this row sees
-                        for (int u = cur.u0; u < cur.u1; ++u) {
-                            const int p0 = u * kUnit;
-                            if (p0 + kUnit <= cur.q.len) continue;
-                            for (int k = 0; k < kUnit; ++k) {
-                                const int x = p0 + k;
-                                if (x < cur.q.len || !(visible(cur.q, sh.chain, m, node, x) & 1)) continue;
-                                const int page = __ldcg(a.block_table + (size_t)cur.b * sh.max_blocks + x / sh.page_size);
-                                if (page < 0 || page >= a.n_pages) continue;
-                                const C* vr = (const C*)a.vc + page * a.page_stride + cur.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + c;
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    const float f = (float)vr[i];
-                                    if (!isfinite(f)) o[i] = __float_as_uint(__uint_as_float(o[i]) + f);
-                                }
-                            }
-                        }
-                    }
+                    if (odd) add_odd<C>(a, cur, node, c, o);
                     if (whole) {
                         T* to = (T*)a.out + (int64_t)(cur.q.r0 + node) * a.out_stride + head * HD + c;
                         constexpr int V = Vec<T>::N;
@@ -755,6 +719,149 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::fence_before();
             __syncwarp();
             if (lane == 0) arrive(&o_free);
+        }
+    } else {
+        const int grp = warp >> 2, quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
+        const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16);
+        unsigned j = 0;  // of the segment's first unit
+        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+            const int n = g.u1 - g.u0, start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile);  // units; rows that exist
+            const bool active = quarter * 32 < rows;
+            const int node0 = start / sh.group, node = node0 + node_of(start - node0 * sh.group, min(mine32, rows - 1));
+            uint64_t m[4] = {0, 0, 0, 0};
+            if (!sh.chain && mine32 < rows)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(g.q.r0 + node) * a.words + w);
+            // positions below it are seen by every row of the tile
+            const int all_seen = min(sh.chain ? g.q.len + node0 + 1 : g.q.len, g.q.total);
+            const int first = (int)((j ^ (unsigned)grp) & 1u);  // this group's first unit of the segment
+            float ref = -INFINITY, l = 0.f, sc = a.scale2;  // what the weights are relative to (and kShift), their sum
+            for (int i = first; i < n; i += 2) {
+                const unsigned ju = j + (unsigned)i, turn = ju / 3, buf = ju - 3 * turn;
+                const int p0 = (g.u0 + i) * kUnit;
+                const uint32_t ts = tl + 128u + 128u * buf;
+                if (!wait(s_full + buf, turn)) break;
+                tc::fence_after();
+                if constexpr (PARTS == 2)
+                    if (i == first) sc = a.scale2 * s_scale[n_seg & 3][mine32];
+                const bool tail = p0 + kUnit > all_seen;
+                // The weights of half of the unit are there: V, if some row does not see all of it, and the word to
+                // the multiplying warp.  (Unit ju - 2 is used up: then the slots' fills before these
+                // ones are complete, and the parity of the wait means these.)
+                auto half_done = [&](int half) {
+                    if (tail && ok) {
+                        const unsigned s = 2 * ju + half;
+                        const int x0 = p0 + 64 * half, lo_row = max(min(g.q.len, g.q.total) - x0, 0);
+                        // (copies that begin behind the last position have brought zeros)
+                        const int hi_row = min((max(g.q.total - x0, 0) + (1 << a.box_shift) - 1) >> a.box_shift << a.box_shift, 64);
+                        if (lo_row < hi_row && (ju < 2 || wait(pv_done + (ju - 2) % 3, (ju - 2) / 3)) && wait(v_full + s % nv, s / nv)) {
+                            clean_v<C, HD>(vs + s % nv * L::VSLOT, lo_row, min(g.q.total - x0, 64), hi_row, tid & (kTile - 1), &s_odd);
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        }
+                    }
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive(&p_ready[buf][half]);
+                };
+                if (active) {
+                    // 32 scores of the unit.  (Twice, once for the maximum and once for the weights, in loops that are not
+                    // unrolled: the code of a unit is an eighth of what it was unrolled, and takes fewer registers.)
+                    uint32_t x[32];
+                    auto load = [&](int c) {
+                        ld32(ts + 32 * c, x);
+                        wait_ld();
+                    };
+                    if (tail) {  // scores of positions that the row does not see: -inf
+                        uint64_t v = 0;
+#pragma unroll 1
+                        for (int c = 0; c < kUnit / 32; ++c) {
+                            v = c & 1 ? v >> 32 : visible(g.q, sh.chain, m, node, p0 + 32 * c);
+                            load(c);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (!((uint32_t)v >> k & 1u)) x[k] = 0xff800000u;
+                            st32(ts + 32 * c, x);
+                        }
+                        wait_st();
+                    }
+                    float bm = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < kUnit / 32; ++c) {
+                        load(c);
+                        float m4[4] = {bm, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) m4[k >> 1 & 3] = max3(m4[k >> 1 & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                        bm = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]);
+                    }
+                    bm = mine32 < rows ? bm * sc : -INFINITY;  // (lanes of no row hold anything)
+                    // from the unit before, and on to the next one (in every unit, so that the groups stay in step)
+                    float r = bm - kShift;
+                    if (ju && !wait(&ref_ready[grp ^ 1][quarter], (ju - 1) >> 1)) break;
+                    if (i > 0) {
+                        r = *(volatile float*)&s_ref[grp ^ 1][mine32];
+                        if (__any_sync(0xffffffffu, bm - kShift > r + kSlack)) {
+                            // the accumulator moves to the new maximum (all rows of the warp)
+                            const unsigned tb = (ju - 1) / 3, bb = ju - 1 - 3 * tb;
+                            if (!wait(pv_done + bb, tb)) break;
+                            tc::fence_after();
+                            const float nr = fmaxf(r, bm - kShift), f = nr == -INFINITY ? 1.f : ex2(r - nr);
+#pragma unroll 1
+                            for (int c = 0; c < HD; c += 32) {
+                                ld32(tl + c, x);
+                                wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+                                st32(tl + c, x);
+                            }
+                            r = nr;
+                        }
+                    }
+                    *(volatile float*)&s_ref[grp][mine32] = r;
+                    __syncwarp();
+                    if (lane == 0) arrive(&ref_ready[grp][quarter]);
+                    if (ref != -INFINITY) l *= ex2(ref - r);
+                    ref = r;
+                    // (a row that has seen nothing yet, or only scores of -inf: weights 0)
+                    const float sub = r == -INFINITY ? 0.f : r;
+#pragma unroll 1
+                    for (int c = 0; c < kUnit / 32; ++c) {
+                        load(c);
+                        f32x2 l4[4] = {0, 0, 0, 0};
+                        // 32 weights in the place of their scores: 16 columns of pairs (hi), 16 of lo
+                        uint32_t ph[16], pl[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            float e0, e1;
+                            of_two(fma2(two(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), two(sc, sc), two(-sub, -sub)), e0, e1);
+                            e0 = ex2(e0);
+                            e1 = ex2(e1);
+                            const f32x2 e = two(e0, e1);
+                            l4[k & 3] = add2(l4[k & 3], e);
+                            if constexpr (PARTS == 2) split_bits(e, ph[k], pl[k]);
+                            else ph[k] = pack2(e0, e1, C());
+                        }
+                        st16(ts + 32 * c, ph);
+                        if constexpr (PARTS == 2) st16(ts + 32 * c + 16, pl);
+                        float la, lb;
+                        of_two(add2(add2(l4[0], l4[1]), add2(l4[2], l4[3])), la, lb);
+                        l += la + lb;
+                        if (c & 1) {
+                            wait_st();
+                            half_done(c >> 1);
+                        }
+                    }
+                } else {
+                    if (ju && !wait(&ref_ready[grp ^ 1][quarter], (ju - 1) >> 1)) break;
+                    if (lane == 0) arrive(&ref_ready[grp][quarter]);
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) half_done(h);
+                }
+            }
+            if (!ok) break;
+            s_end[n_seg & 3][grp][mine32] = make_float2(ref, l);
+            __syncwarp();
+            if (lane == 0) arrive(ends_ready + (n_seg & 3));
             j += (unsigned)n;
         }
     }
@@ -776,12 +883,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Joins the parts of the items that range ends cut.  CTA c of the attention left a
 // Cut if its range ends inside an item; with n such ends in an item, n lines of CTAs
-// (gridDim.y each) share it here: a warp takes 32 rows (a lane each) and 16 dims at a
+// (gridDim.y each) share it here: a warp takes 32 rows (a lane each) and 16 bytes of dims at a
 // time, first the largest maximum of the parts, then the weighted sums, in the order
 // of the parts.  Bound by L2 latency: all loads of a few parts are under way at once.
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnOpArgs a) {
-    constexpr int W = kJoinThreads / 32, D = 16;
+    constexpr int W = kJoinThreads / 32, D = Vec<T>::N;
     pdl_launch_dependents();
     pdl_wait();
     const int cta = blockIdx.x, lane = threadIdx.x & 31;
@@ -794,12 +901,12 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnOpArgs a) 
         if (row >= rows) continue;
         auto part_of = [&](int p) { return (size_t)(p * 2 + (p == first ? slot : 0)); };
         float top = -INFINITY;
-#pragma unroll 8
+#pragma unroll 16
         for (int p = first; p <= last; ++p) top = fmaxf(top, __ldcg(a.stats + part_of(p) * 2 * kTile + row));
         float l = 0.f, o[D];
 #pragma unroll
         for (int i = 0; i < D; ++i) o[i] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int p = first; p <= last; ++p) {
             const float* st = a.stats + part_of(p) * 2 * kTile + row;
             const float m = __ldcg(st), lp = __ldcg(st + kTile);

@@ -3,9 +3,9 @@ functions are compiled with nvcc into a small program that draws batches and wal
 every CTA's range.
 
 Checked for each batch: every unit of every item is in exactly one CTA's range; the
-ranges differ by at most one unit; a CTA leaves at most two parts, the first of
-them in slot 0; and for an item that range ends cut, the CTAs that cta_of and
-range_start name are those that hold its parts, in order, with the slots they use.
+ranges differ by at most one unit, counted with what items count more; a CTA leaves
+at most two parts, that of its first segment in slot 0; and for an item that range ends cut,
+the CTAs that `holders` names are those that hold its parts, in order, with the slots they use.
 Tiles cover the rows, and a chain's tile stops at its last row's position.
 """
 import os
@@ -74,29 +74,27 @@ int main(int argc, char** argv) {
             int b = 0;
             while (!(before[b] <= lo && lo < before[b + 1])) ++b;
             Walk w;
-            walk_init(w, s, tile, b, req_of(s, b), lo - before[b], hi - lo);
+            walk_init(w, s, tile, b, req_of(s, b), lo - before[b], lo, hi - lo);
             Seg g;
-            long long at = lo;
             int n_parts = 0;
             for (bool first = true; walk_next(w, s, tile, g); first = false) {
                 const auto item = std::make_tuple(g.b, g.kvh, g.mt);
                 if (g.u0 >= g.u1 || g.u1 > g.n || g.kvh >= s.n_kv_heads || g.b >= B || g.q.n < 1) return bad("segment", it);
                 for (int u = g.u0; u < g.u1; ++u) {
-                    if (cta_of(U, ctas, at + u - g.u0) != c) return bad("cta_of", it);
+                    const long long at = g.item + kItemCost + u;
+                    if (cta_of(U, ctas, at) != c || at < lo || at >= hi) return bad("cta_of", it);
                     seen[item].push_back(u);
                 }
                 if (g.u0 > 0 || g.u1 < g.n) {
                     parts[item].push_back({c, first ? 0 : 1});
                     if (++n_parts > 2) return bad("three parts", it);
                     if (g.u1 < g.n) {
-                        const long long i0 = at - g.u0;
-                        const int f = cta_of(U, ctas, i0), l = cta_of(U, ctas, i0 + g.n - 1);
-                        cuts[item].push_back(std::make_tuple(f, l, range_start(U, ctas, f) == i0 ? 0 : 1));
+                        int f, l, later;
+                        holders(g, U, ctas, f, l, later);
+                        cuts[item].push_back(std::make_tuple(f, l, later));
                     }
                 }
-                at += g.u1 - g.u0;
             }
-            if (at != hi) return bad("range", it);
         }
         if (U && most - least > 1) return bad("balance", it);
         for (int b = 0; b < B; ++b) {
