@@ -228,9 +228,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // bounded wait; false after kWaitNs, or once another thread of the CTA has given up
-__device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail) {
-    if (tc::mb_try(b, parity)) return true;
+__device__ __noinline__ bool mb_wait_on(uint64_t* b, unsigned parity, volatile int* fail) {
     const unsigned long long t0 = tc::gtime();
+#pragma unroll 1
     while (!tc::mb_try(b, parity)) {
         if (*fail) return false;
         if (tc::gtime() - t0 > kWaitNs) {
@@ -239,6 +239,9 @@ __device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile i
         }
     }
     return true;
+}
+__device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail) {
+    return tc::mb_try(b, parity) || mb_wait_on(b, parity, fail);
 }
 
 // the upper 11 bits of two values, and the rest
@@ -330,27 +333,26 @@ __device__ __noinline__ void clean_v(unsigned char* v8, int lo, int end, int hi,
     }
 }
 
-// Adds to 32 dims from c on of a row's sums the values that are not finite, of the
-// segment's nodes that the row sees (they were left out of the products).
+// What the values that are not finite, of the segment's nodes that a row sees, add to dim d of its
+// sum (they were left out of the products).
 template <typename C>
-__device__ __noinline__ void add_odd(const AttnOpArgs& a, const Seg& g, int node, int c, uint32_t (&o)[32]) {
+__device__ __noinline__ float odd_sum(const AttnOpArgs& a, const Seg& g, int node, int d) {
     const Shape& sh = a.shape;
     uint64_t m[4] = {0, 0, 0, 0};
     if (!sh.chain)
 #pragma unroll
         for (int w = 0; w < 4; ++w)
             if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(g.q.r0 + node) * a.words + w);
+    float sum = 0.f;
+#pragma unroll 1
     for (int x = max(g.u0 * kUnit, g.q.len); x < min(g.u1 * kUnit, g.q.total); ++x) {
         if (!(visible(g.q, sh.chain, m, node, x) & 1)) continue;
         const int page = __ldcg(a.block_table + (size_t)g.b * sh.max_blocks + x / sh.page_size);
         if (page < 0 || page >= a.n_pages) continue;
-        const C* v = (const C*)a.vc + page * a.page_stride + g.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + c;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float f = (float)v[i];
-            if (!isfinite(f)) o[i] = __float_as_uint(__uint_as_float(o[i]) + f);
-        }
+        const float f = (float)((const C*)a.vc)[page * a.page_stride + g.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + d];
+        if (!isfinite(f)) sum += f;
     }
+    return sum;
 }
 
 template <typename T, int HD>
@@ -379,6 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tid == 0) {
         s_fail = s_odd = 0;
         s_b = -1;
+#pragma unroll 1
         for (int i = 0; i < kMaxSlots; ++i) {
             tc::mb_init(k_full + i, 1);
             tc::mb_init(k_empty + i, 1);
@@ -416,6 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int b0 = min(tid * per, sh.n_requests), b1 = min(b0 + per, sh.n_requests);
     long long mine = 0;
     Req last{};
+#pragma unroll 1
     for (int b = b0; b < b1; ++b) {
         last = req_of(sh, b);
         if (last.clipped && last.n && blockIdx.x == 0) say(a.status, SSD_STATUS_TABLE);
@@ -431,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     before -= mine;
     long long units = 0;
+#pragma unroll 4
     for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) before += s_sum[w];
         units += s_sum[w];
@@ -439,6 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const long long lo = cta < ctas ? range_start(units, ctas, cta) : 0, hi = cta < ctas ? range_start(units, ctas, cta + 1) : 0;
     if (before <= lo && lo < before + mine) {
         long long off = lo - before;
+#pragma unroll 1
         for (int b = b0; b < b1; ++b) {
             const Req q = per == 1 ? last : req_of(sh, b);
             const long long n = head_units(sh, q, tile) * sh.n_kv_heads;
@@ -493,6 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int n = (g.u1 - g.u0) * (is_v ? 2 : BOXES);  // slots of the segment
             long long x0 = (long long)g.u0 * kUnit;
             int got = fetch(x0), ahead = fetch(x0 + batch);
+#pragma unroll 1
             for (int i = 0; i < n; ++i) {
                 const long long x = (long long)g.u0 * kUnit + (is_v ? i * 64 : i / BOXES * kUnit);  // the slot's first position
                 if (x - x0 >= batch) {
@@ -516,6 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (++slot == n_slots) slot = 0, phase ^= 1u;
                 if (!is_v && n_seg && i == BOXES) {  // the rows of q that will be asked for at the end of the segment before, into L2
                     const int start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
+#pragma unroll 1
                     for (int r = lane; r < rows; r += 32) {
                         const int node = node_of(rem, r), head = g.kvh * sh.group + rem + r - node * sh.group;
                         const T* row = (const T*)a.q + (int64_t)(g.q.r0 + node0 + node) * a.q_stride + head * HD;
@@ -531,6 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
             if (!wait(&q_ready, n_seg)) break;
             const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
+#pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
                 // P of unit j - 3, which held these columns, is used up
                 if (turn && !wait(pv_done + buf, turn - 1)) break;
@@ -563,6 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t v0 = tc::sdesc(smem_u32(vs)) + ((uint64_t)((L::VBOX >> 4) - 1) << 16);
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;
         for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+#pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
                 const bool fresh = u == g.u0;
                 if (fresh && n_seg && !wait(&o_free, n_seg - 1)) break;
@@ -697,22 +707,36 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ld32(tl + c, o);
                     wait_ld();
                     if (!valid) continue;
-                    if (odd) add_odd<C>(a, cur, node, c, o);
                     if (whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
                         T* to = (T*)a.out + (int64_t)(cur.q.r0 + node) * a.out_stride + head * HD + c;
                         constexpr int V = Vec<T>::N;
 #pragma unroll
                         for (int i = 0; i < 32; i += V) {
                             float f[V];
 #pragma unroll
-                            for (int k = 0; k < V; ++k) f[k] = __uint_as_float(o[i + k]) * inv;
+                            for (int k = 0; k < V; ++k) f[k] = __uint_as_float(o[i + k]);
                             *reinterpret_cast<uint4*>(to + i) = Vec<T>::put(f);
                         }
+                        if (odd)
+#pragma unroll 1
+                            for (int i = 0; i < 32; ++i) {
+                                const float f = odd_sum<C>(a, cur, node, c + i);
+                                if (f != 0.f) to[i] = (T)((float)to[i] + f);
+                            }
                     } else {
                         float4* to = a.part + ((size_t)(cta * 2 + slot) * (HD / 4) + c / 4) * kTile + mine32;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             to[(i / 4) * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+                        if (odd)
+#pragma unroll 1
+                            for (int i = 0; i < 32; ++i) {
+                                float* p = reinterpret_cast<float*>(to + (i >> 2) * kTile) + (i & 3);
+                                const float f = odd_sum<C>(a, cur, node, c + i);
+                                if (f != 0.f) *p += f;
+                            }
                     }
                 }
             }
@@ -737,6 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int all_seen = min(sh.chain ? g.q.len + node0 + 1 : g.q.len, g.q.total);
             const int first = (int)((j ^ (unsigned)grp) & 1u);  // this group's first unit of the segment
             float ref = -INFINITY, l = 0.f, sc = a.scale2;  // what the weights are relative to (and kShift), their sum
+#pragma unroll 1
             for (int i = first; i < n; i += 2) {
                 const unsigned ju = j + (unsigned)i, turn = ju / 3, buf = ju - 3 * turn;
                 const int p0 = (g.u0 + i) * kUnit;

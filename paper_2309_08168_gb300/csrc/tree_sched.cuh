@@ -23,7 +23,7 @@ namespace ssd {
 namespace tree {
 
 constexpr int kUnit = 128;  // positions
-constexpr int kItemCost = 2;
+constexpr int kItemCost = 3;
 
 struct Shape {
     int n_requests, n_rows, max_blocks, page_size, n_kv_heads, group, chain;
@@ -70,11 +70,14 @@ __host__ __device__ __forceinline__ int units_of(const Shape& s, const Req& q, i
     }
     return (keys + kUnit - 1) / kUnit;
 }
-// units of one KV head of a request, with what its items count more
-__host__ __device__ __forceinline__ long long head_units(const Shape& s, const Req& q, int tile) {
+// units of one KV head of a request, with what its items count more.  (Functions of their own, and
+// no unrolling, here and below: these run once or a few times in a CTA's life, and
+// their instructions come from L2 at first use.)
+__host__ __device__ __noinline__ inline long long head_units(const Shape& s, const Req& q, int tile) {
     const int n = tiles_of(s, q, tile);
     if (!s.chain) return (long long)n * (n ? units_of(s, q, tile, 0) + kItemCost : 0);
     long long u = (long long)n * kItemCost;
+#pragma unroll 1
     for (int mt = 0; mt < n; ++mt) u += units_of(s, q, tile, mt);
     return u;
 }
@@ -84,11 +87,11 @@ __host__ __device__ __forceinline__ int ctas_of(long long units, int grid) {
     return units < 1 ? 1 : units < grid ? (int)units : grid;
 }
 // (in 32 bits where that is enough: a 64-bit division is some 100 instructions)
-__host__ __device__ __forceinline__ long long range_start(long long units, int ctas, int c) {
+__host__ __device__ __noinline__ inline long long range_start(long long units, int ctas, int c) {
     const long long x = units * c;
     return x >> 32 ? x / ctas : (long long)((uint32_t)x / (uint32_t)ctas);
 }
-__host__ __device__ __forceinline__ int cta_of(long long units, int ctas, long long u) {
+__host__ __device__ __noinline__ inline int cta_of(long long units, int ctas, long long u) {
     const long long x = (u + 1) * ctas - 1;
     return x >> 32 ? (int)(x / units) : (int)((uint32_t)x / (uint32_t)units);
 }
@@ -116,10 +119,12 @@ __host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int 
     w.kvh = (off | per) >> 32 ? (int)(off / per) : (int)((uint32_t)off / (uint32_t)per);
     off -= w.kvh * per;
     w.mt = 0;
+#pragma unroll 1
     for (int n; off >= (n = units_of(s, w.q, tile, w.mt) + kItemCost); ++w.mt) off -= n;
     w.u = (int)off;
 }
 __host__ __device__ __forceinline__ bool walk_next(Walk& w, const Shape& s, int tile, Seg& g) {
+#pragma unroll 1
     while (w.left > 0) {
         const int n = units_of(s, w.q, tile, w.mt), rest = n + kItemCost - w.u;
         const int take = rest < w.left ? rest : (int)w.left, from = w.u - kItemCost, to = from + take;
@@ -138,6 +143,7 @@ __host__ __device__ __forceinline__ bool walk_next(Walk& w, const Shape& s, int 
             w.mt = 0;
             if (++w.kvh == s.n_kv_heads) {
                 w.kvh = 0;
+#pragma unroll 1
                 do w.q = req_of(s, ++w.b);
                 while (w.q.n == 0);  // (units are left, so there is one)
             }
