@@ -264,26 +264,42 @@ def _refuse(what: str):
     raise SSDError(SSD_ERR_INVALID_ARG, what)
 
 
-def _dev(t, what: str, dtype: str, device, shape=None):
-    """Address of a contiguous CUDA tensor of this type (and shape) on `device`, or None for None."""
+def _dev(t, what: str, dtype, device: int, n: int):
+    """Address of a contiguous tensor of n values of this type on CUDA device `device`, or None for None."""
     if t is None:
         return None
-    if not t.is_cuda or t.device != device or str(t.dtype) != dtype or not t.is_contiguous():
-        _refuse(f"{what}: a contiguous {dtype} tensor on {device} is wanted")
-    if shape is not None and tuple(t.shape) != shape:
-        _refuse(f"{what}: shape {tuple(t.shape)}, {shape} is wanted")
+    if t.get_device() != device or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{what}: a contiguous {dtype} tensor of {n} values on CUDA device {device} is wanted, got {t.dtype}, shape {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t, what: str, device, dtype, n_rows: int, heads: int | None, hd: int):
+def _rows(t, what: str, device: int, dtype, n_rows: int, heads: int, hd: int):
     """(address, row stride) of rows [row][head][dim] whose heads lie behind one another."""
-    if not t.is_cuda or t.device != device or (dtype is not None and t.dtype != dtype) or str(t.dtype) not in _ROW_TYPES:
-        _refuse(f"{what}: fp32, fp16 or bf16 rows on {device} are wanted, all of one type")
-    if t.dim() != 3 or t.shape[0] != n_rows or t.shape[2] != hd or (heads is not None and t.shape[1] != heads):
-        _refuse(f"{what}: shape {tuple(t.shape)}, ({n_rows}, {heads if heads is not None else 'heads'}, {hd}) is wanted")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != hd):
+    shape, stride = t.shape, t.stride()
+    if t.get_device() != device or t.dtype is not dtype or len(shape) != 3 or shape[0] != n_rows or shape[1] != heads or shape[2] != hd:
+        _refuse(f"{what}: {dtype} of shape ({n_rows}, {heads}, {hd}) on CUDA device {device} is wanted, got {t.dtype}, {tuple(shape)} on {t.device}")
+    if stride[2] != 1 or (stride[1] != hd and heads > 1):
         _refuse(f"{what}: the heads of a row must lie behind one another")
-    return t.data_ptr(), t.stride(0) if n_rows > 1 else t.shape[1] * hd
+    return t.data_ptr(), stride[0] if n_rows > 1 else heads * hd
+
+
+def _row_type(t, what: str) -> int:
+    k = _ROW_TYPES.get(t.dtype)
+    if k is None:
+        k = _ROW_TYPES.get(str(t.dtype))
+        if k is None or t.dim() != 3:
+            _refuse(f"{what}: fp32, fp16 or bf16 rows [row][head][dim] are wanted")
+        _ROW_TYPES[t.dtype] = k
+    if t.dim() != 3:
+        _refuse(f"{what}: rows [row][head][dim] are wanted")
+    return k
+
+
+def _of_type(t, what: str, name: str):
+    """t's type, which has to be this one."""
+    if t is not None and str(t.dtype) != name:
+        _refuse(f"{what}: {name} is wanted, got {t.dtype}")
+    return t.dtype if t is not None else None
 
 
 class PagedKV:
@@ -295,7 +311,7 @@ class PagedKV:
             _refuse("k and v: CUDA tensors [layer][page][kv_head][position][dim] of one shape, type and memory order are wanted")
         if str(k.dtype) not in ("torch.float16", "torch.bfloat16") or k.stride(4) != 1:
             _refuse("k and v: fp16 or bf16 with adjacent dims are wanted")
-        self.k, self.v, self.device = k, v, k.device
+        self.k, self.v, self.device = k, v, k.get_device()
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.struct = ssd_pages(k.data_ptr(), v.data_ptr(), _ROW_TYPES[str(k.dtype)], *(k.shape[i] for i in (0, 1, 2, 3, 4)), *k.stride()[:4])
 
@@ -305,14 +321,15 @@ class TreeBatch:
     Keeps the tensors; their contents may change between calls."""
 
     def __init__(self, row_start, lens, block_table, n_rows: int, max_rows: int):
-        n, self.device = lens.numel(), lens.device
-        if block_table.dim() != 2:
-            _refuse("block_table: [request][block] is wanted")
+        n, self.i32 = lens.numel(), _of_type(lens, "lens", "torch.int32")
+        if not lens.is_cuda or block_table.dim() != 2 or block_table.shape[0] != n:
+            _refuse("lens [request] and block_table [request][block] on a CUDA device are wanted")
+        self.device = lens.get_device()
         self.keep = (row_start, lens, block_table)
         self.n_requests, self.n_rows, self.max_rows, self.max_blocks = n, n_rows, max_rows, block_table.shape[1]
-        self.struct = ssd_batch(n, n_rows, max_rows, self.max_blocks, _dev(row_start, "row_start", "torch.int32", lens.device, (n + 1,)),
-                                _dev(lens, "lens", "torch.int32", lens.device, (n,)),
-                                _dev(block_table, "block_table", "torch.int32", lens.device, (n, self.max_blocks)))
+        self.struct = ssd_batch(n, n_rows, max_rows, self.max_blocks, _dev(row_start, "row_start", self.i32, self.device, n + 1),
+                                _dev(lens, "lens", self.i32, self.device, n),
+                                _dev(block_table, "block_table", self.i32, self.device, n * self.max_blocks))
 
 
 def ssd_tree_plan(batch: TreeBatch, page_size: int, n_pages: int, parents, held, held_out, ring, ends, ends_out, slots,
@@ -320,14 +337,21 @@ def ssd_tree_plan(batch: TreeBatch, page_size: int, n_pages: int, parents, held,
     """Pages, slots, positions and ancestor masks of a round.  parents int32 [n_rows] or None (chains); held, held_out
     int32 [n]; ring int32 [n_pages]; ends, ends_out int64 [2]; slots, positions int32 [n_rows]; masks int64 [n_rows][words]
     (bit patterns) with parents; status int32 [1] or None."""
-    d, n, r, i32 = batch.device, batch.n_requests, batch.n_rows, "torch.int32"
-    words = masks.shape[1] if masks is not None and masks.dim() == 2 else 0
-    _check(lib.ssd_tree_plan(batch.struct, page_size, n_pages, _dev(parents, "parents", i32, d, (r,)), _dev(held, "held", i32, d, (n,)),
-                             _dev(held_out, "held_out", i32, d, (n,)), _dev(ring, "ring", i32, d, (n_pages,)),
-                             _dev(ends, "ends", "torch.int64", d, (2,)), _dev(ends_out, "ends_out", "torch.int64", d, (2,)),
-                             _dev(slots, "slots", i32, d, (r,)), _dev(positions, "positions", i32, d, (r,)),
-                             _dev(masks, "masks", "torch.int64", d, (r, words)), words, _dev(status, "status", i32, d, (1,)),
-                             cuda_stream))
+    d, n, r, i32, i64 = batch.device, batch.n_requests, batch.n_rows, batch.i32, _of_type(ends, "ends", "torch.int64")
+    words = _words(masks)
+    _check(lib.ssd_tree_plan(batch.struct, page_size, n_pages, _dev(parents, "parents", i32, d, r), _dev(held, "held", i32, d, n),
+                             _dev(held_out, "held_out", i32, d, n), _dev(ring, "ring", i32, d, n_pages), _dev(ends, "ends", i64, d, 2),
+                             _dev(ends_out, "ends_out", i64, d, 2), _dev(slots, "slots", i32, d, r),
+                             _dev(positions, "positions", i32, d, r), _dev(masks, "masks", i64, d, r * words), words,
+                             _dev(status, "status", i32, d, 1), cuda_stream))
+
+
+def _words(masks) -> int:
+    if masks is None:
+        return 0
+    if masks.dim() != 2:
+        _refuse("masks: [row][word] is wanted")
+    return masks.shape[1]
 
 
 def ssd_rope_init(rot_dim: int, theta: float = 1e4, interleaved: bool = False, scaling: int = SSD_ROPE_PLAIN, factor: float = 1.0,
@@ -341,12 +365,11 @@ def ssd_rope_kv(cache: PagedKV, layer: int, rope: ssd_rope, q, k, v, positions, 
                 cuda_stream: int | None = None) -> None:
     """Turns q [n][heads][hd] and k [n][kv_heads][hd] to positions int32 [n]; q to q_out, k and v [n][kv_heads][hd] to
     rows slots int32 [n] of the cache's layer."""
-    d, n, hd = cache.device, q.shape[0], cache.head_dim
-    rows = [x for t, what, heads in ((q, "q", None), (k, "k", cache.n_kv_heads), (v, "v", cache.n_kv_heads))
-            for x in _rows(t, what, d, q.dtype, n, heads, hd)]
-    _check(lib.ssd_rope_kv(cache.struct, layer, rope, _ROW_TYPES[str(q.dtype)], n, q.shape[1], *rows,
-                           _dev(positions, "positions", "torch.int32", d, (n,)), _dev(slots, "slots", "torch.int32", d, (n,)),
-                           *_rows(q_out, "q_out", d, q.dtype, n, q.shape[1], hd), cuda_stream))
+    kind, d, t, n, h, g, hd = _row_type(q, "q"), cache.device, q.dtype, q.shape[0], q.shape[1], cache.n_kv_heads, cache.head_dim
+    i32 = _of_type(slots, "slots", "torch.int32")
+    _check(lib.ssd_rope_kv(cache.struct, layer, rope, kind, n, h, *_rows(q, "q", d, t, n, h, hd), *_rows(k, "k", d, t, n, g, hd),
+                           *_rows(v, "v", d, t, n, g, hd), _dev(positions, "positions", i32, d, n), _dev(slots, "slots", i32, d, n),
+                           *_rows(q_out, "q_out", d, t, n, h, hd), cuda_stream))
 
 
 def ssd_tree_attention_workspace(cache: PagedKV) -> int:
@@ -360,30 +383,29 @@ def ssd_tree_attention(batch: TreeBatch, cache: PagedKV, layer: int, q, masks, s
                        cuda_stream: int | None = None) -> None:
     """out [n_rows][heads][hd] = attention of q over the requests' cached positions and the nodes that masks
     int64 [n_rows][words] show (None: chains).  workspace: a contiguous uint8 tensor."""
-    d, n = cache.device, batch.n_rows
+    kind, d, t, n, h, hd = _row_type(q, "q"), cache.device, q.dtype, batch.n_rows, q.shape[1], cache.head_dim
     if batch.device != d:
         _refuse("the batch and the cache are on different devices")
-    qp, qs = _rows(q, "q", d, None, n, None, cache.head_dim)
-    op, os_ = _rows(out, "out", d, q.dtype, n, q.shape[1], cache.head_dim)
-    words = masks.shape[1] if masks is not None and masks.dim() == 2 else 0
-    _check(lib.ssd_tree_attention(batch.struct, cache.struct, layer, _ROW_TYPES[str(q.dtype)], q.shape[1], qp, qs,
-                                  _dev(masks, "masks", "torch.int64", d, (n, words)), words, scale, op, os_,
-                                  _dev(workspace, "workspace", "torch.uint8", d), workspace.numel(),
-                                  _dev(status, "status", "torch.int32", d, (1,)), cuda_stream))
+    words = _words(masks)
+    _check(lib.ssd_tree_attention(batch.struct, cache.struct, layer, kind, h, *_rows(q, "q", d, t, n, h, hd),
+                                  _dev(masks, "masks", _of_type(masks, "masks", "torch.int64"), d, n * words), words, scale,
+                                  *_rows(out, "out", d, t, n, h, hd),
+                                  _dev(workspace, "workspace", _of_type(workspace, "workspace", "torch.uint8"), d, workspace.numel()),
+                                  workspace.numel(), _dev(status, "status", batch.i32, d, 1), cuda_stream))
 
 
 def ssd_tree_commit(batch: TreeBatch, cache: PagedKV | None, parents, tokens, target, accepted, next_token, lens_out, path,
                     emitted, cuda_stream: int | None = None) -> None:
     """Walks every tree along target int32 [n_rows]: accepted, next_token, lens_out int32 [n]; path, emitted int32
     [n_rows]; moves the accepted rows of every layer of the cache (None: tokens only).  parents None: chains."""
-    d, n, r, i32 = batch.device, batch.n_requests, batch.n_rows, "torch.int32"
+    d, n, r, i32 = batch.device, batch.n_requests, batch.n_rows, batch.i32
     if cache is not None and cache.device != d:
         _refuse("the batch and the cache are on different devices")
-    _check(lib.ssd_tree_commit(batch.struct, cache.struct if cache is not None else None, _dev(parents, "parents", i32, d, (r,)),
-                               _dev(tokens, "tokens", i32, d, (r,)), _dev(target, "target", i32, d, (r,)),
-                               _dev(accepted, "accepted", i32, d, (n,)), _dev(next_token, "next_token", i32, d, (n,)),
-                               _dev(lens_out, "lens_out", i32, d, (n,)), _dev(path, "path", i32, d, (r,)),
-                               _dev(emitted, "emitted", i32, d, (r,)), cuda_stream))
+    _check(lib.ssd_tree_commit(batch.struct, cache.struct if cache is not None else None, _dev(parents, "parents", i32, d, r),
+                               _dev(tokens, "tokens", i32, d, r), _dev(target, "target", i32, d, r),
+                               _dev(accepted, "accepted", i32, d, n), _dev(next_token, "next_token", i32, d, n),
+                               _dev(lens_out, "lens_out", i32, d, n), _dev(path, "path", i32, d, r),
+                               _dev(emitted, "emitted", i32, d, r), cuda_stream))
 
 
 def ssd_destroy(h: int) -> None:
