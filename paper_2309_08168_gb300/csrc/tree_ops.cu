@@ -13,8 +13,7 @@ namespace {
 // ---------------------------------------------------------------------------
 // ssd_tree_plan
 // ---------------------------------------------------------------------------
-constexpr int kPlanThreads = 256;
-static_assert(kPlanThreads >= kMaxNodes, "a thread per node");
+constexpr int kPlanThreads = 128, kNodesPerThread = kMaxNodes / kPlanThreads;
 
 struct PlanArgs {
     int n_requests, n_rows, max_blocks, page_size, n_pages, words;
@@ -29,165 +28,201 @@ struct PlanArgs {
 
 // what a request needs beyond what it holds, and gives back
 struct Want {
-    long long need;  // pages of its positions
-    int held, fresh, back;
+    int len, held, fresh, back;
     bool live, fits;
 };
-__device__ __forceinline__ Want want_of(const PlanArgs& a, int b) {
+__device__ __forceinline__ Want want_of(const PlanArgs& a, int b, const Rows& rows) {
     Want w;
-    const int len = __ldcg(a.lens + b);
+    w.len = __ldcg(a.lens + b);
     w.held = min(max(__ldcg(a.held + b), 0), a.max_blocks);
-    w.live = len >= 0;
-    w.need = w.live ? ((long long)len + rows_of(a.row_start, b, a.n_rows).n + a.page_size - 1) / a.page_size : 0;
-    w.fits = w.need <= a.max_blocks;
-    w.fresh = w.live && w.fits ? max((int)w.need - w.held, 0) : 0;
+    w.live = w.len >= 0;
+    // (divided in 32 bits; what needs more does not fit, as a cache has less than 2^31 positions)
+    const unsigned long long last = (unsigned long long)(w.live ? w.len : 0) + (unsigned)rows.n + (unsigned)a.page_size - 1u;
+    const unsigned need = !w.live ? 0u : last >> 32 ? 0xffffffffu : (unsigned)last / (unsigned)a.page_size;
+    w.fits = need <= (unsigned)a.max_blocks;
+    w.fresh = w.live && w.fits ? max((int)need - w.held, 0) : 0;
     w.back = w.live ? 0 : w.held;
     return w;
 }
 
-// One CTA per request.  The requests' places in the queue of free pages are a
-// prefix sum over all of them, which every CTA forms for itself (three words a
-// request, from L2) rather than wait for another launch; masks and depths of a
-// tree come from pointer doubling: after step s a node knows its ancestors up
-// to 2^s levels above.
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
-    __shared__ long long s_fresh[kPlanThreads / 32], s_back[kPlanThreads / 32], s_own[2], s_top;
+// One CTA per request.  Bound by latency: a request's place in the queue of free pages
+// is a sum over those before it, which every CTA forms for itself (three words a
+// request, from L2, all threads at once) rather than wait for another launch, while its own
+// rows' parents are on their way; masks and depths of a tree come from pointer
+// doubling: after step s a node knows its ancestors up to 2^s levels above.
+// 128 threads, so that a thousand requests run at once: with 256, and a scan over
+// all requests in every CTA, 1000 trees of 33 to 64 nodes took 19.0 us.
+__global__ void __launch_bounds__(kPlanThreads, 10) plan_kernel(const PlanArgs a) {
+    __shared__ long long s_sum[2][kPlanThreads / 32], s_top[kPlanThreads / 32];
     __shared__ int s_up[kMaxNodes], s_depth[kMaxNodes];
     __shared__ uint64_t s_mask[4][kMaxNodes];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, b = blockIdx.x;
     pdl_launch_dependents();
     pdl_wait();
-    // prefix sums over the requests, a run of them per thread
-    const int per = (a.n_requests + kPlanThreads - 1) / kPlanThreads;
-    const int b0 = min(tid * per, a.n_requests), b1 = min(b0 + per, a.n_requests);
-    long long fresh = 0, back = 0;
-    for (int i = b0; i < b1; ++i) {
-        const Want w = want_of(a, i);
-        fresh += w.fresh;
-        back += w.back;
-    }
-    long long pf = fresh, pb = back;  // inclusive over the warp, then exclusive over the block
+    const Rows rows = rows_of(a.row_start, b, a.n_rows);
+    const int nodes = a.parents ? min(rows.n, 64 * a.words) : 0;
+    int up[kNodesPerThread];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, pf, o), y = __shfl_up_sync(0xffffffffu, pb, o);
-        if (lane >= o) pf += x, pb += y;
+    for (int k = 0; k < kNodesPerThread; ++k) {
+        const int i = tid + k * kPlanThreads;
+        up[k] = i < nodes ? __ldcg(a.parents + rows.r0 + i) : -1;
     }
-    if (lane == 31) s_fresh[warp] = pf, s_back[warp] = pb;
-    if (tid == 0) s_top = 0;
-    __syncthreads();
-    pf -= fresh;
-    pb -= back;
-    for (int w = 0; w < warp; ++w) pf += s_fresh[w], pb += s_back[w];
+    const Want w = want_of(a, b, rows);
+    long long sums[2] = {0, 0};  // pages taken and given back by the requests before
+#pragma unroll 2
+    for (int i = tid; i < b; i += kPlanThreads) {
+        const Want o = want_of(a, i, rows_of(a.row_start, i, a.n_rows));
+        sums[0] += o.fresh;
+        sums[1] += o.back;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], o);
+        if (lane == 0) s_sum[k][warp] = sums[k];
+    }
     const long long head = __ldcg(a.ends), tail = __ldcg(a.ends + 1);
     const long long avail = min(max(tail - head, 0ll), (long long)a.n_pages);
-    if (b == 0) {  // this CTA also leaves the queue's new ends
-        long long top = 0, run = pf;
-        for (int i = b0; i < b1; ++i) {
-            run += want_of(a, i).fresh;
-            if (run <= avail) top = run;
-        }
-        if (top > 0) atomicMax((unsigned long long*)&s_top, (unsigned long long)top);
-    }
-    if (b0 <= b && b < b1) {
-        for (int i = b0; i < b; ++i) {
-            const Want w = want_of(a, i);
-            pf += w.fresh;
-            pb += w.back;
-        }
-        s_own[0] = pf;
-        s_own[1] = pb;
-    }
     __syncthreads();
-    const Want w = want_of(a, b);
-    const Rows rows = rows_of(a.row_start, b, a.n_rows);
-    const long long first = s_own[0];
+    long long first = 0, returned = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanThreads / 32; ++k) first += s_sum[0][k], returned += s_sum[1][k];
     const bool given = w.live && w.fits && (w.fresh == 0 || first + w.fresh <= avail);
-    // ring[(head + x) mod n_pages]
+    // ring[(head + x) mod n_pages]; x stays below n_pages where the counts are sound
     const int h0 = (int)(((head % a.n_pages) + a.n_pages) % a.n_pages), t0 = (int)(((tail % a.n_pages) + a.n_pages) % a.n_pages);
-    auto ring_at = [&](int base, long long x) { return (int)((base + x) % a.n_pages); };
+    auto ring_at = [&](int base, long long x) {
+        const long long y = base + x;
+        return (int)(y < a.n_pages ? y : y < 2ll * a.n_pages ? y - a.n_pages : y % a.n_pages);
+    };
     int32_t* table = a.block_table + (size_t)b * a.max_blocks;
     if (tid == 0) {
         a.held_out[b] = !w.live ? 0 : given ? w.held + w.fresh : w.held;
         if (w.live && !w.fits) say(a.status, SSD_STATUS_TABLE);
         if (w.live && w.fits && !given) say(a.status, SSD_STATUS_PAGES);
-        if (b == 0) {
-            long long total = 0;
-            for (int i = 0; i < kPlanThreads / 32; ++i) total += s_back[i];
-            a.ends_out[0] = head + s_top;
-            a.ends_out[1] = tail + total;
-        }
     }
     if (given)
         for (int j = tid; j < w.fresh; j += kPlanThreads) table[w.held + j] = __ldcg(a.ring + ring_at(h0, first + j));
     if (!w.live)
-        for (int j = tid; j < w.back; j += kPlanThreads) a.ring[ring_at(t0, s_own[1] + j)] = __ldcg(table + j);
+        for (int j = tid; j < w.back; j += kPlanThreads) a.ring[ring_at(t0, returned + j)] = __ldcg(table + j);
 
     // the rows: depths and masks of a tree first
-    const int len = __ldcg(a.lens + b);
-    const int nodes = a.parents ? min(rows.n, 64 * a.words) : 0;
     if (a.parents && rows.n > 0) {
-        int up = -1;
-        bool bad = false;
-        if (tid < nodes) {
-            up = __ldcg(a.parents + rows.r0 + tid);
-            if (up < -1 || up >= tid) {
+        bool bad = tid == 0 && rows.n > nodes;
+#pragma unroll
+        for (int k = 0; k < kNodesPerThread; ++k) {
+            const int i = tid + k * kPlanThreads;
+            if (up[k] < -1 || up[k] >= i) {
                 bad = true;
-                up = -1;
+                up[k] = -1;
             }
-        }
-        if (tid < kMaxNodes) {
-            s_up[tid] = up;
-            s_depth[tid] = up >= 0;
+            s_up[i] = up[k];
+            s_depth[i] = up[k] >= 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int q = 0; q < 4; ++q) {
                 uint64_t m = 0;
-                if (tid < nodes && tid >> 6 == k) m |= 1ull << (tid & 63);
-                if (up >= 0 && up >> 6 == k) m |= 1ull << (up & 63);
-                s_mask[k][tid] = m;
+                if (i < nodes && i >> 6 == q) m |= 1ull << (i & 63);
+                if (up[k] >= 0 && up[k] >> 6 == q) m |= 1ull << (up[k] & 63);
+                if (q < a.words) s_mask[q][i] = m;
             }
         }
-        if (bad || (tid == 0 && rows.n > nodes)) say(a.status, SSD_STATUS_PARENT);
-        // (a node's word holds itself and the next 2^s ancestors, s_up the one after those)
-        while (__syncthreads_or(up >= 0)) {
-            uint64_t m[4];
-            int d = 0, next = -1;
-            if (up >= 0) {
-                next = s_up[up];
-                d = s_depth[up];
+        if (bad) say(a.status, SSD_STATUS_PARENT);
+        // (a node's words hold itself and the next 2^s ancestors, s_up the one after those)
+        auto more = [&] {
+            bool any = false;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) m[k] = s_mask[k][up];
-            }
+            for (int k = 0; k < kNodesPerThread; ++k) any = any || up[k] >= 0;
+            return any;
+        };
+        while (__syncthreads_or(more())) {
+            uint64_t m[kNodesPerThread][4];
+            int d[kNodesPerThread], next[kNodesPerThread];
+#pragma unroll
+            for (int k = 0; k < kNodesPerThread; ++k)
+                if (up[k] >= 0) {
+                    next[k] = s_up[up[k]];
+                    d[k] = s_depth[up[k]];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q < a.words) m[k][q] = s_mask[q][up[k]];
+                }
             __syncthreads();
-            if (up >= 0) {
-                s_up[tid] = next;
-                s_depth[tid] += d;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s_mask[k][tid] |= m[k];
-                up = next;
-            }
+            for (int k = 0; k < kNodesPerThread; ++k)
+                if (up[k] >= 0) {
+                    const int i = tid + k * kPlanThreads;
+                    s_up[i] = next[k];
+                    s_depth[i] += d[k];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q < a.words) s_mask[q][i] |= m[k][q];
+                    up[k] = next[k];
+                }
         }
     }
     for (int i = tid; i < rows.n; i += kPlanThreads) {
-        const long long at = (long long)len + i;
+        const unsigned at = (unsigned)w.len + (unsigned)i;
         int slot = -1;
         if (given) {
-            const int j = (int)(at / a.page_size);  // < need <= max_blocks
+            const int j = (int)(at / (unsigned)a.page_size);  // < the pages needed <= max_blocks
             const int page = j < w.held ? __ldcg(table + j) : __ldcg(a.ring + ring_at(h0, first + j - w.held));
-            if (page >= 0 && page < a.n_pages) slot = page * a.page_size + (int)(at - (long long)j * a.page_size);
+            if (page >= 0 && page < a.n_pages) slot = page * a.page_size + (int)(at - (unsigned)j * (unsigned)a.page_size);
         }
         a.slots[rows.r0 + i] = slot;
-        a.positions[rows.r0 + i] = a.parents ? len + (i < nodes ? s_depth[i] : 0) : (int)at;
+        a.positions[rows.r0 + i] = a.parents ? w.len + (i < nodes ? s_depth[i] : 0) : (int)at;
         if (a.parents)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (k < a.words) a.masks[(size_t)(rows.r0 + i) * a.words + k] = i < nodes ? s_mask[k][i] : 0ull;
+    }
+    if (b) return;
+    // The first CTA also leaves the queue's new ends: the pages taken are the largest sum over
+    // the first requests, in order, that the queue covers (a run of requests per thread).
+    const int per = (a.n_requests + kPlanThreads - 1) / kPlanThreads;
+    const int b0 = min(tid * per, a.n_requests), b1 = min(b0 + per, a.n_requests);
+    long long fresh = 0, back = 0;
+    for (int i = b0; i < b1; ++i) {
+        const Want o = want_of(a, i, rows_of(a.row_start, i, a.n_rows));
+        fresh += o.fresh;
+        back += o.back;
+    }
+    long long run = fresh;  // inclusive over the warp, then exclusive over the block
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += x;
+        back += __shfl_xor_sync(0xffffffffu, back, o);
+    }
+    __syncthreads();
+    if (lane == 31) s_sum[0][warp] = run;
+    if (lane == 0) s_sum[1][warp] = back;
+    __syncthreads();
+    run -= fresh;
+    for (int k = 0; k < warp; ++k) run += s_sum[0][k];
+    long long top = 0;
+    for (int i = b0; i < b1; ++i) {
+        run += want_of(a, i, rows_of(a.row_start, i, a.n_rows)).fresh;
+        if (run <= avail) top = run;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
+    if (tid == 0) {
+        long long total = 0;
+        top = 0;
+        for (int k = 0; k < kPlanThreads / 32; ++k) {
+            top = max(top, s_top[k]);
+            total += s_sum[1][k];
+        }
+        a.ends_out[0] = head + top;
+        a.ends_out[1] = tail + total;
     }
 }
 
 // ---------------------------------------------------------------------------
 // ssd_rope_kv
 // ---------------------------------------------------------------------------
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 128;
 
 struct RopeArgs {
     const void *q, *k, *v;
@@ -200,90 +235,112 @@ struct RopeArgs {
     ssd_rope rope;
 };
 
-// Rows of a CTA's grid line blockIdx.x; its units (16 bytes of a head, or the
-// two halves of 16 bytes of pairs) are shared by the gridDim.y CTAs of the row.
+// A CTA takes a row (blockIdx.x), or with gridDim.y > 1 a share of its heads.  A thread has
+// one place in a head - 16 bytes, or the two halves of 16 bytes of pairs - and goes
+// through the heads, kRopeAhead at a time, all loads before the first store: the kernel is
+// bound by HBM (or L2) and by the loads under way.
 //
 // The angle of pair i at position p is p f_i.  f_i / 2 pi is held as a fraction
 // of 2^64, so the product modulo 2^64 is the angle's fraction of a turn exactly,
 // at any position; fp32 (p f_i) would be off by 0.06 radians at p = 10^6.
 //
 // T: rows, C: cache
+constexpr int kRopeAhead = 4;
 template <typename T, typename C>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
     constexpr int V = Vec<T>::N;
     __shared__ float2 s_cs[64];
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x, half = a.rope.rot_dim / 2;
+    const int slot = __ldcg(a.slots + row);
     if (threadIdx.x < half) {
         const uint64_t turn = (uint64_t)(int64_t)__ldcg(a.positions + row) * a.rope.turns[threadIdx.x];
         float s, c;
         sincospif((float)((int64_t)turn >> 32) * 0x1p-31f, &s, &c);
         s_cs[threadIdx.x] = make_float2(c * a.rope.amplitude, s * a.rope.amplitude);
     }
-    const int slot = __ldcg(a.slots + row);
     const bool cached = slot >= 0 && slot < a.n_pages * a.page_size;
     const int64_t at = cached ? (int64_t)(slot / a.page_size) * a.page_stride + (int64_t)(slot % a.page_size) * a.pos_stride : 0;
-    __syncthreads();
-    // units of a rotated head: pairs first, then what passes
-    const int n_pair = a.rope.interleaved ? a.rope.rot_dim / V : half / V, n_rot = n_pair + (a.hd - a.rope.rot_dim) / V;
-    const int n_pass = a.hd / V;
-    const int n_q = a.n_heads * n_rot, n_k = a.n_kv_heads * n_rot, n_v = a.n_kv_heads * n_pass;
-    const T* q = (const T*)a.q + (int64_t)row * a.q_stride;
-    const T* k = (const T*)a.k + (int64_t)row * a.k_stride;
-    const T* v = (const T*)a.v + (int64_t)row * a.v_stride;
-    T* qo = (T*)a.q_out + (int64_t)row * a.q_out_stride;
-    const int n_all = n_q + (cached ? n_k + n_v : 0);
     auto to_cache = [&](void* base, int head, int e, const float (&f)[V]) {
         C* p = (C*)base + at + (int64_t)head * a.head_stride + e;
-        if constexpr (V == 8) {
-            *reinterpret_cast<uint4*>(p) = Vec<C>::put(f);
-        } else {
-            *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1], C()), pack2(f[2], f[3], C()));
-        }
+        if constexpr (V == 8) *reinterpret_cast<uint4*>(p) = Vec<C>::put(f);
+        else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1], C()), pack2(f[2], f[3], C()));
     };
-    for (int u = blockIdx.y * kRopeThreads + threadIdx.x; u < n_all; u += gridDim.y * kRopeThreads) {
-        if (u >= n_q + n_k) {
-            const int w = u - n_q - n_k, head = w / n_pass, e = (w - head * n_pass) * V;
-            float f[V];
-            Vec<T>::get(__ldcg(reinterpret_cast<const uint4*>(v + head * a.hd + e)), f);
-            to_cache(a.vc, head, e, f);
-            continue;
+    const int lines = kRopeThreads * gridDim.y, line = blockIdx.y * kRopeThreads + threadIdx.x;  // threads of the row
+    // values first: they need no angles
+    const int n_pass = a.hd / V;
+    if (cached) {
+        const int c = line % n_pass, step = lines / n_pass;
+        const T* v = (const T*)a.v + (int64_t)row * a.v_stride + c * V;
+        for (int h = line / n_pass; h < a.n_kv_heads; h += kRopeAhead * step) {
+            uint4 x[kRopeAhead];
+#pragma unroll
+            for (int i = 0; i < kRopeAhead; ++i)
+                if (h + i * step < a.n_kv_heads) x[i] = __ldcg(reinterpret_cast<const uint4*>(v + (h + i * step) * a.hd));
+#pragma unroll
+            for (int i = 0; i < kRopeAhead; ++i)
+                if (h + i * step < a.n_kv_heads) {
+                    float f[V];
+                    Vec<T>::get(x[i], f);
+                    to_cache(a.vc, h + i * step, c * V, f);
+                }
         }
-        const bool is_q = u < n_q;
-        const int w = is_q ? u : u - n_q, head = w / n_rot, c = w - head * n_rot;
-        const T* src = (is_q ? q : k) + head * a.hd;
-        auto store = [&](int e, const float (&f)[V]) {
-            if (is_q) *reinterpret_cast<uint4*>(qo + head * a.hd + e) = Vec<T>::put(f);
-            else to_cache(a.kc, head, e, f);
-        };
-        if (c >= n_pair) {
-            const int e = a.rope.rot_dim + (c - n_pair) * V;
+    }
+    __syncthreads();
+    // queries and keys, heads 0 .. n_heads - 1 and n_heads .. ; a head's pairs first, then what passes
+    const int n_pair = a.rope.interleaved ? a.rope.rot_dim / V : half / V, n_rot = n_pair + (a.hd - a.rope.rot_dim) / V;
+    const int c = line % n_rot, step = lines / n_rot, heads = a.n_heads + (cached ? a.n_kv_heads : 0);
+    if (line >= step * n_rot) return;  // (no whole head is left for these threads)
+    const bool pair = c < n_pair, two = pair && !a.rope.interleaved;
+    const int e = pair ? c * V : a.rope.rot_dim + (c - n_pair) * V;
+    const T* q = (const T*)a.q + (int64_t)row * a.q_stride + e;
+    const T* k = (const T*)a.k + (int64_t)row * a.k_stride + e;
+    T* qo = (T*)a.q_out + (int64_t)row * a.q_out_stride + e;
+    for (int h0 = line / n_rot; h0 < heads; h0 += kRopeAhead * step) {
+        uint4 x[kRopeAhead], y[kRopeAhead];
+#pragma unroll
+        for (int i = 0; i < kRopeAhead; ++i) {
+            const int h = h0 + i * step;
+            if (h < heads) {
+                const T* src = h < a.n_heads ? q + (int64_t)h * a.hd : k + (int64_t)(h - a.n_heads) * a.hd;
+                x[i] = __ldcg(reinterpret_cast<const uint4*>(src));
+                if (two) y[i] = __ldcg(reinterpret_cast<const uint4*>(src + half));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRopeAhead; ++i) {
+            const int h = h0 + i * step;
+            if (h >= heads) break;
+            auto store = [&](int more, const float (&f)[V]) {
+                if (h < a.n_heads) *reinterpret_cast<uint4*>(qo + (int64_t)h * a.hd + more) = Vec<T>::put(f);
+                else to_cache(a.kc, h - a.n_heads, e + more, f);
+            };
             float f[V];
-            Vec<T>::get(__ldcg(reinterpret_cast<const uint4*>(src + e)), f);
-            store(e, f);
-        } else if (a.rope.interleaved) {
-            float f[V], o[V];
-            Vec<T>::get(__ldcg(reinterpret_cast<const uint4*>(src + c * V)), f);
+            Vec<T>::get(x[i], f);
+            if (two) {
+                float g[V], o[V], p[V];
+                Vec<T>::get(y[i], g);
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                const float2 cs = s_cs[c * (V / 2) + i];
-                o[2 * i] = f[2 * i] * cs.x - f[2 * i + 1] * cs.y;
-                o[2 * i + 1] = f[2 * i + 1] * cs.x + f[2 * i] * cs.y;
-            }
-            store(c * V, o);
-        } else {
-            float f[V], g[V], o[V], p[V];
-            Vec<T>::get(__ldcg(reinterpret_cast<const uint4*>(src + c * V)), f);
-            Vec<T>::get(__ldcg(reinterpret_cast<const uint4*>(src + half + c * V)), g);
+                for (int j = 0; j < V; ++j) {
+                    const float2 cs = s_cs[c * V + j];
+                    o[j] = f[j] * cs.x - g[j] * cs.y;
+                    p[j] = g[j] * cs.x + f[j] * cs.y;
+                }
+                store(0, o);
+                store(half, p);
+            } else if (pair) {
+                float o[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 cs = s_cs[c * V + i];
-                o[i] = f[i] * cs.x - g[i] * cs.y;
-                p[i] = g[i] * cs.x + f[i] * cs.y;
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 cs = s_cs[c * (V / 2) + j];
+                    o[2 * j] = f[2 * j] * cs.x - f[2 * j + 1] * cs.y;
+                    o[2 * j + 1] = f[2 * j + 1] * cs.x + f[2 * j] * cs.y;
+                }
+                store(0, o);
+            } else {
+                store(0, f);
             }
-            store(c * V, o);
-            store(half + c * V, p);
         }
     }
 }
@@ -291,7 +348,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
 // ---------------------------------------------------------------------------
 // ssd_tree_commit
 // ---------------------------------------------------------------------------
-constexpr int kCommitThreads = 256;
+constexpr int kCommitThreads = 256, kCommitAhead = 4, kCommitColumns = 2;
 static_assert(kCommitThreads >= kMaxNodes, "a thread per node");
 
 struct CommitArgs {
@@ -304,8 +361,8 @@ struct CommitArgs {
 };
 
 // A request's CTAs (gridDim.y) each walk its path - a warp, eight nodes a lane -
-// and move their share of (K or V, layer, head, 16 bytes) columns.  A thread takes
-// a column along the whole path in order, four rows at a time: path[j] >= j and
+// and move their share of (K or V, layer, head, 16 bytes) columns.  A thread takes two
+// columns along the whole path in order, four rows at a time: path[j] >= j and
 // the path rises, so nothing is overwritten before it is read.
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArgs a) {
     __shared__ int s_parent[kMaxNodes], s_token[kMaxNodes], s_target[kMaxNodes], s_path[kMaxNodes], s_n;
@@ -372,24 +429,35 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArgs
         }
     }
     if (!a.kc) return;
-    const int per_layer = 2 * a.n_kv_heads * a.chunks;
-    const long long columns = (long long)a.n_layers * per_layer;
-    for (long long col = (long long)blockIdx.y * kCommitThreads + tid; col < columns; col += (long long)gridDim.y * kCommitThreads) {
-        const int layer = (int)(col / per_layer), r = (int)(col - (long long)layer * per_layer);
-        const int kv = r / (a.n_kv_heads * a.chunks), r2 = r - kv * a.n_kv_heads * a.chunks, head = r2 / a.chunks, c = r2 - head * a.chunks;
-        char* base = (char*)(kv ? a.vc : a.kc) + 2 * (layer * a.layer_stride + head * a.head_stride + c * 8);
-        for (int j = 1; j <= n; j += 4) {
-            uint4 x[4];
-            int64_t src[4], dst[4];
+    const unsigned per_layer = 2u * a.n_kv_heads * a.chunks, per_kv = (unsigned)(a.n_kv_heads * a.chunks);
+    const unsigned columns = (unsigned)a.n_layers * per_layer, lines = gridDim.y * kCommitThreads;
+    for (unsigned col = blockIdx.y * kCommitThreads + tid; col < columns; col += kCommitColumns * lines) {
+        char* base[kCommitColumns];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                src[i] = -1;
+        for (int k = 0; k < kCommitColumns; ++k) {
+            const unsigned x = min(col + k * lines, columns - 1);
+            const unsigned layer = x / per_layer, r = x - layer * per_layer, kv = r >= per_kv, r2 = r - kv * per_kv;
+            const unsigned head = r2 / (unsigned)a.chunks, c = r2 - head * (unsigned)a.chunks;
+            base[k] = (char*)(kv ? a.vc : a.kc) + 2 * (layer * a.layer_stride + head * a.head_stride + c * 8);
+        }
+        for (int j = 1; j <= n; j += kCommitAhead) {
+            uint4 x[kCommitColumns][kCommitAhead];
+            int64_t src[kCommitAhead], dst[kCommitAhead];
+#pragma unroll
+            for (int i = 0; i < kCommitAhead; ++i) {
+                src[i] = dst[i] = -1;
                 if (j + i <= n && s_path[j + i] != j + i) src[i] = s_off[s_path[j + i]], dst[i] = s_off[j + i];
-                if (src[i] >= 0) x[i] = __ldcg(reinterpret_cast<const uint4*>(base + 2 * src[i]));
+                if (src[i] >= 0)
+#pragma unroll
+                    for (int k = 0; k < kCommitColumns; ++k)
+                        if (col + k * lines < columns) x[k][i] = __ldcg(reinterpret_cast<const uint4*>(base[k] + 2 * src[i]));
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (src[i] >= 0 && dst[i] >= 0) *reinterpret_cast<uint4*>(base + 2 * dst[i]) = x[i];
+            for (int i = 0; i < kCommitAhead; ++i)
+                if (src[i] >= 0 && dst[i] >= 0)
+#pragma unroll
+                    for (int k = 0; k < kCommitColumns; ++k)
+                        if (col + k * lines < columns) *reinterpret_cast<uint4*>(base[k] + 2 * dst[i]) = x[k][i];
         }
     }
 }
@@ -513,7 +581,7 @@ extern "C" int ssd_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* ro
     const int per16 = dtype == SSD_F32 ? 4 : 8;
     const long long units = (long long)(n_heads + 2 * cache->n_kv_heads) * hd / per16;
     int split = 1;
-    while (split < 64 && (long long)n_rows * split < 304 && units > (long long)kRopeThreads * split) split *= 2;
+    while (split < 64 && (long long)n_rows * split < 608 && units > (long long)kRopeThreads * split) split *= 2;
     const dim3 grid((unsigned)n_rows, (unsigned)split);
     if (dtype == SSD_F32) return launch(call, rope_kernel<float, f16>, grid, kRopeThreads, 0, cuda_stream, a);
     if (dtype == SSD_F16) return launch(call, rope_kernel<f16, f16>, grid, kRopeThreads, 0, cuda_stream, a);
@@ -559,7 +627,8 @@ extern "C" int ssd_tree_commit(const ssd_batch* batch, const ssd_pages* cache, c
         a.head_stride = cache->head_stride;
         a.pos_stride = cache->pos_stride;
         const long long columns = 2ll * cache->n_layers * cache->n_kv_heads * a.chunks;
-        while (split < 64 && columns > (long long)kCommitThreads * split && (long long)batch->n_requests * split < 1216) split *= 2;
+        if (columns >= (1ll << 30)) return refuse_arg(call, "need n_layers * n_kv_heads * head_dim < 2^32");
+        while (split < 64 && columns > (long long)kCommitThreads * split && (long long)batch->n_requests * split < 304) split *= 2;
     }
     return launch(call, commit_kernel, dim3((unsigned)batch->n_requests, (unsigned)split), kCommitThreads, 0, cuda_stream, a);
 }
