@@ -60,7 +60,7 @@ namespace tree {
 namespace {
 
 constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp16
-constexpr unsigned long long kWaitNs = 2000000000ull;
+constexpr long long kWaitClocks = 4000000000ll;  // 2 s at 2 GHz
 constexpr int kTile = 128;  // rows: the TMEM lanes
 constexpr int kThreads = 512;
 constexpr int kTmem = 512;  // columns: O at 0, S / P of unit j at 128 + 128 (j mod 3)
@@ -227,13 +227,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// bounded wait; false after kWaitNs, or once another thread of the CTA has given up
+// bounded wait; false after kWaitClocks, or once another thread of the CTA has given up
 __device__ __noinline__ bool mb_wait_on(uint64_t* b, unsigned parity, volatile int* fail) {
-    const unsigned long long t0 = tc::gtime();
+    const long long t0 = clock64();
 #pragma unroll 1
     while (!tc::mb_try(b, parity)) {
         if (*fail) return false;
-        if (tc::gtime() - t0 > kWaitNs) {
+        if (clock64() - t0 > kWaitClocks) {
             *fail = 1;
             return false;
         }
@@ -266,31 +266,32 @@ __device__ __forceinline__ void split_bits(f32x2 v, uint32_t& hi, uint32_t& lo) 
     lo = half2_of(rest(v, h));
 }
 
-// which of the positions p0 .. p0 + 63 node `node` (mask words m) sees, as bits
-__device__ __noinline__ uint64_t visible(const Req& q, int chain, const uint64_t (&m)[4], int node, int p0) {
-    const int end = q.total - p0;  // the unit's positions below it exist
+// which of the positions p0 .. p0 + 63 node `node` (mask words m0 ..) of a request sees, as bits.  (Arguments of
+// functions that are not inlined are values: a reference would put what it refers to into local memory.)
+__device__ __noinline__ uint64_t visible(int len, int total, int chain, uint64_t m0, uint64_t m1, uint64_t m2, uint64_t m3, int node, int p0) {
+    const int end = total - p0;  // the unit's positions below it exist
     uint64_t v;
     if (chain) {
-        const long long last = (long long)q.len + node - p0;
+        const long long last = (long long)len + node - p0;
         v = last >= 63 ? ~0ull : last < 0 ? 0ull : (2ull << last) - 1ull;
     } else {
-        const int j0 = p0 - q.len;  // node of the unit's first position
+        const int j0 = p0 - len;  // node of the unit's first position
         if (j0 <= -64) {
             v = ~0ull;
         } else if (j0 <= 0) {
-            v = j0 == 0 ? m[0] : (m[0] << -j0) | ((1ull << -j0) - 1ull);
+            v = j0 == 0 ? m0 : (m0 << -j0) | ((1ull << -j0) - 1ull);
         } else {
             const int w = j0 >> 6, s = j0 & 63;
-            const uint64_t a = w == 0 ? m[0] : w == 1 ? m[1] : w == 2 ? m[2] : w == 3 ? m[3] : 0ull;
-            const uint64_t b = w == 0 ? m[1] : w == 1 ? m[2] : w == 2 ? m[3] : 0ull;
+            const uint64_t a = w == 0 ? m0 : w == 1 ? m1 : w == 2 ? m2 : w == 3 ? m3 : 0ull;
+            const uint64_t b = w == 0 ? m1 : w == 1 ? m2 : w == 2 ? m3 : 0ull;
             v = s ? (a >> s) | (b << (64 - s)) : a;
         }
     }
     return end >= 64 ? v : end <= 0 ? 0ull : v & ((1ull << end) - 1ull);
 }
 
-// (one copy for all roles)
-__device__ __noinline__ bool next_seg(Walk& w, const Shape& s, int tile, Seg& g) { return walk_next(w, s, tile, g); }
+
+__device__ __forceinline__ bool next_seg(Walk& w, const Shape& s, int tile, Seg& g) { return walk_next(w, s, tile, g); }
 
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, f16) { return ((u & 0x7c00u) == 0x7c00u) | ((u & 0x7c000000u) == 0x7c000000u) << 1; }
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, bf16) { return ((u & 0x7f80u) == 0x7f80u) | ((u & 0x7f800000u) == 0x7f800000u) << 1; }
@@ -335,21 +336,26 @@ __device__ __noinline__ void clean_v(unsigned char* v8, int lo, int end, int hi,
 
 // What the values that are not finite, of the segment's nodes that a row sees, add to dim d of its
 // sum (they were left out of the products).
+struct OddArgs {
+    const uint64_t* masks;   // of the row (nullptr: chain)
+    const int32_t* table;    // of the request
+    const void* v;           // of the layer and head, at dim 0
+    int64_t page_stride, pos_stride;
+    int words, page_size, n_pages;
+};
 template <typename C>
-__device__ __noinline__ float odd_sum(const AttnOpArgs& a, const Seg& g, int node, int d) {
-    const Shape& sh = a.shape;
+__device__ __noinline__ float odd_sum(OddArgs a, int len, int total, int node, int from, int to, int d) {
     uint64_t m[4] = {0, 0, 0, 0};
-    if (!sh.chain)
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(g.q.r0 + node) * a.words + w);
+    for (int w = 0; w < 4; ++w)
+        if (a.masks && w < a.words) m[w] = __ldcg(a.masks + w);
     float sum = 0.f;
 #pragma unroll 1
-    for (int x = max(g.u0 * kUnit, g.q.len); x < min(g.u1 * kUnit, g.q.total); ++x) {
-        if (!(visible(g.q, sh.chain, m, node, x) & 1)) continue;
-        const int page = __ldcg(a.block_table + (size_t)g.b * sh.max_blocks + x / sh.page_size);
+    for (int x = max(from, len); x < min(to, total); ++x) {
+        if (!(visible(len, total, a.masks == nullptr, m[0], m[1], m[2], m[3], node, x) & 1)) continue;
+        const int page = __ldcg(a.table + x / a.page_size);
         if (page < 0 || page >= a.n_pages) continue;
-        const float f = (float)((const C*)a.vc)[page * a.page_stride + g.kvh * a.head_stride + (x % sh.page_size) * a.pos_stride + d];
+        const float f = (float)((const C*)a.v)[page * a.page_stride + (x % a.page_size) * a.pos_stride + d];
         if (!isfinite(f)) sum += f;
     }
     return sum;
@@ -696,6 +702,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 e = s_end[n_seg & 3][last][mine32], f = s_end[n_seg & 3][last ^ 1][mine32];
                 const float sum = e.y + f.y * (f.x == -INFINITY ? 0.f : ex2(f.x - e.x)), inv = sum == 0.f ? 0.f : 1.f / sum;
                 const bool odd = *(volatile int*)&s_odd;
+                auto odd_at = [&](int d) {
+                    const OddArgs oa = {sh.chain ? nullptr : a.masks + (size_t)(cur.q.r0 + node) * a.words, a.block_table + (size_t)cur.b * sh.max_blocks,
+                                        (const C*)a.vc + cur.kvh * a.head_stride, a.page_stride, a.pos_stride, a.words, sh.page_size, a.n_pages};
+                    return odd_sum<C>(oa, cur.q.len, cur.q.total, node, cur.u0 * kUnit, cur.u1 * kUnit, d);
+                };
                 if (!whole && valid) {
                     float* st = a.stats + (size_t)(cta * 2 + slot) * 2 * kTile + mine32;
                     st[0] = e.x;
@@ -722,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (odd)
 #pragma unroll 1
                             for (int i = 0; i < 32; ++i) {
-                                const float f = odd_sum<C>(a, cur, node, c + i);
+                                const float f = odd_at(c + i);
                                 if (f != 0.f) to[i] = (T)((float)to[i] + f);
                             }
                     } else {
@@ -734,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                             for (int i = 0; i < 32; ++i) {
                                 float* p = reinterpret_cast<float*>(to + (i >> 2) * kTile) + (i & 3);
-                                const float f = odd_sum<C>(a, cur, node, c + i);
+                                const float f = odd_at(c + i);
                                 if (f != 0.f) *p += f;
                             }
                     }
@@ -801,7 +812,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         uint64_t v = 0;
 #pragma unroll 1
                         for (int c = 0; c < kUnit / 32; ++c) {
-                            v = c & 1 ? v >> 32 : visible(g.q, sh.chain, m, node, p0 + 32 * c);
+                            v = c & 1 ? v >> 32 : visible(g.q.len, g.q.total, sh.chain, m[0], m[1], m[2], m[3], node, p0 + 32 * c);
                             load(c);
 #pragma unroll
                             for (int k = 0; k < 32; ++k)

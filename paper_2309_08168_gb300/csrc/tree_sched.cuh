@@ -70,10 +70,10 @@ __host__ __device__ __forceinline__ int units_of(const Shape& s, const Req& q, i
     }
     return (keys + kUnit - 1) / kUnit;
 }
-// units of one KV head of a request, with what its items count more.  (Functions of their own, and
-// no unrolling, here and below: these run once or a few times in a CTA's life, and
-// their instructions come from L2 at first use.)
-__host__ __device__ __noinline__ inline long long head_units(const Shape& s, const Req& q, int tile) {
+// units of one KV head of a request, with what its items count more.  (No unrolling, here and
+// below: these run once or a few times in a CTA's life, and their instructions come from
+// L2 at first use.)
+__host__ __device__ __forceinline__ long long head_units(const Shape& s, const Req& q, int tile) {
     const int n = tiles_of(s, q, tile);
     if (!s.chain) return (long long)n * (n ? units_of(s, q, tile, 0) + kItemCost : 0);
     long long u = (long long)n * kItemCost;
