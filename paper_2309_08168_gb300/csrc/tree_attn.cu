@@ -65,7 +65,7 @@ constexpr int kTile = 128;  // rows: the TMEM lanes
 constexpr int kThreads = 512;
 constexpr int kTmem = 512;  // columns: O at 0, S / P of unit j at 128 + 128 (j mod 3)
 constexpr int kMaxSlots = 12;
-constexpr int kJoinThreads = 256, kJoinLines = 4;
+constexpr int kJoinThreads = 128, kJoinLines = 16;
 
 // what a CTA whose range ends inside an item leaves for join_kernel
 struct alignas(16) Cut {
@@ -919,57 +919,86 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Joins the parts of the items that range ends cut.  CTA c of the attention left a
 // Cut if its range ends inside an item; with n such ends in an item, n lines of CTAs
-// (gridDim.y each) share it here: a warp takes 32 rows (a lane each) and 16 bytes of dims at a
-// time, first the largest maximum of the parts, then the weighted sums, in the order
-// of the parts.  Bound by L2 latency: all loads of a few parts are under way at once.
+// (gridDim.y each) share it here.  A piece of work is 32 rows (a lane each) and 16 bytes of
+// dims; 1, 2, 4 or 8 warps take up to four parts of it each at once, in the order of
+// the parts, and the first one adds their sums, in order.  Bound by L2 latency: with more
+// parts a warp one after the other (19 parts of 8 items) the long request took 4 us more.
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnOpArgs a) {
-    constexpr int W = kJoinThreads / 32, D = Vec<T>::N;
+    constexpr int W = kJoinThreads / 32, D = Vec<T>::N, AHEAD = 4;
+    __shared__ float s_o[W][D + 2][32];
     pdl_launch_dependents();
     pdl_wait();
-    const int cta = blockIdx.x, lane = threadIdx.x & 31;
+    const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int4 c0 = __ldcg(reinterpret_cast<const int4*>(a.cuts + cta)), c1 = __ldcg(reinterpret_cast<const int4*>(a.cuts + cta) + 1);
     const int first = c0.x, last = c0.y, slot = c0.z, row0 = c0.w, rows = c1.x, r0 = c1.y, kvh = c1.z;
     if (last < 0) return;
-    const int warps = (last - first) * (int)gridDim.y * W, items = (rows + 31) / 32 * (HD / D);
-    for (int w = ((cta - first) * (int)gridDim.y + blockIdx.y) * W + (threadIdx.x >> 5); w < items; w += warps) {
-        const int chunk = w % (HD / D), row = w / (HD / D) * 32 + lane;
-        if (row >= rows) continue;
-        auto part_of = [&](int p) { return (size_t)(p * 2 + (p == first ? slot : 0)); };
-        float top = -INFINITY;
-#pragma unroll 16
-        for (int p = first; p <= last; ++p) top = fmaxf(top, __ldcg(a.stats + part_of(p) * 2 * kTile + row));
-        float l = 0.f, o[D];
+    const int parts = last - first + 1;
+    int team = 1;  // warps of a piece
+    while (team < W && parts > AHEAD * team) team *= 2;
+    const int per = (parts + team - 1) / team, mate = warp & (team - 1), teams = W / team;
+    const int lines = (last - first) * (int)gridDim.y, items = (rows + 31) / 32 * (HD / D);
+    for (int w0 = ((cta - first) * (int)gridDim.y + blockIdx.y) * teams; w0 < items; w0 += lines * teams) {  // (the same for the CTA's warps)
+        const int w = w0 + warp / team, chunk = w % (HD / D), row = w / (HD / D) * 32 + lane;
+        const bool mine = w < items && row < rows;
+        float top = -INFINITY, l = 0.f, o[D];
 #pragma unroll
         for (int i = 0; i < D; ++i) o[i] = 0.f;
-#pragma unroll 8
-        for (int p = first; p <= last; ++p) {
-            const float* st = a.stats + part_of(p) * 2 * kTile + row;
-            const float m = __ldcg(st), lp = __ldcg(st + kTile);
-            float4 x[D / 4];
+        auto add = [&](float m, float lp, const float (&x)[D]) {
+            const float t = fmaxf(top, m), f = top == -INFINITY ? 0.f : ex2(top - t), g = m == -INFINITY ? 0.f : ex2(m - t);  // (0 x NaN stays NaN)
+            l = l * f + lp * g;
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) x[i] = __ldcg(a.part + (part_of(p) * (HD / 4) + chunk * (D / 4) + i) * kTile + row);
-            const float f = m == -INFINITY ? 0.f : ex2(m - top);  // (0 x NaN stays NaN)
-            l = fmaf(lp, f, l);
+            for (int i = 0; i < D; ++i) o[i] = o[i] * f + x[i] * g;
+            top = t;
+        };
+        const int p1 = min(first + (mate + 1) * per, last + 1);
+        if (mine)
+            for (int p = first + mate * per; p < p1; p += AHEAD) {
+                float m[AHEAD], lp[AHEAD];
+                float4 x[AHEAD][D / 4];
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) {
-                o[4 * i] = fmaf(x[i].x, f, o[4 * i]);
-                o[4 * i + 1] = fmaf(x[i].y, f, o[4 * i + 1]);
-                o[4 * i + 2] = fmaf(x[i].z, f, o[4 * i + 2]);
-                o[4 * i + 3] = fmaf(x[i].w, f, o[4 * i + 3]);
+                for (int i = 0; i < AHEAD; ++i)
+                    if (p + i < p1) {
+                        const size_t part = (size_t)((p + i) * 2 + (p + i == first ? slot : 0));
+                        const float* st = a.stats + part * 2 * kTile + row;
+                        m[i] = __ldcg(st);
+                        lp[i] = __ldcg(st + kTile);
+#pragma unroll
+                        for (int k = 0; k < D / 4; ++k) x[i][k] = __ldcg(a.part + (part * (HD / 4) + chunk * (D / 4) + k) * kTile + row);
+                    }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (p + i < p1) {
+                        float f[D];
+#pragma unroll
+                        for (int k = 0; k < D / 4; ++k) f[4 * k] = x[i][k].x, f[4 * k + 1] = x[i][k].y, f[4 * k + 2] = x[i][k].z, f[4 * k + 3] = x[i][k].w;
+                        add(m[i], lp[i], f);
+                    }
             }
+        if (team > 1) {
+            if (mate) {
+                s_o[warp][0][lane] = top;
+                s_o[warp][1][lane] = l;
+#pragma unroll
+                for (int i = 0; i < D; ++i) s_o[warp][2 + i][lane] = o[i];
+            }
+            __syncthreads();
+            if (!mate)
+                for (int k = 1; k < team; ++k) {
+                    float f[D];
+#pragma unroll
+                    for (int i = 0; i < D; ++i) f[i] = s_o[warp + k][2 + i][lane];
+                    add(s_o[warp + k][0][lane], s_o[warp + k][1][lane], f);
+                }
+            __syncthreads();
         }
+        if (!mine || mate) continue;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int r = row0 + row, node = r / a.shape.group, head = kvh * a.shape.group + r - node * a.shape.group;
         T* to = (T*)a.out + (int64_t)(r0 + node) * a.out_stride + head * HD + chunk * D;
-        constexpr int V = Vec<T>::N;
 #pragma unroll
-        for (int i = 0; i < D; i += V) {
-            float f[V];
-#pragma unroll
-            for (int k = 0; k < V; ++k) f[k] = o[i + k] * inv;
-            *reinterpret_cast<uint4*>(to + i) = Vec<T>::put(f);
-        }
+        for (int i = 0; i < D; ++i) o[i] *= inv;
+        *reinterpret_cast<uint4*>(to) = Vec<T>::put(o);
     }
 }
 
