@@ -338,6 +338,8 @@ def ssd_tree_plan(batch: TreeBatch, page_size: int, n_pages: int, parents, held,
     int32 [n]; ring int32 [n_pages]; ends, ends_out int64 [2]; slots, positions int32 [n_rows]; masks int64 [n_rows][words]
     (bit patterns) with parents; status int32 [1] or None."""
     d, n, r, i32, i64 = batch.device, batch.n_requests, batch.n_rows, batch.i32, _of_type(ends, "ends", "torch.int64")
+    if r == 0:  # (pages only)
+        parents = masks = None
     words = _words(masks)
     _check(lib.ssd_tree_plan(batch.struct, page_size, n_pages, _dev(parents, "parents", i32, d, r), _dev(held, "held", i32, d, n),
                              _dev(held_out, "held_out", i32, d, n), _dev(ring, "ring", i32, d, n_pages), _dev(ends, "ends", i64, d, 2),

@@ -293,9 +293,6 @@ __device__ __noinline__ uint64_t visible(int len, int total, int chain, uint64_t
     return end >= 64 ? v : end <= 0 ? 0ull : v & ((1ull << end) - 1ull);
 }
 
-
-__device__ __forceinline__ bool next_seg(Walk& w, const Shape& s, int tile, Seg& g) { return walk_next(w, s, tile, g); }
-
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, f16) { return ((u & 0x7c00u) == 0x7c00u) | ((u & 0x7c000000u) == 0x7c000000u) << 1; }
 __device__ __forceinline__ uint32_t exps_all_ones(uint32_t u, bf16) { return ((u & 0x7f80u) == 0x7f80u) | ((u & 0x7f800000u) == 0x7f800000u) << 1; }
 
@@ -337,31 +334,40 @@ __device__ __noinline__ void clean_v(unsigned char* v8, int lo, int end, int hi,
     }
 }
 
-// What the values that are not finite, of the segment's nodes that a row sees, add to dim d of its
-// sum (they were left out of the products).
+// Adds to 32 dims of a row's result, in memory, the values that are not finite of positions
+// from .. to - 1 that the row sees (clean_v left them out of the products).  Dim i lies at
+// out[(i / 4) * stride + i % 4].
 struct OddArgs {
     const uint64_t* masks;   // of the row (nullptr: chain)
     const int32_t* table;    // of the request
-    const void* v;           // of the layer and head, at dim 0
+    const void* v;           // of the layer and head, at the first dim
     int64_t page_stride, pos_stride;
     int words, page_size, n_pages;
 };
-template <typename C>
-__device__ __noinline__ float odd_sum(OddArgs a, int len, int total, int node, int from, int to, int d) {
+template <typename C, typename E>
+__device__ __noinline__ void add_odd(OddArgs a, int len, int total, int node, int from, int to, E* out, int stride) {
     uint64_t m[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < 4; ++w)
         if (a.masks && w < a.words) m[w] = __ldcg(a.masks + w);
-    float sum = 0.f;
 #pragma unroll 1
     for (int x = max(from, len); x < min(to, total); ++x) {
         if (!(visible(len, total, a.masks == nullptr, m[0], m[1], m[2], m[3], node, x) & 1)) continue;
         const int page = __ldcg(a.table + x / a.page_size);
         if (page < 0 || page >= a.n_pages) continue;
-        const float f = (float)((const C*)a.v)[page * a.page_stride + (x % a.page_size) * a.pos_stride + d];
-        if (!isfinite(f)) sum += f;
+        const uint4* v = reinterpret_cast<const uint4*>((const C*)a.v + page * a.page_stride + (x % a.page_size) * a.pos_stride);
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            float f[8];
+            Vec<C>::get(__ldcg(v + i), f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (!isfinite(f[k])) {
+                    E* p = out + (2 * i + k / 4) * stride + k % 4;
+                    *p = (E)((float)*p + f[k]);
+                }
+        }
     }
-    return sum;
 }
 
 template <typename T, int HD>
@@ -497,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool mine_too = lane < (is_v ? copies * BOXES : copies);
         const unsigned bytes = is_v ? L::VSLOT : L::KSLOT;
         unsigned slot = 0, phase = 1;
-        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
             const int32_t* table = a.block_table + (size_t)g.b * sh.max_blocks;
             auto fetch = [&](long long x) {  // page of this lane's copy of the 32 from x on; -1: outside, reads as zeros
                 x += lane << a.box_shift;
@@ -545,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t q0 = tc::sdesc(smem_u32(smem)), k0 = tc::sdesc(smem_u32(ks));
         const uint32_t qb = (uint32_t)tile * 128;  // 64 dims of the tile's q
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;  // unit 3 turn + buf
-        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
             if (!wait(&q_ready, n_seg)) break;
             const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
 #pragma unroll 1
@@ -580,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // V: hd dims (MN) x 16 positions (K) per MMA; 8 positions are 1024 bytes apart, 64 dims a box
         const uint64_t v0 = tc::sdesc(smem_u32(vs)) + ((uint64_t)((L::VBOX >> 4) - 1) << 16);
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;
-        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
                 const bool fresh = u == g.u0;
@@ -668,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             if (lane == 0) arrive(&q_ready);
         };
-        bool more = next_seg(walk, sh, tile, g);
+        bool more = walk_next(walk, sh, tile, g);
         if (more) load_q(g, 0);
         unsigned j_end = 0;  // units of the CTA up to the segment's end
         for (unsigned n_seg = 0; more && ok; ++n_seg) {
@@ -679,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const unsigned buf = (j_end - 1) % 3, turn = (j_end - 1) / 3;  // of the segment's last unit
             // The next rows' q: into the other buffer (the last segment but this one is finished), or, with
             // one buffer, once all scores of this segment are there
-            more = next_seg(walk, sh, tile, g);
+            more = walk_next(walk, sh, tile, g);
             if (more) {
                 if (tile != 32 && !wait(&q_free, n_seg)) break;
                 load_q(g, n_seg + 1);
@@ -705,10 +711,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 e = s_end[n_seg & 3][last][mine32], f = s_end[n_seg & 3][last ^ 1][mine32];
                 const float sum = e.y + f.y * (f.x == -INFINITY ? 0.f : ex2(f.x - e.x)), inv = sum == 0.f ? 0.f : 1.f / sum;
                 const bool odd = *(volatile int*)&s_odd;
-                auto odd_at = [&](int d) {
+                // positions below it are seen by every row, and their values multiplied as they are
+                const int all_seen = min(sh.chain ? cur.q.len + node0 + 1 : cur.q.len, cur.q.total);
+                auto odd_to = [&](int c, auto* to, int stride) {
                     const OddArgs oa = {sh.chain ? nullptr : a.masks + (size_t)(cur.q.r0 + node) * a.words, a.block_table + (size_t)cur.b * sh.max_blocks,
-                                        (const C*)a.vc + cur.kvh * a.head_stride, a.page_stride, a.pos_stride, a.words, sh.page_size, a.n_pages};
-                    return odd_sum<C>(oa, cur.q.len, cur.q.total, node, cur.u0 * kUnit, cur.u1 * kUnit, d);
+                                        (const C*)a.vc + cur.kvh * a.head_stride + c, a.page_stride, a.pos_stride, a.words, sh.page_size, a.n_pages};
+                    add_odd<C>(oa, cur.q.len, cur.q.total, node, max(cur.u0, all_seen / kUnit) * kUnit, cur.u1 * kUnit, to, stride);
                 };
                 if (!whole && valid) {
                     float* st = a.stats + (size_t)(cta * 2 + slot) * 2 * kTile + mine32;
@@ -733,24 +741,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                             for (int k = 0; k < V; ++k) f[k] = __uint_as_float(o[i + k]);
                             *reinterpret_cast<uint4*>(to + i) = Vec<T>::put(f);
                         }
-                        if (odd)
-#pragma unroll 1
-                            for (int i = 0; i < 32; ++i) {
-                                const float f = odd_at(c + i);
-                                if (f != 0.f) to[i] = (T)((float)to[i] + f);
-                            }
+                        if (odd) odd_to(c, to, 4);
                     } else {
                         float4* to = a.part + ((size_t)(cta * 2 + slot) * (HD / 4) + c / 4) * kTile + mine32;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             to[(i / 4) * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
-                        if (odd)
-#pragma unroll 1
-                            for (int i = 0; i < 32; ++i) {
-                                float* p = reinterpret_cast<float*>(to + (i >> 2) * kTile) + (i & 3);
-                                const float f = odd_at(c + i);
-                                if (f != 0.f) *p += f;
-                            }
+                        if (odd) odd_to(c, reinterpret_cast<float*>(to), 4 * kTile);
                     }
                 }
             }
@@ -762,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int grp = warp >> 2, quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
         const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16);
         unsigned j = 0;  // of the segment's first unit
-        for (unsigned n_seg = 0; ok && next_seg(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
             const int n = g.u1 - g.u0, start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile);  // units; rows that exist
             const bool active = quarter * 32 < rows;
             const int node0 = start / sh.group, node = node0 + node_of(start - node0 * sh.group, min(mine32, rows - 1));

@@ -2,6 +2,7 @@
 // pages, slots, positions and masks of a round's rows (ssd_tree_plan), rotary
 // positions with the write of keys and values (ssd_rope_kv), and the walk along
 // the accepted path with the move of its keys and values (ssd_tree_commit).
+#include <algorithm>
 #include <cmath>
 
 #include "tree_ops.cuh"
@@ -45,7 +46,7 @@ __device__ __forceinline__ Want want_of(const PlanArgs& a, int b, const Rows& ro
     return w;
 }
 
-// One CTA per request.  Bound by latency: a request's place in the queue of free pages
+// One CTA per request; a chain's rows are shared by gridDim.y of them.  Bound by latency: a request's place in the queue of free pages
 // is a sum over those before it, which every CTA forms for itself (three words a
 // request, from L2, all threads at once) rather than wait for another launch, while its own
 // rows' parents are on their way; masks and depths of a tree come from pointer
@@ -95,14 +96,14 @@ __global__ void __launch_bounds__(kPlanThreads, 10) plan_kernel(const PlanArgs a
         return (int)(y < a.n_pages ? y : y < 2ll * a.n_pages ? y - a.n_pages : y % a.n_pages);
     };
     int32_t* table = a.block_table + (size_t)b * a.max_blocks;
-    if (tid == 0) {
+    if (tid == 0 && blockIdx.y == 0) {
         a.held_out[b] = !w.live ? 0 : given ? w.held + w.fresh : w.held;
         if (w.live && !w.fits) say(a.status, SSD_STATUS_TABLE);
         if (w.live && w.fits && !given) say(a.status, SSD_STATUS_PAGES);
     }
-    if (given)
+    if (given && blockIdx.y == 0)
         for (int j = tid; j < w.fresh; j += kPlanThreads) table[w.held + j] = __ldcg(a.ring + ring_at(h0, first + j));
-    if (!w.live)
+    if (!w.live && blockIdx.y == 0)
         for (int j = tid; j < w.back; j += kPlanThreads) a.ring[ring_at(t0, returned + j)] = __ldcg(table + j);
 
     // the rows: depths and masks of a tree first
@@ -159,7 +160,8 @@ __global__ void __launch_bounds__(kPlanThreads, 10) plan_kernel(const PlanArgs a
                 }
         }
     }
-    for (int i = tid; i < rows.n; i += kPlanThreads) {
+#pragma unroll 2
+    for (int i = blockIdx.y * kPlanThreads + tid; i < rows.n; i += kPlanThreads * gridDim.y) {
         const unsigned at = (unsigned)w.len + (unsigned)i;
         int slot = -1;
         if (given) {
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(kPlanThreads, 10) plan_kernel(const PlanArgs a
             for (int k = 0; k < 4; ++k)
                 if (k < a.words) a.masks[(size_t)(rows.r0 + i) * a.words + k] = i < nodes ? s_mask[k][i] : 0ull;
     }
-    if (b) return;
+    if (b || blockIdx.y) return;
     // The first CTA also leaves the queue's new ends: the pages taken are the largest sum over
     // the first requests, in order, that the queue covers (a run of requests per thread).
     const int per = (a.n_requests + kPlanThreads - 1) / kPlanThreads;
@@ -501,7 +503,9 @@ extern "C" int ssd_tree_plan(const ssd_batch* batch, int page_size, int n_pages,
     a.positions = positions;
     a.masks = masks;
     a.status = status;
-    return launch(call, plan_kernel, dim3((unsigned)a.n_requests), kPlanThreads, 0, cuda_stream, a);
+    // a tree is one CTA's (its threads are its nodes), a chain's rows are several CTAs', four a thread
+    const int lines = parents ? 1 : (int)std::min(64ll, ((long long)batch->max_rows + 4 * kPlanThreads - 1) / (4 * kPlanThreads));
+    return launch(call, plan_kernel, dim3((unsigned)a.n_requests, (unsigned)lines), kPlanThreads, 0, cuda_stream, a);
 }
 
 extern "C" int ssd_rope_init(int rot_dim, int interleaved, int scaling, double theta, double factor, double original_len,

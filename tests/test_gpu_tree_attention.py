@@ -108,6 +108,8 @@ class Case:
     (4, 2, 32, [40, 700], [130, 100], "tree", False),  # three mask words
     (2, 2, 16, [100, 33], [200, 300], None, False),  # prompt chunks
     (64, 1, 16, [77], [3], "tree", False),  # one KV head for all
+    (200, 1, 16, [130], [2], "tree", False),  # a node's heads in two tiles
+    (3, 1, 16, [700, 20], [150, 60], None, False),  # chains whose nodes end inside a tile
 ])
 def test_attention(ssd, kind, hd, heads, kv, page, lens, counts, masks, apart):
     c = Case(np.random.default_rng(heads * 100 + page), kind, heads, kv, hd, page, lens, counts, masks, apart=apart)
@@ -124,6 +126,64 @@ def test_attention(ssd, kind, hd, heads, kv, page, lens, counts, masks, apart):
 def test_attention_along_a_long_cache(ssd, kind, heads, kv, lens, counts):
     c = Case(np.random.default_rng(len(lens) + heads), kind, heads, kv, 128, 64, lens, counts)
     c.check(c.run(ssd))
+
+
+@pytest.mark.parametrize("kind,heads,kv,hd,page,n,rows,length,masks", [
+    ("f32", 32, 32, 128, 16, 24, 1, 1500, None), ("f16", 32, 8, 128, 48, 20, 17, 1300, "tree"), ("bf16", 16, 2, 64, 64, 30, 40, 900, "tree"),
+    ("f32", 16, 16, 128, 16, 3, 700, 600, None), ("bf16", 32, 4, 128, 32, 2, 900, 300, None), ("f32", 24, 8, 64, 80, 50, 9, 700, "tree")])
+def test_many_items(ssd, kind, heads, kv, hd, page, n, rows, length, masks):
+    """More items than CTAs: ranges with several items, against 64-bit sums on the GPU; the same bits every time."""
+    rng = np.random.default_rng(heads + n)
+    counts, lens = rng.integers((rows + 1) // 2, rows + 1, n), rng.integers(length // 6, length + 1, n)
+    c = Case(rng, kind, heads, kv, hd, page, lens, counts, masks)
+    out = c.run(ssd)
+    g, scale = heads // kv, 1 / math.sqrt(hd)
+    for b in range(n):
+        r0, r1, total = int(c.row_start[b]), int(c.row_start[b + 1]), int(c.lens[b] + counts[b])
+        x = np.arange(total)
+        p, o = torch.from_numpy(c.table[b, x // page].astype(np.int64)).cuda(), torch.from_numpy(x % page).cuda()
+        k, v = (t[0, p, :, o].double() for t in (c.k, c.v))
+        seen = torch.ones(r1 - r0, total, dtype=torch.bool, device="cuda")
+        if masks is None:
+            seen = torch.from_numpy(x[None] <= int(c.lens[b]) + np.arange(r1 - r0)[:, None]).cuda()
+        else:
+            j = torch.arange(r1 - r0, device="cuda")
+            seen[:, int(c.lens[b]):] = (dev(c.masks)[r0:r1][:, j // 64] >> (j % 64)) & 1 == 1
+        q = c.q[r0:r1].double().unflatten(1, (kv, g))
+        s = torch.einsum("tkgd,pkd->tkgp", q, k) * scale
+        sums = torch.einsum("tkgd,pkd->tkgp", q.abs(), k.abs()).amax(-1) * scale
+        w = torch.softmax(s.masked_fill(~seen[:, None, None], -math.inf), -1)
+        want = torch.einsum("tkgp,pkd->tkgd", w, v).flatten(1, 2)
+        # as in Case.check
+        d = sums.flatten(1, 2)[..., None] * (2.0**-22 * (hd / 16 + 5)) + 2.0**-20
+        pe = {"f32": 2.0**-21, "f16": 2.0**-11, "bf16": 2.0**-8}[kind]
+        tol = v.abs().max() * (2 * torch.expm1(d) + 2 * pe + 2 * 2.0**-22 * (total / 16 + 20)) + want.abs() * {"f32": 2.0**-24}.get(kind, pe) * 1.01 + 2.0**-25
+        assert bool(((out[r0:r1].double() - want).abs() <= tol).all())
+    for _ in range(10):
+        assert torch.equal(out, c.run(ssd))
+
+
+def test_the_largest_row_count_only_chooses_the_tile(ssd):
+    for heads, kv, counts, said in ((4, 4, [70, 3], 1), (8, 2, [40, 60], 2), (2, 2, [3, 1], 500)):
+        c = Case(np.random.default_rng(14), "f16", heads, kv, 128, 16, [300, 40], counts)
+        c.max_rows = said
+        c.check(c.run(ssd))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_values_that_are_not_finite_in_a_prompt(ssd, kind):
+    """A NaN in the values of one position of a chain reaches the rows from it on, an infinity in one dim of another
+    position only that dim; the rows before do not change."""
+    c = Case(np.random.default_rng(15), kind, 2, 1, 64, 16, [70], [400], None)
+    clean = c.run(ssd)
+    for node, dim, what in ((300, slice(None), float("nan")), (130, 9, float("inf"))):
+        x = 70 + node
+        c.v[0, int(c.table[0, x // 16]), :, x % 16, dim] = what
+    out = c.run(ssd)
+    assert torch.equal(out[:130], clean[:130])
+    keep = [d for d in range(64) if d != 9]
+    assert torch.equal(out[130:300][:, :, keep], clean[130:300][:, :, keep]) and not out[130:300, :, 9].isfinite().any()
+    assert out[300:400].isnan().all()
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])

@@ -100,11 +100,22 @@ def plan_case(rng, n, most_rows, most_len, page, kind, words, spare=5, ended=0.2
 @pytest.mark.parametrize("n,rows,length,page,kind,words", [
     (1, 1, 0, 16, "tree", 1), (1, 5, 37, 16, "tree", 1), (3, 64, 100, 16, "tree", 1), (7, 65, 100, 48, "tree", 2), (5, 200, 40, 64, "tree", 4),
     (2, 256, 40, 16, "chain", 4), (2, 256, 1000, 256, "star", 4), (2, 130, 10, 16, "roots", 3), (4, 300, 70, 16, "chain", 0), (300, 9, 60, 16, "tree", 1),
-    (1500, 3, 200, 16, "tree", 1), (4096, 1, 33, 16, "none", 0), (2, 3000, 5, 80, "none", 0)])
+    (1500, 3, 200, 16, "tree", 1), (4096, 1, 33, 16, "none", 0), (2, 3000, 5, 80, "none", 0), (1, 40000, 7, 48, "none", 0), (5, 0, 90, 16, "tree", 1)])
 def test_plan(ssd, n, rows, length, page, kind, words):
     rng = np.random.default_rng(n * 7 + rows)
     c = plan_case(rng, n, rows, length, page, kind, words)
     same_plan(run_plan(ssd, *c, times=2), ref.plan(*c[:7], c[7], len(c[5]), c[8], c[9]))
+
+
+def test_plan_without_rows(ssd):
+    """Only pages: ended requests give theirs back."""
+    rng = np.random.default_rng(2)
+    c = list(plan_case(rng, 6, 0, 90, 16, "tree", 1, ended=0.5, extra_rows=0))
+    c[9] = 1
+    got = run_plan(ssd, *c)
+    want = ref.plan(*c[:7], c[7], len(c[5]), c[8], c[9])
+    for k in ("table", "ring", "held", "ends"):
+        assert np.array_equal(got[k], want[k]), k
 
 
 def test_plan_short_of_pages(ssd):
