@@ -63,7 +63,7 @@ constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp
 constexpr long long kWaitClocks = 4000000000ll;  // 2 s at 2 GHz
 constexpr int kTile = 128;  // rows: the TMEM lanes
 constexpr int kThreads = 512;
-constexpr int kTmem = 512;  // columns: O at 0, S / P of unit j at 128 + 128 (j mod 3)
+constexpr int kTmem = 512;  // columns (Lay)
 constexpr int kMaxSlots = 12;
 constexpr int kJoinThreads = 128, kJoinLines = 16;
 
@@ -117,6 +117,8 @@ struct Lay {
     static constexpr int VBOX = 64 * 128;             // 64 dims of 64 positions of V
     static constexpr int VSLOT = BOXES * VBOX;
     static constexpr int RING = 213 * 1024;           // shared memory for q and the rings
+    // TMEM columns: O; fp32 rows' sums of earlier units; S / P of unit j at S0 + 128 (j mod NB)
+    static constexpr int M0 = HD, S0 = PARTS == 2 && HD == 128 ? 256 : 128, NB = (kTmem - S0) / kUnit;
     // two buffers of a tile of 32 rows, one of 128
     static __host__ __device__ constexpr int q_bytes(int tile) { return PARTS * BOXES * tile * 128; }
     static __host__ __device__ constexpr int q_all(int tile) { return q_bytes(tile) * (tile == 32 ? 2 : 1); }
@@ -177,6 +179,9 @@ __device__ __forceinline__ void ld32(uint32_t t, uint32_t (&r)[32]) {
         "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
         : SSD_R8(r, 0), SSD_R8(r, 8), SSD_R8(r, 16), SSD_R8(r, 24)
         : "r"(t));
+}
+__device__ __forceinline__ void ld16(uint32_t t, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : SSD_R8(r, 0), SSD_R8(r, 8) : "r"(t));
 }
 __device__ __forceinline__ void st32(uint32_t t, const uint32_t (&r)[32]) {
     asm volatile(
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     attn_kernel(const __grid_constant__ AttnOpArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
     using L = Lay<T, HD>;
     using C = typename Types<T>::C;
-    constexpr int BOXES = L::BOXES, PARTS = L::PARTS;
+    constexpr int BOXES = L::BOXES, PARTS = L::PARTS, NB = L::NB;
     const int tile = a.tile;
     const unsigned nk = a.nk, nv = a.nv;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -391,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // (four segments: scores are at most three units ahead of the accumulator)
     __shared__ float s_scale[4][kTile];    // [segment & 3]: power of two that a row of q was divided by
     __shared__ float2 s_end[4][2][kTile];  // [segment & 3][group]: what a row's weights are relative to, and their sum
-    __shared__ float s_ref[2][kTile];      // [group]: the same after the group's last unit
+    __shared__ float s_ref[4][kTile];      // [unit & 3]: what a unit's weights are relative to
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         s_fail = s_odd = 0;
@@ -556,60 +561,79 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
-                // P of unit j - 3, which held these columns, is used up
+                // P of unit j - NB, which held these columns, is used up
                 if (turn && !wait(pv_done + buf, turn - 1)) break;
+                const uint32_t d = tmem + (uint32_t)L::S0 + 128u * buf;
+                auto multiply = [&](int h, int b, unsigned slot, bool more) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mma_ss(d, qs + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
+                               idesc<C>(kUnit, false), (more || k) ? 1u : 0u);
+                };
+                unsigned slots[BOXES];
 #pragma unroll
                 for (int b = 0; b < BOXES; ++b) {
                     if (!wait(k_full + slot, phase)) break;
-                    tc::fence_after();
-                    if (elect_one()) {
-                        const uint32_t d = tmem + 128u + 128u * buf;
-#pragma unroll
-                        for (int h = 0; h < PARTS; ++h)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                mma_ss(d, qs + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
-                                       idesc<C>(kUnit, false), (b | h | k) ? 1u : 0u);
-                        commit(k_empty + slot);
-                        if (b == BOXES - 1) {
-                            commit(s_full + buf);
-                            if (u == g.u1 - 1) commit(&q_free);
-                        }
-                    }
-                    __syncwarp();
+                    slots[b] = slot;
                     if (++slot == nk) slot = 0, phase ^= 1u;
+                    if (PARTS == 1) {
+                        tc::fence_after();
+                        if (elect_one()) {
+                            multiply(0, b, slots[b], b > 0);
+                            commit(k_empty + slots[b]);
+                        }
+                        __syncwarp();
+                    }
                 }
-                if (++buf == 3) buf = 0, ++turn;
+                if (!ok) break;
+                tc::fence_after();
+                if (elect_one()) {
+                    if (PARTS == 2)  // lo first: the accumulator truncates at every step, relative to what it holds
+#pragma unroll
+                        for (int h = 1; h >= 0; --h)
+#pragma unroll
+                            for (int b = 0; b < BOXES; ++b) {
+                                multiply(h, b, slots[b], h == 0 || b > 0);
+                                if (h == 0) commit(k_empty + slots[b]);
+                            }
+                    commit(s_full + buf);
+                    if (u == g.u1 - 1) commit(&q_free);
+                }
+                __syncwarp();
+                if (++buf == NB) buf = 0, ++turn;
             }
         }
     } else if (warp == 11) {
         // V: hd dims (MN) x 16 positions (K) per MMA; 8 positions are 1024 bytes apart, 64 dims a box
         const uint64_t v0 = tc::sdesc(smem_u32(vs)) + ((uint64_t)((L::VBOX >> 4) - 1) << 16);
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;
+        // fp32 rows: every unit's products start from 0, once the last ones have been added to the sums; 16-bit
+        // rows: every segment's, once the last one's are written
+        unsigned taken = 0;
         for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
-                const bool fresh = u == g.u0;
-                if (fresh && n_seg && !wait(&o_free, n_seg - 1)) break;
+                const bool fresh = PARTS == 2 || u == g.u0;
+                if (fresh && taken++ && !wait(&o_free, taken - 2)) break;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     if (!wait(&p_ready[buf][half], turn) || !wait(v_full + slot, phase)) break;
                     tc::fence_after();
                     if (elect_one()) {
-                        const uint32_t p = tmem + 128u + 128u * buf + 64u * half;
+                        const uint32_t p = tmem + (uint32_t)L::S0 + 128u * buf + 64u * half;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
+                        for (int h = PARTS - 1; h >= 0; --h)  // (lo first, as above)
 #pragma unroll
-                            for (int h = 0; h < PARTS; ++h)
+                            for (int k = 0; k < 4; ++k)
                                 mma_ts(tmem, p + 32u * (k >> 1) + 16u * h + 8u * (k & 1), v0 + (uint64_t)((slot * L::VSLOT + k * 2048) >> 4), idesc<C>(HD, true),
-                                       (!fresh || half || k || h) ? 1u : 0u);
+                                       (!fresh || half || k || h < PARTS - 1) ? 1u : 0u);
                         commit(v_empty + slot);
                         if (half) commit(pv_done + buf);
                     }
                     __syncwarp();
                     if (++slot == nv) slot = 0, phase ^= 1u;
                 }
-                if (++buf == 3) buf = 0, ++turn;
+                if (++buf == NB) buf = 0, ++turn;
             }
         }
     } else if (warp >= 12) {
@@ -676,20 +700,71 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         bool more = walk_next(walk, sh, tile, g);
         if (more) load_q(g, 0);
-        unsigned j_end = 0;  // units of the CTA up to the segment's end
+        unsigned j = 0;  // of the segment's first unit
         for (unsigned n_seg = 0; more && ok; ++n_seg) {
             const Seg cur = g;
-            const int start = cur.mt * tile, rows = min(cur.q.n * sh.group - start, tile);
-            const bool valid = mine32 < rows, whole = cur.u0 == 0 && cur.u1 == cur.n;
-            j_end += (unsigned)(cur.u1 - cur.u0);
-            const unsigned buf = (j_end - 1) % 3, turn = (j_end - 1) / 3;  // of the segment's last unit
+            const int n = cur.u1 - cur.u0, start = cur.mt * tile, rows = min(cur.q.n * sh.group - start, tile);
+            const bool active = quarter * 32 < rows, valid = mine32 < rows, whole = cur.u0 == 0 && cur.u1 == cur.n;
+            const unsigned j_last = j + (unsigned)n - 1, buf = j_last % NB, turn = j_last / NB;
+            float ref = -INFINITY;  // fp32 rows: what the sums are relative to
+            float top = 0.f, sum = 0.f;  // what the result is relative to, and the weights' sum
+            auto ends = [&] {
+                if (!wait(ends_ready + (n_seg & 3), n_seg >> 2)) return false;
+                // (the last unit's group has what the accumulator is relative to now)
+                const float2 e = s_end[n_seg & 3][j_last & 1u][mine32], f = s_end[n_seg & 3][~j_last & 1u][mine32];
+                top = e.x;
+                sum = e.y + f.y * (f.x == -INFINITY ? 0.f : ex2(f.x - e.x));
+                return true;
+            };
             // The next rows' q: into the other buffer (the last segment but this one is finished), or, with
             // one buffer, once all scores of this segment are there
-            more = walk_next(walk, sh, tile, g);
-            if (more) {
-                if (tile != 32 && !wait(&q_free, n_seg)) break;
-                load_q(g, n_seg + 1);
+            auto next_q = [&] {
+                more = walk_next(walk, sh, tile, g);
+                if (more && (tile == 32 || wait(&q_free, n_seg))) load_q(g, n_seg + 1);
+            };
+            if constexpr (PARTS == 2) {
+                // The tensor cores truncate their sums at every step, relative to what the sum is then: over 1000 positions
+                // 3e-6 to 9e-6 of it, over 4000 1e-5 to 4e-5, all of one sign.  So fp32 rows' products are summed over
+                // one unit, and the units here.
+                const int q_at = tile == 32 && n > 1 ? 1 : n - 1;
+#pragma unroll 1
+                for (int i = 0; i < n; ++i) {
+                    if (i == q_at) next_q();
+                    const unsigned ju = j + (unsigned)i, tb = ju / NB;
+                    if (i == n - 1 && !ends()) break;
+                    if (!wait(pv_done + (ju - tb * NB), tb)) break;
+                    tc::fence_after();
+                    if (active) {
+                        const float r = *(volatile float*)&s_ref[ju & 3][mine32], f = ref == -INFINITY ? 0.f : ex2(ref - r);
+#pragma unroll 1
+                        for (int c = 0; c < HD; c += 16) {
+                            uint32_t o[16], m[16];
+                            ld16(tl + c, o);
+                            if (i) ld16(tl + L::M0 + c, m);
+                            wait_ld();
+                            if (i)
+#pragma unroll
+                                for (int k = 0; k < 16; k += 2) {
+                                    float a0, a1;
+                                    of_two(fma2(two(__uint_as_float(m[k]), __uint_as_float(m[k + 1])), two(f, f), two(__uint_as_float(o[k]), __uint_as_float(o[k + 1]))), a0, a1);
+                                    o[k] = __float_as_uint(a0);
+                                    o[k + 1] = __float_as_uint(a1);
+                                }
+                            st16(tl + L::M0 + c, o);
+                        }
+                        wait_st();
+                        ref = r;
+                    }
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive(&o_free);
+                }
+            } else {
+                next_q();
+                if (ok && ends()) wait(pv_done + buf, turn);
+                tc::fence_after();
             }
+            if (!ok) break;
             const int slot = n_seg ? 1 : 0;
             if (tid == 12 * 32 && cur.u1 < cur.n) {
                 Cut c;
@@ -703,13 +778,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const int node0 = start / sh.group, rem = start - node0 * sh.group, row = min(mine32, rows - 1);
             const int node = node0 + node_of(rem, row), head = cur.kvh * sh.group + rem + row - (node - node0) * sh.group;
-            if (!wait(ends_ready + (n_seg & 3), n_seg >> 2) || !wait(pv_done + buf, turn)) break;
-            tc::fence_after();
-            if (quarter * 32 < rows) {
-                // the last unit's group has what the accumulator is relative to now
-                const int last = (int)((j_end - 1) & 1u);
-                const float2 e = s_end[n_seg & 3][last][mine32], f = s_end[n_seg & 3][last ^ 1][mine32];
-                const float sum = e.y + f.y * (f.x == -INFINITY ? 0.f : ex2(f.x - e.x)), inv = sum == 0.f ? 0.f : 1.f / sum;
+            if (active) {
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 const bool odd = *(volatile int*)&s_odd;
                 // positions below it are seen by every row, and their values multiplied as they are
                 const int all_seen = min(sh.chain ? cur.q.len + node0 + 1 : cur.q.len, cur.q.total);
@@ -720,13 +790,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 };
                 if (!whole && valid) {
                     float* st = a.stats + (size_t)(cta * 2 + slot) * 2 * kTile + mine32;
-                    st[0] = e.x;
+                    st[0] = top;
                     st[kTile] = sum;
                 }
 #pragma unroll 1
                 for (int c = 0; c < HD; c += 32) {
                     uint32_t o[32];
-                    ld32(tl + c, o);
+                    ld32(tl + (PARTS == 2 ? L::M0 : 0) + c, o);
                     wait_ld();
                     if (!valid) continue;
                     if (whole) {
@@ -751,9 +821,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) arrive(&o_free);
+            if constexpr (PARTS == 1) {
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(&o_free);
+            }
+            j += (unsigned)n;
         }
     } else {
         const int grp = warp >> 2, quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
@@ -774,9 +847,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             float ref = -INFINITY, l = 0.f, sc = a.scale2;  // what the weights are relative to (and kShift), their sum
 #pragma unroll 1
             for (int i = first; i < n; i += 2) {
-                const unsigned ju = j + (unsigned)i, turn = ju / 3, buf = ju - 3 * turn;
+                const unsigned ju = j + (unsigned)i, turn = ju / NB, buf = ju - NB * turn;
                 const int p0 = (g.u0 + i) * kUnit;
-                const uint32_t ts = tl + 128u + 128u * buf;
+                const uint32_t ts = tl + (uint32_t)L::S0 + 128u * buf;
                 if (!wait(s_full + buf, turn)) break;
                 tc::fence_after();
                 if constexpr (PARTS == 2)
@@ -791,7 +864,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int x0 = p0 + 64 * half, lo_row = max(min(g.q.len, g.q.total) - x0, 0);
                         // (copies that begin behind the last position have brought zeros)
                         const int hi_row = min((max(g.q.total - x0, 0) + (1 << a.box_shift) - 1) >> a.box_shift << a.box_shift, 64);
-                        if (lo_row < hi_row && (ju < 2 || wait(pv_done + (ju - 2) % 3, (ju - 2) / 3)) && wait(v_full + s % nv, s / nv)) {
+                        if (lo_row < hi_row && (ju < 2 || wait(pv_done + (ju - 2) % NB, (ju - 2) / NB)) && wait(v_full + s % nv, s / nv)) {
                             clean_v<C, HD>(vs + s % nv * L::VSLOT, lo_row, min(g.q.total - x0, 64), hi_row, tid & (kTile - 1), &s_odd);
                             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         }
@@ -835,25 +908,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float r = bm - kShift;
                     if (ju && !wait(&ref_ready[grp ^ 1][quarter], (ju - 1) >> 1)) break;
                     if (i > 0) {
-                        r = *(volatile float*)&s_ref[grp ^ 1][mine32];
+                        r = *(volatile float*)&s_ref[(ju - 1) & 3][mine32];
                         if (__any_sync(0xffffffffu, bm - kShift > r + kSlack)) {
-                            // the accumulator moves to the new maximum (all rows of the warp)
-                            const unsigned tb = (ju - 1) / 3, bb = ju - 1 - 3 * tb;
-                            if (!wait(pv_done + bb, tb)) break;
-                            tc::fence_after();
-                            const float nr = fmaxf(r, bm - kShift), f = nr == -INFINITY ? 1.f : ex2(r - nr);
+                            const float nr = fmaxf(r, bm - kShift);
+                            if constexpr (PARTS == 1) {  // the accumulator moves to the new maximum (all rows of the warp)
+                                const unsigned tb = (ju - 1) / NB, bb = ju - 1 - NB * tb;
+                                if (!wait(pv_done + bb, tb)) break;
+                                tc::fence_after();
+                                const float f = nr == -INFINITY ? 1.f : ex2(r - nr);
 #pragma unroll 1
-                            for (int c = 0; c < HD; c += 32) {
-                                ld32(tl + c, x);
-                                wait_ld();
+                                for (int c = 0; c < HD; c += 32) {
+                                    ld32(tl + c, x);
+                                    wait_ld();
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-                                st32(tl + c, x);
+                                    for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+                                    st32(tl + c, x);
+                                }
                             }
                             r = nr;
                         }
                     }
-                    *(volatile float*)&s_ref[grp][mine32] = r;
+                    *(volatile float*)&s_ref[ju & 3][mine32] = r;
                     __syncwarp();
                     if (lane == 0) arrive(&ref_ready[grp][quarter]);
                     if (ref != -INFINITY) l *= ex2(ref - r);
