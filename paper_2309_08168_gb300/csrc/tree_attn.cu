@@ -274,12 +274,13 @@ __device__ __forceinline__ void split_bits(f32x2 v, uint32_t& hi, uint32_t& lo) 
     lo = half2_of(rest(v, h));
 }
 
-// which of the positions p0 .. p0 + 63 node `node` (mask words m0 ..) of a request sees, as bits.  (Arguments of
-// functions that are not inlined are values: a reference would put what it refers to into local memory.)
-__device__ __noinline__ uint64_t visible(int len, int total, int chain, uint64_t m0, uint64_t m1, uint64_t m2, uint64_t m3, int node, int p0) {
+// Which of the positions p0 .. p0 + 63 node `node` of a request sees, as bits; masks: its row's words, nullptr: a
+// chain.  (Arguments of functions that are not inlined are values: a reference would put what it refers to into
+// local memory.  The words are read here, for the few units that need them, rather than kept in registers.)
+__device__ __noinline__ uint64_t visible(int len, int total, const uint64_t* masks, int words, int node, int p0) {
     const int end = total - p0;  // the unit's positions below it exist
     uint64_t v;
-    if (chain) {
+    if (!masks) {
         const long long last = (long long)len + node - p0;
         v = last >= 63 ? ~0ull : last < 0 ? 0ull : (2ull << last) - 1ull;
     } else {
@@ -287,12 +288,12 @@ __device__ __noinline__ uint64_t visible(int len, int total, int chain, uint64_t
         if (j0 <= -64) {
             v = ~0ull;
         } else if (j0 <= 0) {
-            v = j0 == 0 ? m0 : (m0 << -j0) | ((1ull << -j0) - 1ull);
+            const uint64_t m = __ldcg(masks);
+            v = j0 == 0 ? m : (m << -j0) | ((1ull << -j0) - 1ull);
         } else {
             const int w = j0 >> 6, s = j0 & 63;
-            const uint64_t a = w == 0 ? m0 : w == 1 ? m1 : w == 2 ? m2 : w == 3 ? m3 : 0ull;
-            const uint64_t b = w == 0 ? m1 : w == 1 ? m2 : w == 2 ? m3 : 0ull;
-            v = s ? (a >> s) | (b << (64 - s)) : a;
+            v = w < words ? __ldcg(masks + w) >> s : 0ull;
+            if (s && w + 1 < words) v |= __ldcg(masks + w + 1) << (64 - s);
         }
     }
     return end >= 64 ? v : end <= 0 ? 0ull : v & ((1ull << end) - 1ull);
@@ -351,13 +352,9 @@ struct OddArgs {
 };
 template <typename C, typename E>
 __device__ __noinline__ void add_odd(OddArgs a, int len, int total, int node, int from, int to, E* out, int stride) {
-    uint64_t m[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-        if (a.masks && w < a.words) m[w] = __ldcg(a.masks + w);
 #pragma unroll 1
     for (int x = max(from, len); x < min(to, total); ++x) {
-        if (!(visible(len, total, a.masks == nullptr, m[0], m[1], m[2], m[3], node, x) & 1)) continue;
+        if (!(visible(len, total, a.masks, a.words, node, x) & 1)) continue;
         const int page = __ldcg(a.table + x / a.page_size);
         if (page < 0 || page >= a.n_pages) continue;
         const uint4* v = reinterpret_cast<const uint4*>((const C*)a.v + page * a.page_stride + (x % a.page_size) * a.pos_stride);
@@ -836,11 +833,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int n = g.u1 - g.u0, start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile);  // units; rows that exist
             const bool active = quarter * 32 < rows;
             const int node0 = start / sh.group, node = node0 + node_of(start - node0 * sh.group, min(mine32, rows - 1));
-            uint64_t m[4] = {0, 0, 0, 0};
-            if (!sh.chain && mine32 < rows)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    if (w < a.words) m[w] = __ldcg(a.masks + (size_t)(g.q.r0 + node) * a.words + w);
             // positions below it are seen by every row of the tile
             const int all_seen = min(sh.chain ? g.q.len + node0 + 1 : g.q.len, g.q.total);
             const int first = (int)((j ^ (unsigned)grp) & 1u);  // this group's first unit of the segment
@@ -885,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         uint64_t v = 0;
 #pragma unroll 1
                         for (int c = 0; c < kUnit / 32; ++c) {
-                            v = c & 1 ? v >> 32 : visible(g.q.len, g.q.total, sh.chain, m[0], m[1], m[2], m[3], node, p0 + 32 * c);
+                            v = c & 1 ? v >> 32 : visible(g.q.len, g.q.total, sh.chain ? nullptr : a.masks + (size_t)(g.q.r0 + node) * a.words, a.words, node, p0 + 32 * c);
                             load(c);
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
