@@ -310,6 +310,26 @@ def test_on_another_stream_and_in_graphs_that_share_a_workspace(ssd):
     assert all(torch.equal(o, w) for o, w in zip(outs, want))
 
 
+def test_two_calls_at_once(ssd):
+    """Two streams, a workspace each: neither call changes the other's bits."""
+    cases = [Case(np.random.default_rng(20 + i), kind, heads, kv, 128, 16, lens, counts)
+             for i, (kind, heads, kv, lens, counts) in enumerate((("f32", 16, 4, [2000] * 6, [9] * 6), ("bf16", 32, 4, [1500] * 5, [33] * 5)))]
+    want = [c.run(ssd) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    spaces = [torch.empty(ssd.ssd_tree_attention_workspace(ssd.PagedKV(c.k, c.v)), dtype=torch.uint8, device="cuda") for c in cases]
+    calls, outs = [], []
+    for c in cases:
+        kv, o = ssd.PagedKV(c.k, c.v), torch.full(c.q.shape, 77.0, dtype=c.q.dtype, device="cuda")
+        outs.append(o)
+        calls.append((ssd.TreeBatch(dev(c.row_start), dev(c.lens), dev(c.table), c.n_rows, c.max_rows), kv, 0, c.q, dev(c.masks), 1 / math.sqrt(c.hd), o))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, ws, st in zip(calls, spaces, streams):
+            ssd.ssd_tree_attention(*a, ws, None, st.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
 def test_a_captured_call_follows_the_lengths(ssd):
     """Lengths, starts and tables are read when the graph runs."""
     c = Case(np.random.default_rng(11), "f32", 4, 2, 64, 16, [900, 800], [9, 3])
