@@ -52,8 +52,7 @@
 #include <mutex>
 
 #include "tc_gemm.cuh"
-#include "tree_ops.cuh"
-#include "tree_sched.cuh"
+#include "tree_attn.cuh"
 
 namespace ssd {
 namespace tree {
@@ -61,54 +60,10 @@ namespace {
 
 constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp16
 constexpr long long kWaitClocks = 4000000000ll;  // 2 s at 2 GHz
-constexpr int kTile = 128;  // rows: the TMEM lanes
 constexpr int kThreads = 512;
 constexpr int kTmem = 512;  // columns (Lay)
 constexpr int kMaxSlots = 12;
 constexpr int kJoinThreads = 128, kJoinLines = 16;
-
-// what a CTA whose range ends inside an item leaves for join_kernel
-struct alignas(16) Cut {
-    int first, last;  // CTAs that hold parts of the item; last < 0: the range does not end inside one
-    int first_slot;   // the first one's part is its slot 0 or 1 (the others': 0)
-    int row0, rows;   // of the request: first row of its tile, rows of the tile that exist
-    int r0, kvh, pad;
-};
-
-struct AttnOpArgs {
-    Shape shape;
-    int grid;
-    const int32_t* block_table;
-    const void* q;
-    void* out;
-    int64_t q_stride, out_stride;
-    const uint64_t* masks;
-    int words;
-    const void* vc;  // the layer's V
-    int64_t page_stride, head_stride, pos_stride;
-    int n_heads, n_pages;
-    int box_shift;  // positions per copy, log2: 16 .. 64 of them, which divide page_size
-    int at_pos, at_head, at_page;  // which coordinate (1 .. 3) of the tensor maps is which
-    float scale2;  // log2(e) * scale
-    int tile;      // rows: 32 or 128
-    unsigned nk, nv;    // slots of the rings
-    uint64_t group_inv;  // ceil(2^32 / group)
-    Cut* cuts;     // [grid]
-    float* stats;  // [grid][2][2][kTile]: maximum, sum
-    float4* part;  // [grid][2][HD / 4][kTile]
-    int32_t* status;
-};
-
-template <typename T>
-struct Types {
-    typedef T C;
-    static constexpr int PARTS = 1;
-};
-template <>
-struct Types<float> {
-    typedef f16 C;
-    static constexpr int PARTS = 2;
-};
 
 template <typename T, int HD>
 struct Lay {
@@ -197,38 +152,9 @@ __device__ __forceinline__ void st16(uint32_t t, const uint32_t (&r)[16]) {
 }
 #undef SSD_R8
 #undef SSD_I8
-// 2^x; below 2^-126: 0
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// two fp32 values in one register pair: fma, add and mul of both in one instruction
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 two(float a, float b) {
-    f32x2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void of_two(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -387,9 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ __align__(8) uint64_t q_ready, q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
-    __shared__ long long s_sum[kThreads / 32], s_off;
-    __shared__ int s_b;
-    __shared__ Req s_req;  // the request that the range starts in
+    __shared__ RangeOf<kThreads> s_range;
     // (four segments: scores are at most three units ahead of the accumulator)
     __shared__ float s_scale[4][kTile];    // [segment & 3]: power of two that a row of q was divided by
     __shared__ float2 s_end[4][2][kTile];  // [segment & 3][group]: what a row's weights are relative to, and their sum
@@ -397,7 +321,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         s_fail = s_odd = 0;
-        s_b = -1;
 #pragma unroll 1
         for (int i = 0; i < kMaxSlots; ++i) {
             tc::mb_init(k_full + i, 1);
@@ -430,56 +353,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_wait();  // everything below may come from the previous kernel
     if (tid == 0) a.cuts[blockIdx.x].last = -1;
 
-    // this CTA's range: units of all requests, a run of requests per thread
     const Shape& sh = a.shape;
-    const int per = (sh.n_requests + kThreads - 1) / kThreads;
-    const int b0 = min(tid * per, sh.n_requests), b1 = min(b0 + per, sh.n_requests);
-    long long mine = 0;
-    Req last{};
-#pragma unroll 1
-    for (int b = b0; b < b1; ++b) {
-        last = req_of(sh, b);
-        if (last.clipped && last.n && blockIdx.x == 0) say(a.status, SSD_STATUS_TABLE);
-        mine += head_units(sh, last, tile) * sh.n_kv_heads;
-    }
-    long long before = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, before, o);
-        if (lane >= o) before += x;
-    }
-    if (lane == 31) s_sum[warp] = before;
-    __syncthreads();
-    before -= mine;
-    long long units = 0;
-#pragma unroll 4
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) before += s_sum[w];
-        units += s_sum[w];
-    }
-    const int ctas = ctas_of(units, a.grid), cta = blockIdx.x;
-    const long long lo = cta < ctas ? range_start(units, ctas, cta) : 0, hi = cta < ctas ? range_start(units, ctas, cta + 1) : 0;
-    if (before <= lo && lo < before + mine) {
-        long long off = lo - before;
-#pragma unroll 1
-        for (int b = b0; b < b1; ++b) {
-            const Req q = per == 1 ? last : req_of(sh, b);
-            const long long n = head_units(sh, q, tile) * sh.n_kv_heads;
-            if (off < n) {
-                s_b = b;
-                s_req = q;
-                s_off = off;
-                break;
-            }
-            off -= n;
-        }
-    }
+    const int cta = blockIdx.x;
     tc::fence_before();
-    __syncthreads();
+    Walk walk;
+    int ctas;
+    const long long units = range_of<kThreads>(a, tile, s_range, walk, ctas);
     tc::fence_after();
     const uint32_t tmem = s_tmem;
-    Walk walk;
-    walk_init(walk, sh, tile, s_b, s_req, s_off, lo, hi - lo);
     Seg g;
     bool ok = true;
     auto wait = [&](uint64_t* b, unsigned phase) {
@@ -1140,22 +1021,23 @@ int encode(const char* call, CUtensorMap* m, const void* base, const ssd_pages* 
 }
 
 template <typename T, int HD>
-int run_hd(const char* call, AttnOpArgs& a, const CUtensorMap& k, const CUtensorMap& v, int n_sms, void* workspace, void* stream) {
+int run_hd(const char* call, AttnOpArgs& a, int dtype, const CUtensorMap& k, const CUtensorMap& v, void* stream) {
     using L = Lay<T, HD>;
-    a.grid = n_sms;
-    a.nk = (unsigned)L::nk(a.tile);
-    a.nv = (unsigned)L::nv(a.tile);
-    a.cuts = (Cut*)workspace;
-    a.part = (float4*)(a.cuts + a.grid);
-    a.stats = (float*)(a.part + (size_t)a.grid * 2 * (HD / 4) * kTile);
-    if (int rc = launch(call, attn_kernel<T, HD>, dim3((unsigned)a.grid), kThreads, L::BYTES, stream, a, k, v)) return rc;
+    int rc;
+    if (a.tile <= kFewRows) {
+        rc = launch_few(call, a, dtype, HD, stream);
+    } else {
+        a.nk = (unsigned)L::nk(a.tile);
+        a.nv = (unsigned)L::nv(a.tile);
+        rc = launch(call, attn_kernel<T, HD>, dim3((unsigned)a.grid), kThreads, L::BYTES, stream, a, k, v);
+    }
     // an item of one unit is never cut
-    if ((long long)a.shape.max_blocks * a.shape.page_size <= kUnit || a.grid == 1) return SSD_OK;
+    if (rc || (long long)a.shape.max_blocks * a.shape.page_size <= kUnit || a.grid == 1) return rc;
     return launch(call, join_kernel<T, HD>, dim3((unsigned)(a.grid - 1), kJoinLines), kJoinThreads, 0, stream, a);
 }
 template <typename T>
-int run(const char* call, AttnOpArgs& a, int hd, const CUtensorMap& k, const CUtensorMap& v, int n_sms, void* ws, void* stream) {
-    return hd == 64 ? run_hd<T, 64>(call, a, k, v, n_sms, ws, stream) : run_hd<T, 128>(call, a, k, v, n_sms, ws, stream);
+int run(const char* call, AttnOpArgs& a, int dtype, int hd, const CUtensorMap& k, const CUtensorMap& v, void* stream) {
+    return hd == 64 ? run_hd<T, 64>(call, a, dtype, k, v, stream) : run_hd<T, 128>(call, a, dtype, k, v, stream);
 }
 
 }  // namespace
@@ -1220,6 +1102,7 @@ extern "C" int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache
     a.out_stride = out_stride;
     a.masks = masks;
     a.words = mask_words;
+    a.kc = (const char*)cache->k + 2 * layer * cache->layer_stride;
     a.vc = (const char*)cache->v + 2 * layer * cache->layer_stride;
     a.page_stride = cache->page_stride;
     a.head_stride = cache->head_stride;
@@ -1229,13 +1112,20 @@ extern "C" int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache
     a.box_shift = cache->page_size % 64 == 0 ? 6 : cache->page_size % 32 == 0 ? 5 : 4;
     a.scale2 = (float)(1.4426950408889634 * scale);
     a.status = status;
-    a.tile = (long long)batch->max_rows * group <= 32 ? 32 : kTile;
+    const long long rows = (long long)batch->max_rows * group;
+    a.tile = rows <= kFewRows ? (int)rows : rows <= 32 ? 32 : kTile;
     a.group_inv = ((1ull << 32) + group - 1) / group;
+    a.grid = n_sms;
+    a.cuts = (Cut*)workspace;
+    a.part = (float4*)(a.cuts + a.grid);
+    a.stats = (float*)(a.part + (size_t)a.grid * 2 * (cache->head_dim / 4) * kTile);
     CUtensorMap k, v;
-    if (int rc = encode(call, &k, (const char*)cache->k + 2 * layer * cache->layer_stride, cache, a)) return rc;
-    if (int rc = encode(call, &v, a.vc, cache, a)) return rc;
+    if (a.tile > kFewRows) {
+        if (int rc = encode(call, &k, a.kc, cache, a)) return rc;
+        if (int rc = encode(call, &v, a.vc, cache, a)) return rc;
+    }
     const int hd = cache->head_dim;
-    if (dtype == SSD_F32) return run<float>(call, a, hd, k, v, n_sms, workspace, cuda_stream);
-    if (dtype == SSD_F16) return run<f16>(call, a, hd, k, v, n_sms, workspace, cuda_stream);
-    return run<bf16>(call, a, hd, k, v, n_sms, workspace, cuda_stream);
+    if (dtype == SSD_F32) return run<float>(call, a, dtype, hd, k, v, cuda_stream);
+    if (dtype == SSD_F16) return run<f16>(call, a, dtype, hd, k, v, cuda_stream);
+    return run<bf16>(call, a, dtype, hd, k, v, cuda_stream);
 }

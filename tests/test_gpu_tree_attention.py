@@ -170,6 +170,44 @@ def test_the_largest_row_count_only_chooses_the_tile(ssd):
         c.check(c.run(ssd))
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("hd,page", [(64, 16), (64, 48), (128, 16), (128, 80)])
+@pytest.mark.parametrize("group", [1, 2])
+def test_tiles_of_few_rows(ssd, kind, hd, page, group):
+    """Trees and chains as tiles of one row or two: rows that see nothing, nodes of NaN that some rows do not see, pages outside
+    the cache, items of less than a block, of more than a warp looks up at once, and more items than CTAs."""
+    rng = np.random.default_rng(30 + hd + group)
+    lens, counts = [0, 1, 15, 127, 130, 700, -1, 18000, 31], [3, 1, 17, 1, 70, 2, 0, 1, 33]
+    for masks in ("star", None):
+        c = Case(rng, kind, 2 * group, 2, hd, page, lens, counts, masks)
+        c.max_rows = 1
+        if masks:
+            c.masks[1] = 0  # of a request with nothing cached
+        clean = c.run(ssd)
+        c.check(clean)
+        assert masks is None or (clean[1] == 0).all()
+        # the 20th node of request 4: seen by itself (star) or by the rows from it on (chain)
+        x, hit = 130 + 20, int(c.row_start[4]) + 20
+        for t in (c.k, c.v):
+            t[0, int(c.table[4, x // page]), :, x % page] = float("nan")
+        out, hits = c.run(ssd), [hit] if masks else range(hit, int(c.row_start[5]))
+        others = [r for r in range(c.n_rows) if r not in hits]
+        assert torch.equal(out[others], clean[others]) and out[list(hits)].isnan().all()
+        c.table[5, 2], c.table[7, 3] = -1, 10**6
+        c.row_start, c.lens, c.table = c.row_start[5:].copy(), c.lens[5:], np.ascontiguousarray(c.table[5:])  # without the NaN's request
+        c.check(c.run(ssd))
+
+
+@pytest.mark.parametrize("kind,kv,group,hd,n,length", [("f32", 32, 1, 128, 24, 900), ("f16", 24, 2, 128, 20, 1300), ("bf16", 40, 1, 64, 30, 500), ("f32", 16, 2, 64, 40, 70)])
+def test_single_tokens_of_many_requests(ssd, kind, kv, group, hd, n, length):
+    rng = np.random.default_rng(40 + n)
+    c = Case(rng, kind, kv * group, kv, hd, 16, rng.integers(0, length + 1, n), [1] * n, None)
+    out = c.run(ssd)
+    c.check(out)
+    for _ in range(10):
+        assert torch.equal(out, c.run(ssd))
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_values_that_are_not_finite_in_a_prompt(ssd, kind):
     """A NaN in the values of one position of a chain reaches the rows from it on, an infinity in one dim of another

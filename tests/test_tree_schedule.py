@@ -27,7 +27,7 @@ static int bad(const char* what, int it) { printf("%s in batch %d\n", what, it);
 int main(int argc, char** argv) {
     srand(atoi(argv[1]));
     for (int it = 0; it < atoi(argv[2]); ++it) {
-        const int B = 1 + rand() % (rand() % 3 ? 6 : 60), tile = rand() % 2 ? 32 : 128, grid = rand() % 4 ? 304 : 1 + rand() % 40;
+        const int B = 1 + rand() % (rand() % 3 ? 6 : 60), tile = rand() % 4 ? rand() % 2 ? 32 : 128 : 1 + rand() % 2, grid = rand() % 4 ? 304 : 1 + rand() % 40;
         Shape s{};
         s.n_requests = B;
         s.page_size = 16 * (1 + rand() % 6);

@@ -25,13 +25,13 @@ def test_waits_are_decided_by_the_warp():
     assert len(re.findall(r"\bmb_try\(", src)) == 2 and len(re.findall(r"\bwait\(", src)) >= 12
 
 
-@pytest.mark.parametrize("name", ["tree_attn.cu", "tree_ops.cu", "tree_ops.cuh", "tree_sched.cuh"])
+@pytest.mark.parametrize("name", ["tree_attn.cu", "tree_attn.cuh", "tree_few.cu", "tree_ops.cu", "tree_ops.cuh", "tree_sched.cuh"])
 def test_no_non_coherent_loads(name):
     src = source(name)
     assert "global.nc" not in src and "__ldg(" not in src and "__restrict__" not in src
 
 
-@pytest.mark.parametrize("name,kernels", [("tree_attn.cu", ["attn_kernel", "join_kernel"]), ("tree_ops.cu", ["plan_kernel", "rope_kernel", "commit_kernel"])])
+@pytest.mark.parametrize("name,kernels", [("tree_attn.cu", ["attn_kernel", "join_kernel"]), ("tree_few.cu", ["few_kernel"]), ("tree_ops.cu", ["plan_kernel", "rope_kernel", "commit_kernel"])])
 def test_kernels_wait_for_the_one_before(name, kernels):
     src = source(name)
     for k in kernels:
