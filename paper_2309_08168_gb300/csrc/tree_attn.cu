@@ -17,16 +17,26 @@
 //   warp 11    : issues O += P V (P in TMEM over the columns of S, V as it lies in the
 //                cache, MN-major, N = hd);
 //   warps 0-3, 4-7 : softmax of the even and of the odd units, a row per thread: S from
-//                TMEM, P back to it.  Three units' S and P have a place, so that the tensor
-//                cores multiply for two while both groups work; there is one
-//                accumulator, and the maximum that weights are relative to goes from unit
-//                to unit, from a group's warp to the other's (before its weights are
-//                computed, so that the groups overlap).
-//   warps 12-15 : q of the next item to shared memory; at an item's end O / sum, or O,
-//                maximum and sum to the workspace if other CTAs hold parts of the
-//                item, while the others are at the next item.  join_kernel adds those.
+//                TMEM, P back to it.  Three units' S and P have a place (two for fp32 rows of
+//                128 dims), so that the tensor cores multiply for one while both groups work;
+//                there is one accumulator, and the maximum that weights are relative to goes
+//                from unit to unit, from a group's warp to the other's (before its weights
+//                are computed, so that the groups overlap).
+//   warps 12-15 : q of the next item to shared memory; fp32 rows: adds each unit's product
+//                to its sums; at an item's end O / sum, or O, maximum and sum to the
+//                workspace if other CTAs hold parts of the item, while the others are at
+//                the next item.  join_kernel adds those.
 // The tile has 128 rows; 32 where no request has more, which leaves the ring the
-// shared memory of the other rows' q (their lanes then hold what no one reads).
+// shared memory of the other rows' q (their lanes then hold what no one reads).  Two rows or
+// less are few_kernel's (tree_few.cu).
+//
+// Measured, with join_kernel (copy rate 6.79 TB/s, tensor cores 1.92 PFLOP/s):
+//   9 nodes, 8 heads a KV head, 100001 positions, fp16: 72 us, 5.7 TB/s - HBM;
+//   6 trees of 33 nodes, 8 heads a KV head, 4096 positions, bf16: 33 us, 2.0 TB/s - 8 us until the
+//     first unit's scores, then 1.0 us a unit (S, softmax, P V of a buffer one after the other), join 5;
+//   2048 rows over 4000 positions, 8 heads a KV head, bf16: 332 us, 1.02 PFLOP/s - the exponentials;
+//   2 x 1023 rows over 700 positions, 40 heads, fp32: 148 us, 0.32 PFLOP/s counted once, 0.64 done
+//     (two passes each): fp32 rows' two buffers, and the sums of every unit.
 //
 // O is rescaled only when a row's maximum has grown by more than kSlack (log2)
 // over the one its weights are relative to (the running softmax of Milakov and
@@ -38,7 +48,11 @@
 // row of q is scaled by a power of two first, which the scores take back, so that
 // no fp32 value is too large or too small for the pair; hi is rounded towards
 // zero and lo is not 0, so that an infinite key gives the product the sign of q.
-// 16-bit rows: q as it is; the weights rounded to the type once, like the output.
+// The tensor cores cut off what their sums cannot hold, always downwards in size: adding up
+// 4000 positions in one accumulator made results too small by 3e-5.  So each unit's
+// product starts from zero (lo first) and is added in fp32: 7.5e-7 at any length.
+// 16-bit rows: q as it is; the weights rounded to the type once, like the output (half a step: 2^-8, 2^-11);
+// the cut adds 5e-9 of the result a position of a CTA's share, 2e-4 after 50000.
 //
 // Units with positions that some row does not see: scores by the row's 64 mask
 // bits, and V rows behind the last position, which may hold anything, are set

@@ -8,8 +8,8 @@
 namespace ssd {
 namespace tree {
 
-constexpr int kTile = 128;  // most rows of a tile
-constexpr int kFewRows = 2; // most rows of a tile of few_kernel
+constexpr int kTile = 128;   // most rows of a tile
+constexpr int kFewRows = 2;  // most rows of a tile of few_kernel
 
 // what a CTA whose range ends inside an item leaves for join_kernel
 struct alignas(16) Cut {
