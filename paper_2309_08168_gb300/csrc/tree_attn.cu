@@ -76,7 +76,7 @@ constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp
 constexpr long long kWaitClocks = 4000000000ll;  // 2 s at 2 GHz
 constexpr int kThreads = 512;
 constexpr int kTmem = 512;  // columns (Lay)
-constexpr int kMaxSlots = 12;
+constexpr int kMaxSlots = 12, kSegs = 32;
 constexpr int kJoinThreads = 128, kJoinLines = 16;
 
 template <typename T, int HD>
@@ -85,7 +85,7 @@ struct Lay {
     static constexpr int KSLOT = kUnit * 128;         // 64 dims of a unit's K
     static constexpr int VBOX = 64 * 128;             // 64 dims of 64 positions of V
     static constexpr int VSLOT = BOXES * VBOX;
-    static constexpr int RING = 213 * 1024;           // shared memory for q and the rings
+    static constexpr int RING = 210 * 1024;           // shared memory for q and the rings
     // TMEM columns: O; fp32 rows' sums of earlier units; S / P of unit j at S0 + 128 (j mod NB)
     static constexpr int M0 = HD, S0 = PARTS == 2 && HD == 128 ? 256 : 128, NB = (kTmem - S0) / kUnit;
     // two buffers of a tile of 32 rows, one of 128
@@ -190,6 +190,19 @@ __device__ __noinline__ bool mb_wait_on(uint64_t* b, unsigned parity, volatile i
 }
 __device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail) {
     return tc::mb_try(b, parity) || mb_wait_on(b, parity, fail);
+}
+
+__device__ __noinline__ bool known_wait(volatile int* known, int i, volatile int* fail) {
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (*known <= i) {
+        if (*fail) return false;
+        if (clock64() - t0 > kWaitClocks) {
+            *fail = 1;
+            return false;
+        }
+    }
+    return true;
 }
 
 // the upper 11 bits of two values, and the rest
@@ -328,13 +341,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
     __shared__ RangeOf<kThreads> s_range;
+    // The CTA's segments, written by the K producer one ahead of itself, the one behind the last with n = 0; s_known: how
+    // many so far.  (K is at most kMaxSlots units ahead of the scores, those three ahead of what is multiplied, and
+    // results at most a segment behind that: a place is not written again before everyone has left it.)
+    __shared__ Seg s_seg[kSegs];
+    __shared__ int s_known;
     // (four segments: scores are at most three units ahead of the accumulator)
     __shared__ float s_scale[4][kTile];    // [segment & 3]: power of two that a row of q was divided by
     __shared__ float2 s_end[4][2][kTile];  // [segment & 3][group]: what a row's weights are relative to, and their sum
     __shared__ float s_ref[4][kTile];      // [unit & 3]: what a unit's weights are relative to
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        s_fail = s_odd = 0;
+        s_fail = s_odd = s_known = 0;
 #pragma unroll 1
         for (int i = 0; i < kMaxSlots; ++i) {
             tc::mb_init(k_full + i, 1);
@@ -382,6 +400,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         return ok;
     };
 
+    // segment i to g, if there is one
+    auto segment = [&](unsigned i) {
+        ok = ok && __all_sync(0xffffffffu, *(volatile int*)&s_known > (int)i || known_wait(&s_known, (int)i, &s_fail));
+        __threadfence_block();
+        g = s_seg[i % kSegs];
+        return ok && g.n > 0;
+    };
+
     // node of row `row` of a tile whose first row is `rem` heads into its first node, from that node on
     auto node_of = [&](int rem, int row) { return (int)(((uint64_t)(unsigned)(rem + row) * a.group_inv) >> 32); };
 
@@ -400,7 +426,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool mine_too = lane < (is_v ? copies * BOXES : copies);
         const unsigned bytes = is_v ? L::VSLOT : L::KSLOT;
         unsigned slot = 0, phase = 1;
-        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+        unsigned published = 0;
+        bool more = true;
+        for (unsigned n_seg = 0; ok; ++n_seg) {
+            if (!is_v)
+#pragma unroll 1
+                for (; published < n_seg + 2 && more; ++published) {
+                    more = walk_next(walk, sh, tile, g);
+                    if (!more) g.n = 0;
+                    if (lane == 0) {
+                        s_seg[published % kSegs] = g;
+                        __threadfence_block();
+                        *(volatile int*)&s_known = (int)published + 1;
+                    }
+                    __syncwarp();
+                }
+            if (!segment(n_seg)) break;
             const int32_t* table = a.block_table + (size_t)g.b * sh.max_blocks;
             auto fetch = [&](long long x) {  // page of this lane's copy of the 32 from x on; -1: outside, reads as zeros
                 x += lane << a.box_shift;
@@ -448,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t q0 = tc::sdesc(smem_u32(smem)), k0 = tc::sdesc(smem_u32(ks));
         const uint32_t qb = (uint32_t)tile * 128;  // 64 dims of the tile's q
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;  // unit 3 turn + buf
-        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
             if (!wait(&q_ready, n_seg)) break;
             const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
 #pragma unroll 1
@@ -502,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // fp32 rows: every unit's products start from 0, once the last ones have been added to the sums; 16-bit
         // rows: every segment's, once the last one's are written
         unsigned taken = 0;
-        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
                 const bool fresh = PARTS == 2 || u == g.u0;
@@ -590,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             if (lane == 0) arrive(&q_ready);
         };
-        bool more = walk_next(walk, sh, tile, g);
+        bool more = segment(0);
         if (more) load_q(g, 0);
         unsigned j = 0;  // of the segment's first unit
         for (unsigned n_seg = 0; more && ok; ++n_seg) {
@@ -611,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // The next rows' q: into the other buffer (the last segment but this one is finished), or, with
             // one buffer, once all scores of this segment are there
             auto next_q = [&] {
-                more = walk_next(walk, sh, tile, g);
+                more = segment(n_seg + 1);
                 if (more && (tile == 32 || wait(&q_free, n_seg))) load_q(g, n_seg + 1);
             };
             if constexpr (PARTS == 2) {
@@ -724,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int grp = warp >> 2, quarter = warp & 3, mine32 = quarter * 32 + lane;  // this thread's row of the tile
         const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16);
         unsigned j = 0;  // of the segment's first unit
-        for (unsigned n_seg = 0; ok && walk_next(walk, sh, tile, g); ++n_seg) {
+        for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
             const int n = g.u1 - g.u0, start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile);  // units; rows that exist
             const bool active = quarter * 32 < rows;
             const int node0 = start / sh.group, node = node0 + node_of(start - node0 * sh.group, min(mine32, rows - 1));
