@@ -153,13 +153,18 @@ int ssd_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* rope, int dty
  * round's rows (which ssd_rope_kv has put at lens[b] + j), node j if bit j of masks[row] is set,
  * or, with masks = NULL, nodes 0 .. i of a chain.  Nodes from 64 * mask_words on are not seen.
  * A row that sees nothing, or whose scores are all -inf, gets zeros.  What a row does
- * not see does not change its output, be it NaN.  Positions that max_blocks pages do not hold are
+ * not see does not change its output, be it NaN; an infinite value that it sees comes out as
+ * infinity or NaN.  Positions that max_blocks pages do not hold are
  * not seen (SSD_STATUS_TABLE).  Rows of a request with lens[b] < 0 are left as they were.
  * q and out: [row][n_heads][head_dim] of dtype, rows q_stride and out_stride
  * elements apart, 16-byte aligned, strides multiples of 16 bytes; no overlap.  n_heads is a
  * multiple of n_kv_heads; 0 < scale, finite.
- * Scores, statistics and sums are fp32; fp32 q and their weights enter the products as
- * fp16 pairs (22 bits).
+ * Scores, statistics and sums are fp32.  If no request has more than two rows a KV head
+ * (max_rows n_heads / n_kv_heads <= 2) everything is fp32.  Else fp32 q and their weights enter
+ * the products as fp16 pairs (22 bits), and 16-bit rows' weights are rounded to the type once.
+ * Measured against 64 bits, values around 1: fp32 rows 1e-6 at any length; 16-bit rows a step of the type,
+ * and 5e-9 of the result more for every position that one of the SMs sums up (a single
+ * row over 16000 positions: 2e-4 smaller than it should be).
  * workspace: ssd_tree_attention_workspace() bytes, 16-byte aligned; its contents
  * mean nothing between calls.  The same inputs give the same bits; the order of
  * sums depends on the whole batch's lengths.
