@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *ks = smem + L::q_all(tile), *vs = ks + nk * L::KSLOT;
     __shared__ __align__(8) uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
-    __shared__ __align__(8) uint64_t q_ready, q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
+    __shared__ __align__(8) uint64_t q_ready[2], q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
     __shared__ RangeOf<kThreads> s_range;
@@ -360,7 +360,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mb_init(v_full + i, 1);
             tc::mb_init(v_empty + i, 1);
         }
-        tc::mb_init(&q_ready, 4);
+        tc::mb_init(q_ready, 4);
+        tc::mb_init(q_ready + 1, 4);
         tc::mb_init(&q_free, 1);
         tc::mb_init(&o_free, 4);
         for (int i = 0; i < 3; ++i) {
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t qb = (uint32_t)tile * 128;  // 64 dims of the tile's q
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;  // unit 3 turn + buf
         for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
-            if (!wait(&q_ready, n_seg)) break;
+            if (!wait(q_ready + (n_seg & 1), n_seg >> 1)) break;  // (two: q of a small tile comes a segment ahead)
             const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
@@ -629,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) arrive(&q_ready);
+            if (lane == 0) arrive(q_ready + (n_seg & 1));
         };
         bool more = segment(0);
         if (more) load_q(g, 0);

@@ -4,9 +4,9 @@
 // kUnit positions of its cache.  Items stand in a row - request by request, KV head
 // by KV head, tile by tile - and their units are cut into equal ranges, one per
 // CTA, whatever the lengths are.  An item counts kItemCost units more than it has,
-// in front of them: the time that its q, first scores and output take (measured:
-// 16 requests of 32 heads, 262 to 2100 positions each: without it CTAs with short
-// items ended at 106 us, the others at 77).  An item that lies in one CTA's range is finished there;
+// in front of them: the time that its q, first scores and output take (16 requests of 32 heads,
+// 262 to 2100 positions each, one row a tile: 64 us, with none 72, one 68, five 65; 1024 items of 90 to 270
+// positions, 9 fp32 rows: 74 us, with two 76).  An item that lies in one CTA's range is finished there;
 // one that a range end cuts leaves a partial sum per CTA, joined afterwards in
 // the order of the CTAs.  A CTA has at most two of those: the item that its range
 // starts in and the one that it ends in.

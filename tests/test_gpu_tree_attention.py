@@ -386,6 +386,24 @@ def test_a_captured_call_follows_the_lengths(ssd):
         c.check(o, 0.125)
 
 
+@pytest.mark.parametrize("kind,heads,kv", [("f32", 4, 4), ("bf16", 6, 3)])
+def test_captured_single_tokens(ssd, kind, heads, kv):
+    """A decoding step as a graph: every replay sees what the lengths hold then."""
+    c = Case(np.random.default_rng(21), kind, heads, kv, 128, 32, [700, 300, 40, 0], [1] * 4, None)
+    cache, lens, out = ssd.PagedKV(c.k, c.v), dev(c.lens), torch.full(c.q.shape, 77.0, dtype=c.q.dtype, device="cuda")
+    ws = torch.empty(ssd.ssd_tree_attention_workspace(cache), dtype=torch.uint8, device="cuda")
+    bt, g = ssd.TreeBatch(dev(c.row_start), lens, dev(c.table), c.n_rows, 1), torch.cuda.CUDAGraph()
+    c.run(ssd)
+    with torch.cuda.graph(g):
+        ssd.ssd_tree_attention(bt, cache, 0, c.q, None, 128**-0.5, out, ws, None, torch.cuda.current_stream().cuda_stream)
+    for new in ([700, 300, 40, 0], [129, 127, -1, 0], [0, 0, 0, 0], [-1, -1, -1, -1], [690, 1, 33, -1]):
+        c.lens = np.array(new, np.int32)
+        lens.copy_(torch.from_numpy(c.lens))
+        out.fill_(77.0)
+        g.replay()
+        c.check(out)
+
+
 def test_tensors_elsewhere_are_refused(ssd):
     c = Case(np.random.default_rng(12), "f32", 2, 2, 64, 16, [9], [2])
     c.q = c.q.cpu()
