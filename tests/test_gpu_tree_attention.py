@@ -122,7 +122,8 @@ def test_attention(ssd, kind, hd, heads, kv, page, lens, counts, masks, apart):
 
 
 @pytest.mark.parametrize("kind,heads,kv,lens,counts", [("f32", 2, 2, [6000], [1]), ("f16", 8, 1, [20001], [3]), ("bf16", 4, 2, [3000, 9, 7000], [20, 1, 64]),
-                                                       ("f32", 4, 4, [2500] + [20] * 40, [3] * 41)])
+                                                       ("f32", 4, 4, [2500] + [20] * 40, [3] * 41),
+                                                       ("bf16", 4, 2, [5, -1, 130] * 500, [3, 0, 2] * 500)])
 def test_attention_along_a_long_cache(ssd, kind, heads, kv, lens, counts):
     c = Case(np.random.default_rng(len(lens) + heads), kind, heads, kv, 128, 64, lens, counts)
     c.check(c.run(ssd))
@@ -198,7 +199,8 @@ def test_tiles_of_few_rows(ssd, kind, hd, page, group):
         c.check(c.run(ssd))
 
 
-@pytest.mark.parametrize("kind,kv,group,hd,n,length", [("f32", 32, 1, 128, 24, 900), ("f16", 24, 2, 128, 20, 1300), ("bf16", 40, 1, 64, 30, 500), ("f32", 16, 2, 64, 40, 70)])
+@pytest.mark.parametrize("kind,kv,group,hd,n,length", [("f32", 32, 1, 128, 24, 900), ("f16", 24, 2, 128, 20, 1300), ("bf16", 40, 1, 64, 30, 500), ("f32", 16, 2, 64, 40, 70),
+                                                      ("f16", 2, 1, 64, 1500, 40)])
 def test_single_tokens_of_many_requests(ssd, kind, kv, group, hd, n, length):
     rng = np.random.default_rng(40 + n)
     c = Case(rng, kind, kv * group, kv, hd, 16, rng.integers(0, length + 1, n), [1] * n, None)
@@ -415,6 +417,53 @@ def test_tensors_elsewhere_are_refused(ssd):
     b = ssd.ssd_batch(1, 1, 1, 1, host.data_ptr(), host.data_ptr(), host.data_ptr())
     assert ssd.lib.ssd_tree_plan(b, 16, 10, None, *[host.data_ptr() + 16 * i for i in range(7)], None, 0, None, None) == ssd.SSD_ERR_INVALID_ARG
     assert "current device" in ssd.ssd_last_error()
+
+
+@pytest.mark.parametrize("heads,kv,rows", [(2, 2, 1), (4, 2, 9)])
+def test_offsets_beyond_32_bits(ssd, heads, kv, rows):
+    """Pages and layers more than 2^32 bytes apart: the cache's rows, the attention over them and the moved rows are those
+    of a compact cache."""
+    page, hd, n_pages, layers = 16, 64, 3, 2
+    far = 2**31 + 64
+    big = torch.empty(layers * n_pages * far, dtype=torch.float16, device="cuda")  # 26 GB, of which little is touched
+    inner = (2 * page * hd, hd, 1)  # [kv_head][position][dim], K and V one after the other in a head's place
+    spread = [big[o:].as_strided((layers, n_pages, kv, page, hd), (n_pages * far, far) + inner) for o in (0, page * hd)]
+    small = [torch.zeros(layers, n_pages, kv, page, hd, dtype=torch.float16, device="cuda") for _ in range(2)]
+    for t in spread:
+        t.zero_()
+    table, s = dev(np.array([[2, 0, 1]], np.int32)), torch.cuda.current_stream().cuda_stream
+    rope = ssd.ssd_rope_init(hd)
+    res = []
+    for k, v in (spread, small):
+        rng = np.random.default_rng(23)
+        cache, out = ssd.PagedKV(k, v), []
+        ws = torch.empty(ssd.ssd_tree_attention_workspace(cache), dtype=torch.uint8, device="cuda")
+        def step(n, length):
+            q, kk, vv = (torch.from_numpy(rng.standard_normal((n, h, hd)).astype(np.float32)).cuda().half() for h in (heads, kv, kv))
+            x = np.arange(length, length + n)
+            slots = np.array([2, 0, 1])[x // page] * page + x % page
+            for layer in range(layers):
+                ssd.ssd_rope_kv(cache, layer, rope, q, kk, vv, dev(x.astype(np.int32)), dev(slots.astype(np.int32)), q, s)
+            bt = ssd.TreeBatch(dev(np.array([0, n], np.int32)), ints(1).fill_(length), table, n, n)
+            o = torch.empty_like(q)
+            ssd.ssd_tree_attention(bt, cache, layers - 1, q, None, hd**-0.5, o, ws, None, s)
+            return o, bt
+        out.append(step(30, 0)[0])
+        o, bt = step(rows, 30)
+        out.append(o)
+        # every draft but the first is right: node 2's chain, as children of the root
+        parents = np.array([-1, 0] + [0] * (rows > 2) + list(range(2, rows - 1)), np.int32)[:rows]
+        tokens, target = np.arange(rows, dtype=np.int32), np.full(rows, 99, np.int32)
+        if rows > 2:
+            target[0], target[2:rows - 1] = 2, np.arange(3, rows)
+        got = [ints(1) for _ in range(3)] + [ints(rows) for _ in range(2)]
+        ssd.ssd_tree_commit(bt, cache, dev(parents), dev(tokens), dev(target), *got, s)
+        assert int(got[0]) == max(rows - 2, 0)
+        out += [k.clone(), v.clone()]
+        res.append(out)
+    assert all(torch.equal(x, y) for x, y in zip(*res)) and float(res[1][2][1, 2].abs().sum()) > 0
+    del big, spread, cache, t, k, v
+    torch.cuda.empty_cache()
 
 
 # -- a round of all of them ---------------------------------------------------
