@@ -660,7 +660,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // The tensor cores truncate their sums at every step, relative to what the sum is then: over 1000 positions
                 // 3e-6 to 9e-6 of it, over 4000 1e-5 to 4e-5, all of one sign.  So fp32 rows' products are summed over
                 // one unit, and the units here.
-                const int q_at = tile == 32 && n > 1 ? 1 : n - 1;
+                // (one buffer: before the products that are still to be added, as scores are up to NB units ahead of them; with
+                // q asked for after all others were added, multiplying stopped for 10 us an item, and for 5 so)
+                const int q_at = tile == 32 ? min(1, n - 1) : max(n - NB, 0);
 #pragma unroll 1
                 for (int i = 0; i < n; ++i) {
                     if (i == q_at) next_q();

@@ -92,7 +92,7 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
 // Returns the units of all; every thread has passed two barriers.
 template <int THREADS>
 struct RangeOf {
-    long long sum[THREADS / 32], off;
+    long long sum[THREADS / 32], off, head;  // head: units of a KV head of it
     int b;
     Req req;  // the request that the range starts in
 };
@@ -102,13 +102,14 @@ __device__ __forceinline__ long long range_of(const AttnOpArgs& a, int tile, Ran
     const Shape& sh = a.shape;
     const int per = (sh.n_requests + THREADS - 1) / THREADS;
     const int b0 = min(tid * per, sh.n_requests), b1 = min(b0 + per, sh.n_requests);
-    long long mine = 0;
+    long long mine = 0, head = 0;  // (a prompt's is a sum over its tiles: formed once, if the thread has one request)
     Req last{};
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) {
         last = req_of(sh, b);
         if (last.clipped && last.n && blockIdx.x == 0) say(a.status, SSD_STATUS_TABLE);
-        mine += head_units(sh, last, tile) * sh.n_kv_heads;
+        head = head_units(sh, last, tile);
+        mine += head * sh.n_kv_heads;
     }
     long long before = mine;
 #pragma unroll
@@ -133,8 +134,10 @@ __device__ __forceinline__ long long range_of(const AttnOpArgs& a, int tile, Ran
 #pragma unroll 1
         for (int b = b0; b < b1; ++b) {
             const Req q = per == 1 ? last : req_of(sh, b);
-            const long long n = head_units(sh, q, tile) * sh.n_kv_heads;
+            if (per != 1) head = head_units(sh, q, tile);
+            const long long n = head * sh.n_kv_heads;
             if (off < n) {
+                s.head = head;
                 s.b = b;
                 s.req = q;
                 s.off = off;
@@ -144,7 +147,7 @@ __device__ __forceinline__ long long range_of(const AttnOpArgs& a, int tile, Ran
         }
     }
     __syncthreads();
-    walk_init(walk, sh, tile, s.b, s.req, s.off, lo, hi - lo);
+    walk_init(walk, sh, tile, s.b, s.req, s.off, lo, hi - lo, s.head);
     return units;
 }
 #endif

@@ -64,7 +64,7 @@ __host__ __device__ __forceinline__ int tiles_of(const Shape& s, const Req& q, i
 __host__ __device__ __forceinline__ int units_of(const Shape& s, const Req& q, int tile, int mt) {
     int keys = q.total;
     if (s.chain) {
-        const int last = ((mt + 1) * tile - 1) / s.group;  // the tile's last node
+        const int row = (mt + 1) * tile - 1, last = s.group == 1 ? row : row / s.group;  // the tile's last node
         const long long seen = (long long)q.len + (last < q.n - 1 ? last : q.n - 1) + 1;
         if (seen < keys) keys = (int)seen;
     }
@@ -108,20 +108,22 @@ struct Walk {
     long long at, left;
     Req q;
 };
-// `off`: units of request b (q) before the range [at, at + left)
-__host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int tile, int b, const Req& q, long long off, long long at, long long left) {
+// `off`: units of request b (q; `per` for each KV head) before the range [at, at + left)
+__host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int tile, int b, const Req& q, long long off, long long at, long long left, long long per) {
     w.at = at;
     w.left = left;
     if (left <= 0) return;
     w.b = b;
     w.q = q;
-    const long long per = head_units(s, w.q, tile);
     w.kvh = (off | per) >> 32 ? (int)(off / per) : (int)((uint32_t)off / (uint32_t)per);
     off -= w.kvh * per;
     w.mt = 0;
 #pragma unroll 1
     for (int n; off >= (n = units_of(s, w.q, tile, w.mt) + kItemCost); ++w.mt) off -= n;
     w.u = (int)off;
+}
+__host__ __device__ __forceinline__ void walk_init(Walk& w, const Shape& s, int tile, int b, const Req& q, long long off, long long at, long long left) {
+    walk_init(w, s, tile, b, q, off, at, left, head_units(s, q, tile));
 }
 __host__ __device__ __forceinline__ bool walk_next(Walk& w, const Shape& s, int tile, Seg& g) {
 #pragma unroll 1
