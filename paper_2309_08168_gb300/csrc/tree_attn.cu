@@ -149,9 +149,6 @@ __device__ __forceinline__ void ld32(uint32_t t, uint32_t (&r)[32]) {
         : SSD_R8(r, 0), SSD_R8(r, 8), SSD_R8(r, 16), SSD_R8(r, 24)
         : "r"(t));
 }
-__device__ __forceinline__ void ld16(uint32_t t, uint32_t (&r)[16]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : SSD_R8(r, 0), SSD_R8(r, 8) : "r"(t));
-}
 __device__ __forceinline__ void st32(uint32_t t, const uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -584,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int piece = lane % LPR;
             const uint32_t box = (uint32_t)tile * 128;
             unsigned char* to = smem + (tile == 32 ? (n_seg & 1) * L::q_bytes(32) : 0) + (piece >> 3) * box;
-#pragma unroll 1
+#pragma unroll 4
             for (int r = quarter * RPI + lane / LPR; r < rows; r += 4 * RPI) {
                 const int node = node_of(rem, r), head = s.kvh * sh.group + rem + r - node * sh.group;
                 const T* from = (const T*)a.q + (int64_t)(s.q.r0 + node0 + node) * a.q_stride + head * HD + piece * V;
@@ -673,20 +670,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (active) {
                         const float r = *(volatile float*)&s_ref[ju & 3][mine32], f = ref == -INFINITY ? 0.f : ex2(ref - r);
 #pragma unroll 1
-                        for (int c = 0; c < HD; c += 16) {
-                            uint32_t o[16], m[16];
-                            ld16(tl + c, o);
-                            if (i) ld16(tl + L::M0 + c, m);
+                        for (int c = 0; c < HD; c += 32) {
+                            uint32_t o[32], m[32];
+                            ld32(tl + c, o);
+                            if (i) ld32(tl + L::M0 + c, m);
                             wait_ld();
                             if (i)
 #pragma unroll
-                                for (int k = 0; k < 16; k += 2) {
+                                for (int k = 0; k < 32; k += 2) {
                                     float a0, a1;
                                     of_two(fma2(two(__uint_as_float(m[k]), __uint_as_float(m[k + 1])), two(f, f), two(__uint_as_float(o[k]), __uint_as_float(o[k + 1]))), a0, a1);
                                     o[k] = __float_as_uint(a0);
                                     o[k + 1] = __float_as_uint(a1);
                                 }
-                            st16(tl + L::M0 + c, o);
+                            st32(tl + L::M0 + c, o);
                         }
                         wait_st();
                         ref = r;
