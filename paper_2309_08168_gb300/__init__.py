@@ -257,6 +257,7 @@ def ssd_debug_trace_forward(h: int, draft: bool, rows: int, detail_op: int = -1)
 
 # -- operators on the caller's device tensors (include/ssd_ops.h) -------------
 
+_TYPES: dict = {}  # name -> type, those met so far
 _ROW_TYPES = {"torch.float32": SSD_F32, "torch.float16": SSD_F16, "torch.bfloat16": SSD_BF16}
 
 
@@ -276,7 +277,7 @@ def _dev(t, what: str, dtype, device: int, n: int):
 def _rows(t, what: str, device: int, dtype, n_rows: int, heads: int, hd: int):
     """(address, row stride) of rows [row][head][dim] whose heads lie behind one another."""
     shape, stride = t.shape, t.stride()
-    if t.get_device() != device or t.dtype is not dtype or len(shape) != 3 or shape[0] != n_rows or shape[1] != heads or shape[2] != hd:
+    if shape != (n_rows, heads, hd) or t.dtype is not dtype or t.get_device() != device:
         _refuse(f"{what}: {dtype} of shape ({n_rows}, {heads}, {hd}) on CUDA device {device} is wanted, got {t.dtype}, {tuple(shape)} on {t.device}")
     if stride[2] != 1 or (stride[1] != hd and heads > 1):
         _refuse(f"{what}: the heads of a row must lie behind one another")
@@ -297,9 +298,14 @@ def _row_type(t, what: str) -> int:
 
 def _of_type(t, what: str, name: str):
     """t's type, which has to be this one."""
-    if t is not None and str(t.dtype) != name:
-        _refuse(f"{what}: {name} is wanted, got {t.dtype}")
-    return t.dtype if t is not None else None
+    if t is None:
+        return None
+    k = t.dtype
+    if _TYPES.get(name) is not k:
+        if str(k) != name:
+            _refuse(f"{what}: {name} is wanted, got {k}")
+        _TYPES[name] = k
+    return k
 
 
 class PagedKV:

@@ -35,8 +35,9 @@
 //   6 trees of 33 nodes, 8 heads a KV head, 4096 positions, bf16: 33 us, 2.0 TB/s - 8 us until the
 //     first unit's scores, then 1.0 us a unit (S, softmax, P V of a buffer one after the other), join 5;
 //   2048 rows over 4000 positions, 8 heads a KV head, bf16: 332 us, 1.02 PFLOP/s - the exponentials;
-//   2 x 1023 rows over 700 positions, 40 heads, fp32: 148 us, 0.32 PFLOP/s counted once, 0.64 done
-//     (two passes each): fp32 rows' two buffers, and the sums of every unit.
+//   2 x 1023 rows over 700 positions, 40 heads, fp32: 136 us, 0.35 PFLOP/s counted once, 0.7 done
+//     (two passes each) - 1.9 us a unit, as its product and the sum of the one before take turns at the
+//     accumulator, and 7 us an item until its q, which has one buffer, is there as pairs.
 //
 // O is rescaled only when a row's maximum has grown by more than kSlack (log2)
 // over the one its weights are relative to (the running softmax of Milakov and
