@@ -26,16 +26,15 @@
 //                to its sums; at an item's end O / sum, or O, maximum and sum to the
 //                workspace if other CTAs hold parts of the item, while the others are at
 //                the next item.  join_kernel adds those.
-// The tile has 128 rows; 32 where no request has more, which leaves the ring the
-// shared memory of the other rows' q (their lanes then hold what no one reads).  Two rows or
-// less are few_kernel's (tree_few.cu).
+// The tile has 128 rows (with fewer, the others' lanes hold what no one reads; tiles of 32, with q of two
+// items in shared memory, were no faster); two rows or less are few_kernel's (tree_few.cu).
 //
 // Measured, with join_kernel (copy rate 6.79 TB/s, tensor cores 1.92 PFLOP/s):
 //   9 nodes, 8 heads a KV head, 100001 positions, fp16: 72 us, 5.7 TB/s - HBM;
-//   6 trees of 33 nodes, 8 heads a KV head, 4096 positions, bf16: 33 us, 2.0 TB/s - 8 us until the
+//   6 trees of 33 nodes, 8 heads a KV head, 4096 positions, bf16: 32 us, 2.1 TB/s - 8 us until the
 //     first unit's scores, then 1.0 us a unit (S, softmax, P V of a buffer one after the other), join 5;
-//   2048 rows over 4000 positions, 8 heads a KV head, bf16: 332 us, 1.02 PFLOP/s - the exponentials;
-//   2 x 1023 rows over 700 positions, 40 heads, fp32: 136 us, 0.35 PFLOP/s counted once, 0.7 done
+//   2048 rows over 4000 positions, 8 heads a KV head, bf16: 315 us, 1.07 PFLOP/s - the exponentials;
+//   2 x 1023 rows over 700 positions, 40 heads, fp32: 134 us, 0.35 PFLOP/s counted once, 0.7 done
 //     (two passes each) - 1.9 us a unit, as its product and the sum of the one before take turns at the
 //     accumulator, and 7 us an item until its q, which has one buffer, is there as pairs.
 //
@@ -89,24 +88,15 @@ struct Lay {
     static constexpr int RING = 210 * 1024;           // shared memory for q and the rings
     // TMEM columns: O; fp32 rows' sums of earlier units; S / P of unit j at S0 + 128 (j mod NB)
     static constexpr int M0 = HD, S0 = PARTS == 2 && HD == 128 ? 256 : 128, NB = (kTmem - S0) / kUnit;
-    // two buffers of a tile of 32 rows, one of 128
-    static __host__ __device__ constexpr int q_bytes(int tile) { return PARTS * BOXES * tile * 128; }
-    static __host__ __device__ constexpr int q_all(int tile) { return q_bytes(tile) * (tile == 32 ? 2 : 1); }
+    static constexpr int QBOX = kTile * 128;          // 64 dims of the tile's q
+    static constexpr int Q_ALL = PARTS * BOXES * QBOX;
     // Slots.  The scores wait for K more often than the products for V, which is asked for at the same time and
     // needed later: K takes 13 / 20 of the rings (9 / 20: tree of 33 nodes 33.0 us against 32.2, long request
     // 73.5 against 71.9), but leaves two units of V (softmax: half_done).
-    static constexpr int nk(int tile) {
-        const int room = RING - q_all(tile), share = room * 13 / 20 / KSLOT, most = (room - 4 * VSLOT) / KSLOT;
-        const int n = share < most ? share : most;
-        return n < kMaxSlots ? n : kMaxSlots;
-    }
-    static constexpr int nv(int tile) {
-        const int n = (RING - q_all(tile) - nk(tile) * KSLOT) / VSLOT;
-        return n < kMaxSlots ? n : kMaxSlots;
-    }
-    static_assert(nk(128) >= 2 * BOXES && nv(128) >= 4, "a unit of K and two of V");
-    // (the MMA reads 128 rows of q whatever the tile is: what lies behind is shared memory of the ring)
-    static_assert(q_all(32) - 32 * 128 + 128 * 128 <= RING, "");
+    static constexpr int ROOM = RING - Q_ALL, MOST_K = (ROOM - 4 * VSLOT) / KSLOT, SHARE = ROOM * 13 / 20 / KSLOT;
+    static constexpr int least(int a, int b) { return a < b ? a : b; }
+    static constexpr unsigned NK = least(least(SHARE, MOST_K), kMaxSlots), NV = least((ROOM - (int)NK * KSLOT) / VSLOT, kMaxSlots);
+    static_assert(NK >= 2 * BOXES && NV >= 4, "a unit of K and two of V");
     static constexpr size_t BYTES = 1024 + (size_t)RING;
 };
 
@@ -329,13 +319,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     using L = Lay<T, HD>;
     using C = typename Types<T>::C;
     constexpr int BOXES = L::BOXES, PARTS = L::PARTS, NB = L::NB;
-    const int tile = a.tile;
-    const unsigned nk = a.nk, nv = a.nv;
+    constexpr unsigned NK = L::NK, NV = L::NV;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    unsigned char *ks = smem + L::q_all(tile), *vs = ks + nk * L::KSLOT;
+    unsigned char *ks = smem + L::Q_ALL, *vs = ks + NK * L::KSLOT;
     __shared__ __align__(8) uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
-    __shared__ __align__(8) uint64_t q_ready[2], q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
+    __shared__ __align__(8) uint64_t q_ready, q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
     __shared__ RangeOf<kThreads> s_range;
@@ -358,8 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mb_init(v_full + i, 1);
             tc::mb_init(v_empty + i, 1);
         }
-        tc::mb_init(q_ready, 4);
-        tc::mb_init(q_ready + 1, 4);
+        tc::mb_init(&q_ready, 4);
         tc::mb_init(&q_free, 1);
         tc::mb_init(&o_free, 4);
         for (int i = 0; i < 3; ++i) {
@@ -389,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::fence_before();
     Walk walk;
     int ctas;
-    const long long units = range_of<kThreads>(a, tile, s_range, walk, ctas);
+    const long long units = range_of<kThreads>(a, kTile, s_range, walk, ctas);
     tc::fence_after();
     const uint32_t tmem = s_tmem;
     Seg g;
@@ -414,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // page ids are asked for 32 copies (of one 64-dim half) ahead, one per lane
         asm volatile("fence.proxy.async.global;" ::: "memory");  // K / V rows that the previous kernel wrote
         const bool is_v = warp == 9;
-        const unsigned n_slots = is_v ? nv : nk;
+        const unsigned n_slots = is_v ? NV : NK;
         unsigned char* ring = is_v ? vs : ks;
         uint64_t *full = is_v ? v_full : k_full, *empty = is_v ? v_empty : k_empty;
         const CUtensorMap* map = is_v ? &tm_v : &tm_k;
@@ -431,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!is_v)
 #pragma unroll 1
                 for (; published < n_seg + 2 && more; ++published) {
-                    more = walk_next(walk, sh, tile, g);
+                    more = walk_next(walk, sh, kTile, g);
                     if (!more) g.n = 0;
                     if (lane == 0) {
                         s_seg[published % kSegs] = g;
@@ -474,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 if (++slot == n_slots) slot = 0, phase ^= 1u;
                 if (!is_v && n_seg && i == BOXES) {  // the rows of q that will be asked for at the end of the segment before, into L2
-                    const int start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
+                    const int start = g.mt * kTile, rows = min(g.q.n * sh.group - start, kTile), node0 = start / sh.group, rem = start - node0 * sh.group;
 #pragma unroll 1
                     for (int r = lane; r < rows; r += 32) {
                         const int node = node_of(rem, r), head = g.kvh * sh.group + rem + r - node * sh.group;
@@ -486,11 +474,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == 10) {
         const uint64_t q0 = tc::sdesc(smem_u32(smem)), k0 = tc::sdesc(smem_u32(ks));
-        const uint32_t qb = (uint32_t)tile * 128;  // 64 dims of the tile's q
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;  // unit 3 turn + buf
         for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
-            if (!wait(q_ready + (n_seg & 1), n_seg >> 1)) break;  // (two: q of a small tile comes a segment ahead)
-            const uint64_t qs = q0 + (tile == 32 ? (uint64_t)((n_seg & 1) * (L::q_bytes(32) >> 4)) : 0);
+            if (!wait(&q_ready, n_seg)) break;
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
                 // P of unit j - NB, which held these columns, is used up
@@ -499,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 auto multiply = [&](int h, int b, unsigned slot, bool more) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        mma_ss(d, qs + (uint64_t)(((h * BOXES + b) * qb + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
+                        mma_ss(d, q0 + (uint64_t)(((h * BOXES + b) * L::QBOX + k * 32) >> 4), k0 + (uint64_t)((slot * L::KSLOT + k * 32) >> 4),
                                idesc<C>(kUnit, false), (more || k) ? 1u : 0u);
                 };
                 unsigned slots[BOXES];
@@ -507,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int b = 0; b < BOXES; ++b) {
                     if (!wait(k_full + slot, phase)) break;
                     slots[b] = slot;
-                    if (++slot == nk) slot = 0, phase ^= 1u;
+                    if (++slot == NK) slot = 0, phase ^= 1u;
                     if (PARTS == 1) {
                         tc::fence_after();
                         if (elect_one()) {
@@ -563,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (half) commit(pv_done + buf);
                     }
                     __syncwarp();
-                    if (++slot == nv) slot = 0, phase ^= 1u;
+                    if (++slot == NV) slot = 0, phase ^= 1u;
                 }
                 if (++buf == NB) buf = 0, ++turn;
             }
@@ -578,10 +564,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         // and are converted there.
         auto load_q = [&](const Seg& s, unsigned n_seg) {
             constexpr int V = Vec<T>::N, LPR = HD / V, RPI = 32 / LPR;  // lanes per row, rows per step
-            const int start = s.mt * tile, rows = min(s.q.n * sh.group - start, tile), node0 = start / sh.group, rem = start - node0 * sh.group;
+            const int start = s.mt * kTile, rows = min(s.q.n * sh.group - start, kTile), node0 = start / sh.group, rem = start - node0 * sh.group;
             const int piece = lane % LPR;
-            const uint32_t box = (uint32_t)tile * 128;
-            unsigned char* to = smem + (tile == 32 ? (n_seg & 1) * L::q_bytes(32) : 0) + (piece >> 3) * box;
+            unsigned char* to = smem + (piece >> 3) * L::QBOX;
 #pragma unroll 4
             for (int r = quarter * RPI + lane / LPR; r < rows; r += 4 * RPI) {
                 const int node = node_of(rem, r), head = s.kvh * sh.group + rem + r - node * sh.group;
@@ -593,13 +578,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (PARTS == 2) {
                 constexpr int N = 4;  // steps at once
                 const int e = piece * V;
-                unsigned char* hi = smem + (tile == 32 ? (n_seg & 1) * L::q_bytes(32) : 0) + (e >> 6) * box + (e & 7) * 2;
+                unsigned char* hi = smem + (e >> 6) * L::QBOX + (e & 7) * 2;
 #pragma unroll 1
                 for (int i0 = quarter * RPI + lane / LPR; i0 - lane / LPR < rows; i0 += N * 4 * RPI) {
                     uint4 x[N];
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const int r = min(i0 + i * 4 * RPI, tile - 1);
+                        const int r = min(i0 + i * 4 * RPI, kTile - 1);
                         x[i] = *reinterpret_cast<const uint4*>(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
                     }
                     __syncwarp();
@@ -620,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (r < rows) {
                             unsigned char* at = hi + r * 128 + ((((e & 63) >> 3) ^ (r & 7)) << 4);
                             *reinterpret_cast<uint2*>(at) = h;
-                            *reinterpret_cast<uint2*>(at + BOXES * box) = l;
+                            *reinterpret_cast<uint2*>(at + BOXES * L::QBOX) = l;
                             if (piece == 0) s_scale[n_seg & 3][r] = __uint_as_float((uint32_t)(127 + e2) << 23);
                         }
                     }
@@ -628,14 +613,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) arrive(q_ready + (n_seg & 1));
+            if (lane == 0) arrive(&q_ready);
         };
         bool more = segment(0);
         if (more) load_q(g, 0);
         unsigned j = 0;  // of the segment's first unit
         for (unsigned n_seg = 0; more && ok; ++n_seg) {
             const Seg cur = g;
-            const int n = cur.u1 - cur.u0, start = cur.mt * tile, rows = min(cur.q.n * sh.group - start, tile);
+            const int n = cur.u1 - cur.u0, start = cur.mt * kTile, rows = min(cur.q.n * sh.group - start, kTile);
             const bool active = quarter * 32 < rows, valid = mine32 < rows, whole = cur.u0 == 0 && cur.u1 == cur.n;
             const unsigned j_last = j + (unsigned)n - 1, buf = j_last % NB, turn = j_last / NB;
             float ref = -INFINITY;  // fp32 rows: what the sums are relative to
@@ -648,19 +633,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 sum = e.y + f.y * (f.x == -INFINITY ? 0.f : ex2(f.x - e.x));
                 return true;
             };
-            // The next rows' q: into the other buffer (the last segment but this one is finished), or, with
-            // one buffer, once all scores of this segment are there
+            // the next rows' q, once all scores of this segment are there
             auto next_q = [&] {
                 more = segment(n_seg + 1);
-                if (more && (tile == 32 || wait(&q_free, n_seg))) load_q(g, n_seg + 1);
+                if (more && wait(&q_free, n_seg)) load_q(g, n_seg + 1);
             };
             if constexpr (PARTS == 2) {
                 // The tensor cores truncate their sums at every step, relative to what the sum is then: over 1000 positions
                 // 3e-6 to 9e-6 of it, over 4000 1e-5 to 4e-5, all of one sign.  So fp32 rows' products are summed over
                 // one unit, and the units here.
-                // (one buffer: before the products that are still to be added, as scores are up to NB units ahead of them; with
+                // (before the products that are still to be added, as scores are up to NB units ahead of them; with
                 // q asked for after all others were added, multiplying stopped for 10 us an item, and for 5 so)
-                const int q_at = tile == 32 ? min(1, n - 1) : max(n - NB, 0);
+                const int q_at = max(n - NB, 0);
 #pragma unroll 1
                 for (int i = 0; i < n; ++i) {
                     if (i == q_at) next_q();
@@ -767,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t tl = tmem + ((uint32_t)(quarter * 32) << 16);
         unsigned j = 0;  // of the segment's first unit
         for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
-            const int n = g.u1 - g.u0, start = g.mt * tile, rows = min(g.q.n * sh.group - start, tile);  // units; rows that exist
+            const int n = g.u1 - g.u0, start = g.mt * kTile, rows = min(g.q.n * sh.group - start, kTile);  // units; rows that exist
             const bool active = quarter * 32 < rows;
             const int node0 = start / sh.group, node = node0 + node_of(start - node0 * sh.group, min(mine32, rows - 1));
             // positions below it are seen by every row of the tile
@@ -793,8 +777,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int x0 = p0 + 64 * half, lo_row = max(min(g.q.len, g.q.total) - x0, 0);
                         // (copies that begin behind the last position have brought zeros)
                         const int hi_row = min((max(g.q.total - x0, 0) + (1 << a.box_shift) - 1) >> a.box_shift << a.box_shift, 64);
-                        if (lo_row < hi_row && (ju < 2 || wait(pv_done + (ju - 2) % NB, (ju - 2) / NB)) && wait(v_full + s % nv, s / nv)) {
-                            clean_v<C, HD>(vs + s % nv * L::VSLOT, lo_row, min(g.q.total - x0, 64), hi_row, tid & (kTile - 1), &s_odd);
+                        if (lo_row < hi_row && (ju < 2 || wait(pv_done + (ju - 2) % NB, (ju - 2) / NB)) && wait(v_full + s % NV, s / NV)) {
+                            clean_v<C, HD>(vs + s % NV * L::VSLOT, lo_row, min(g.q.total - x0, 64), hi_row, tid & (kTile - 1), &s_odd);
                             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         }
                     }
@@ -1083,8 +1067,6 @@ int run_hd(const char* call, AttnOpArgs& a, int dtype, const CUtensorMap& k, con
     if (a.tile <= kFewRows) {
         rc = launch_few(call, a, dtype, HD, stream);
     } else {
-        a.nk = (unsigned)L::nk(a.tile);
-        a.nv = (unsigned)L::nv(a.tile);
         rc = launch(call, attn_kernel<T, HD>, dim3((unsigned)a.grid), kThreads, L::BYTES, stream, a, k, v);
     }
     // an item of one unit is never cut
@@ -1169,7 +1151,7 @@ extern "C" int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache
     a.scale2 = (float)(1.4426950408889634 * scale);
     a.status = status;
     const long long rows = (long long)batch->max_rows * group;
-    a.tile = rows <= kFewRows ? (int)rows : rows <= 32 ? 32 : kTile;
+    a.tile = rows <= kFewRows ? (int)rows : kTile;  // (both sides measured: tree_few.cu)
     a.group_inv = ((1ull << 32) + group - 1) / group;
     a.grid = n_sms;
     a.cuts = (Cut*)workspace;

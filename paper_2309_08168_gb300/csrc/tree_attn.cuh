@@ -34,8 +34,7 @@ struct AttnOpArgs {
     int box_shift;  // positions per copy, log2: 16 .. 64 of them, which divide page_size
     int at_pos, at_head, at_page;  // which coordinate (1 .. 3) of the tensor maps is which
     float scale2;  // log2(e) * scale
-    int tile;      // rows: up to kFewRows, 32 or 128
-    unsigned nk, nv;    // slots of the rings
+    int tile;      // rows: up to kFewRows, or kTile
     uint64_t group_inv;  // ceil(2^32 / group)
     Cut* cuts;     // [grid]
     float* stats;  // [grid][2][2][kTile]: maximum, sum

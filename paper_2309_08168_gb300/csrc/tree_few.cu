@@ -15,11 +15,11 @@
 // item's first K on its way; parts of items that other CTAs share go to the workspace for
 // join_kernel.
 //
-// Measured (with join_kernel), against the tensor cores' kernel in a tile of 32 rows: single tokens of 16
+// Measured (with join_kernel), against the tensor cores' kernel: single tokens of 16
 // requests, 262 to 2100 positions, 32 heads of 128 dims, fp32 64 us (5.5 TB/s, 81 % of the copy rate)
-// against 92, fp16 63 against 71; two heads a KV head 70 against 93 and 71; head_dim 64, 32 requests 70
+// against 88, fp16 64 against 71; two heads a KV head 70.5 against 89 and 70.2 against 70.8; head_dim 64, 32 requests 70
 // against 100; one request of 4000 positions 22 against 30, of 200 9.8 against 16.  Four rows a tile:
-// 96 against 90 (fp32) and 69 (fp16), as the arithmetic of a block then takes as long as its loads; so
+// 96 against 90 (fp32) and 69 (fp16) then, as the arithmetic of a block then takes as long as its loads; so
 // two rows are the most.  What is left: 7 us until the first block is there, 3 to join, uneven blocks.
 #include "tree_attn.cuh"
 
