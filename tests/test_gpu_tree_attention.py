@@ -173,15 +173,15 @@ def test_the_largest_row_count_only_chooses_the_tile(ssd):
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("hd,page", [(64, 16), (64, 48), (128, 16), (128, 80)])
-@pytest.mark.parametrize("group", [1, 2])
-def test_tiles_of_few_rows(ssd, kind, hd, page, group):
-    """Trees and chains as tiles of one row or two: rows that see nothing, nodes of NaN that some rows do not see, pages outside
+@pytest.mark.parametrize("group,said", [(1, 1), (2, 1), (1, 2)])
+def test_tiles_of_few_rows(ssd, kind, hd, page, group, said):
+    """Trees and chains as tiles of one row or two (heads of a node, or nodes): rows that see nothing, nodes of NaN that some rows do not see, pages outside
     the cache, items of less than a block, of more than a warp looks up at once, and more items than CTAs."""
     rng = np.random.default_rng(30 + hd + group)
     lens, counts = [0, 1, 15, 127, 130, 700, -1, 18000, 31], [3, 1, 17, 1, 70, 2, 0, 1, 33]
     for masks in ("star", None):
         c = Case(rng, kind, 2 * group, 2, hd, page, lens, counts, masks)
-        c.max_rows = 1
+        c.max_rows = said
         if masks:
             c.masks[1] = 0  # of a request with nothing cached
         clean = c.run(ssd)
