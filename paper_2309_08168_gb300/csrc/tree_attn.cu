@@ -40,19 +40,19 @@
 //
 // O is rescaled only when a row's maximum has grown by more than kSlack (log2)
 // over the one its weights are relative to (the running softmax of Milakov and
-// Gimelshein, 2018).  Weights are relative to the maximum less kShift, so that
-// fp16 keeps 22 bits of pairs, and 11 of single weights, down to 2^-20 of the
-// largest one.
+// Gimelshein, 2018).  Weights are relative to the maximum less kShift, and enter the product as pairs hi + lo of the
+// cache's type: in fp16 22 bits down to 2^-20 of the largest one, in bf16 16 bits.  (Rounded to the type
+// once, as their sum is not, they made the error of 16-bit rows 1.4 times that of rounding the result: 2.3e-3 against
+// 1.7e-3 in bf16.  The second pass costs 2 % of the time where HBM bounds, 9 % on trees, 18 % on prompts.)
 //
-// fp32 rows: q and the weights enter the products as fp16 pairs hi + lo (22 bits).  A
+// fp32 rows: q enters its product as fp16 pairs too.  A
 // row of q is scaled by a power of two first, which the scores take back, so that
 // no fp32 value is too large or too small for the pair; hi is rounded towards
 // zero and lo is not 0, so that an infinite key gives the product the sign of q.
 // The tensor cores cut off what their sums cannot hold, always downwards in size: adding up
 // 4000 positions in one accumulator made results too small by 3e-5.  So each unit's
 // product starts from zero (lo first) and is added in fp32: 7.5e-7 at any length.
-// 16-bit rows: q as it is; the weights rounded to the type once, like the output (half a step: 2^-8, 2^-11);
-// the cut adds 5e-9 of the result a position of a CTA's share, 2e-4 after 50000.
+// 16-bit rows: q as it is; the cut adds up to 1e-8 of the result a position of a CTA's share, 3e-4 after 50000.
 //
 // Units with positions that some row does not see: scores by the row's 64 mask
 // bits, and V rows behind the last position, which may hold anything, are set
@@ -208,11 +208,19 @@ __device__ __forceinline__ void split_away(f32x2 v, uint32_t& hi, uint32_t& lo) 
     hi = half2_of(h);
     lo = half2_of(fma2(v, two(0x1p-24f, 0x1p-24f), rest(v, h)));
 }
-// weights as fp16 pairs: hi the upper 11 bits, lo the rest
-__device__ __forceinline__ void split_bits(f32x2 v, uint32_t& hi, uint32_t& lo) {
+// two weights as pairs of the cache's type: hi the upper bits (fp16 11, bf16 8), lo the rest
+__device__ __forceinline__ void split_bits(f32x2 v, uint32_t& hi, uint32_t& lo, f16) {
     const f32x2 h = upper(v);
     hi = half2_of(h);
     lo = half2_of(rest(v, h));
+}
+__device__ __forceinline__ void split_bits(f32x2 v, uint32_t& hi, uint32_t& lo, bf16) {
+    const f32x2 h = v & 0xffff0000ffff0000ull;
+    float a, b;
+    of_two(h, a, b);
+    hi = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    of_two(rest(v, h), a, b);
+    lo = pack2(a, b, bf16());
 }
 
 // Which of the positions p0 .. p0 + 63 node `node` of a request sees, as bits; masks: its row's words, nullptr: a
@@ -540,11 +548,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (elect_one()) {
                         const uint32_t p = tmem + (uint32_t)L::S0 + 128u * buf + 64u * half;
 #pragma unroll
-                        for (int h = PARTS - 1; h >= 0; --h)  // (lo first, as above)
+                        for (int h = 1; h >= 0; --h)  // (lo first, as above)
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 mma_ts(tmem, p + 32u * (k >> 1) + 16u * h + 8u * (k & 1), v0 + (uint64_t)((slot * L::VSLOT + k * 2048) >> 4), idesc<C>(HD, true),
-                                       (!fresh || half || k || h < PARTS - 1) ? 1u : 0u);
+                                       (!fresh || half || k || h == 0) ? 1u : 0u);
                         commit(v_empty + slot);
                         if (half) commit(pv_done + buf);
                     }
@@ -862,11 +870,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                             e1 = ex2(e1);
                             const f32x2 e = two(e0, e1);
                             l4[k & 3] = add2(l4[k & 3], e);
-                            if constexpr (PARTS == 2) split_bits(e, ph[k], pl[k]);
-                            else ph[k] = pack2(e0, e1, C());
+                            split_bits(e, ph[k], pl[k], C());
                         }
                         st16(ts + 32 * c, ph);
-                        if constexpr (PARTS == 2) st16(ts + 32 * c + 16, pl);
+                        st16(ts + 32 * c + 16, pl);
                         float la, lb;
                         of_two(add2(add2(l4[0], l4[1]), add2(l4[2], l4[3])), la, lb);
                         l += la + lb;
