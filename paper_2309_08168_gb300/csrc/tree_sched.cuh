@@ -93,7 +93,7 @@ __host__ __device__ __noinline__ inline long long range_start(long long units, i
 }
 __host__ __device__ __noinline__ inline int cta_of(long long units, int ctas, long long u) {
     const long long x = (u + 1) * ctas - 1;
-    return x >> 32 ? (int)(x / units) : (int)((uint32_t)x / (uint32_t)units);
+    return (x | units) >> 32 ? (int)(x / units) : (int)((uint32_t)x / (uint32_t)units);
 }
 
 // One CTA's share of an item: units [u0, u1) of n, u0 < u1.

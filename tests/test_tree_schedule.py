@@ -135,3 +135,66 @@ def program(tmp_path_factory):
 def test_every_unit_once_and_parts_where_the_join_looks(program, seed):
     r = subprocess.run([program, str(seed), "400"], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout
+
+
+# Batches of 2^32 units and more (too long to run): the CTA of a unit against one division in 64 bits, the ranges'
+# starts around it, and the holders of the items that the range ends cut.
+LARGE = r"""
+#include "tree_sched.cuh"
+#include <cstdio>
+using namespace ssd::tree;
+int main() {
+    const int grids[] = {1, 40, 152, 304};
+    const long long around[] = {1ll << 31, 1ll << 32, 3ll << 32, 1ll << 40};
+    for (int ctas : grids)
+        for (long long top : around)
+            for (long long U = top - 2; U <= top + 8200; U += U < top + 2 ? 1 : 911)
+                for (int c = 0; c < ctas; ++c) {
+                    const long long lo = range_start(U, ctas, c);
+                    if (lo != U * c / ctas) return printf("start %lld %d\n", U, c), 1;
+                    for (long long u : {lo - 1, lo, lo + 1, (long long)c, 1000ll * c})
+                        if (u >= 0 && u < U && cta_of(U, ctas, u) != (int)(((u + 1) * ctas - 1) / U)) return printf("cta_of %lld %d %lld\n", U, ctas, u), 1;
+                }
+    // one prompt over eight KV heads of eight heads
+    for (int rows = 1482451; rows < 1482481; rows += 3) {
+        int32_t start[2] = {0, rows}, lens[1] = {0};
+        Shape s{};
+        s.n_requests = 1;
+        s.n_rows = rows;
+        s.page_size = 64;
+        s.max_blocks = (rows + 63) / 64;
+        s.n_kv_heads = s.group = 8;
+        s.chain = 1;
+        s.row_start = start;
+        s.lens = lens;
+        const Req q = req_of(s, 0);
+        const long long per = head_units(s, q, 128), U = per * 8;
+        if (U < 1ll << 32) return printf("units %lld\n", U), 1;
+        const int ctas = ctas_of(U, 152);
+        for (int c = 0; c < ctas; c += 1 + c % 3 * 37) {
+            const long long lo = range_start(U, ctas, c), hi = range_start(U, ctas, c + 1);
+            Walk w;
+            walk_init(w, s, 128, 0, q, lo, lo, hi - lo, per);
+            Seg g;
+            while (walk_next(w, s, 128, g))
+                if (g.u1 < g.n) {
+                    int first, last, later;
+                    holders(g, U, ctas, first, last, later);
+                    if (first > c || last < c || last >= ctas || range_start(U, ctas, first) > g.item + kItemCost || range_start(U, ctas, first + 1) <= g.item + kItemCost ||
+                        range_start(U, ctas, last) > g.item + kItemCost + g.n - 1)
+                        return printf("holders of %d rows, CTA %d: %d .. %d\n", rows, c, first, last), 1;
+                }
+        }
+    }
+    printf("ok\n");
+    return 0;
+}
+"""
+
+
+def test_more_units_than_32_bits(tmp_path):
+    (tmp_path / "l.cu").write_text(LARGE)
+    subprocess.check_call(["nvcc", "-O2", "-std=c++17", "-gencode", "arch=compute_103a,code=sm_103a", "-I", os.path.join(ROOT, "paper_2309_08168_gb300", "csrc"),
+                           str(tmp_path / "l.cu"), "-o", str(tmp_path / "l")])
+    r = subprocess.run([str(tmp_path / "l")], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout
