@@ -831,12 +831,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (i > 0) {
                         r = *(volatile float*)&s_ref[(ju - 1) & 3][mine32];
                         if (__any_sync(0xffffffffu, bm - kShift > r + kSlack)) {
-                            const float nr = fmaxf(r, bm - kShift);
-                            if constexpr (PARTS == 1) {  // the accumulator moves to the new maximum (all rows of the warp)
+                            const float nr = bm - kShift > r + kSlack ? bm - kShift : r;  // (each row by what it sees alone)
+                            if constexpr (PARTS == 1) {  // the accumulator moves to the new maximum (the other rows of the warp: by a factor of 1)
                                 const unsigned tb = (ju - 1) / NB, bb = ju - 1 - NB * tb;
                                 if (!wait(pv_done + bb, tb)) break;
                                 tc::fence_after();
-                                const float f = nr == -INFINITY ? 1.f : ex2(r - nr);
+                                const float f = nr == r ? 1.f : ex2(r - nr);
 #pragma unroll 1
                                 for (int c = 0; c < HD; c += 32) {
                                     ld32(tl + c, x);

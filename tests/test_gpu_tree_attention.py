@@ -262,6 +262,26 @@ def test_what_a_row_does_not_see_does_not_matter(ssd, kind, heads, kv, counts):
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,kv,hd,rows", [(8, 8, 128, 25), (8, 8, 64, 32), (32, 8, 128, 12), (16, 8, 64, 40)])
+def test_a_large_key_that_a_row_does_not_see(ssd, kind, heads, kv, hd, rows):
+    """A node of an item's second unit, most of which every row sees, has a key of fifty times the size: the row of it moves to its
+    score, the others of its warp keep their bits (their reference and what they have summed up).  With 320 items most lie in one
+    CTA's range."""
+    n, rng = 40, np.random.default_rng(60 + rows)
+    lens = rng.integers(200, 257 - rows, n)
+    c = Case(rng, kind, heads, kv, hd, 16, lens, [rows] * n, "star")
+    clean = c.run(ssd)
+    node = rng.integers(1, rows, n)
+    x = torch.from_numpy(lens + node)
+    c.k[0, torch.from_numpy(c.table[np.arange(n), x // 16].astype(np.int64)).cuda(), :, (x % 16).cuda()] *= 50
+    out = c.run(ssd)
+    hit = (np.arange(n) * rows + node).tolist()
+    rest = [r for r in range(n * rows) if r not in hit]
+    assert torch.equal(out[rest], clean[rest]) and not torch.equal(out[hit], clean[hit])
+    c.check(out)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows", [3, 40])
 def test_scores_of_minus_infinity_have_no_weight(ssd, kind, rows):
     """Keys of -inf in one dim, against positive queries there; a row all of whose scores are -inf is zero."""
