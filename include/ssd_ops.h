@@ -162,9 +162,8 @@ int ssd_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* rope, int dty
  * Scores, statistics and sums are fp32.  If no request has more than two rows a KV head
  * (max_rows n_heads / n_kv_heads <= 2) everything is fp32.  Else the weights, and q of fp32 rows, enter
  * the products as pairs of the cache's type (fp16 22 bits, bf16 16).
- * Measured against 64 bits, values around 1: fp32 rows 1e-6 at any length; 16-bit rows what rounding the exact result to the type
- * costs, and up to 1e-8 of the result more for every position that one of the SMs sums up (16000: 1e-4
- * smaller than it should be).
+ * Measured against 64 bits, values around 1, at any length: fp32 rows 1e-6; 16-bit rows what rounding the exact result to the type
+ * costs, and up to 4e-5 of the result more (tensor cores sum up to 3072 positions and cut off what their sums do not hold).
  * workspace: ssd_tree_attention_workspace() bytes, 16-byte aligned; its contents
  * mean nothing between calls.  The same inputs give the same bits; the order of
  * sums depends on the whole batch's lengths.

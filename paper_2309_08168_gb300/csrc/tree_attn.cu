@@ -49,10 +49,11 @@
 // row of q is scaled by a power of two first, which the scores take back, so that
 // no fp32 value is too large or too small for the pair; hi is rounded towards
 // zero and lo is not 0, so that an infinite key gives the product the sign of q.
-// The tensor cores cut off what their sums cannot hold, always downwards in size: adding up
-// 4000 positions in one accumulator made results too small by 3e-5.  So each unit's
-// product starts from zero (lo first) and is added in fp32: 7.5e-7 at any length.
-// 16-bit rows: q as it is; the cut adds up to 1e-8 of the result a position of a CTA's share, 3e-4 after 50000.
+// The tensor cores cut off what their sums cannot hold, always downwards in size: 1.5e-8 of the sum a
+// position, 6e-4 after 100000 in one accumulator.  So a run of units (Lay::RUN) starts from zero
+// (lo first), and runs are added in fp32.  fp32 rows: a run is a unit, 1e-6 at any length.  16-bit rows: 24 units, 4e-5 at any length
+// (of fp16's half step, 2.4e-4 to 4.9e-4, a sixth; 32 units 5e-5).  A run's end is a gap of 3 to 4 us in the products: 100001 positions
+// 73.6 -> 78.7 us, 160 items of 60000 472 -> 508, bf16 prompt of 2048 rows 366 -> 382; shorter items as before.
 //
 // Units with positions that some row does not see: scores by the row's 64 mask
 // bits, and V rows behind the last position, which may hold anything, are set
@@ -88,6 +89,11 @@ struct Lay {
     static constexpr int RING = 210 * 1024;           // shared memory for q and the rings
     // TMEM columns: O; fp32 rows' sums of earlier units; S / P of unit j at S0 + 128 (j mod NB)
     static constexpr int M0 = HD, S0 = PARTS == 2 && HD == 128 ? 256 : 128, NB = (kTmem - S0) / kUnit;
+    // Units whose products are added in the accumulator, from zero on; then they are added to the sums in fp32, in TMEM if
+    // it has room for those, else in the workspace (above).  (Sums in TMEM with two S / P buffers instead of three: bf16 prompt
+    // 438 us against 382; copies of the accumulator added up behind the next run's products: no faster.)
+    static constexpr int RUN = PARTS == 2 ? 1 : 24;
+    static constexpr bool SUMS_IN_TMEM = M0 + HD <= S0;
     static constexpr int QBOX = kTile * 128;          // 64 dims of the tile's q
     static constexpr int Q_ALL = PARTS * BOXES * QBOX;
     // Slots.  The scores wait for K more often than the products for V, which is asked for at the same time and
@@ -321,6 +327,34 @@ __device__ __noinline__ void add_odd(OddArgs a, int len, int total, int node, in
     }
 }
 
+// 32 dims of a row, 16 bytes of them kTile apart
+__device__ __forceinline__ void to_memory(float4* to, const uint32_t (&o)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4)
+        to[(i / 4) * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+}
+// and back
+__device__ __forceinline__ void from_memory(const float4* from, uint32_t (&o)[32]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float4 x = __ldcg(from + k * kTile);
+        o[4 * k] = __float_as_uint(x.x), o[4 * k + 1] = __float_as_uint(x.y), o[4 * k + 2] = __float_as_uint(x.z), o[4 * k + 3] = __float_as_uint(x.w);
+    }
+}
+// o += f times those
+__device__ __forceinline__ void add_memory(const float4* from, float f, uint32_t (&o)[32]) {
+    float4 m[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = __ldcg(from + k * kTile);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        o[4 * k] = __float_as_uint(fmaf(f, m[k].x, __uint_as_float(o[4 * k])));
+        o[4 * k + 1] = __float_as_uint(fmaf(f, m[k].y, __uint_as_float(o[4 * k + 1])));
+        o[4 * k + 2] = __float_as_uint(fmaf(f, m[k].z, __uint_as_float(o[4 * k + 2])));
+        o[4 * k + 3] = __float_as_uint(fmaf(f, m[k].w, __uint_as_float(o[4 * k + 3])));
+    }
+}
+
 template <typename T, int HD>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_kernel(const __grid_constant__ AttnOpArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
@@ -332,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *ks = smem + L::Q_ALL, *vs = ks + NK * L::KSLOT;
     __shared__ __align__(8) uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
-    __shared__ __align__(8) uint64_t q_ready, q_free, o_free, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
+    __shared__ __align__(8) uint64_t q_ready, q_free, o_free, run_done, s_full[3], p_ready[3][2], pv_done[3], ends_ready[4], ref_ready[2][4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_fail, s_odd;  // a wait gave up; a node's value is not finite
     __shared__ RangeOf<kThreads> s_range;
@@ -358,6 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::mb_init(&q_ready, 4);
         tc::mb_init(&q_free, 1);
         tc::mb_init(&o_free, 4);
+        tc::mb_init(&run_done, 1);
         for (int i = 0; i < 3; ++i) {
             tc::mb_init(s_full + i, 1);
             tc::mb_init(&p_ready[i][0], 4);
@@ -533,13 +568,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         // V: hd dims (MN) x 16 positions (K) per MMA; 8 positions are 1024 bytes apart, 64 dims a box
         const uint64_t v0 = tc::sdesc(smem_u32(vs)) + ((uint64_t)((L::VBOX >> 4) - 1) << 16);
         unsigned slot = 0, phase = 0, buf = 0, turn = 0;
-        // fp32 rows: every unit's products start from 0, once the last ones have been added to the sums; 16-bit
-        // rows: every segment's, once the last one's are written
+        // every run's products start from 0, once the last one's have been added to the sums or written
         unsigned taken = 0;
         for (unsigned n_seg = 0; ok && segment(n_seg); ++n_seg) {
 #pragma unroll 1
             for (int u = g.u0; u < g.u1 && ok; ++u) {
-                const bool fresh = PARTS == 2 || u == g.u0;
+                const bool fresh = (u - g.u0) % L::RUN == 0;
                 if (fresh && taken++ && !wait(&o_free, taken - 2)) break;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -554,7 +588,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 mma_ts(tmem, p + 32u * (k >> 1) + 16u * h + 8u * (k & 1), v0 + (uint64_t)((slot * L::VSLOT + k * 2048) >> 4), idesc<C>(HD, true),
                                        (!fresh || half || k || h == 0) ? 1u : 0u);
                         commit(v_empty + slot);
-                        if (half) commit(pv_done + buf);
+                        if (half) {
+                            commit(pv_done + buf);
+                            if ((u - g.u0) % L::RUN == L::RUN - 1 || u == g.u1 - 1) commit(&run_done);
+                        }
                     }
                     __syncwarp();
                     if (++slot == NV) slot = 0, phase ^= 1u;
@@ -625,13 +662,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         bool more = segment(0);
         if (more) load_q(g, 0);
-        unsigned j = 0;  // of the segment's first unit
+        unsigned j = 0;       // of the segment's first unit
+        unsigned n_runs = 0;  // (the accumulator is one run's until o_free, so this warp is never a phase behind)
         for (unsigned n_seg = 0; more && ok; ++n_seg) {
             const Seg cur = g;
             const int n = cur.u1 - cur.u0, start = cur.mt * kTile, rows = min(cur.q.n * sh.group - start, kTile);
             const bool active = quarter * 32 < rows, valid = mine32 < rows, whole = cur.u0 == 0 && cur.u1 == cur.n;
-            const unsigned j_last = j + (unsigned)n - 1, buf = j_last % NB, turn = j_last / NB;
-            float ref = -INFINITY;  // fp32 rows: what the sums are relative to
+            const unsigned j_last = j + (unsigned)n - 1;
+            float ref = -INFINITY;  // what the sums of earlier runs are relative to
             float top = 0.f, sum = 0.f;  // what the result is relative to, and the weights' sum
             auto ends = [&] {
                 if (!wait(ends_ready + (n_seg & 3), n_seg >> 2)) return false;
@@ -646,26 +684,29 @@ __global__ void __launch_bounds__(kThreads, 1)
                 more = segment(n_seg + 1);
                 if (more && wait(&q_free, n_seg)) load_q(g, n_seg + 1);
             };
-            if constexpr (PARTS == 2) {
-                // The tensor cores truncate their sums at every step, relative to what the sum is then: over 1000 positions
-                // 3e-6 to 9e-6 of it, over 4000 1e-5 to 4e-5, all of one sign.  So fp32 rows' products are summed over
-                // one unit, and the units here.
-                // (before the products that are still to be added, as scores are up to NB units ahead of them; with
-                // q asked for after all others were added, multiplying stopped for 10 us an item, and for 5 so)
-                const int q_at = max(n - NB, 0);
+            // the segment's place in the workspace (written again by the next segment only if this one is the whole item)
+            const int slot = n_seg ? 1 : 0;
+            float4* const part = a.part + (size_t)(cta * 2 + slot) * (HD / 4) * kTile + mine32;
+            // (q before the products that are still to be added, as scores are up to NB units ahead of them: with fp32 rows' q
+            // asked for after all others were added, multiplying stopped for 10 us an item, and for 5 so; 16-bit rows:
+            // before the last run's, as nothing of an earlier one waits for it)
+            const int runs = (n + L::RUN - 1) / L::RUN, q_at = L::RUN == 1 ? max(n - NB, 0) : runs - 1;
 #pragma unroll 1
-                for (int i = 0; i < n; ++i) {
-                    if (i == q_at) next_q();
-                    const unsigned ju = j + (unsigned)i, tb = ju / NB;
-                    if (i == n - 1 && !ends()) break;
-                    if (!wait(pv_done + (ju - tb * NB), tb)) break;
-                    tc::fence_after();
-                    if (active) {
-                        const float r = *(volatile float*)&s_ref[ju & 3][mine32], f = ref == -INFINITY ? 0.f : ex2(ref - r);
+            for (int i = 0; i < runs; ++i) {
+                if (i == q_at) next_q();
+                const unsigned ju = min(j + (unsigned)((i + 1) * L::RUN) - 1, j_last);
+                if (i == runs - 1 && !ends()) break;
+                if (!wait(&run_done, L::RUN == 1 ? ju : n_runs++)) break;
+                tc::fence_after();
+                if (L::RUN > 1 && runs == 1) break;  // (written from the accumulator)
+                const float r = *(volatile float*)&s_ref[ju & 3][mine32], f = ref == -INFINITY ? 0.f : ex2(ref - r);
+                if (active) {
 #pragma unroll 1
-                        for (int c = 0; c < HD; c += 32) {
-                            uint32_t o[32], m[32];
-                            ld32(tl + c, o);
+                    for (int c = 0; c < HD; c += 32) {
+                        uint32_t o[32];
+                        ld32(tl + c, o);
+                        if constexpr (L::SUMS_IN_TMEM) {
+                            uint32_t m[32];
                             if (i) ld32(tl + L::M0 + c, m);
                             wait_ld();
                             if (i)
@@ -677,21 +718,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                                     o[k + 1] = __float_as_uint(a1);
                                 }
                             st32(tl + L::M0 + c, o);
+                        } else {
+                            wait_ld();
+                            if (i) add_memory(part + c / 4 * kTile, f, o);
+                            if (valid) to_memory(part + c / 4 * kTile, o);
                         }
-                        wait_st();
-                        ref = r;
                     }
-                    tc::fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive(&o_free);
+                    if constexpr (L::SUMS_IN_TMEM) wait_st();
                 }
-            } else {
-                next_q();
-                if (ok && ends()) wait(pv_done + buf, turn);
-                tc::fence_after();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(&o_free);
+                ref = r;
             }
             if (!ok) break;
-            const int slot = n_seg ? 1 : 0;
             if (tid == 12 * 32 && cur.u1 < cur.n) {
                 Cut c;
                 holders(cur, units, ctas, c.first, c.last, c.first_slot);
@@ -722,8 +762,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                 for (int c = 0; c < HD; c += 32) {
                     uint32_t o[32];
-                    ld32(tl + (PARTS == 2 ? L::M0 : 0) + c, o);
-                    wait_ld();
+                    if (L::SUMS_IN_TMEM || runs == 1) {
+                        ld32(tl + (L::RUN == 1 || runs > 1 ? L::M0 : 0) + c, o);
+                        wait_ld();
+                    } else {
+                        from_memory(part + c / 4 * kTile, o);
+                    }
                     if (!valid) continue;
                     if (whole) {
 #pragma unroll
@@ -739,15 +783,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         if (odd) odd_to(c, to, 4);
                     } else {
-                        float4* to = a.part + ((size_t)(cta * 2 + slot) * (HD / 4) + c / 4) * kTile + mine32;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            to[(i / 4) * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+                        float4* to = part + c / 4 * kTile;
+                        to_memory(to, o);
                         if (odd) odd_to(c, reinterpret_cast<float*>(to), 4 * kTile);
                     }
                 }
             }
-            if constexpr (PARTS == 1) {
+            if (L::RUN > 1 && runs == 1) {
                 tc::fence_before();
                 __syncwarp();
                 if (lane == 0) arrive(&o_free);
@@ -832,7 +874,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         r = *(volatile float*)&s_ref[(ju - 1) & 3][mine32];
                         if (__any_sync(0xffffffffu, bm - kShift > r + kSlack)) {
                             const float nr = bm - kShift > r + kSlack ? bm - kShift : r;  // (each row by what it sees alone)
-                            if constexpr (PARTS == 1) {  // the accumulator moves to the new maximum (the other rows of the warp: by a factor of 1)
+                            if (L::RUN > 1 && i % L::RUN) {  // (a run's first unit finds it empty) the accumulator moves to the new maximum (the other rows of the warp: by a factor of 1)
                                 const unsigned tb = (ju - 1) / NB, bb = ju - 1 - NB * tb;
                                 if (!wait(pv_done + bb, tb)) break;
                                 tc::fence_after();
