@@ -164,6 +164,8 @@ int ssd_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* rope, int dty
  * the products as pairs of the cache's type (fp16 22 bits, bf16 16).
  * Measured against 64 bits, values around 1, at any length: fp32 rows 1e-6; 16-bit rows what rounding the exact result to the type
  * costs, and up to 4e-5 of the result more (tensor cores sum up to 3072 positions and cut off what their sums do not hold).
+ * A wait inside the call that has not ended after two seconds gives up (SSD_STATUS_TIMEOUT): the call ends, and
+ * without `status` no one can tell that its output is not valid.
  * workspace: ssd_tree_attention_workspace() bytes, 16-byte aligned; its contents
  * mean nothing between calls.  The same inputs give the same bits; the order of
  * sums depends on the whole batch's lengths.
@@ -176,6 +178,11 @@ int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache, int layer
 /* Bytes of workspace for a cache of this head_dim on the current device, whatever the batch.
  * Errors: INVALID_ARG, CUDA. */
 int ssd_tree_attention_workspace(int head_dim, size_t* bytes);
+
+/* Test hook for the bounded waits of ssd_tree_attention: in the next call of the process whose tiles have
+ * more than two rows, CTA `cta` never asks for its keys, and waits give up after wait_limit_s (0 < wait_limit_s <= 10; else 2 s).  The call ends with
+ * SSD_STATUS_TIMEOUT, its output is not valid, and the calls after it are not affected.  cta < 0 disarms. */
+void ssd_debug_tree_stall(int cta, double wait_limit_s);
 
 /* The end of a round.  tokens[row]: the drafted token of each node (that of a root,
  * node 0, is the last token of the sequence, which no cache row holds yet);

@@ -30,7 +30,7 @@ EXPORTS = ("ssd_create", "ssd_set_skip", "ssd_set_sampling", "ssd_set_draft_exit
            "ssd_debug_forward", "ssd_debug_spec_accept", "ssd_debug_time_forward", "ssd_destroy",
            "ssd_last_error", "ssd_linear_noalloc", "ssd_debug_trace_forward", "ssd_debug_stall_barrier")
 
-# every symbol include/ssd_ops.h declares
+# the operators that include/ssd_ops.h declares (and ssd_debug_tree_stall)
 OPERATOR_EXPORTS = ("ssd_tree_plan", "ssd_rope_init", "ssd_rope_kv", "ssd_tree_attention",
                     "ssd_tree_attention_workspace", "ssd_tree_commit")
 SSD_F32, SSD_F16, SSD_BF16 = 0, 1, 2
@@ -120,6 +120,7 @@ def _load():
     lib.ssd_tree_attention.argtypes = [BP, PP, I, I, I, _VP, L, _VP, I, ctypes.c_float, _VP, L, _VP, ctypes.c_size_t, _VP, _VP]
     lib.ssd_tree_attention_workspace.argtypes = [I, ctypes.POINTER(ctypes.c_size_t)]
     lib.ssd_tree_commit.argtypes = [BP, PP] + [_VP] * 9
+    lib.ssd_debug_tree_stall.argtypes, lib.ssd_debug_tree_stall.restype = [I, ctypes.c_double], None
     for n in OPERATOR_EXPORTS:
         getattr(lib, n).restype = ctypes.c_int
     lib.ssd_destroy.argtypes = [H]
@@ -390,7 +391,8 @@ def ssd_tree_attention_workspace(cache: PagedKV) -> int:
 def ssd_tree_attention(batch: TreeBatch, cache: PagedKV, layer: int, q, masks, scale: float, out, workspace, status=None,
                        cuda_stream: int | None = None) -> None:
     """out [n_rows][heads][hd] = attention of q over the requests' cached positions and the nodes that masks
-    int64 [n_rows][words] show (None: chains).  workspace: a contiguous uint8 tensor."""
+    int64 [n_rows][words] show (None: chains).  workspace: a contiguous uint8 tensor.  What only the device can see (a table that is
+    too narrow, a wait that gave up and left an output that is not valid) is told by status int32 [1] alone, set to 0 before."""
     kind, d, t, n, h, hd = _row_type(q, "q"), cache.device, q.dtype, batch.n_rows, q.shape[1], cache.head_dim
     if batch.device != d:
         _refuse("the batch and the cache are on different devices")
@@ -400,6 +402,14 @@ def ssd_tree_attention(batch: TreeBatch, cache: PagedKV, layer: int, q, masks, s
                                   *_rows(out, "out", d, t, n, h, hd),
                                   _dev(workspace, "workspace", _of_type(workspace, "workspace", "torch.uint8"), d, workspace.numel()),
                                   workspace.numel(), _dev(status, "status", batch.i32, d, 1), cuda_stream))
+
+
+def ssd_debug_tree_stall(cta: int, wait_limit_s: float = 0.01) -> None:
+    """Test hook: a CTA of the next ssd_tree_attention call (tiles of more than two rows) never asks for its keys, so its waits
+    give up after wait_limit_s."""
+    if cta >= 0 and not 0.0 < wait_limit_s <= 10.0:
+        _refuse("ssd_debug_tree_stall: 0 < wait_limit_s <= 10 is wanted")
+    lib.ssd_debug_tree_stall(cta, wait_limit_s)
 
 
 def ssd_tree_commit(batch: TreeBatch, cache: PagedKV | None, parents, tokens, target, accepted, next_token, lens_out, path,

@@ -74,7 +74,7 @@ namespace tree {
 namespace {
 
 constexpr float kSlack = 8.f, kShift = 6.f;  // weights up to 2^14: finite in fp16
-constexpr long long kWaitClocks = 4000000000ll;  // 2 s at 2 GHz
+constexpr double kWaitSeconds = 2.0, kClocksPerSecond = 2e9;
 constexpr int kThreads = 512;
 constexpr int kTmem = 512;  // columns (Lay)
 constexpr int kMaxSlots = 12, kSegs = 32;
@@ -169,29 +169,29 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// bounded wait; false after kWaitClocks, or once another thread of the CTA has given up
-__device__ __noinline__ bool mb_wait_on(uint64_t* b, unsigned parity, volatile int* fail) {
+// bounded wait; false after `limit` clocks, or once another thread of the CTA has given up
+__device__ __noinline__ bool mb_wait_on(uint64_t* b, unsigned parity, volatile int* fail, long long limit) {
     const long long t0 = clock64();
 #pragma unroll 1
     while (!tc::mb_try(b, parity)) {
         if (*fail) return false;
-        if (clock64() - t0 > kWaitClocks) {
+        if (clock64() - t0 > limit) {
             *fail = 1;
             return false;
         }
     }
     return true;
 }
-__device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail) {
-    return tc::mb_try(b, parity) || mb_wait_on(b, parity, fail);
+__device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail, long long limit) {
+    return tc::mb_try(b, parity) || mb_wait_on(b, parity, fail, limit);
 }
 
-__device__ __noinline__ bool known_wait(volatile int* known, int i, volatile int* fail) {
+__device__ __noinline__ bool known_wait(volatile int* known, int i, volatile int* fail, long long limit) {
     const long long t0 = clock64();
 #pragma unroll 1
     while (*known <= i) {
         if (*fail) return false;
-        if (clock64() - t0 > kWaitClocks) {
+        if (clock64() - t0 > limit) {
             *fail = 1;
             return false;
         }
@@ -426,13 +426,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     Seg g;
     bool ok = true;
     auto wait = [&](uint64_t* b, unsigned phase) {
-        ok = ok && __all_sync(0xffffffffu, mb_wait(b, phase & 1u, &s_fail));
+        ok = ok && __all_sync(0xffffffffu, mb_wait(b, phase & 1u, &s_fail, a.wait_clocks));
         return ok;
     };
 
     // segment i to g, if there is one
     auto segment = [&](unsigned i) {
-        ok = ok && __all_sync(0xffffffffu, *(volatile int*)&s_known > (int)i || known_wait(&s_known, (int)i, &s_fail));
+        ok = ok && __all_sync(0xffffffffu, *(volatile int*)&s_known > (int)i || known_wait(&s_known, (int)i, &s_fail, a.wait_clocks));
         __threadfence_block();
         g = s_seg[i % kSegs];
         return ok && g.n > 0;
@@ -472,6 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     __syncwarp();
                 }
             if (!segment(n_seg)) break;
+            if (!is_v && cta == a.stall) break;  // (ssd_debug_tree_stall)
             const int32_t* table = a.block_table + (size_t)g.b * sh.max_blocks;
             auto fetch = [&](long long x) {  // page of this lane's copy of the 32 from x on; -1: outside, reads as zeros
                 x += lane << a.box_shift;
@@ -1055,6 +1056,9 @@ constexpr int kMaxDevices = 64;
 AttnDevice g_attn_dev[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 std::mutex g_attn_mu;
+// ssd_debug_tree_stall, for one call (guarded by g_attn_mu)
+int g_stall = -1;
+double g_stall_wait_s = 0.0;
 
 template <typename T>
 cudaError_t set_up_type() {
@@ -1134,6 +1138,12 @@ int run(const char* call, AttnOpArgs& a, int dtype, int hd, const CUtensorMap& k
 using namespace ssd;
 using namespace ssd::tree;
 
+extern "C" void ssd_debug_tree_stall(int cta, double wait_limit_s) {
+    std::lock_guard<std::mutex> lock(g_attn_mu);
+    g_stall = cta >= 0 && wait_limit_s > 0.0 && wait_limit_s <= 10.0 ? cta : -1;
+    g_stall_wait_s = wait_limit_s;
+}
+
 extern "C" int ssd_tree_attention_workspace(int head_dim, size_t* bytes) {
     static const char call[] = "ssd_tree_attention_workspace";
     if (!bytes) return refuse_arg(call, "NULL pointer");
@@ -1196,6 +1206,8 @@ extern "C" int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache
     a.pos_stride = cache->pos_stride;
     a.n_heads = n_heads;
     a.n_pages = cache->n_pages;
+    a.stall = -1;
+    a.wait_clocks = (long long)(kWaitSeconds * kClocksPerSecond);
     a.box_shift = cache->page_size % 64 == 0 ? 6 : cache->page_size % 32 == 0 ? 5 : 4;
     a.scale2 = (float)(1.4426950408889634 * scale);
     a.status = status;
@@ -1210,6 +1222,12 @@ extern "C" int ssd_tree_attention(const ssd_batch* batch, const ssd_pages* cache
     if (a.tile > kFewRows) {
         if (int rc = encode(call, &k, a.kc, cache, a)) return rc;
         if (int rc = encode(call, &v, a.vc, cache, a)) return rc;
+        std::lock_guard<std::mutex> lock(g_attn_mu);
+        if (g_stall >= 0) {
+            a.stall = g_stall;
+            a.wait_clocks = (long long)(g_stall_wait_s * kClocksPerSecond);
+            g_stall = -1;
+        }
     }
     const int hd = cache->head_dim;
     if (dtype == SSD_F32) return run<float>(call, a, dtype, hd, k, v, cuda_stream);

@@ -40,6 +40,8 @@ struct AttnOpArgs {
     float* stats;  // [grid][2][2][kTile]: maximum, sum
     float4* part;  // [grid][2][HD / 4][kTile]
     int32_t* status;
+    long long wait_clocks;  // after which a wait gives up
+    int stall;              // a CTA that asks for no keys, so that waits of it give up; -1: none
 };
 
 // of the rows' type: the cache's, and how many of those hold a value of q on the tensor cores

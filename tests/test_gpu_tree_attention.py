@@ -486,6 +486,38 @@ def test_offsets_beyond_32_bits(ssd, heads, kv, rows):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cta", [0, 7, 151])
+def test_a_wait_that_gives_up(ssd, kind, cta):
+    """A CTA whose keys never come: its waits end after their limit, the call ends and says so, rows of requests that it has no part in are as ever, and so
+    are the calls after it."""
+    c = Case(np.random.default_rng(70), kind, 8, 4, 128, 16, [700] * 60, [9] * 60)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.full((ssd.ssd_tree_attention_workspace(ssd.PagedKV(c.k, c.v)),), 255, dtype=torch.uint8, device="cuda")
+    want = c.run(ssd, status=status, workspace=ws)
+    assert int(status) == 0
+    ssd.ssd_debug_tree_stall(cta, 0.01)
+    out = c.run(ssd, status=status)  # (with a workspace of its own, without an older call's parts)
+    assert int(status) == ssd.SSD_STATUS_TIMEOUT
+    same = (out == want).flatten(1).all(1)[:int(c.row_start[-1])].view(60, 9).all(1)
+    assert 50 <= int(same.sum()) < 60  # (a CTA has 240 items of six units and three more / 152 of them)
+    status.zero_()
+    assert torch.equal(c.run(ssd, status=status, workspace=ws), want) and int(status) == 0
+    ssd.ssd_debug_tree_stall(cta, 0.01)
+    ssd.ssd_debug_tree_stall(-1)
+    assert torch.equal(c.run(ssd, status=status, workspace=ws), want) and int(status) == 0
+
+
+def test_tiles_of_few_rows_have_no_waits(ssd):
+    """Such a call does not stall."""
+    few = Case(np.random.default_rng(71), "f16", 4, 4, 64, 16, [300], [1], None)
+    ssd.ssd_debug_tree_stall(0, 0.01)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    few.check(few.run(ssd, status=status))
+    assert int(status) == 0
+    ssd.ssd_debug_tree_stall(-1)
+
+
 # -- a round of all of them ---------------------------------------------------
 
 @pytest.mark.parametrize("kind,heads,kv,hd,page,tree", [("f32", 4, 2, 64, 16, True), ("f16", 8, 1, 128, 48, True), ("bf16", 4, 4, 64, 16, False)])

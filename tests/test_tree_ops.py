@@ -192,3 +192,10 @@ def test_reference_plan_is_consistent():
     assert (got["slots"][3:20] == -1).all() and got["status"] == 1  # two pages more: none is left after request 0's and 3 has to wait
     assert got["ends"].tolist() == [2, 5] and got["ring"][3:5].tolist() == [2, 6]
     assert got["held"].tolist() == [2, 0, 2, 1] and got["slots"][20] == -1
+
+
+def test_stalls_without_a_limit_are_refused(ssd):
+    for bad in (0.0, -1.0, 11.0, math.nan):
+        with pytest.raises(ssd.SSDError):
+            ssd.ssd_debug_tree_stall(0, bad)
+    ssd.ssd_debug_tree_stall(-1)
