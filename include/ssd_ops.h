@@ -48,7 +48,7 @@ typedef enum { SSD_F32 = 0, SSD_F16 = 1, SSD_BF16 = 2 } ssd_dtype;
 /* Bits of a status word (device int32, set by the caller to 0; may be NULL). */
 #define SSD_STATUS_PAGES 1   /* ssd_tree_plan: too few free pages; some requests got none */
 #define SSD_STATUS_TABLE 2   /* a request is longer than its row of the block table */
-#define SSD_STATUS_PARENT 4  /* a parent is not an earlier node of the same tree */
+#define SSD_STATUS_PARENT 4  /* a parent is not an earlier node of the same tree, or a tree has more nodes than its masks have bits */
 #define SSD_STATUS_TIMEOUT 8 /* ssd_tree_attention: a bounded wait gave up; its output is not valid */
 
 /* A paged KV cache.  Element (layer, page, kv_head, position in the page, dim)
@@ -151,7 +151,8 @@ int ssd_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* rope, int dty
  *   out[row][h] = sum_x w_x V[x][g] / sum_x w_x,  w_x = exp(scale q[row][h] . K[x][g] - max),  g = h n_kv_heads / n_heads,
  * over the positions x that the row sees: the lens[b] cached ones and, of its own
  * round's rows (which ssd_rope_kv has put at lens[b] + j), node j if bit j of masks[row] is set,
- * or, with masks = NULL, nodes 0 .. i of a chain.  Nodes from 64 * mask_words on are not seen.
+ * or, with masks = NULL, nodes 0 .. i of a chain.  Nodes from 64 * mask_words on are not seen
+ * (SSD_STATUS_PARENT).
  * A row that sees nothing, or whose scores are all -inf, gets zeros.  What a row does
  * not see does not change its output, be it NaN; an infinite value that it sees comes out as
  * infinity or NaN.  Positions that max_blocks pages do not hold are
@@ -195,7 +196,8 @@ void ssd_debug_tree_stall(int cta, double wait_limit_s);
  *   emitted[row_start[b] + j] = token of step j + 1, j < n, and next_token at j = n;
  * and in every layer the keys and values at lens[b] + path[j] move to lens[b] + j.
  * A request without rows, or with lens[b] < 0, gets accepted = -1, next_token = -1,
- * lens_out = lens.  Trees have up to 256 nodes (further ones are not looked at); a
+ * lens_out = lens.  The walk goes over the first 256 nodes of a request: a path ends
+ * there at the latest, with what the target chose after its last node, so what is accepted is still the target's own text.  A
  * child has a higher index than its parent (others are not reached); parents = NULL: chains.
  * cache = NULL: tokens only, nothing moves.
  * Errors: INVALID_ARG, CUDA. */

@@ -109,6 +109,7 @@ __device__ __forceinline__ long long range_of(const AttnOpArgs& a, int tile, Ran
     for (int b = b0; b < b1; ++b) {
         last = req_of(sh, b);
         if (last.clipped && last.n && blockIdx.x == 0) say(a.status, SSD_STATUS_TABLE);
+        if (!sh.chain && last.n > 64 * a.words && blockIdx.x == 0) say(a.status, SSD_STATUS_PARENT);
         head = head_units(sh, last, tile);
         mine += head * sh.n_kv_heads;
     }

@@ -320,6 +320,20 @@ def test_table_too_narrow(ssd):
         assert int(status) == ssd.SSD_STATUS_TABLE
 
 
+@pytest.mark.parametrize("heads,kv,said", [(8, 2, 70), (2, 2, 1), (4, 2, 1)])
+@pytest.mark.parametrize("words", [1, 2])
+def test_more_nodes_than_mask_bits(ssd, heads, kv, said, words):
+    """Nodes behind the masks' bits are seen by no row, and the call says so; one that has ended does
+    not count."""
+    n = 64 * words
+    for lens, counts, bits in (([40, 9, -1], [3, n + 6, 0], 4), ([40, 9, -1], [3, n, n + 9], 0)):
+        c = Case(np.random.default_rng(72), "f16", heads, kv, 64, 16, lens, counts, words=words)
+        c.max_rows = said
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        c.check(c.run(ssd, status=status))
+        assert int(status) == bits == (ssd.SSD_STATUS_PARENT if bits else 0)
+
+
 def test_broken_row_starts_stay_inside(ssd):
     for rows in (2, 60):
         c = Case(np.random.default_rng(7), "f16", 4, 2, 64, 16, [60, 20], [rows, rows], extra_rows=0)
