@@ -280,6 +280,8 @@ def _rows(t, what: str, device: int, dtype, n_rows: int, heads: int, hd: int):
     shape, stride = t.shape, t.stride()
     if shape != (n_rows, heads, hd) or t.dtype is not dtype or t.get_device() != device:
         _refuse(f"{what}: {dtype} of shape ({n_rows}, {heads}, {hd}) on CUDA device {device} is wanted, got {t.dtype}, {tuple(shape)} on {t.device}")
+    if n_rows == 0:  # (strides of no rows mean nothing)
+        return None, heads * hd
     if stride[2] != 1 or (stride[1] != hd and heads > 1):
         _refuse(f"{what}: the heads of a row must lie behind one another")
     return t.data_ptr(), stride[0] if n_rows > 1 else heads * hd
@@ -358,7 +360,7 @@ def ssd_tree_plan(batch: TreeBatch, page_size: int, n_pages: int, parents, held,
 def _words(masks) -> int:
     if masks is None:
         return 0
-    if masks.dim() != 2:
+    if masks.dim() != 2 or masks.shape[1] == 0:
         _refuse("masks: [row][word] is wanted")
     return masks.shape[1]
 
@@ -396,6 +398,8 @@ def ssd_tree_attention(batch: TreeBatch, cache: PagedKV, layer: int, q, masks, s
     kind, d, t, n, h, hd = _row_type(q, "q"), cache.device, q.dtype, batch.n_rows, q.shape[1], cache.head_dim
     if batch.device != d:
         _refuse("the batch and the cache are on different devices")
+    if n == 0:
+        masks = None
     words = _words(masks)
     _check(lib.ssd_tree_attention(batch.struct, cache.struct, layer, kind, h, *_rows(q, "q", d, t, n, h, hd),
                                   _dev(masks, "masks", _of_type(masks, "masks", "torch.int64"), d, n * words), words, scale,

@@ -440,6 +440,23 @@ def test_captured_single_tokens(ssd, kind, heads, kv):
         c.check(out)
 
 
+def test_empty_rounds_and_empty_masks(ssd):
+    """A round without rows is a call that does nothing, with masks as without; masks of no words are refused, not taken for none."""
+    c = Case(np.random.default_rng(73), "f16", 4, 2, 64, 16, [9, 30], [0, 0], extra_rows=0)
+    c.max_rows = 1
+    assert c.masks.shape == (0, 1)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert c.run(ssd, status=status).shape == (0, 4, 64)
+    c.masks = None
+    c.run(ssd, status=status)
+    c = Case(np.random.default_rng(74), "f16", 4, 2, 64, 16, [9, 30], [3, 2])
+    c.masks = c.masks[:, :0]
+    with pytest.raises(ssd.SSDError):
+        c.run(ssd, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+
+
 def test_tensors_elsewhere_are_refused(ssd):
     c = Case(np.random.default_rng(12), "f32", 2, 2, 64, 16, [9], [2])
     c.q = c.q.cpu()

@@ -224,6 +224,14 @@ def test_rope(ssd, kind, n, heads, kv, hd, rot, inter, page, scaling, far):
     assert kc.isnan().all() and vc.isnan().all()
 
 
+def test_rope_of_no_rows(ssd):
+    kc, vc = (torch.full((1, 1, 2, 16, 64), 3.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    for q, k, v in (([torch.empty(0, h, 64, device="cuda") for h in (4, 2, 2)]), [torch.empty(5, h, 64, device="cuda").transpose(0, 1)[:, :0].transpose(0, 1) for h in (4, 2, 2)]):
+        none = torch.empty(0, dtype=torch.int32, device="cuda")
+        ssd.ssd_rope_kv(ssd.PagedKV(kc, vc), 0, ssd.ssd_rope_init(64), q, k, v, none, none, torch.empty_like(q), torch.cuda.current_stream().cuda_stream)
+    assert (kc == 3).all() and (vc == 3).all()
+
+
 def test_rope_in_place_and_repeated_slots(ssd):
     """q_out in q's place; two rows with one slot: the cache holds one of them."""
     t = torch.float32
