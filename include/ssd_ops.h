@@ -191,7 +191,7 @@ void ssd_debug_tree_stall(int cta, double wait_limit_s);
  * sample).  From node 0 the path goes to the lowest child whose token is the
  * node's target, until there is none: n nodes accepted.  For request b:
  *   accepted[b] = n;  next_token[b] = target of the last node on the path;
- *   lens_out[b] = lens[b] + 1 + n (an array of its own);
+ *   lens_out[b] = lens[b] + 1 + n;
  *   path[row_start[b] + j] = node at step j = 0 .. n (path[row_start[b]] = 0);
  *   emitted[row_start[b] + j] = token of step j + 1, j < n, and next_token at j = n;
  * and in every layer the keys and values at lens[b] + path[j] move to lens[b] + j.
@@ -199,7 +199,7 @@ void ssd_debug_tree_stall(int cta, double wait_limit_s);
  * lens_out = lens.  The walk goes over the first 256 nodes of a request: a path ends
  * there at the latest, with what the target chose after its last node, so what is accepted is still the target's own text.  A
  * child has a higher index than its parent (others are not reached); parents = NULL: chains.
- * cache = NULL: tokens only, nothing moves.
+ * cache = NULL: tokens only, nothing moves.  The results are arrays of their own: none overlaps another or an input.
  * Errors: INVALID_ARG, CUDA. */
 int ssd_tree_commit(const ssd_batch* batch, const ssd_pages* cache, const int32_t* parents, const int32_t* tokens,
                     const int32_t* target, int32_t* accepted, int32_t* next_token, int32_t* lens_out, int32_t* path,

@@ -607,7 +607,15 @@ extern "C" int ssd_tree_commit(const ssd_batch* batch, const ssd_pages* cache, c
         if (int rc = check_pages(call, cache)) return rc;
     if (!accepted || !next_token || !lens_out) return refuse_arg(call, "NULL pointer");
     if (batch->n_rows > 0 && (!tokens || !target || !path || !emitted)) return refuse_arg(call, "NULL pointer");
-    if (lens_out == batch->lens) return refuse_arg(call, "lens_out must be an array of its own");
+    // (a request's CTAs each walk the path from what they read, while one of them writes the results)
+    const void* const in[] = {batch->row_start, batch->lens, batch->block_table, parents, tokens, target};
+    const void* const out[] = {accepted, next_token, lens_out, path, emitted};
+    for (int i = 0; i < 5; ++i) {
+        for (const void* p : in)
+            if (out[i] && out[i] == p) return refuse_arg(call, "the results must be arrays of their own");
+        for (int j = 0; j < i; ++j)
+            if (out[i] && out[i] == out[j]) return refuse_arg(call, "the results must be arrays of their own");
+    }
     if (int rc = check_device(call, batch->lens)) return rc;
     CommitArgs a{};
     a.n_rows = batch->n_rows;

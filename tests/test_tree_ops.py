@@ -199,3 +199,16 @@ def test_stalls_without_a_limit_are_refused(ssd):
         with pytest.raises(ssd.SSDError):
             ssd.ssd_debug_tree_stall(0, bad)
     ssd.ssd_debug_tree_stall(-1)
+
+
+def test_commit_refuses_results_in_the_place_of_inputs(ssd):
+    """Every result in every input's place, and in each other's; with arrays of their own the call gets as far as the device."""
+    own = {n: (i + 10) * P for i, n in enumerate(("parents", "tokens", "target", "acc", "nxt", "lens_out", "path", "emitted"))}
+    b = batch(ssd, row_start=P, lens=2 * P, block_table=3 * P)
+    assert commit(ssd, bt=b, **own) != ssd.SSD_OK and "arrays of their own" not in ssd.ssd_last_error()
+    results = ("acc", "nxt", "lens_out", "path", "emitted")
+    for r in results:
+        for at in (P, 2 * P, 3 * P, *(own[x] for x in own if x != r)):
+            refused(ssd, commit(ssd, bt=b, **{**own, r: at}), "ssd_tree_commit")
+            assert "arrays of their own" in ssd.ssd_last_error()
+    assert "arrays of their own" not in (commit(ssd, bt=b, **{**own, "parents": None}), ssd.ssd_last_error())[1]
