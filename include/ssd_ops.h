@@ -91,6 +91,10 @@ typedef struct {
  *     all it needs and those after it that need any get nothing (SSD_STATUS_PAGES); a request that
  *     needs more than max_blocks gets nothing and the others go on
  *     (SSD_STATUS_TABLE).  A request never gives pages back while it runs.
+ *     A request that got nothing has no place for this round's rows: they are not written (slots of -1), its attention is not
+ *     valid, and the caller keeps lens[b] and leaves its commit's results.  ssd_tree_attention and ssd_tree_commit go by block_table
+ *     alone, so entries behind the pages that a request holds must be -1 (or outside [0, n_pages)) for them not to
+ *     read, and move rows in, pages of others: this call leaves those entries as they are, of ended requests too.
  *   - One with lens[b] < 0 gives its pages back: they are appended to the queue,
  *     requests in order, and can be taken from the next call on.
  *   - held_out and ends_out get the new counts (arrays of their own: held and

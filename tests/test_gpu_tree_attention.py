@@ -549,6 +549,44 @@ def test_tiles_of_few_rows_have_no_waits(ssd):
     ssd.ssd_debug_tree_stall(-1)
 
 
+def test_a_request_without_pages_touches_no_others(ssd):
+    """One of two requests gets no page for its round's rows.  With -1 behind the pages that it holds, the rest of the round reads and
+    moves nothing of anyone else's, and the other request's round is as it would be alone."""
+    rng = np.random.default_rng(75)
+    page, n_pages, kv, hd, n = 16, 6, 2, 64, 7
+    table, lens = np.array([[3, -1, -1], [0, -1, -1]], np.int32), np.array([12, 14], np.int32)
+    parents = np.tile(np.array([-1, 0, 0, 0, 0, 0, 5], np.int32), 2)  # accepted: nodes 5 and 6, which lie in a second page
+    tokens, target = np.tile(np.arange(n, dtype=np.int32), 2), np.full(2 * n, 99, np.int32)
+    target[[0, n]], target[[5, n + 5]] = 5, 6
+    kc, vc = (torch.from_numpy(rng.standard_normal((1, n_pages, kv, page, hd)).astype(np.float32)).cuda().half() for _ in range(2))
+    before = kc.clone(), vc.clone()
+    cache, ring, ends, held = ssd.PagedKV(kc, vc), dev(np.array([5, 1, 2, 4, -9, -9], np.int32)), torch.tensor([0, 1], device="cuda"), dev(np.array([1, 1], np.int32))
+    tb, rows = dev(table), dev(np.array([0, n, 2 * n], np.int32))
+    bt = ssd.TreeBatch(rows, dev(lens), tb, 2 * n, n)
+    held2, ends2, slots, pos, masks, status = ints(2), torch.zeros_like(ends), ints(2 * n), ints(2 * n), torch.zeros(2 * n, 1, dtype=torch.int64, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    ssd.ssd_tree_plan(bt, page, n_pages, dev(parents), held, held2, ring, ends, ends2, slots, pos, masks, status, s)
+    assert int(status) == ssd.SSD_STATUS_PAGES and tb.cpu().tolist() == [[3, 5, -1], [0, -1, -1]] and (slots[n:] == -1).all()
+    q, k, v = (torch.randn(2 * n, h, hd, device="cuda").half() for h in (4, kv, kv))
+    ssd.ssd_rope_kv(cache, 0, ssd.ssd_rope_init(hd), q, k, v, pos, slots, q, s)
+    out, ws = torch.full_like(q, 77.0), torch.empty(ssd.ssd_tree_attention_workspace(cache), dtype=torch.uint8, device="cuda")
+    ssd.ssd_tree_attention(bt, cache, 0, q, masks, 0.125, out, ws, status, s)
+    got = [ints(2), ints(2), ints(2), ints(2 * n), ints(2 * n)]
+    written = kc.clone(), vc.clone()
+    ssd.ssd_tree_commit(bt, cache, dev(parents), dev(tokens), dev(target), *got, s)
+    torch.cuda.synchronize()
+    assert got[0].cpu().tolist() == [2, 2] and int(got[2][0]) == 15
+    for t, w, b in zip((kc, vc), written, before):
+        assert torch.equal(t[:, [0, 1, 2, 4]], b[:, [0, 1, 2, 4]])  # the held page of request 1 and those of no one
+        assert torch.equal(t[0, 3, :, 13], w[0, 5, :, 1]) and torch.equal(t[0, 3, :, 14], w[0, 5, :, 2])
+    alone = ssd.TreeBatch(rows[:2].clone(), dev(lens[:1]), tb[:1].clone(), n, n)
+    kc.copy_(written[0])
+    vc.copy_(written[1])
+    first = torch.empty_like(out[:n])
+    ssd.ssd_tree_attention(alone, cache, 0, q[:n], masks[:n].clone(), 0.125, first, ws, status, s)
+    assert torch.equal(first, out[:n])
+
+
 # -- a round of all of them ---------------------------------------------------
 
 @pytest.mark.parametrize("kind,heads,kv,hd,page,tree", [("f32", 4, 2, 64, 16, True), ("f16", 8, 1, 128, 48, True), ("bf16", 4, 4, 64, 16, False)])
