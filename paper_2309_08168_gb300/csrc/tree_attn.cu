@@ -4,10 +4,10 @@
 //   o = sum_x w_x v_x / sum_x w_x,  w_x = 2^(s_x - m),  s_x = log2(e) scale q . k_x
 //
 // over the positions x that a row sees, m a running maximum.  All query heads
-// that share a KV head, and all nodes of the request's tree, are rows of one
-// tile, so K and V are read once for all of them: with R rows a position costs
-// 4 hd bytes and 4 hd R flops.  Up to some 250 rows the bound is HBM, beyond it the
-// tensor cores and the exponentials.
+// that share a KV head, and all nodes of the request's tree, are rows of tiles
+// of 128, each of which reads K and V once: with R rows of a tile a position costs
+// 4 hd bytes and 4 hd R flops.  Up to one tile a request the bound is HBM; further tiles
+// find K and V in L2.
 //
 // A CTA (one per SM) walks its range of units (tree_sched.cuh), 128 positions at a time:
 //   warps 8, 9 : TMA producers of K and of V, a lane per copy of 16 to 64 rows of a page,
@@ -30,13 +30,20 @@
 // items in shared memory, were no faster); two rows or less are few_kernel's (tree_few.cu).
 //
 // Measured, with join_kernel (copy rate 6.79 TB/s, tensor cores 1.92 PFLOP/s):
-//   9 nodes, 8 heads a KV head, 100001 positions, fp16: 72 us, 5.7 TB/s - HBM;
-//   6 trees of 33 nodes, 8 heads a KV head, 4096 positions, bf16: 32 us, 2.1 TB/s - 8 us until the
-//     first unit's scores, then 1.0 us a unit (S, softmax, P V of a buffer one after the other), join 5;
-//   2048 rows over 4000 positions, 8 heads a KV head, bf16: 315 us, 1.07 PFLOP/s - the exponentials;
-//   2 x 1023 rows over 700 positions, 40 heads, fp32: 134 us, 0.35 PFLOP/s counted once, 0.7 done
+//   9 nodes, 8 heads a KV head, 100001 positions, fp16: 78 us, 5.2 TB/s - HBM, and the gap where a run of
+//     units ends (below);
+//   6 trees of 33 nodes, 8 heads a KV head, 4096 positions, bf16: 36 us, 1.9 TB/s - 8 us until the
+//     first unit's scores, then 1.4 us a unit (S, softmax, P V of a buffer one after the other), join 5;
+//   2048 rows over 4000 positions, 8 heads a KV head, bf16: 382 us, 0.88 PFLOP/s counted once, 1.3 done (P V in two
+//     passes) - 1.4 us a unit: no part is busy all of the time (tensor pipe 59 % of the cycles, L2 31 % of its rate,
+//     issue slots 50 %).  By clock stamps a softmax group waits for scores for 54 % of its unit, computes
+//     weights for 31 %, the maximum for 9 % and waits for the reference for 6 %; the warp of P V waits for weights for a tenth
+//     of the time and for V for a third, with three units of V in the ring as with two;
+//   2 x 1023 rows over 700 positions, 40 heads, fp32: 135 us, 0.35 PFLOP/s counted once, 0.7 done
 //     (two passes each) - 1.9 us a unit, as its product and the sum of the one before take turns at the
-//     accumulator, and 7 us an item until its q, which has one buffer, is there as pairs.
+//     accumulator, and 7 us an item until its q, which has one buffer, is there as pairs;
+//   32 trees of 9 nodes, 32 heads, 90 to 270 positions: fp16 56 us, fp32 68, for 13 us of bytes - the hand-offs at the
+//     ends of 1024 items of two or three units.
 //
 // O is rescaled only when a row's maximum has grown by more than kSlack (log2)
 // over the one its weights are relative to (the running softmax of Milakov and
@@ -97,8 +104,8 @@ struct Lay {
     static constexpr int QBOX = kTile * 128;          // 64 dims of the tile's q
     static constexpr int Q_ALL = PARTS * BOXES * QBOX;
     // Slots.  The scores wait for K more often than the products for V, which is asked for at the same time and
-    // needed later: K takes 13 / 20 of the rings (9 / 20: tree of 33 nodes 33.0 us against 32.2, long request
-    // 73.5 against 71.9), but leaves two units of V (softmax: half_done).
+    // needed later: K takes 13 / 20 of the rings (10 and 11 / 20: the same within 1 %; 9 / 20: 2 % slower), but leaves two
+    // units of V (softmax: half_done).
     static constexpr int ROOM = RING - Q_ALL, MOST_K = (ROOM - 4 * VSLOT) / KSLOT, SHARE = ROOM * 13 / 20 / KSLOT;
     static constexpr int least(int a, int b) { return a < b ? a : b; }
     static constexpr unsigned NK = least(least(SHARE, MOST_K), kMaxSlots), NV = least((ROOM - (int)NK * KSLOT) / VSLOT, kMaxSlots);

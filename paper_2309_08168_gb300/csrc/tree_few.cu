@@ -17,9 +17,9 @@
 //
 // Measured (with join_kernel), against the tensor cores' kernel: single tokens of 16
 // requests, 262 to 2100 positions, 32 heads of 128 dims, fp32 64 us (5.5 TB/s, 81 % of the copy rate)
-// against 88, fp16 64 against 71; two heads a KV head 70.5 against 89 and 70.2 against 70.8; head_dim 64, 32 requests 70
-// against 100; one request of 4000 positions 22 against 30, of 200 9.8 against 16.  Four rows a tile:
-// 96 against 90 (fp32) and 69 (fp16) then, as the arithmetic of a block then takes as long as its loads; so
+// against 88, fp16 64 against 77; two heads a KV head 71 against 88 and 71 against 77; head_dim 64, 32 requests 69
+// against 99 (fp16) and 136 (fp32); one request of 4000 positions 17 against 27, of 200 9.6 against 16.  Four rows a tile:
+// 96 against 88 (fp32) and 74 (fp16), as the arithmetic of a block then takes as long as its loads; so
 // two rows are the most.  What is left: 7 us until the first block is there, 3 to join, uneven blocks.
 #include "tree_attn.cuh"
 

@@ -52,8 +52,8 @@ __device__ __forceinline__ Want want_of(const PlanArgs& a, int b, const Rows& ro
 // rows' parents are on their way; masks and depths of a tree come from pointer
 // doubling: after step s a node knows its ancestors up to 2^s levels above.
 // 128 threads, so that a thousand requests run at once: with 256, and a scan over
-// all requests in every CTA, 1000 trees of 33 to 64 nodes took 19.0 us; now 11.2 (0.9 MB, 0.08 TB/s), one
-// tree of 5 nodes 4.4.  A chain of 8191 rows: one CTA 24.3, shared 5.5.
+// all requests in every CTA, 1000 trees of 33 to 64 nodes took 19.0 us; now 12.0 (0.9 MB, 0.08 TB/s), one
+// tree of 5 nodes 4.3.  A chain of 8191 rows: one CTA 24.3, shared 5.5.
 __global__ void __launch_bounds__(kPlanThreads, 10) plan_kernel(const PlanArgs a) {
     __shared__ long long s_sum[2][kPlanThreads / 32], s_top[kPlanThreads / 32];
     __shared__ int s_up[kMaxNodes], s_depth[kMaxNodes];
@@ -369,8 +369,8 @@ struct CommitArgs {
 // and move their share of (K or V, layer, head, 16 bytes) columns.  A thread takes two
 // columns along the whole path in order, four rows at a time: path[j] >= j and
 // the path rises, so nothing is overwritten before it is read.  Measured: 48 trees of
-// 64 nodes, 32 layers of 8 heads of 128 13.0 us (44 MB with the accepted paths, 3.4 TB/s: bound by the
-// chain path - page - rows of a few thousand scattered 16-byte columns); one tree 3.0 us.
+// 64 nodes, 32 layers of 8 heads of 128 12.5 us (44 MB with the accepted paths, 3.5 TB/s: bound by the
+// chain path - page - rows of a few thousand scattered 16-byte columns); one tree 2.8 us.
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArgs a) {
     __shared__ int s_parent[kMaxNodes], s_token[kMaxNodes], s_target[kMaxNodes], s_path[kMaxNodes], s_n;
     __shared__ int64_t s_off[kMaxNodes];  // cache row at lens + i, -1: none

@@ -6,7 +6,7 @@
 // CTA, whatever the lengths are.  An item counts kItemCost units more than it has,
 // in front of them: the time that its q, first scores and output take (16 requests of 32 heads,
 // 262 to 2100 positions each, one row a tile: 64 us, with none 72, one 68, five 65; 1024 items of 90 to 270
-// positions, 9 fp32 rows: 74 us, with two 76).  An item that lies in one CTA's range is finished there;
+// positions, 9 fp32 rows: 74 us when it was chosen, with two 76).  An item that lies in one CTA's range is finished there;
 // one that a range end cuts leaves a partial sum per CTA, joined afterwards in
 // the order of the CTAs.  A CTA has at most two of those: the item that its range
 // starts in and the one that it ends in.
