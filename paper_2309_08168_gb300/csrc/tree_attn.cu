@@ -22,8 +22,8 @@
 //                there is one accumulator, and the maximum that weights are relative to goes
 //                from unit to unit, from a group's warp to the other's (before its weights
 //                are computed, so that the groups overlap).
-//   warps 12-15 : q of the next item to shared memory; fp32 rows: adds each unit's product
-//                to its sums; at an item's end O / sum, or O, maximum and sum to the
+//   warps 12-15 : q of the next item to shared memory; adds each run's product (fp32 rows: a
+//                unit's) to the sums; at an item's end O / sum, or O, maximum and sum to the
 //                workspace if other CTAs hold parts of the item, while the others are at
 //                the next item.  join_kernel adds those.
 // The tile has 128 rows (with fewer, the others' lanes hold what no one reads; tiles of 32, with q of two
@@ -60,7 +60,8 @@
 // position, 6e-4 after 100000 in one accumulator.  So a run of units (Lay::RUN) starts from zero
 // (lo first), and runs are added in fp32.  fp32 rows: a run is a unit, 1e-6 at any length.  16-bit rows: 24 units, 4e-5 at any length
 // (of fp16's half step, 2.4e-4 to 4.9e-4, a sixth; 32 units 5e-5).  A run's end is a gap of 3 to 4 us in the products: 100001 positions
-// 73.6 -> 78.7 us, 160 items of 60000 472 -> 508, bf16 prompt of 2048 rows 366 -> 382; shorter items as before.
+// 73.6 -> 78.7 us, 160 items of 60000 472 -> 508, bf16 prompt of 2048 rows 366 -> 382, items of two or three units
+// (code that they do not reach) 54 -> 56.
 //
 // Units with positions that some row does not see: scores by the row's 64 mask
 // bits, and V rows behind the last position, which may hold anything, are set
@@ -94,7 +95,7 @@ struct Lay {
     static constexpr int VBOX = 64 * 128;             // 64 dims of 64 positions of V
     static constexpr int VSLOT = BOXES * VBOX;
     static constexpr int RING = 210 * 1024;           // shared memory for q and the rings
-    // TMEM columns: O; fp32 rows' sums of earlier units; S / P of unit j at S0 + 128 (j mod NB)
+    // TMEM columns: O; sums of earlier runs, if SUMS_IN_TMEM; S / P of unit j at S0 + 128 (j mod NB)
     static constexpr int M0 = HD, S0 = PARTS == 2 && HD == 128 ? 256 : 128, NB = (kTmem - S0) / kUnit;
     // Units whose products are added in the accumulator, from zero on; then they are added to the sums in fp32, in TMEM if
     // it has room for those, else in the workspace (above).  (Sums in TMEM with two S / P buffers instead of three: bf16 prompt
