@@ -2,7 +2,7 @@
 
 Argument marshalling only: every step of the decode path runs in the CUDA
 library (csrc/, built for sm_103a by build.py).  The functions keep the C
-ABI's names (include/ssd.h, include/ssd_ops.h).  Importing this module fails
+ABI's names (include/ssd.h, include/ssd_ops.h, include/ssd_step.h).  Importing this module fails
 loudly when the library has not been built; there is no fallback path.
 """
 from __future__ import annotations
@@ -33,6 +33,11 @@ EXPORTS = ("ssd_create", "ssd_set_skip", "ssd_set_sampling", "ssd_set_draft_exit
 # the operators that include/ssd_ops.h declares (and ssd_debug_tree_stall)
 OPERATOR_EXPORTS = ("ssd_tree_plan", "ssd_rope_init", "ssd_rope_kv", "ssd_tree_attention",
                     "ssd_tree_attention_workspace", "ssd_tree_commit")
+# and those of include/ssd_step.h
+STEP_EXPORTS = ("ssd_rope_axes_init", "ssd_norm_rope_kv", "ssd_logits_adjust", "ssd_logits_choose", "ssd_moe_route", "ssd_moe_mlp",
+                "ssd_moe_workspace")
+SSD_AXES_SECTIONS, SSD_AXES_IN_TURNS = 0, 1
+SSD_MOE_SOFTMAX, SSD_MOE_SIGMOID = 0, 1
 SSD_F32, SSD_F16, SSD_BF16 = 0, 1, 2
 SSD_STATUS_PAGES, SSD_STATUS_TABLE, SSD_STATUS_PARENT, SSD_STATUS_TIMEOUT = 1, 2, 4, 8
 SSD_ROPE_PLAIN, SSD_ROPE_LINEAR, SSD_ROPE_BY_PARTS = 0, 1, 2
@@ -83,6 +88,27 @@ class ssd_rope(ctypes.Structure):
                 ("turns", ctypes.c_uint64 * 64)]
 
 
+class ssd_rope_axes(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int), ("axis", ctypes.c_uint8 * 64)]
+
+
+class ssd_head_norm(ctypes.Structure):
+    _fields_ = [("q_gain", _VP), ("k_gain", _VP), ("eps", ctypes.c_float)]
+
+
+class ssd_logit_rules(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("vocab", "n_requests", "n_rows", "max_rows")] + \
+               [(n, _VP) for n in ("row_start", "history", "history_len", "prompt_len")] + \
+               [("history_stride", ctypes.c_int64), ("max_history", ctypes.c_int), ("mask_words", ctypes.c_int)] + \
+               [(n, _VP) for n in ("tokens", "masks", "repetition", "presence", "frequency", "bias", "bias_of", "allowed", "allowed_of")] + \
+               [("bias_stride", ctypes.c_int64), ("allowed_stride", ctypes.c_int64), ("n_bias", ctypes.c_int), ("n_allowed", ctypes.c_int)]
+
+
+class ssd_moe(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("gate", "up", "down")] + [(n, ctypes.c_int64) for n in ("gate_stride", "up_stride", "down_stride")] + \
+               [(n, ctypes.c_int) for n in ("dtype", "n_experts", "d", "f")]
+
+
 class SSDError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{msg} (code {code})")
@@ -121,7 +147,15 @@ def _load():
     lib.ssd_tree_attention_workspace.argtypes = [I, ctypes.POINTER(ctypes.c_size_t)]
     lib.ssd_tree_commit.argtypes = [BP, PP] + [_VP] * 9
     lib.ssd_debug_tree_stall.argtypes, lib.ssd_debug_tree_stall.restype = [I, ctypes.c_double], None
-    for n in OPERATOR_EXPORTS:
+    AP, NP, LP, MP = (ctypes.POINTER(x) for x in (ssd_rope_axes, ssd_head_norm, ssd_logit_rules, ssd_moe))
+    lib.ssd_rope_axes_init.argtypes = [RP, I, I, ctypes.POINTER(I), AP]
+    lib.ssd_norm_rope_kv.argtypes = [PP, I, RP, AP, NP, I, I, I, _VP, L, _VP, L, _VP, L, _VP, _VP, _VP, L, _VP]
+    lib.ssd_logits_adjust.argtypes = [LP, I, _VP, L, _VP, L, _VP]
+    lib.ssd_logits_choose.argtypes = [LP, I, _VP, L, I, _VP, _VP, _VP, _VP]
+    lib.ssd_moe_route.argtypes = [I, I, I, I, I, _VP, L, _VP, _VP, I, I, ctypes.c_float, _VP, _VP, _VP]
+    lib.ssd_moe_mlp.argtypes = [MP, I, I, _VP, L, _VP, _VP, _VP, L, _VP, L, _VP, ctypes.c_size_t, _VP]
+    lib.ssd_moe_workspace.argtypes = [MP, I, I, ctypes.POINTER(ctypes.c_size_t)]
+    for n in OPERATOR_EXPORTS + STEP_EXPORTS:
         getattr(lib, n).restype = ctypes.c_int
     lib.ssd_destroy.argtypes = [H]
     lib.ssd_destroy.restype = None
@@ -428,6 +462,179 @@ def ssd_tree_commit(batch: TreeBatch, cache: PagedKV | None, parents, tokens, ta
                                _dev(accepted, "accepted", i32, d, n), _dev(next_token, "next_token", i32, d, n),
                                _dev(lens_out, "lens_out", i32, d, n), _dev(path, "path", i32, d, r),
                                _dev(emitted, "emitted", i32, d, r), cuda_stream))
+
+
+# -- operators of a decoding step around those (include/ssd_step.h) -----------
+
+def ssd_rope_axes_init(rope: ssd_rope, layout: int, pairs) -> ssd_rope_axes:
+    """Which axis turns each pair: pairs has the number of pairs of every axis."""
+    out, pairs = ssd_rope_axes(), [int(x) for x in pairs]
+    _check(lib.ssd_rope_axes_init(rope, layout, len(pairs), (ctypes.c_int * max(1, len(pairs)))(*pairs), out))
+    return out
+
+
+class HeadNorm:
+    """Gains fp32 [head_dim] of the queries' and the keys' heads (None: not normalised) on one CUDA device, and eps.  Keeps the tensors."""
+
+    def __init__(self, q_gain, k_gain, eps: float):
+        self.keep, self.sizes, self.device = (q_gain, k_gain), set(), None
+        for t in self.keep:
+            if t is not None:
+                if not t.is_cuda or self.device not in (None, t.get_device()):
+                    _refuse("gains on one CUDA device are wanted")
+                self.device = t.get_device()
+                self.sizes.add(t.numel())
+        ptr = [_dev(t, "gain", _of_type(t, "gain", "torch.float32"), self.device, t.numel()) if t is not None else None for t in self.keep]
+        self.struct = ssd_head_norm(*ptr, eps)
+
+
+def ssd_norm_rope_kv(cache: PagedKV, layer: int, rope: ssd_rope, q, k, v, positions, slots, q_out, axes: ssd_rope_axes | None = None,
+                     norm: HeadNorm | None = None, cuda_stream: int | None = None) -> None:
+    """ssd_rope_kv with norms of q's and k's heads before the rotation; positions int32 [axes][n] (without axes [n])."""
+    kind, d, t, n, h, g, hd = _row_type(q, "q"), cache.device, q.dtype, q.shape[0], q.shape[1], cache.n_kv_heads, cache.head_dim
+    i32 = _of_type(slots, "slots", "torch.int32")
+    if norm is not None and norm.device is not None and (norm.device != d or norm.sizes != {hd}):
+        _refuse(f"gains of {hd} values on CUDA device {d} are wanted")
+    _check(lib.ssd_norm_rope_kv(cache.struct, layer, rope, axes, norm.struct if norm is not None else None, kind, n, h, *_rows(q, "q", d, t, n, h, hd),
+                                *_rows(k, "k", d, t, n, g, hd), *_rows(v, "v", d, t, n, g, hd),
+                                _dev(positions, "positions", i32, d, n * (axes.n_axes if axes is not None else 1)), _dev(slots, "slots", i32, d, n),
+                                *_rows(q_out, "q_out", d, t, n, h, hd), cuda_stream))
+
+
+def _matrix(t, what: str, device: int, dtype, rows: int, width: int):
+    """(address, row stride) of rows of `width` adjacent values."""
+    if tuple(t.shape) != (rows, width) or t.dtype is not dtype or t.get_device() != device or (t.stride(1) != 1 and width > 1 and rows > 0):
+        _refuse(f"{what}: {dtype} of shape ({rows}, {width}) with adjacent values on CUDA device {device} is wanted, got {t.dtype}, {tuple(t.shape)} on {t.device}")
+    return (t.data_ptr(), t.stride(0) if rows > 1 else width) if rows else (None, width)
+
+
+class LogitRules:
+    """What is done to the logits of a round's rows (ssd_logit_rules), all tensors on one CUDA device.  Keeps the tensors; their
+    contents may change between calls.  row_start int32 [requests + 1] with n_rows and max_rows, or None: a row a request.
+    history int32 [requests][max_history] with history_len and prompt_len int32 [requests]; tokens int32 [n_rows] and masks
+    int64 [n_rows][words] (bit patterns; None: chains) of the round's nodes; repetition, presence, frequency fp32 [requests];
+    bias fp32 [sets][vocab] with bias_of int32 [requests]; allowed int32 [sets][ceil(vocab / 32)] (bit patterns) with
+    allowed_of int32 [n_rows]."""
+
+    def __init__(self, vocab: int, n_rows: int, row_start=None, max_rows: int = 1, history=None, history_len=None, prompt_len=None, tokens=None,
+                 masks=None, repetition=None, presence=None, frequency=None, bias=None, bias_of=None, allowed=None, allowed_of=None):
+        all_ = (row_start, history, history_len, prompt_len, tokens, masks, repetition, presence, frequency, bias, bias_of, allowed, allowed_of)
+        self.keep, self.vocab, self.n_rows = all_, vocab, n_rows
+        devices = {t.get_device() for t in all_ if t is not None}
+        if len(devices) > 1 or -1 in devices:
+            _refuse("rules: tensors on one CUDA device are wanted")
+        self.device = d = devices.pop() if devices else None
+        if row_start is not None and row_start.numel() < 2:
+            _refuse("row_start: [requests + 1] is wanted")
+        if (history is None) != (history_len is None) or (prompt_len is not None and history is None):
+            _refuse("history needs history_len, prompt_len needs history")
+        if (bias_of is not None and bias is None) or (allowed_of is not None and allowed is None):
+            _refuse("bias_of needs bias, allowed_of needs allowed")
+        n = self.n_requests = row_start.numel() - 1 if row_start is not None else n_rows
+
+        def dev(t, what, name, size):
+            return _dev(t, what, _of_type(t, what, name), d, size) if t is not None else None
+
+        def table(t, what, name, width, rows=None):
+            if t is None:
+                return None, 0, 0
+            if t.dim() != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows):
+                _refuse(f"{what}: [{rows or 'sets'}][{width}] is wanted, got {tuple(t.shape)}")
+            return (*_matrix(t, what, d, _of_type(t, what, name), t.shape[0], width), t.shape[0])
+        if history is not None and history.dim() != 2:
+            _refuse("history: [request][token] is wanted")
+        hist = table(history, "history", "torch.int32", history.shape[1] if history is not None else 0, n)
+        bia, allo = table(bias, "bias", "torch.float32", vocab), table(allowed, "allowed", "torch.int32", -(-vocab // 32))
+        words = _words(masks)
+        self.struct = ssd_logit_rules(
+            vocab, n, n_rows, max_rows, dev(row_start, "row_start", "torch.int32", n + 1), hist[0], dev(history_len, "history_len", "torch.int32", n),
+            dev(prompt_len, "prompt_len", "torch.int32", n), hist[1], history.shape[1] if history is not None else 0, words,
+            dev(tokens, "tokens", "torch.int32", n_rows), dev(masks, "masks", "torch.int64", n_rows * words),
+            *(dev(t, x, "torch.float32", n) for t, x in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency"))),
+            bia[0], dev(bias_of, "bias_of", "torch.int32", n), allo[0], dev(allowed_of, "allowed_of", "torch.int32", n_rows), bia[1], allo[1], bia[2], allo[2])
+
+
+def _logits(rules: LogitRules, t, what: str):
+    """(type, device, address, row stride) of rows of logits."""
+    kind = _ROW_TYPES.get(t.dtype)
+    if kind is None:
+        kind = _ROW_TYPES.get(str(t.dtype))
+        if kind is None:
+            _refuse(f"{what}: fp32, fp16 or bf16 rows are wanted")
+        _ROW_TYPES[t.dtype] = kind
+    d = t.get_device()
+    if d < 0 or rules.device not in (None, d):
+        _refuse(f"{what}: rows on the rules' CUDA device are wanted")
+    return (kind, d, *_matrix(t, what, d, t.dtype, rules.n_rows, rules.vocab))
+
+
+def ssd_logits_adjust(rules: LogitRules, logits, out, cuda_stream: int | None = None) -> None:
+    """out [n_rows][vocab] = the logits after the rules, of their type (out may be logits)."""
+    kind, d, ptr, stride = _logits(rules, logits, "logits")
+    _check(lib.ssd_logits_adjust(rules.struct, kind, ptr, stride, *_matrix(out, "out", d, logits.dtype, rules.n_rows, rules.vocab), cuda_stream))
+
+
+def ssd_logits_choose(rules: LogitRules, logits, tokens, logprob, total=None, cuda_stream: int | None = None) -> None:
+    """The k best tokens int32 [n_rows][k] of every row after the rules, their log probabilities fp32 [n_rows][k] and the
+    logsumexp fp32 [n_rows] (or None)."""
+    kind, d, ptr, stride = _logits(rules, logits, "logits")
+    if tokens.dim() != 2 or tokens.shape[0] != rules.n_rows:
+        _refuse("tokens: [row][k] is wanted")
+    n, f32 = tokens.numel(), _of_type(logprob, "logprob", "torch.float32")
+    _check(lib.ssd_logits_choose(rules.struct, kind, ptr, stride, tokens.shape[1], _dev(tokens, "tokens", _of_type(tokens, "tokens", "torch.int32"), d, n),
+                                 _dev(logprob, "logprob", f32, d, n), _dev(total, "total", f32, d, rules.n_rows), cuda_stream))
+
+
+class MoeWeights:
+    """Experts' matrices: gate and up [expert][f][d], down [expert][d][f], fp16 or bf16, each expert's contiguous.  Keeps the tensors."""
+
+    def __init__(self, gate, up, down):
+        if gate.dim() != 3 or up.shape != gate.shape or tuple(down.shape) != (gate.shape[0], gate.shape[2], gate.shape[1]):
+            _refuse("gate and up [expert][f][d] and down [expert][d][f] are wanted")
+        for t in (gate, up, down):
+            if str(t.dtype) not in ("torch.float16", "torch.bfloat16") or t.dtype != gate.dtype or not t.is_cuda or t.get_device() != gate.get_device():
+                _refuse("gate, up and down: fp16 or bf16 of one type on one CUDA device are wanted")
+            if t.numel() and (t.stride(2) != 1 or t.stride(1) != t.shape[2]):
+                _refuse("an expert's matrix must be contiguous")
+        self.keep, self.device, self.dtype = (gate, up, down), gate.get_device(), gate.dtype
+        self.n_experts, self.f, self.d = gate.shape
+        strides = [t.stride(0) if self.n_experts > 1 else self.f * self.d for t in self.keep]
+        self.struct = ssd_moe(*(t.data_ptr() for t in self.keep), *strides, _ROW_TYPES[str(gate.dtype)], self.n_experts, self.d, self.f)
+
+
+def ssd_moe_route(x, w_router, ids, weights, score: int = SSD_MOE_SOFTMAX, favour=None, renorm: bool = True, scale: float = 1.0,
+                  cuda_stream: int | None = None) -> None:
+    """The experts ids int32 [n][k] of rows x [n][d] and their weights fp32 [n][k]; w_router [experts][d] of x's type,
+    favour fp32 [experts] (added to the scores that choose) or None."""
+    if x.dim() != 2 or w_router.dim() != 2 or ids.dim() != 2 or not x.is_cuda:
+        _refuse("x [row][d], w_router [expert][d] and ids [row][k] on a CUDA device are wanted")
+    if str(x.dtype) not in ("torch.float16", "torch.bfloat16"):
+        _refuse("x: fp16 or bf16 rows are wanted")
+    (n, d), e, k, dev = x.shape, w_router.shape[0], ids.shape[1], x.get_device()
+    f32 = _of_type(weights, "weights", "torch.float32")
+    _check(lib.ssd_moe_route(_ROW_TYPES[str(x.dtype)], n, d, e, k, *_matrix(x, "x", dev, x.dtype, n, d), _dev(w_router, "w_router", x.dtype, dev, e * d),
+                             _dev(favour, "favour", f32, dev, e), score, int(bool(renorm)), scale,
+                             _dev(ids, "ids", _of_type(ids, "ids", "torch.int32"), dev, n * k), _dev(weights, "weights", f32, dev, n * k), cuda_stream))
+
+
+def ssd_moe_workspace(experts: MoeWeights, n_rows: int, k: int) -> int:
+    """Bytes of workspace that ssd_moe_mlp wants for this many rows and slots."""
+    n = ctypes.c_size_t()
+    _check(lib.ssd_moe_workspace(experts.struct, n_rows, k, n))
+    return n.value
+
+
+def ssd_moe_mlp(experts: MoeWeights, x, ids, weights, out, workspace, residual=None, cuda_stream: int | None = None) -> None:
+    """out [n][d] = residual + the rows x [n][d] through their experts ids int32 [n][k], by weights fp32 [n][k].
+    workspace: a contiguous uint8 tensor."""
+    if x.dim() != 2 or ids.dim() != 2:
+        _refuse("x [row][d] and ids [row][k] are wanted")
+    n, k, d, t = x.shape[0], ids.shape[1], experts.device, experts.dtype
+    _check(lib.ssd_moe_mlp(experts.struct, n, k, *_matrix(x, "x", d, t, n, experts.d), _dev(ids, "ids", _of_type(ids, "ids", "torch.int32"), d, n * k),
+                           _dev(weights, "weights", _of_type(weights, "weights", "torch.float32"), d, n * k),
+                           *(_matrix(residual, "residual", d, t, n, experts.d) if residual is not None else (None, 0)),
+                           *_matrix(out, "out", d, t, n, experts.d),
+                           _dev(workspace, "workspace", _of_type(workspace, "workspace", "torch.uint8"), d, workspace.numel()), workspace.numel(), cuda_stream))
 
 
 def ssd_destroy(h: int) -> None:

@@ -1,0 +1,260 @@
+// step_heads.cu - per-head norms and rotary positions on several axes with the
+// write of keys and values (ssd_norm_rope_kv of ssd_step.h).
+#include <algorithm>
+#include <cmath>
+
+#include "step_ops.cuh"
+
+namespace ssd {
+namespace step {
+
+constexpr int kHeadThreads = 128;
+constexpr int kHeadAhead = 4;  // heads under way in a lane
+
+struct HeadArgs {
+    const void *q, *k, *v;
+    void* q_out;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;  // elements
+    const int32_t *positions, *slots;
+    void *kc, *vc;  // the layer's cache
+    int64_t page_stride, head_stride, pos_stride;
+    const float *q_gain, *k_gain;  // nullptr: no norm
+    float eps;
+    int n_rows, n_heads, n_kv_heads, hd, page_size, n_pages;
+    ssd_rope rope;
+    uint8_t axis[64];
+};
+
+// A CTA takes a row (blockIdx.x), or with gridDim.y > 1 a share of its heads; hd / V lanes hold a
+// head, 16 bytes each, so that the sum of squares is a few shuffles and every byte is read once.
+// Rotated dim e with partner p becomes r (x_e g_e cos +- x_p g_p sin), r = 1 / sqrt(mean x^2 + eps): the
+// products of gains and angles are formed once a row in shared memory (a, b), and the partner's 16 bytes come from
+// the lane that holds them.  Bound by HBM, or for few rows by the chain position - angle - table - store.
+//
+// T: rows, C: cache
+template <typename T, typename C>
+__global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_constant__ HeadArgs a) {
+    constexpr int V = Vec<T>::N;
+    __shared__ float2 s_cs[64];
+    __shared__ __align__(16) float s_a[2][128], s_b[2][128];  // [q, k][dim]
+    pdl_launch_dependents();
+    pdl_wait();
+    const int row = blockIdx.x, rot = a.rope.rot_dim, half = rot / 2, tid = threadIdx.x;
+    const int slot = __ldcg(a.slots + row);
+    if (tid < half) {
+        const int64_t p = __ldcg(a.positions + (int64_t)a.axis[tid] * a.n_rows + row);
+        const uint64_t turn = (uint64_t)p * a.rope.turns[tid];
+        float s, c;
+        sincospif((float)((int64_t)turn >> 32) * 0x1p-31f, &s, &c);
+        s_cs[tid] = make_float2(c * a.rope.amplitude, s * a.rope.amplitude);
+    }
+    const bool cached = slot >= 0 && slot < a.n_pages * a.page_size;
+    const int64_t at = cached ? (int64_t)(slot / a.page_size) * a.page_stride + (int64_t)(slot % a.page_size) * a.pos_stride : 0;
+    auto to_cache = [&](void* base, int head, int e, const float (&f)[V]) {
+        C* p = (C*)base + at + (int64_t)head * a.head_stride + e;
+        if constexpr (V == 8) *reinterpret_cast<uint4*>(p) = Vec<C>::put(f);
+        else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1], C()), pack2(f[2], f[3], C()));
+    };
+    const int per = a.hd / V, c = tid % per, e = c * V;  // lanes of a head (8, 16 or 32), this one's place
+    const int line = (blockIdx.y * kHeadThreads + tid) / per, step = kHeadThreads * gridDim.y / per;
+    const int kv_heads = cached ? a.n_kv_heads : 0, heads = a.n_heads + kv_heads;
+    auto source = [&](int h) {
+        return h < a.n_heads ? (const T*)a.q + (int64_t)row * a.q_stride + (int64_t)h * a.hd + e
+                             : (const T*)a.k + (int64_t)row * a.k_stride + (int64_t)(h - a.n_heads) * a.hd + e;
+    };
+    uint4 x[kHeadAhead];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int i = 0; i < kHeadAhead; ++i)
+            if (h0 + i * step < heads) x[i] = __ldcg(reinterpret_cast<const uint4*>(source(h0 + i * step)));
+    };
+    // values first: they need no angles; the first heads are on their way meanwhile
+    load(line);
+    for (int h = line; h < kv_heads; h += kHeadAhead * step) {
+        const T* v = (const T*)a.v + (int64_t)row * a.v_stride + e;
+        uint4 y[kHeadAhead];
+#pragma unroll
+        for (int i = 0; i < kHeadAhead; ++i)
+            if (h + i * step < kv_heads) y[i] = __ldcg(reinterpret_cast<const uint4*>(v + (int64_t)(h + i * step) * a.hd));
+#pragma unroll
+        for (int i = 0; i < kHeadAhead; ++i)
+            if (h + i * step < kv_heads) {
+                float f[V];
+                Vec<T>::get(y[i], f);
+                to_cache(a.vc, h + i * step, e, f);
+            }
+    }
+    __syncthreads();
+    if (tid < a.hd) {
+        const bool rotated = tid < rot, inter = a.rope.interleaved;
+        const int pair = inter ? tid / 2 : tid < half ? tid : tid - half;
+        const bool first = inter ? tid % 2 == 0 : tid < half;
+        const int partner = inter ? tid ^ 1 : first ? tid + half : tid - half;
+        const float2 cs = rotated ? s_cs[pair] : make_float2(1.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float* g = i ? a.k_gain : a.q_gain;
+            s_a[i][tid] = cs.x * (g ? __ldcg(g + tid) : 1.f);
+            s_b[i][tid] = rotated ? (first ? -cs.y : cs.y) * (g ? __ldcg(g + partner) : 1.f) : 0.f;
+        }
+    }
+    __syncthreads();
+    // where the partners of this lane's dims are: its own 16 bytes (neighbours), or another lane's
+    const bool rotated = e < rot;
+    const int lane = tid % 32, other = a.rope.interleaved || !rotated ? lane : e < half ? lane + half / V : lane - half / V;
+    const float inv_hd = 1.f / (float)a.hd;
+    for (int h0 = line; __any_sync(0xffffffffu, h0 < heads); h0 += kHeadAhead * step) {
+        if (h0 != line) load(h0);
+        // (all lanes of a warp take part in the shuffles; those without a head shuffle what they hold)
+        float r[kHeadAhead];
+#pragma unroll
+        for (int i = 0; i < kHeadAhead; ++i) {
+            if (h0 + i * step >= heads) x[i] = make_uint4(0u, 0u, 0u, 0u);
+            float f[V];
+            Vec<T>::get(x[i], f);
+            r[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) r[i] = fmaf(f[j], f[j], r[i]);
+        }
+        if (a.q_gain || a.k_gain) {
+            for (int o = per / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < kHeadAhead; ++i) r[i] += __shfl_xor_sync(0xffffffffu, r[i], o);
+        }
+#pragma unroll
+        for (int i = 0; i < kHeadAhead; ++i) {
+            const int h = h0 + i * step;
+            uint4 y;
+            y.x = __shfl_sync(0xffffffffu, x[i].x, other);
+            y.y = __shfl_sync(0xffffffffu, x[i].y, other);
+            y.z = __shfl_sync(0xffffffffu, x[i].z, other);
+            y.w = __shfl_sync(0xffffffffu, x[i].w, other);
+            if (h >= heads) continue;
+            const int kind = h < a.n_heads ? 0 : 1;
+            const float scale = (kind ? a.k_gain : a.q_gain) ? rsqrtf(fmaf(r[i], inv_hd, a.eps)) : 1.f;
+            float f[V], g[V], A[V];
+            Vec<T>::get(x[i], f);
+            Vec<T>::get(y, g);
+#pragma unroll
+            for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(A + j) = *reinterpret_cast<const float4*>(&s_a[kind][e + j]);
+            if (rotated) {
+                float B[V];
+#pragma unroll
+                for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(B + j) = *reinterpret_cast<const float4*>(&s_b[kind][e + j]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float p = a.rope.interleaved ? f[j ^ 1] : g[j];
+                    A[j] = scale * (f[j] * A[j] + p * B[j]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) A[j] *= scale * f[j];
+            }
+            if (kind) to_cache(a.kc, h - a.n_heads, e, A);
+            else *reinterpret_cast<uint4*>((T*)a.q_out + (int64_t)row * a.q_out_stride + (int64_t)h * a.hd + e) = Vec<T>::put(A);
+        }
+    }
+}
+
+}  // namespace step
+}  // namespace ssd
+
+using namespace ssd;
+using namespace ssd::step;
+
+static bool rope_ok(const ssd_rope* rope, int most) {
+    return rope && rope->rot_dim >= 16 && rope->rot_dim % 16 == 0 && rope->rot_dim <= most;
+}
+
+extern "C" int ssd_rope_axes_init(const ssd_rope* rope, int layout, int n_axes, const int* pairs, ssd_rope_axes* out) {
+    static const char call[] = "ssd_rope_axes_init";
+    if (!out || !pairs) return refuse_arg(call, "NULL pointer");
+    if (!rope_ok(rope, 128)) return refuse_arg(call, "rope must come from ssd_rope_init");
+    if (layout != SSD_AXES_SECTIONS && layout != SSD_AXES_IN_TURNS) return refuse_arg(call, "unknown layout");
+    if (n_axes < 1 || n_axes > 4) return refuse_arg(call, "need 1 .. 4 axes");
+    const int half = rope->rot_dim / 2;
+    int left = half;
+    for (int i = 0; i < n_axes; ++i) {
+        if (pairs[i] < 0 || pairs[i] > left) return refuse_arg(call, "pairs must be counts that add up to rot_dim / 2");
+        left -= pairs[i];
+    }
+    if (left) return refuse_arg(call, "pairs must be counts that add up to rot_dim / 2");
+    ssd_rope_axes r{};
+    r.n_axes = n_axes;
+    if (layout == SSD_AXES_SECTIONS) {
+        for (int a = 0, i = 0; a < n_axes; ++a)
+            for (int j = 0; j < pairs[a]; ++j) r.axis[i++] = (uint8_t)a;
+    } else {
+        for (int i = 0; i < half; ++i) r.axis[i] = (uint8_t)(i / n_axes < pairs[i % n_axes] ? i % n_axes : 0);
+    }
+    *out = r;
+    return SSD_OK;
+}
+
+extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* rope, const ssd_rope_axes* axes,
+                                const ssd_head_norm* norm, int dtype, int n_rows, int n_heads, const void* q, int64_t q_stride,
+                                const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                                const int32_t* slots, void* q_out, int64_t q_out_stride, void* cuda_stream) {
+    static const char call[] = "ssd_norm_rope_kv";
+    if (int rc = check_pages(call, cache)) return rc;
+    if (layer < 0 || layer >= cache->n_layers) return refuse_arg(call, "no such layer");
+    if (int rc = check_rows_type(call, dtype, cache)) return rc;
+    if (!rope_ok(rope, cache->head_dim)) return refuse_arg(call, "rope must come from ssd_rope_init, with rot_dim <= head_dim");
+    HeadArgs a{};
+    if (axes) {
+        if (axes->n_axes < 1 || axes->n_axes > 4) return refuse_arg(call, "axes must come from ssd_rope_axes_init");
+        for (int i = 0; i < rope->rot_dim / 2; ++i) {
+            if (axes->axis[i] >= axes->n_axes) return refuse_arg(call, "axes must come from ssd_rope_axes_init");
+            a.axis[i] = axes->axis[i];
+        }
+    }
+    if (norm && (norm->q_gain || norm->k_gain)) {
+        if (!(norm->eps > 0.f) || !std::isfinite(norm->eps)) return refuse_arg(call, "need eps > 0, finite");
+        if (((uintptr_t)norm->q_gain | (uintptr_t)norm->k_gain) & 15u) return refuse_arg(call, "gains must be 16-byte aligned");
+        a.q_gain = norm->q_gain;
+        a.k_gain = norm->k_gain;
+        a.eps = norm->eps;
+    }
+    if (n_rows < 0 || n_heads < 1 || n_heads > 65536) return refuse_arg(call, "need n_rows >= 0 and 1 <= n_heads <= 65536");
+    if (n_rows == 0) return SSD_OK;
+    if (!q || !k || !v || !positions || !slots || !q_out) return refuse_arg(call, "NULL pointer");
+    const int hd = cache->head_dim;
+    if (int rc = check_rows(call, "q", q, q_stride, dtype, (int64_t)n_heads * hd)) return rc;
+    if (int rc = check_rows(call, "q_out", q_out, q_out_stride, dtype, (int64_t)n_heads * hd)) return rc;
+    if (int rc = check_rows(call, "k", k, k_stride, dtype, (int64_t)cache->n_kv_heads * hd)) return rc;
+    if (int rc = check_rows(call, "v", v, v_stride, dtype, (int64_t)cache->n_kv_heads * hd)) return rc;
+    if (q == q_out && q_stride != q_out_stride) return refuse_arg(call, "q_out in q's place needs its stride");
+    if (q_out == k || q_out == v) return refuse_arg(call, "q_out must not be k or v");
+    if (int rc = check_device(call, cache->k)) return rc;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_out = q_out;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_out_stride = q_out_stride;
+    a.positions = positions;
+    a.slots = slots;
+    a.kc = (char*)cache->k + 2 * layer * cache->layer_stride;
+    a.vc = (char*)cache->v + 2 * layer * cache->layer_stride;
+    a.page_stride = cache->page_stride;
+    a.head_stride = cache->head_stride;
+    a.pos_stride = cache->pos_stride;
+    a.n_rows = n_rows;
+    a.n_heads = n_heads;
+    a.n_kv_heads = cache->n_kv_heads;
+    a.hd = hd;
+    a.page_size = cache->page_size;
+    a.n_pages = cache->n_pages;
+    a.rope = *rope;
+    // few rows: a row's heads over several CTAs, until there are four per SM
+    const int per16 = dtype == SSD_F32 ? 4 : 8;
+    const long long units = (long long)(n_heads + cache->n_kv_heads) * hd / per16;
+    int split = 1;
+    while (split < 64 && (long long)n_rows * split < 608 && units > (long long)kHeadThreads * split) split *= 2;
+    const dim3 grid((unsigned)n_rows, (unsigned)split);
+    if (dtype == SSD_F32) return launch(call, heads_kernel<float, f16>, grid, kHeadThreads, 0, cuda_stream, a);
+    if (dtype == SSD_F16) return launch(call, heads_kernel<f16, f16>, grid, kHeadThreads, 0, cuda_stream, a);
+    return launch(call, heads_kernel<bf16, bf16>, grid, kHeadThreads, 0, cuda_stream, a);
+}

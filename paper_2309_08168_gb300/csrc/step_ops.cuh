@@ -1,0 +1,41 @@
+// step_ops.cuh - what the operators of ssd_step.h share.
+#pragma once
+
+#include "ssd_step.h"
+#include "tree_ops.cuh"
+
+namespace ssd {
+namespace step {
+using namespace tree;
+
+// whether two ranges of bytes meet; NULL meets nothing
+inline bool meet(const void* a, size_t na, const void* b, size_t nb) {
+    return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+// bytes from the first row's start to the last row's end
+inline size_t span(int n_rows, int64_t stride, int64_t width, int dtype) {
+    return ((size_t)(n_rows - 1) * (size_t)stride + (size_t)width) * (dtype == SSD_F32 ? 4 : 2);
+}
+
+// ---------------------------------------------------------------------------
+// clusters
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_address(const void* p, uint32_t cta) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(smem_u32(p)), "r"(cta));
+    return at;
+}
+__device__ __forceinline__ uint64_t peer_load(const void* p, uint32_t cta) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];\n" : "=l"(v) : "r"(peer_address(p, cta)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void peer_store(void* p, uint32_t cta, uint64_t v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;\n" ::"r"(peer_address(p, cta)), "l"(v) : "memory");
+}
+
+}  // namespace step
+}  // namespace ssd
