@@ -8,12 +8,12 @@
 namespace ssd {
 namespace step {
 
-constexpr int kLogitThreads = 512, kLogitWarps = kLogitThreads / 32;
+constexpr int kLogitThreads = 256, kLogitWarps = kLogitThreads / 32;
 constexpr int kMaxVocab = 262144;
-constexpr int kMaxSlice = 32832;  // tokens of a CTA: at most 9 chunks of 8 in each of its threads
+constexpr int kMaxSlice = 131136;  // tokens of a CTA: at most 17 chunks of 8 in each of its threads
 constexpr int kMaxSplit = 8;      // CTAs of a row: one portable cluster
 constexpr int kMaxBest = 16;
-constexpr int kCandidates = kMaxBest * ((kMaxSlice / 8 + kLogitThreads - 1) / kLogitThreads) * 8;
+constexpr int kJoinWarps = kMaxSplit * kMaxBest / 32;
 constexpr uint32_t kPrompt = 0x80000000u;  // a token's count: times that the model said it, and this bit if the prompt holds it
 
 struct LogitArgs {
@@ -25,6 +25,9 @@ struct LogitArgs {
     float *logprob, *total;
     int k, slice, rows;  // tokens of a CTA (a multiple of 64), rows of a cluster
     int counted;         // whether anything is penalised
+    // dynamic shared memory: candidates of the k best, words of the row's mask from at_show on, and from at_bits on what has been
+    // said: n_words words of bits, the bits before each four of them, counts
+    int at_show, at_bits, n_words;
 };
 
 // what a float sorts by; 0 is below all of them (-inf gives 0x007fffff)
@@ -36,8 +39,39 @@ __device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float(o
 // (logit, token) as one number: larger logits first, of equal ones the lower token; 0 is none
 __device__ __forceinline__ uint64_t key_of(float v, int x) { return (uint64_t)order_of(v) << 32 | (uint32_t)~x; }
 
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
 // exp(v - m) for v <= m, 1 for v = m = inf
-__device__ __forceinline__ float weight(float v, float m) { return v == m ? 1.f : exp2f((v - m) * 1.4426950408889634f); }
+__device__ __forceinline__ float weight(float v, float m) { return v == m ? 1.f : exp2_of((v - m) * kLog2e); }
+__device__ __forceinline__ void copy4(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;\n" ::: "memory"); }
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 of_pair(uint64_t p) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(r.x), "=f"(r.y) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
 
 // what the CTAs of a row hand to the one that joins them
 struct Partial {
@@ -71,62 +105,86 @@ struct Chunk {
 };
 
 // A row's tokens are cut into slices of a CTA each (a cluster joins them), those into chunks of 8 that start on
-// 16 bytes of the logits (a: how far the row's first one lies before its first token), chunk j in thread j mod 512.
+// 16 bytes of the logits (how far the row's first one lies before its first token depends on the row), chunk j in thread j mod 256.
 //
-// The counts of what a text has said are made once for the rows of one request that a cluster takes, in shared memory, for the CTA's
-// slice alone: history tokens are added by all threads, a row's nodes before the row and taken off after it.  A bit for each
-// token tells whether there is anything to look up, so that the pass over the logits asks two words per 8 tokens.
+// What a text has said is worked out once for the rows of one request that a cluster takes, for the CTA's
+// slice alone: a bit for every token that the history or some node of the round says, and a count for each of these bits
+// (found by the number of bits before it).  A row's nodes are added to the counts before the row and taken off after it.
 //
 // The k best: each thread keeps its own best; the k-th largest of these is a bound that at least k tokens reach, and only
 // tokens of the k threads above it can be among the k best.  Their chunks are read once more (from L2), what reaches the bound is
 // ranked by counting, and ranks below k are the answer.  All keys differ (the token is part of them), so ties need no care.
-template <typename T, bool kChoose>
-__global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_constant__ LogitArgs a) {
+//
+// The pass is bound by the instructions it issues (8 fp16 tokens: 8 conversions, 8 exponentials, a maximum, and two in one where the
+// chip has it), so a thread keeps its best chunk rather than its best token, and sums weights relative to a whole number above its
+// best, which seldom changes.
+//
+// kRules: whether the rules have any part
+template <typename T, bool kChoose, bool kRules>
+__global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logits_kernel(const __grid_constant__ LogitArgs a) {
     constexpr int V = Vec<T>::N;  // tokens in 16 bytes
-    constexpr int kAhead = 2;     // chunks of 8 tokens under way in a thread
-    extern __shared__ __align__(16) uint32_t s_dyn[];
-    __shared__ int s_request[2], s_n;
+    constexpr int kParts = 8 / V;
+    constexpr int kAhead = kRules ? 2 : V / 2;  // chunks under way in a thread
+    extern __shared__ __align__(16) unsigned char s_dyn[];
+    __shared__ int s_request, s_rows[2], s_n, s_scan[kLogitWarps];
     __shared__ float s_m[kLogitWarps], s_s[kLogitWarps];
     __shared__ uint64_t s_first[kLogitWarps * kMaxBest], s_bound;
     __shared__ int s_from[kMaxBest], s_found;
-    __shared__ uint64_t s_cand[kChoose ? kCandidates : 1];
     __shared__ Partial s_part[2];
+    uint64_t* s_cand = reinterpret_cast<uint64_t*>(s_dyn);
+    uint32_t* s_show = reinterpret_cast<uint32_t*>(s_dyn + a.at_show);
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, split = gridDim.x, vocab = a.r.vocab;
-    const int lo = blockIdx.x * a.slice;
+    const int lo = blockIdx.x * a.slice, deep = (a.slice / 8 + kLogitThreads - 1) / kLogitThreads;  // chunks of a thread
     const int row0 = blockIdx.y * a.rows, row1 = min(row0 + a.rows, a.r.n_rows);
-    // counts of tokens lo - 8 .. lo + slice - 1 (chunks may start up to 7 tokens before the slice)
-    const int width = a.slice + 8;
-    uint32_t *s_said = s_dyn, *s_count = s_dyn + (width + 31) / 32;
-    // adds (or takes off) one token that the model has said
-    auto say_token = [&](int x, bool off) {
-        const int i = x - lo + 8;
-        if (x < 0 || x >= vocab || i < 0 || i >= width) return;
-        if (!off) {
-            atomicAdd(s_count + i, 1u);
-            atomicOr(s_said + i / 32, 1u << i % 32);
-        } else if (atomicSub(s_count + i, 1u) == 1u) {
-            atomicAnd(s_said + i / 32, ~(1u << i % 32));
+
+    // -- what has been said of tokens lo - 8 .. lo + slice - 1 (chunks may start up to 7 tokens before the slice)
+    const int n_words = a.n_words;
+    uint32_t *s_bits = reinterpret_cast<uint32_t*>(s_dyn + a.at_bits), *s_before = s_bits + n_words, *s_count = s_before + n_words / 4;
+    auto place = [&](int x) { return x >= 0 && x < vocab && x >= lo - 8 && x < lo + a.slice ? x - lo + 8 : -1; };
+    const uint4* fours = reinterpret_cast<const uint4*>(s_bits);
+    auto count_of = [&](int i) {  // bits before bit i
+        const uint4 u = fours[i / 128];
+        const int r = i / 32 % 4;
+        const uint32_t below = (1u << i % 32) - 1u;
+        return s_before[i / 128] + __popc(r > 0 ? u.x : u.x & below) + (r > 0 ? __popc(r > 1 ? u.y : u.y & below) : 0) +
+               (r > 1 ? __popc(r > 2 ? u.z : u.z & below) : 0) + (r > 2 ? __popc(u.w & below) : 0);
+    };
+    int said = 0, prompt = 0;  // tokens of the request's history, those of them that are the prompt's
+    // history tokens, several loads at once; f(token's place, whether it is the prompt's)
+    auto history = [&](int b, auto&& f) {
+        const int n = min(max(said, 0), a.r.max_history);
+        const int32_t* h = a.r.history + (int64_t)b * a.r.history_stride;
+        for (int j = tid; j < n; j += 8 * kLogitThreads) {
+            int x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = j + i * kLogitThreads < n ? __ldcg(h + j + i * kLogitThreads) : -1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int p = place(x[i]);
+                if (p >= 0) f(p, j + i * kLogitThreads < prompt);
+            }
         }
     };
     int request = -1, start = 0, end = 0;  // of the row before
     int old = -1;                          // the row whose nodes are in the counts
-    auto nodes = [&](int row, bool off) {  // the nodes that a row's mask shows
-        const int n = a.r.masks ? min(end - start, 64 * a.r.mask_words) : row - start + 1;
+    auto reach = [&]() { return a.r.masks ? min(end - start, 64 * a.r.mask_words) : end - start; };
+    auto nodes = [&](int row, uint32_t more) {  // more to the counts of the nodes that a row's mask shows
+        const int n = a.r.masks ? reach() : row - start + 1;
         for (int j = tid; j < n; j += kLogitThreads) {
             const bool seen = !a.r.masks || (__ldcg(reinterpret_cast<const unsigned long long*>(a.r.masks) + (int64_t)row * a.r.mask_words + j / 64) >> (j % 64) & 1);
-            if (seen) say_token(__ldcg(a.r.tokens + start + j), off);
+            const int p = seen ? place(__ldcg(a.r.tokens + start + j)) : -1;
+            if (p >= 0) atomicAdd(s_count + count_of(p), more);
         }
     };
     float again = 1.f, often = 0.f, once = 0.f;
-    const float* bias = nullptr;
+    const float* bias = nullptr;  // of the row's request
+
     int turn = 0;  // which of the two parts
     for (int row = row0; row < row1; ++row) {
         // the request that owns the row
-        if (!a.r.row_start) {
-            start = row, end = row + 1;
-        }
+        if (!a.r.row_start) start = row, end = row + 1;
         const bool fresh = !a.r.row_start || row >= end;
         int owner = request;
         if (a.r.row_start && fresh && !a.counted && !a.r.bias_of) {  // (whose it is does not matter)
@@ -134,82 +192,36 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
             owner = s0 <= row && row < s1 ? 0 : a.r.n_requests;
             end = row + 1;
         } else if (a.r.row_start && fresh) {
-            if (tid == 0) s_request[0] = a.r.n_requests;
+            if (tid == 0) s_request = a.r.n_requests;
             __syncthreads();
             for (int b = tid; b < a.r.n_requests; b += kLogitThreads) {
                 const Rows r = rows_of(a.r.row_start, b, a.r.n_rows);
-                if (r.r0 <= row && row < r.r0 + r.n) atomicMin(&s_request[0], b);
+                if (r.r0 <= row && row < r.r0 + r.n) atomicMin(&s_request, b);
             }
             __syncthreads();
-            owner = s_request[0];
-            if (owner < a.r.n_requests) {
+            owner = s_request;
+            if (owner < a.r.n_requests && tid == owner % kLogitThreads) {
                 const Rows r = rows_of(a.r.row_start, owner, a.r.n_rows);
-                start = r.r0, end = r.r0 + r.n;
-            } else {
-                start = row, end = row + 1;  // (no one's)
+                s_rows[0] = r.r0, s_rows[1] = r.r0 + r.n;
             }
-            __syncthreads();  // (s_request is read before the next search)
+            __syncthreads();
+            start = owner < a.r.n_requests ? s_rows[0] : row;  // (else no one's)
+            end = owner < a.r.n_requests ? s_rows[1] : row + 1;
         } else if (fresh) {
             owner = row;
         }
-        const bool owned = owner < a.r.n_requests;
-        if (owned && fresh) {
-            if (a.counted) {
-                __syncthreads();  // (the counts of the row before are no longer read)
-                for (int i = tid; i < (width + 31) / 32 + width; i += kLogitThreads) s_dyn[i] = 0u;
-                old = -1;
-                again = a.r.repetition ? __ldcg(a.r.repetition + owner) : 1.f;
-                often = a.r.frequency ? __ldcg(a.r.frequency + owner) : 0.f;
-                once = a.r.presence ? __ldcg(a.r.presence + owner) : 0.f;
-                __syncthreads();
-                if (a.r.history) {
-                    const int n = min(max(__ldcg(a.r.history_len + owner), 0), a.r.max_history);
-                    const int prompt = a.r.prompt_len ? __ldcg(a.r.prompt_len + owner) : 0;
-                    const int32_t* h = a.r.history + (int64_t)owner * a.r.history_stride;
-                    for (int j = tid; j < n; j += kLogitThreads) {
-                        const int x = __ldcg(h + j), i = x - lo + 8;
-                        if (j >= prompt) {
-                            say_token(x, false);
-                        } else if (x >= 0 && x < vocab && i >= 0 && i < width) {
-                            atomicOr(s_count + i, kPrompt);
-                            atomicOr(s_said + i / 32, 1u << i % 32);
-                        }
-                    }
-                }
-            }
-            bias = nullptr;
-            if (a.r.bias) {
-                const int b = a.r.bias_of ? __ldcg(a.r.bias_of + owner) : 0;
-                if (b >= 0 && b < a.r.n_bias) bias = a.r.bias + (int64_t)b * a.r.bias_stride;
-            }
-        }
         request = owner;
-        if (!owned) continue;  // (uniform over the cluster: its CTAs have the same rows)
-        if (a.counted && a.r.tokens) {
-            __syncthreads();  // (history counted; the row before read)
-            if (old >= 0) {
-                nodes(old, true);
-                __syncthreads();
-            }
-            nodes(row, false);
-            old = row;
-        }
-        if (a.counted) __syncthreads();
-        const uint32_t* allowed = nullptr;
-        if (a.r.allowed) {
-            const int m = a.r.allowed_of ? __ldcg(a.r.allowed_of + row) : row;
-            if (m >= 0 && m < a.r.n_allowed) allowed = a.r.allowed + (int64_t)m * a.r.allowed_stride;
+        if (owner >= a.r.n_requests) {  // (uniform over the cluster: its CTAs have the same rows)
+            continue;
         }
         const T* src = (const T*)a.logits + (int64_t)row * a.stride;
-        const int before = (int)(((uintptr_t)src & 15u) / sizeof(T));
-        const int first = lo - before, stop = min(lo + a.slice - before, vocab);  // this CTA's tokens: [max(first, 0), stop)
-        const int words = (vocab + 31) / 32;
-        // token x0 + i of a chunk is there
+        const int first = lo - (int)(((uintptr_t)src & 15u) / sizeof(T)), stop = min(first + a.slice, vocab);  // this CTA's tokens: [max(first, 0), stop)
         auto inside = [&](int x) { return x >= 0 && x < vocab; };
-        auto load = [&](int x0, Chunk<T>& c) {
-            if (x0 >= 0 && x0 + 8 <= vocab) {
+        auto whole = [&](int x) { return x >= 0 && x + 8 <= vocab; };
+        auto load = [&](int x0, Chunk<T>& c) {  // (what is outside the row is -inf)
+            if (whole(x0)) {
 #pragma unroll
-                for (int i = 0; i < 8 / V; ++i) c.u[i] = __ldcg(reinterpret_cast<const uint4*>(src + x0) + i);
+                for (int i = 0; i < kParts; ++i) c.u[i] = __ldcg(reinterpret_cast<const uint4*>(src + x0) + i);
             } else {
                 float f[8];
 #pragma unroll
@@ -217,68 +229,190 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
                 c.put(f);
             }
         };
-        auto bits8 = [&](const uint32_t* w, int n_words, int x) -> uint32_t {  // bits x .. x + 7, x >= 0
-            const int i = x / 32, s = x % 32;
-            uint32_t u = i < n_words ? w[i] : 0u;
-            if (s > 24 && i + 1 < n_words) return __funnelshift_r(u, w[i + 1], s) & 255u;
-            return (u >> s) & 255u;
+        // what the row and its request have, asked for at once
+        if (kRules && fresh) {
+            const int b = a.r.bias_of ? __ldcg(a.r.bias_of + owner) : 0;
+            if (a.counted) {
+                again = a.r.repetition ? __ldcg(a.r.repetition + owner) : 1.f;
+                often = a.r.frequency ? __ldcg(a.r.frequency + owner) : 0.f;
+                once = a.r.presence ? __ldcg(a.r.presence + owner) : 0.f;
+                said = a.r.history ? __ldcg(a.r.history_len + owner) : 0;
+                prompt = a.r.prompt_len ? __ldcg(a.r.prompt_len + owner) : 0;
+            }
+            bias = a.r.bias && b >= 0 && b < a.r.n_bias ? a.r.bias + (int64_t)b * a.r.bias_stride : nullptr;
+        }
+        const uint32_t* allowed = nullptr;
+        if (kRules && a.r.allowed) {
+            const int m = a.r.allowed_of ? __ldcg(a.r.allowed_of + row) : row;
+            if (m >= 0 && m < a.r.n_allowed) allowed = a.r.allowed + (int64_t)m * a.r.allowed_stride;
+        }
+        // (from the word on that holds token lo - 8; what lies before the row's first word is not there)
+        const int word0 = (lo - 8) >> 5;
+        if (allowed) {
+            for (int i = max(word0, 0) + tid; i <= (stop - 1) / 32; i += kLogitThreads) copy4(s_show + i - word0, allowed + i);
+        }
+        if (kRules && a.counted && fresh) {
+            __syncthreads();  // (the counts of the row before are no longer read)
+            for (int i = tid; i < n_words; i += kLogitThreads) s_bits[i] = 0u;
+            old = -1;
+            __syncthreads();
+            if (a.r.history) history(owner, [&](int p, bool) { atomicOr(s_bits + p / 32, 1u << p % 32); });
+            if (a.r.tokens)
+                for (int j = tid; j < reach(); j += kLogitThreads) {
+                    const int p = place(__ldcg(a.r.tokens + start + j));
+                    if (p >= 0) atomicOr(s_bits + p / 32, 1u << p % 32);
+                }
+            __syncthreads();
+            // bits before each four words: each thread's words, then the threads'
+            const int n_fours = n_words / 4, each = (n_fours + kLogitThreads - 1) / kLogitThreads, w0 = min(tid * each, n_fours), w1 = min(w0 + each, n_fours);
+            auto bits_of = [&](int w) {
+                const uint4 u = fours[w];
+                return __popc(u.x) + __popc(u.y) + __popc(u.z) + __popc(u.w);
+            };
+            int mine = 0;
+            for (int w = w0; w < w1; ++w) mine += bits_of(w);
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            if (lane == 31) s_scan[warp] = upto;
+            __syncthreads();
+            int at = upto - mine, all = 0;
+            for (int w = 0; w < kLogitWarps; ++w) {
+                if (w < warp) at += s_scan[w];
+                all += s_scan[w];
+            }
+            for (int w = w0; w < w1; ++w) {
+                s_before[w] = (uint32_t)at;
+                at += bits_of(w);
+            }
+            for (int i = tid; i < all; i += kLogitThreads) s_count[i] = 0u;
+            __syncthreads();
+            if (a.r.history)
+                history(owner, [&](int p, bool prompt) {
+                    if (prompt) atomicOr(s_count + count_of(p), kPrompt);
+                    else atomicAdd(s_count + count_of(p), 1u);
+                });
+        }
+        if (kRules && a.counted && a.r.tokens) {
+            __syncthreads();  // (history counted; the row before read)
+            if (old >= 0) nodes(old, ~0u);
+            nodes(row, 1u);
+            old = row;
+        }
+        if (allowed) copies_wait();
+        if (a.counted || allowed) __syncthreads();
+        auto bits8 = [&](const uint32_t* w, int x) -> uint32_t {  // bits x .. x + 7 (of the next word, too, which is always there)
+            return __funnelshift_r(w[x / 32u], w[x / 32u + 1], x % 32u) & 255u;
         };
-        auto rules = [&](int x0, float (&f)[8]) {
+        // the 8 bits of a chunk's tokens in the row's mask; 0: nothing of it is left
+        auto shown = [&](int x0) -> uint32_t { return allowed ? bits8(s_show, x0 - 32 * word0) : 255u; };
+        auto load_bias = [&](int x, float4* add) {
+            if (!bias) return;
+            if (whole(x) && ((uintptr_t)(bias + x) & 15u) == 0) {
+                add[0] = __ldcg(reinterpret_cast<const float4*>(bias + x)), add[1] = __ldcg(reinterpret_cast<const float4*>(bias + x) + 1);
+            } else {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = inside(x + j) ? __ldcg(bias + x + j) : 0.f;
+                add[0] = make_float4(v[0], v[1], v[2], v[3]), add[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        };
+        auto rules = [&](int x0, uint32_t show, const float4* add, float (&f)[8]) {
             if (a.counted) {
                 const int at = x0 - lo + 8;  // >= 0
-                uint32_t m = bits8(s_said, (width + 31) / 32, at);
-                while (m) {
-                    const int i = __ffs((int)m) - 1;
-                    m &= m - 1;
-                    const uint32_t n = s_count[at + i], c = n & ~kPrompt;
-                    float l = f[0];
+                const uint32_t m = bits8(s_bits, at);
+                if (m) {
+                    const uint32_t* counts = s_count + count_of(at);  // of the chunk's said tokens, one behind the other
 #pragma unroll
-                    for (int j = 1; j < 8; ++j) l = i == j ? f[j] : l;
-                    l = l > 0.f ? __fdiv_rn(l, again) : __fmul_rn(l, again);
-                    l = __fsub_rn(l, __fmul_rn(often, (float)c));
-                    if (c) l = __fsub_rn(l, once);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = i == j ? l : f[j];
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t n = m >> j & 1u ? counts[__popc(m & ((1u << j) - 1u))] : 0u, c = n & ~kPrompt;
+                        if (!n) continue;  // (not said, or by another node only)
+                        const float l = __fsub_rn(f[j] > 0.f ? __fdiv_rn(f[j], again) : __fmul_rn(f[j], again), __fmul_rn(often, (float)c));
+                        f[j] = c ? __fsub_rn(l, once) : l;
+                    }
                 }
             }
             if (bias) {
-                if (x0 >= 0 && x0 + 8 <= vocab && ((uintptr_t)(bias + x0) & 15u) == 0) {
-                    const float4 u = __ldcg(reinterpret_cast<const float4*>(bias + x0)), w = __ldcg(reinterpret_cast<const float4*>(bias + x0 + 4));
-                    f[0] += u.x, f[1] += u.y, f[2] += u.z, f[3] += u.w, f[4] += w.x, f[5] += w.y, f[6] += w.z, f[7] += w.w;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (inside(x0 + i)) f[i] += __ldcg(bias + x0 + i);
-                }
+                const float4 u = add[0], w = add[1];
+                f[0] += u.x, f[1] += u.y, f[2] += u.z, f[3] += u.w, f[4] += w.x, f[5] += w.y, f[6] += w.z, f[7] += w.w;
             }
-            if (allowed) {
-                const int x = max(x0, 0);
-                const int i = x / 32, s = x % 32;
-                uint32_t u = __ldcg(allowed + i) >> s;
-                if (s > 24 && i + 1 < words) u |= __ldcg(allowed + i + 1) << (32 - s);
-                u <<= x - x0;
+            if (show != 255u) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = u >> j & 1u ? f[j] : -INFINITY;
+                for (int j = 0; j < 8; ++j) f[j] = show >> j & 1u ? f[j] : -INFINITY;
             }
         };
-        if constexpr (!kChoose) {
-            T* out = (T*)a.out + (int64_t)row * a.out_stride;
-            for (int x = first + 8 * tid; x < stop; x += 8 * kLogitThreads * kAhead) {
-                Chunk<T> c[kAhead];
+        // choose: the largest logit of the thread, its chunk, and the sum of exp(logit - ref)
+        float best = -INFINITY, ref = -INFINITY, sum = 0.f;
+        int at = 0x7fffffff;
+        Chunk<T> kept;
+        T* out = kChoose ? nullptr : (T*)a.out + (int64_t)row * a.out_stride;
+        for (int x = first + 8 * tid; x < stop; x += 8 * kLogitThreads * kAhead) {
+            Chunk<T> c[kAhead];
+            float4 add[2];
+            uint32_t show[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-                    if (x + 8 * kLogitThreads * i < stop) load(x + 8 * kLogitThreads * i, c[i]);
+            for (int i = 0; i < kAhead; ++i) {
+                const int x0 = x + 8 * kLogitThreads * i;
+                show[i] = x0 < stop ? kRules ? shown(x0) : 255u : 0u;
+                if (show[i]) {
+                    load(x0, c[i]);
+                    if (kRules && i == 0) load_bias(x0, add);
+                }
+            }
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const int x0 = x + 8 * kLogitThreads * i;
+            for (int i = 0; i < kAhead; ++i) {
+                const int x0 = x + 8 * kLogitThreads * i;
+                float f[8];
+                if constexpr (kChoose) {
+                    if (show[i]) {
+                        c[i].get(f);
+                        if (kRules) rules(x0, show[i], add, f);
+                    }
+                    if (kRules && i + 1 < kAhead && show[(i + 1) % kAhead]) load_bias(x0 + 8 * kLogitThreads, add);
+                    if (!show[i]) continue;
+                    // (fmaxf passes NaN over)
+                    const float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+                    if (top > best) {
+                        best = top, at = x0;
+                        if (!kRules) kept = c[i];
+                    }
+                    if (top > ref) {
+                        const float up = ceilf(top);
+                        sum *= exp2_of((ref - up) * kLog2e);
+                        ref = up;
+                    }
+                    if (!(top > -INFINITY)) continue;
+                    uint64_t e2 = 0ull;
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float2 d = of_pair(mul_pair(add_pair(pair_of(f[j], f[j + 1]), pair_of(-ref, -ref)), pair_of(kLog2e, kLog2e)));
+                        e2 = add_pair(e2, pair_of(exp2_of(d.x), exp2_of(d.y)));
+                    }
+                    const float2 e = of_pair(e2);
+                    float s = e.x + e.y;
+                    if (!(s < 16.f)) {  // (infinite or NaN among them)
+                        s = 0.f;
+                        for (int j = 0; j < 8; ++j)
+                            if (f[j] == f[j]) s += weight(f[j], ref);
+                    }
+                    sum += s;
+                } else {
                     if (x0 >= stop) break;
-                    float f[8];
-                    c[i].get(f);
-                    rules(x0, f);
-                    if (x0 >= 0 && x0 + 8 <= vocab && ((uintptr_t)(out + x0) & 15u) == 0) {
+                    if (show[i]) {
+                        c[i].get(f);
+                        rules(x0, show[i], add, f);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[j] = -INFINITY;
+                    }
+                    if (i + 1 < kAhead && show[(i + 1) % kAhead]) load_bias(x0 + 8 * kLogitThreads, add);
+                    if (whole(x0) && ((uintptr_t)(out + x0) & 15u) == 0) {
                         c[i].put(f);
 #pragma unroll
-                        for (int j = 0; j < 8 / V; ++j) reinterpret_cast<uint4*>(out + x0)[j] = c[i].u[j];
+                        for (int j = 0; j < kParts; ++j) reinterpret_cast<uint4*>(out + x0)[j] = c[i].u[j];
                     } else {
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
@@ -286,49 +420,21 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
                     }
                 }
             }
+        }
+        if constexpr (!kChoose) {
+            if (a.counted || a.r.allowed) __syncthreads();  // (masks and counts are read)
         } else {
-            // NaN and what is not there count as -inf
-            auto taken = [&](int x0, float (&f)[8]) {
-                rules(x0, f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = (inside(x0 + j) && f[j] == f[j]) ? f[j] + 0.f : -INFINITY;
-            };
-            float best = -INFINITY, sum = 0.f;
-            int token = 0x7fffffff;
-            for (int x = first + 8 * tid; x < stop; x += 8 * kLogitThreads * kAhead) {
-                Chunk<T> c[kAhead];
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-                    if (x + 8 * kLogitThreads * i < stop) load(x + 8 * kLogitThreads * i, c[i]);
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const int x0 = x + 8 * kLogitThreads * i;
-                    if (x0 >= stop) break;
-                    float f[8];
-                    c[i].get(f);
-                    taken(x0, f);
-                    const float was = best;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (f[j] > best) best = f[j], token = x0 + j;
-                    if (best > -INFINITY) {
-                        sum *= weight(was, best);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) sum += weight(f[j], best);
-                    }
-                }
-            }
-            // the CTA's maximum and sum of weights
-            const float m_w = warp_max(best);
-            const float s_w = warp_sum(best > -INFINITY ? sum * weight(best, m_w) : 0.f);
+            // the CTA's reference and sum of weights
+            const float m_w = warp_max(ref);
+            const float s_w = warp_sum(ref > -INFINITY ? sum * weight(ref, m_w) : 0.f);
             if (lane == 0) s_m[warp] = m_w, s_s[warp] = s_w;
-            // each warp's k best of its threads, largest first
-            uint32_t mine = best > -INFINITY ? order_of(best) : 0u;
+            // each warp's k best of its threads, largest first, of equal ones the lowest chunk
+            uint32_t mine = best > -INFINITY ? order_of(best + 0.f) : 0u;
             for (int i = 0; i < a.k; ++i) {
                 const uint32_t o = __reduce_max_sync(0xffffffffu, mine);
-                const uint32_t t = __reduce_min_sync(0xffffffffu, mine == o ? (uint32_t)token : 0xffffffffu);
-                if (lane == 0) s_first[warp * a.k + i] = o ? (uint64_t)o << 32 | (uint32_t)~t : 0ull;
-                if (mine == o && (uint32_t)token == t) mine = 0u;
+                const int x = __reduce_min_sync(0xffffffffu, mine == o ? at : 0x7fffffff);
+                if (lane == 0) s_first[warp * a.k + i] = o ? (uint64_t)o << 32 | (uint32_t)~(x + 8) : 0ull;
+                if (mine == o && at == x) mine = 0u;
             }
             Partial& part = s_part[turn];
             turn ^= 1;
@@ -336,19 +442,33 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
             if (tid == 0) s_n = 0, s_found = 0, s_bound = 1ull;
             __syncthreads();
             const int lists = kLogitWarps * a.k;
-            if (tid < lists) {  // the k best threads, and the last of them as the bound
+            if (a.k == 1) {
+                uint64_t key = 0ull;
+#pragma unroll
+                for (int i = 0; i < kLogitWarps; ++i) key = max(key, s_first[i]);
+                if (key && at == (int)~(uint32_t)key - 8) {  // (this thread's chunk)
+                    float f[8];
+                    float4 add[2];
+                    if (kRules) {
+                        load(at, kept);
+                        load_bias(at, add);
+                    }
+                    kept.get(f);
+                    if (kRules) rules(at, shown(at), add, f);
+                    int token = at + 7;
+#pragma unroll
+                    for (int j = 6; j >= 0; --j) token = f[j] == best ? at + j : token;
+                    part.best[0] = key_of(best + 0.f, token);
+                }
+            } else if (tid < lists) {  // the k best threads, and the last of them as the bound
                 const uint64_t key = s_first[tid];
                 int rank = 0;
                 for (int i = 0; i < lists; ++i) rank += s_first[i] > key;
                 if (key && rank < a.k) {
-                    if (a.k == 1) {
-                        part.best[0] = key;
-                    } else {
-                        const int x = (int)~(uint32_t)key;
-                        s_from[rank] = (x - first) / 8 % kLogitThreads;
-                        if (rank == a.k - 1) s_bound = key;
-                        atomicAdd(&s_found, 1);
-                    }
+                    const int x = (int)~(uint32_t)key - 8;
+                    s_from[rank] = (x - first) / 8 % kLogitThreads;
+                    if (rank == a.k - 1) s_bound = key & ~0xffffffffull;  // (by the logit alone: the token lies somewhere in the chunk)
+                    atomicAdd(&s_found, 1);
                 }
             }
             if (warp == kLogitWarps - 1) {
@@ -358,20 +478,22 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
             }
             if (a.k > 1) {
                 __syncthreads();
-                const int chunks = a.slice / 8, deep = (chunks + kLogitThreads - 1) / kLogitThreads, n_from = s_found;
+                const int n_from = s_found;
                 const uint64_t bound = s_bound;
                 for (int i = tid; i < n_from * deep; i += kLogitThreads) {
                     const int x0 = first + 8 * (s_from[i % n_from] + i / n_from * kLogitThreads);
                     if (x0 >= stop) continue;
                     Chunk<T> c;
                     float f[8];
+                    float4 add[2];
                     load(x0, c);
+                    if (kRules) load_bias(x0, add);
                     c.get(f);
-                    taken(x0, f);
+                    if (kRules) rules(x0, shown(x0), add, f);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (f[j] > -INFINITY) {
-                            const uint64_t key = key_of(f[j], x0 + j);
+                            const uint64_t key = key_of(f[j] + 0.f, x0 + j);  // (0 and -0 are equal)
                             if (key >= bound) s_cand[atomicAdd(&s_n, 1)] = key;
                         }
                 }
@@ -388,11 +510,10 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
             // again after the next row's barrier, which its reader reaches when it has read.)
             if (split > 1) cluster_sync();
             else __syncthreads();
-            if (row % split == (int)blockIdx.x && warp < 1 + (kMaxSplit * kMaxBest) / 32) {
+            if (row % split == (int)blockIdx.x && warp < kJoinWarps) {
                 uint64_t* all = s_first;  // (its readers are behind a barrier)
                 const int n = split * a.k;
-                for (int i = tid; i < n; i += 32 * (1 + (kMaxSplit * kMaxBest) / 32))
-                    all[i] = split > 1 ? peer_load(&part.best[i % a.k], i / a.k) : part.best[i % a.k];
+                for (int i = tid; i < n; i += 32 * kJoinWarps) all[i] = split > 1 ? peer_load(&part.best[i % a.k], i / a.k) : part.best[i % a.k];
                 float m = -INFINITY, s = 0.f;
                 if (lane < split) {
                     const uint64_t u = split > 1 ? peer_load(&part.sum, lane) : part.sum;
@@ -400,8 +521,8 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
                 }
                 const float top = warp_max(m);
                 const float log_sum = logf(warp_sum(m > -INFINITY ? s * weight(m, top) : 0.f));
-                asm volatile("bar.sync 1, %0;\n" ::"n"(32 * (1 + (kMaxSplit * kMaxBest) / 32)) : "memory");
-                for (int i = tid; i < n; i += 32 * (1 + (kMaxSplit * kMaxBest) / 32)) {
+                asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kJoinWarps) : "memory");
+                for (int i = tid; i < n; i += 32 * kJoinWarps) {
                     const uint64_t key = all[i];
                     int rank = 0;
                     for (int j = 0; j < n; ++j) rank += all[j] > key || (all[j] == key && j < i);  // (only keys of 0 are equal)
@@ -419,14 +540,31 @@ __global__ void __launch_bounds__(kLogitThreads, 2) logits_kernel(const __grid_c
     if (kChoose && split > 1) cluster_sync();  // (no CTA leaves while another may read its part)
 }
 
-int smem_of(int slice) { return 4 * ((slice + 8 + 31) / 32 + slice + 8); }
+// lays dynamic shared memory out; returns its bytes.  Counts are kept for as many tokens as can be said in a slice.
+size_t lay_out(LogitArgs& a) {
+    const ssd_logit_rules& r = a.r;
+    const int deep = (a.slice / 8 + kLogitThreads - 1) / kLogitThreads;
+    a.at_show = a.k > 1 ? a.k * deep * 8 * 8 : 0;
+    a.at_bits = a.at_show + (r.allowed ? (a.slice / 32 + 3) * 4 : 0);
+    a.at_bits = (a.at_bits + 15) / 16 * 16;
+    a.n_words = (a.slice + 8 + 127) / 128 * 4;
+    if (!a.counted) return a.at_bits;
+    const long long said = (r.history ? r.max_history : 0ll) + (r.tokens ? r.n_rows : 0ll);
+    return a.at_bits + 4 * (a.n_words + a.n_words / 4 + 1 + (size_t)std::min<long long>(a.slice + 8, said));
+}
+constexpr int kMostShared = 180 * 1024;  // (a slice of 32832 tokens, all of them said: 18 + 4 + 140 KB)
 
 template <typename T>
 int set_up() {
-    const int most = smem_of(kMaxSlice);
-    cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(logits_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(logits_kernel<T, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     return (int)e;
+}
+
+template <typename T>
+cudaError_t start(const cudaLaunchConfig_t& cfg, const LogitArgs& a, bool choose) {
+    if (!choose) return cudaLaunchKernelEx(&cfg, logits_kernel<T, false, true>, a);
+    return a.counted || a.r.bias || a.r.allowed ? cudaLaunchKernelEx(&cfg, logits_kernel<T, true, true>, a) : cudaLaunchKernelEx(&cfg, logits_kernel<T, true, false>, a);
 }
 
 int check_rules(const char* call, const ssd_logit_rules* r, int dtype, const void* logits, int64_t stride) {
@@ -462,15 +600,16 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
         ready[dev][dtype] = 1;
     }
     a.counted = (r.repetition || r.presence || r.frequency) && (r.history || r.tokens);
-    // slices of at most 32768 tokens, and until there are two CTAs for an SM, of at least 2048
-    auto slice_of = [&](int split) { return ((r.vocab + 7 + split - 1) / split + 63) / 64 * 64; };
+    // slices
     int split = 1;
-    while (slice_of(split) > kMaxSlice) split *= 2;
-    while (split < kMaxSplit && (long long)r.n_rows * split < 304 && r.vocab > 2048 * split) split *= 2;
+    auto slice_of = [&](int n) { return ((r.vocab + 7 + n - 1) / n + 63) / 64 * 64; };
     a.slice = slice_of(split);
-    if (a.slice > kMaxSlice) a.slice = kMaxSlice;
-    // rows of a request share their counts: as many to a cluster as leaves two CTAs for an SM
-    a.rows = a.counted ? (int)std::min<long long>(r.max_rows, std::max(1ll, (long long)r.n_rows * split / 304)) : 1;
+    while (split < kMaxSplit && (a.slice > kMaxSlice || lay_out(a) > 56 * 1024 || ((long long)r.n_rows * split < 304 && r.vocab > 2048 * split))) {
+        split *= 2;
+        a.slice = slice_of(split);
+    }
+    // rows of a request share its counts, as many as leave two waves of CTAs
+    a.rows = a.counted ? (int)std::min<long long>(r.max_rows, std::max(1ll, (long long)r.n_rows * split / 912)) : 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)split, (unsigned)((r.n_rows + a.rows - 1) / a.rows), 1);
     if (cfg.gridDim.y > 65535u) {
@@ -478,7 +617,7 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
         cfg.gridDim.y = (unsigned)((r.n_rows + a.rows - 1) / a.rows);
     }
     cfg.blockDim = dim3(kLogitThreads, 1, 1);
-    cfg.dynamicSmemBytes = a.counted ? (size_t)smem_of(a.slice) : 0;
+    cfg.dynamicSmemBytes = lay_out(a);
     cfg.stream = (cudaStream_t)stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -487,14 +626,7 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     attr[1].val.clusterDim.x = (unsigned)split, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = choose && split > 1 ? 2 : 1;
-    cudaError_t e;
-    if (choose) {
-        e = dtype == SSD_F32 ? cudaLaunchKernelEx(&cfg, logits_kernel<float, true>, a) : dtype == SSD_F16 ? cudaLaunchKernelEx(&cfg, logits_kernel<f16, true>, a)
-                                                                                                          : cudaLaunchKernelEx(&cfg, logits_kernel<bf16, true>, a);
-    } else {
-        e = dtype == SSD_F32 ? cudaLaunchKernelEx(&cfg, logits_kernel<float, false>, a) : dtype == SSD_F16 ? cudaLaunchKernelEx(&cfg, logits_kernel<f16, false>, a)
-                                                                                                           : cudaLaunchKernelEx(&cfg, logits_kernel<bf16, false>, a);
-    }
+    const cudaError_t e = dtype == SSD_F32 ? start<float>(cfg, a, choose) : dtype == SSD_F16 ? start<f16>(cfg, a, choose) : start<bf16>(cfg, a, choose);
     return e == cudaSuccess ? SSD_OK : refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
 }
 
