@@ -153,7 +153,8 @@ def _load():
     lib.ssd_logits_adjust.argtypes = [LP, I, _VP, L, _VP, L, _VP]
     lib.ssd_logits_choose.argtypes = [LP, I, _VP, L, I, _VP, _VP, _VP, _VP]
     lib.ssd_moe_route.argtypes = [I, I, I, I, I, _VP, L, _VP, _VP, I, I, ctypes.c_float, _VP, _VP, _VP]
-    lib.ssd_moe_mlp.argtypes = [MP, I, I, _VP, L, _VP, _VP, _VP, L, _VP, L, _VP, ctypes.c_size_t, _VP]
+    lib.ssd_moe_mlp.argtypes = [MP, I, I, _VP, L, _VP, _VP, _VP, L, _VP, L, _VP, ctypes.c_size_t, _VP, _VP]
+    lib.ssd_debug_moe_stall.argtypes, lib.ssd_debug_moe_stall.restype = [I, ctypes.c_double], None
     lib.ssd_moe_workspace.argtypes = [MP, I, I, ctypes.POINTER(ctypes.c_size_t)]
     for n in OPERATOR_EXPORTS + STEP_EXPORTS:
         getattr(lib, n).restype = ctypes.c_int
@@ -624,9 +625,9 @@ def ssd_moe_workspace(experts: MoeWeights, n_rows: int, k: int) -> int:
     return n.value
 
 
-def ssd_moe_mlp(experts: MoeWeights, x, ids, weights, out, workspace, residual=None, cuda_stream: int | None = None) -> None:
+def ssd_moe_mlp(experts: MoeWeights, x, ids, weights, out, workspace, residual=None, status=None, cuda_stream: int | None = None) -> None:
     """out [n][d] = residual + the rows x [n][d] through their experts ids int32 [n][k], by weights fp32 [n][k].
-    workspace: a contiguous uint8 tensor."""
+    workspace: a contiguous uint8 tensor.  A wait that gave up is told by status int32 [1] alone, set to 0 before."""
     if x.dim() != 2 or ids.dim() != 2:
         _refuse("x [row][d] and ids [row][k] are wanted")
     n, k, d, t = x.shape[0], ids.shape[1], experts.device, experts.dtype
@@ -634,7 +635,15 @@ def ssd_moe_mlp(experts: MoeWeights, x, ids, weights, out, workspace, residual=N
                            _dev(weights, "weights", _of_type(weights, "weights", "torch.float32"), d, n * k),
                            *(_matrix(residual, "residual", d, t, n, experts.d) if residual is not None else (None, 0)),
                            *_matrix(out, "out", d, t, n, experts.d),
-                           _dev(workspace, "workspace", _of_type(workspace, "workspace", "torch.uint8"), d, workspace.numel()), workspace.numel(), cuda_stream))
+                           _dev(workspace, "workspace", _of_type(workspace, "workspace", "torch.uint8"), d, workspace.numel()), workspace.numel(),
+                           _dev(status, "status", _of_type(status, "status", "torch.int32"), d, 1), cuda_stream))
+
+
+def ssd_debug_moe_stall(cta: int, wait_limit_s: float = 0.01) -> None:
+    """Test hook: a CTA of the next ssd_moe_mlp call never asks for its weights, so its waits give up after wait_limit_s."""
+    if cta >= 0 and not 0.0 < wait_limit_s <= 10.0:
+        _refuse("ssd_debug_moe_stall: 0 < wait_limit_s <= 10 is wanted")
+    lib.ssd_debug_moe_stall(cta, wait_limit_s)
 
 
 def ssd_destroy(h: int) -> None:

@@ -1,9 +1,14 @@
 // step_moe.cu - a mixture-of-experts layer for the rows of a decoding step:
 // the router (ssd_moe_route) and the experts' products (ssd_moe_mlp) of ssd_step.h.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 
 #include "step_ops.cuh"
+#include "tc_gemm.cuh"
 
 namespace ssd {
 namespace step {
@@ -159,29 +164,28 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
 // ---------------------------------------------------------------------------
 // ssd_moe_mlp
 // ---------------------------------------------------------------------------
-constexpr int kMoeThreads = 256, kMoeWarps = kMoeThreads / 32;
-// rows of an expert that its weights are read for at once (MT: tiles of 16 weight rows in a warp)
-__host__ __device__ constexpr int group_of(int MT) { return MT == 1 ? 8 : 32; }
-constexpr int kMaxGroup = 32;
-constexpr int kChunk = 32;  // k of a chunk: 4 lanes have 16 bytes each of a row
+constexpr int kMoeWarps = 8;                         // that multiply; one more asks for weights
+constexpr int kMoeSums = 32 * kMoeWarps;
+constexpr int kChunk = 32;                           // k of a warp in a stage: 4 lanes have 16 bytes each of a row
+constexpr int kStageK = kChunk * kMoeWarps;
+constexpr double kWaitSeconds = 2.0, kClocksPerSecond = 2e9;
 
 struct MoeArgs {
-    const void *gate, *up, *down, *x, *residual;
+    const void *x, *residual;
     void* out;
     const int32_t* ids;
     const float* weights;
-    int64_t gate_stride, up_stride, down_stride, x_stride, residual_stride, out_stride;
-    void* h;             // [2][pair][f]: silu(gate x) * (up x) as hi + lo
-    float* y;            // [pair][d]: weights * down h
-    unsigned* arrived;   // [tile of d]: groups that have written their part of y
+    int64_t x_stride, residual_stride, out_stride;
+    void* h;   // [2][pair][f]: silu(gate x) * (up x) as hi + lo
+    float* y;  // [pair][part][d]: weights * down h over a part of f
     int n_rows, k, n_experts, d, f;
+    int parts;  // of f, each summed by a unit of its own
+    int up_depth, down_depth;  // stages of the rings
+    int32_t* status;
+    long long wait_clocks;
+    int stall;  // test hook: the CTA of the first kernel that asks for nothing (-1: none)
 };
 
-__device__ __forceinline__ uint4 load_weights(const void* p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, bf16) {
     mma_bf16_16816(d, a0, a1, a2, a3, b0, b1);
 }
@@ -192,307 +196,477 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint4 load_shared(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void tma3d(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(to), "l"(map), "r"(x), "r"(y),
+                 "r"(z), "r"(smem_u32(bar))
+                 : "memory");
+}
+// 16 bytes of a row; zeros and no access if not there
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+// arrives once this thread's copies so far have
+__device__ __forceinline__ void arrive_copies(uint64_t* b) { asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];\n" ::"r"(smem_u32(b)) : "memory"); }
+__device__ __forceinline__ void arrive(uint64_t* b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(b)) : "memory"); }
+// bounded wait; false after `limit` clocks, or once another thread of the CTA has given up
+__device__ __noinline__ bool mb_wait_on(uint64_t* b, unsigned parity, volatile int* fail, long long limit) {
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (!tc::mb_try(b, parity)) {
+        if (*fail) return false;
+        if (clock64() - t0 > limit) {
+            *fail = 1;
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool mb_wait(uint64_t* b, unsigned parity, volatile int* fail, long long limit) {
+    return tc::mb_try(b, parity) || mb_wait_on(b, parity, fail, limit);
+}
+__device__ __forceinline__ void sums_sync() { asm volatile("bar.sync 1, %0;\n" ::"n"(kMoeSums) : "memory"); }
 
-// The rows' experts, as every CTA of both kernels works them out for itself from ids: the (row, slot) pairs of an expert in
-// order, in groups of 8 or 32; a unit of work is a group and a tile of output rows.
-template <int kGroup>
+// The rows' experts, as every CTA of both kernels works them out for itself from ids: the (row, slot) pairs sorted by
+// expert, and groups of up to `size` pairs of one expert.
+__host__ __device__ inline int max_groups(int n_pairs, int n_experts, int size) { return (n_experts < n_pairs ? n_experts : n_pairs) + n_pairs / size; }
+struct Group {
+    int expert, first, n;  // pairs pairs[first ..]
+};
 struct Plan {
     int n_groups;
-    uint16_t* of_pair;  // [pair] expert, 0xffff: none
-    uint16_t* expert;   // [group]
-    uint16_t* first;    // [group] its number among its expert's groups
+    uint32_t* groups;  // expert << 21 | pairs << 15 | first
+    uint16_t* pairs;
+    __device__ __forceinline__ Group operator[](int i) const {
+        const uint32_t g = groups[i];
+        return {(int)(g >> 21), (int)(g & 0x7fffu), (int)(g >> 15 & 63u)};
+    }
 };
-__host__ __device__ inline int max_groups(int n_pairs, int n_experts, int size) { return (n_experts < n_pairs ? n_experts : n_pairs) + n_pairs / size; }
+static_assert(kMaxExperts <= 1 << 11 && kMaxMoeRows * kMaxSlots < 1 << 15, "a group in 32 bits");
 
-template <int kGroup>
-__device__ __forceinline__ Plan<kGroup> make_plan(const MoeArgs& a, unsigned char* smem, int* s_count, int* s_scan) {
-    const int tid = threadIdx.x, n = a.n_rows * a.k;
-    Plan<kGroup> p;
-    p.of_pair = reinterpret_cast<uint16_t*>(smem);
-    p.expert = p.of_pair + n;
-    p.first = p.expert + max_groups(n, a.n_experts, kGroup);
-    for (int e = tid; e < kMaxExperts; e += kMoeThreads) s_count[e] = 0;
+template <int kThreads>
+__device__ __forceinline__ Plan make_plan(const MoeArgs& a, int size, unsigned char* smem, int* s_count, int* s_scan) {
+    const int tid = threadIdx.x, lane = tid % 32, n = a.n_rows * a.k;
+    constexpr int kEach = kMaxExperts / kMoeSums;
+    Plan p;
+    p.groups = reinterpret_cast<uint32_t*>(smem);
+    p.pairs = reinterpret_cast<uint16_t*>(p.groups + max_groups(n, a.n_experts, size));
+    uint16_t* of_pair = p.pairs + n;  // experts, kMaxExperts: none
+    for (int e = tid; e < kMaxExperts; e += kThreads) s_count[e] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kMoeThreads) {
+    for (int i = tid; i < n; i += kThreads) {
         const int e = __ldcg(a.ids + i);
         const bool ok = e >= 0 && e < a.n_experts;
-        p.of_pair[i] = ok ? (uint16_t)e : (uint16_t)0xffff;
+        of_pair[i] = (uint16_t)(ok ? e : kMaxExperts);
         if (ok) atomicAdd(s_count + e, 1);
     }
     __syncthreads();
-    // groups of experts before: 4 experts a thread, summed over the warps
-    constexpr int kEach = kMaxExperts / kMoeThreads;
+    // groups and pairs of the experts before (groups in the upper half): 4 experts a thread, summed over the warps
     int mine[kEach], sum = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        mine[i] = (s_count[tid * kEach + i] + kGroup - 1) / kGroup;
-        sum += mine[i];
+        mine[i] = tid < kMoeSums ? s_count[tid * kEach + i] : 0;
+        sum += (mine[i] + size - 1) / size << 16 | mine[i];
     }
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
         const int v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (tid % 32 >= o) upto += v;
+        if (lane >= o) upto += v;
     }
-    if (tid % 32 == 31) s_scan[tid / 32] = upto;
+    if (lane == 31 && tid < kMoeSums) s_scan[tid / 32] = upto;
     __syncthreads();
     int at = upto - sum;
     p.n_groups = 0;
     for (int w = 0; w < kMoeWarps; ++w) {
         if (w < tid / 32) at += s_scan[w];
-        p.n_groups += s_scan[w];
+        p.n_groups += s_scan[w] >> 16;
     }
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        for (int g = 0; g < mine[i]; ++g, ++at) p.expert[at] = (uint16_t)(tid * kEach + i), p.first[at] = (uint16_t)g;
+    for (int i = 0; i < kEach; ++i) {
+        const int e = tid * kEach + i;
+        if (tid < kMoeSums) s_count[e] = at & 0xffff;  // (where its next pair goes)
+        for (int done = 0; done < mine[i]; done += size, at += 1 << 16)
+            p.groups[at >> 16] = (uint32_t)e << 21 | (uint32_t)min(size, mine[i] - done) << 15 | (uint32_t)((at & 0xffff) + done);
+        at += mine[i];
+    }
+    __syncthreads();
+    // one warp sorts, so that every CTA has the same order
+    if (tid < 32) {
+        for (int i = 0; i < n; i += 32) {
+            const int e = i + lane < n ? of_pair[i + lane] : kMaxExperts;
+            const bool ok = e < kMaxExperts;
+            const unsigned same = __match_any_sync(0xffffffffu, e);
+            const int before = __popc(same & ((1u << lane) - 1u));
+            const int to = ok ? s_count[e] + before : 0;
+            __syncwarp();
+            if (ok) p.pairs[to] = (uint16_t)(i + lane);
+            if (ok && before == 0) s_count[e] = to + __popc(same);
+            __syncwarp();
+        }
+    }
     __syncthreads();
     return p;
 }
 
-// warp 0: the pairs of a group, and how many
-template <int kGroup>
-__device__ __forceinline__ void find_pairs(const Plan<kGroup>& p, int n_pairs, int group, int* s_pairs, int* s_n) {
-    const int lane = threadIdx.x, e = p.expert[group], from = p.first[group] * kGroup;
-    int seen = 0;
-    for (int i = 0; i < n_pairs && seen < from + kGroup; i += 32) {
-        const bool is = i + lane < n_pairs && p.of_pair[i + lane] == e;
-        const unsigned m = __ballot_sync(0xffffffffu, is);
-        const int at = seen + __popc(m & ((1u << lane) - 1u)) - from;
-        if (is && at >= 0 && at < kGroup) s_pairs[at] = i + lane;
-        seen += __popc(m);
-    }
-    if (lane == 0) *s_n = min(seen - from, kGroup);
-}
-
-// Sums of a warp's MT tiles of 16 weight rows and NT tiles of 8 columns over k0 .. k1 (pieces of 8 past k1 count as zeros).
-// wp: this lane's two rows of each tile, xp: its column of each tile and plane, all at their lane % 4 th piece.  The k that a lane
-// holds go to the matrix instruction in an order of their own, the same for both operands, so that every load is 16
-// bytes straight into the fragments.  The next kAhead chunks of weights are under way while those before are multiplied:
-// 16 warps an SM of 4 KB each, which covers HBM's latency.
-template <typename T, int MT, int NT, int PL>
+// Both products: units (group, tile of output rows, part of k), a CTA each, in turns over the grid.  A stage is 256 k of a unit's
+// 32 or 64 weight rows (TMA boxes of 64 k, 128-byte swizzle, zeros past the ends of rows and matrices), in a ring that goes on over
+// the units: while the 8 warps of a CTA join their sums, the next unit's weights are on their way.  A warp multiplies its 32 k of
+// a stage.  Columns (PL planes each): up to 8 come from L2 straight to a warp's registers, a stage ahead, over the units' ends
+// too; more of them (64 weight rows then, so that they are read half as often) are copied into the ring by three warps, since a
+// stage ahead is too late (64 rows, 8 an expert: 1215 us, copied 990).  The k that
+// a lane holds go to the matrix instruction in an order of their own, the same for both operands, so that every operand is 16 bytes
+// in a row; lane group g has row (g / 2) + 4 (g mod 2) of 8, so that the 8 lanes that shared memory serves at once meet
+// different banks.  Bound by HBM: two CTAs have 192 KB of weights under way on an SM.
+//
+// kUp: h = silu(gate x) * (up x); a tile of 16 weight rows is 8 of gate and the same 8 of up, so that both sums of an output are in
+// one lane.  Else y = weights * (down h), h as two planes.
+template <typename T, int NT, bool kUp>
 struct Products {
-    static constexpr int kAhead = 4 / MT;
-    uint4 w[2][kAhead][MT][2];
-    __device__ __forceinline__ void load(int b, const T* const (&wp)[MT][2], int k, int k1) {
-        const int piece = threadIdx.x % 4 * 8;
+    static constexpr int kTiles = NT == 1 ? 2 : 4, kWeightRows = 16 * kTiles;
+    static constexpr int kBox = kWeightRows * 128, kStage = kStageK / 64 * kBox;  // 64 k of them; 16 or 32 KB
+    static constexpr int PL = kUp ? 1 : 2, kRows = kWeightRows / (kUp ? 2 : 1);   // output rows of a unit
+    static constexpr int kColumns = 8 * NT, kCtas = NT == 1 ? 2 : 1;              // of an SM
+    static constexpr bool kCopied = NT > 1;                                       // columns
+    static constexpr int kLoaders = kCopied ? 3 : 0, kThreads = kMoeSums + 32 + 32 * kLoaders;
+    static constexpr int kSums = kMoeWarps * kTiles * 32, kSumBuffers = NT == 1 ? 2 : 1;  // of the warps' sums
+    static constexpr int kColumnBox = kColumns * 128, kSlot = kStage + (kCopied ? PL * kStageK / 64 * kColumnBox : 0);
+    static constexpr int kDepth = kCopied ? 200 * 1024 / kSlot : 5;               // at most
+
+    static __device__ __forceinline__ void run(const MoeArgs& a, const CUtensorMap* map0, const CUtensorMap* map1, const Plan& p, uint32_t ring, float4* s_red, uint64_t* full,
+                                               uint64_t* empty, volatile int* s_fail) {
+        const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, parts = kUp ? 1 : a.parts;
+        const int K = kUp ? a.d : a.f, rows = kUp ? a.f : a.d, tiles = (rows + kRows - 1) / kRows;
+        const int units = p.n_groups * tiles * parts, stages = (K + kStageK - 1) / kStageK;
+        const int64_t plane = (int64_t)a.n_rows * a.k * a.f;
+        const int depth = kUp ? a.up_depth : a.down_depth;
+        bool ok = true;
+        auto begin_of = [&](int u) { return u % parts * stages / parts; };
+        auto end_of = [&](int u) { return (u % parts + 1) * stages / parts; };
+        if (warp == kMoeWarps) {
+            int n = 0;  // stages asked for
+            for (int u = kUp && a.stall == (int)blockIdx.x ? units : (int)blockIdx.x; u < units && ok; u += gridDim.x) {
+                const int rest = u / parts, row = rest % tiles * kRows, expert = p[rest / tiles].expert;
+                const int end = end_of(u);
+                for (int stage = begin_of(u); stage < end; ++stage, ++n) {
+                    const int slot = n % depth;
+                    if (n >= depth) ok = __all_sync(0xffffffffu, mb_wait(empty + slot, (unsigned)(n / depth - 1) & 1u, s_fail, a.wait_clocks));
+                    if (!ok) break;
+                    if (elect_one()) {
+                        tc::mb_arrive_tx(full + slot, kStage);
+                        const uint32_t to = ring + slot * kSlot;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                    w[b][i][m][r] = k + i * kChunk + piece < k1 ? load_weights(wp[m][r] + k + i * kChunk) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    __device__ __forceinline__ void multiply(int b, float (&acc)[MT][NT][4], const T* const (&xp)[PL][NT], int k, int k1) {
-        const int piece = threadIdx.x % 4 * 8;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (k + i * kChunk >= k1) break;
-            const bool in = k + i * kChunk + piece < k1;
-#pragma unroll
-            for (int l = 0; l < PL; ++l)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const uint4 x = in ? *reinterpret_cast<const uint4*>(xp[l][t] + k + i * kChunk) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        const uint4 &u = w[b][i][m][0], &v = w[b][i][m][1];
-                        mma(acc[m][t], u.x, v.x, u.y, v.y, x.x, x.y, T());
-                        mma(acc[m][t], u.z, v.z, u.w, v.w, x.z, x.w, T());
+                        for (int i = 0; i < kStageK / 64; ++i) {
+                            tma3d(to + i * kBox, map0, stage * kStageK + 64 * i, row, expert, full + slot);
+                            if (kUp) tma3d(to + i * kBox + kBox / 2, map1, stage * kStageK + 64 * i, row, expert, full + slot);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok || *s_fail) {  // copies in flight end before the CTA does
+                const long long t0 = clock64();
+                for (int i = max(0, n - depth); i < n; ++i)
+                    while (!tc::mb_try(full + i % depth, (unsigned)(i / depth) & 1u) && clock64() - t0 < 4000000ll) {
+                    }
+            }
+            return;
+        }
+        if (kCopied && warp > kMoeWarps) {
+            // copies columns, a row (512 bytes) at a time: lane l its 16 bytes number l, swizzled as the weights' boxes are
+            if (!kUp) pdl_wait();
+            const int loader = warp - kMoeWarps - 1;
+            const uint32_t to = ring + kStage + lane / 8 * kColumnBox;
+            int n = 0, group = -1, rows_here = 0;
+            unsigned long long row = 0;  // where the group's row number `lane` is
+            for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+                const int end = end_of(u);
+                if (u / parts / tiles != group) {
+                    group = u / parts / tiles;
+                    const Group q = p[group];
+                    rows_here = q.n;
+                    if (lane < q.n) {
+                        const int pair = p.pairs[q.first + lane];
+                        row = (unsigned long long)(kUp ? (const T*)a.x + (int64_t)(pair / a.k) * a.x_stride : (const T*)a.h + (int64_t)pair * a.f);
                     }
                 }
+                for (int stage = begin_of(u); stage < end; ++stage, ++n) {
+                    const int slot = n % depth, k = stage * kStageK + lane * 8;
+                    if (n >= depth) ok = __all_sync(0xffffffffu, mb_wait(empty + slot, (unsigned)(n / depth - 1) & 1u, s_fail, a.wait_clocks));
+                    if (!ok) break;
+                    const bool there = k < K;
+                    const uint32_t into = to + slot * kSlot;
+                    for (int i = loader; i < rows_here; i += kLoaders) {
+                        const T* x = (const T*)__shfl_sync(0xffffffffu, row, i) + (there ? k : 0);
+#pragma unroll
+                        for (int l = 0; l < PL; ++l) copy16(into + l * (kStageK / 64 * kColumnBox) + i * 128 + ((uint32_t)(lane ^ i) % 8) * 16, x + l * plane, there);
+                    }
+                    arrive_copies(full + slot);
+                }
+            }
+            asm volatile("cp.async.wait_all;\n" ::: "memory");
+            return;
         }
+        if (!kUp) pdl_wait();
+        const int g = lane / 4, piece = lane % 4 * 8, row_g = g / 2 + g % 2 * 4;
+        // the columns of the stage that comes next: its unit, number and k, and where this lane's are
+        int xu = blockIdx.x, xs = 0, x_end = 0;
+        const T* xp[NT];
+        auto aim = [&]() {
+            if (kCopied || xu >= units) return;
+            const Group q = p[xu / parts / tiles];
+            xs = begin_of(xu), x_end = end_of(xu);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int pair = p.pairs[q.first + min(8 * t + g, q.n - 1)];
+                xp[t] = (kUp ? (const T*)a.x + (int64_t)(pair / a.k) * a.x_stride : (const T*)a.h + (int64_t)pair * a.f) + xs * kStageK + warp * kChunk + piece;
+            }
+        };
+        auto load_columns = [&](uint4 (&x)[PL][NT]) {
+            if (kCopied || xu >= units) return;
+            if (xs * kStageK + kStageK <= K) {
+#pragma unroll
+                for (int l = 0; l < PL; ++l)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) x[l][t] = __ldcg(reinterpret_cast<const uint4*>(xp[t] + l * plane));
+            } else {  // (zeros past the end, as in the weights' boxes)
+                const bool there = xs * kStageK + warp * kChunk + piece < K;
+#pragma unroll
+                for (int l = 0; l < PL; ++l)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        x[l][t] = make_uint4(0u, 0u, 0u, 0u);
+                        if (there) x[l][t] = __ldcg(reinterpret_cast<const uint4*>(xp[t] + l * plane));
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) xp[t] += kStageK;
+            if (++xs == x_end) {
+                xu += gridDim.x;
+                aim();
+            }
+        };
+        // where this lane's 16 bytes of a row are in a box (swizzled), and its box in the stage
+        const uint32_t mine = ring + warp / 2 * kBox + row_g * 128 + ((uint32_t)(warp % 2 * 4 + lane % 4) ^ (uint32_t)row_g) * 16;
+        const uint32_t columns = ring + kStage + warp / 2 * kColumnBox + (mine - ring - warp / 2 * kBox);
+        int u = blockIdx.x, stage = begin_of(u), end = end_of(u), slot = 0;
+        unsigned phase = 0;
+        int buffer = 0, turn = 0;
+        float acc[kTiles][NT][4] = {};
+        // one stage: columns x, and those of the next one asked for; false after the last
+        auto one = [&](uint4 (&x)[PL][NT], uint4 (&next)[PL][NT]) {
+            load_columns(next);
+            ok = ok && __all_sync(0xffffffffu, mb_wait(full + slot, phase, s_fail, a.wait_clocks));
+            if (ok) {
+                uint4 w[kTiles][2];
+#pragma unroll
+                for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) w[m][r] = load_shared(mine + slot * kSlot + (kUp ? r * (kBox / 2) + m * 1024 : (2 * m + r) * 1024));
+                if (kCopied) {
+#pragma unroll
+                    for (int l = 0; l < PL; ++l)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) x[l][t] = load_shared(columns + slot * kSlot + l * (kStageK / 64 * kColumnBox) + t * 1024);
+                }
+#pragma unroll
+                for (int l = 0; l < PL; ++l)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int m = 0; m < kTiles; ++m) mma(acc[m][t], w[m][0].x, w[m][1].x, w[m][0].y, w[m][1].y, x[l][t].x, x[l][t].y, T());
+#pragma unroll
+                for (int l = 0; l < PL; ++l)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int m = 0; m < kTiles; ++m) mma(acc[m][t], w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w, x[l][t].z, x[l][t].w, T());
+            }
+            __syncwarp();
+            if (lane == 0) arrive(empty + slot);
+            if (++slot == depth) slot = 0, phase ^= 1u;
+            if (++stage < end) return true;
+            // the warps' sums, in order: [warp][tile][lane], one tile of columns after the other.  With one tile the buffers take turns,
+            // so that the warps that do not add go on (what they write next is read by then: there is a barrier in between).
+            const int part = u % parts, rest = u / parts, row0 = rest % tiles * kRows;
+            const Group q = p[rest / tiles];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float4* red = s_red + buffer * kSums;
+#pragma unroll
+                for (int m = 0; m < kTiles; ++m) red[(warp * kTiles + m) * 32 + lane] = make_float4(acc[m][t][0], acc[m][t][1], acc[m][t][2], acc[m][t][3]);
+                sums_sync();
+                const int m = (warp + turn) % kMoeWarps;  // (tiles go to other warps from unit to unit)
+                if (m < kTiles) {
+                    float4 v = red[m * 32 + lane];
+#pragma unroll
+                    for (int j = 1; j < kMoeWarps; ++j) {
+                        const float4 o = red[(j * kTiles + m) * 32 + lane];
+                        v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+                    }
+                    finish(a, p, q, row0 + m * (kUp ? 8 : 16) + row_g, rows, t * 8 + (kCopied ? lane % 4 : lane % 4 * 2), part, plane, v);
+                }
+                if (kSumBuffers == 1) sums_sync();
+                else buffer ^= 1;
+                turn += kTiles;
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) acc[i][t][0] = acc[i][t][1] = acc[i][t][2] = acc[i][t][3] = 0.f;
+            }
+            u += gridDim.x;
+            if (u >= units) return false;
+            stage = begin_of(u), end = end_of(u);
+            return true;
+        };
+        uint4 x0[PL][NT], x1[PL][NT];
+        if (u < units) {
+            aim();
+            load_columns(x0);
+            if (kCopied) {
+                while (one(x0, x0)) {
+                }
+            } else {
+                while (one(x0, x1) && one(x1, x0)) {
+                }
+            }
+        }
+        if (!ok && lane == 0) say(a.status, SSD_STATUS_TIMEOUT);
     }
-    __device__ __forceinline__ void run(float (&acc)[MT][NT][4], const T* const (&wp)[MT][2], const T* const (&xp)[PL][NT], int k0, int k1) {
-        constexpr int kStep = kAhead * kChunk;
-        load(0, wp, k0, k1);
-        for (int k = k0; k < k1; k += 2 * kStep) {
-            load(1, wp, k + kStep, k1);
-            multiply(0, acc, xp, k, k1);
-            load(0, wp, k + 2 * kStep, k1);
-            multiply(1, acc, xp, k + kStep, k1);
+
+    // sums of output rows `row` (up: of gate and up) and `row` + 8 (down), columns col and col + 1 (of copied columns: col + 4, in the order of row_g)
+    static __device__ __forceinline__ void finish(const MoeArgs& a, const Plan& p, const Group& q, int row, int rows, int col, int part, int64_t plane, const float4& v) {
+        constexpr int kNext = kCopied ? 4 : 1;
+        if (kUp) {
+            const float h[2] = {v.x / (1.f + expf(-v.x)) * v.z, v.y / (1.f + expf(-v.y)) * v.w};
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (row < rows && col + j * kNext < q.n) {
+                    T* to = (T*)a.h + (int64_t)p.pairs[q.first + col + j * kNext] * a.f + row;
+                    const T hi = (T)h[j];
+                    to[0] = hi;
+                    to[plane] = isfinite((float)hi) ? (T)(h[j] - (float)hi) : (T)0.f;
+                }
+        } else {
+            const float y[2][2] = {{v.x, v.y}, {v.z, v.w}};
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (col + j * kNext < q.n) {
+                    const int pair = p.pairs[q.first + col + j * kNext];
+                    const float w = __ldcg(a.weights + pair);
+                    float* to = a.y + ((int64_t)pair * a.parts + part) * a.d + row;
+                    if (row < rows) to[0] = w * y[0][j];
+                    if (row + 8 < rows) to[8] = w * y[1][j];
+                }
         }
     }
 };
 
-// h = silu(gate x) * (up x).  A tile of 16 weight rows is 8 of gate and the same 8 of up, so that both sums of an output are in
-// one lane.  The CTA's 8 warps take parts of d, added in order through shared memory.
-template <typename T, int MT, int NT>
-__device__ __forceinline__ void up_unit(const MoeArgs& a, int e, int f0, int n, const int* s_pairs, float4* s_red) {
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, piece = lane % 4 * 8;
-    const int chunks = (a.d + kChunk - 1) / kChunk, each = (chunks + kMoeWarps - 1) / kMoeWarps;
-    const T *wp[MT][2], *xp[1][NT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int64_t at = (int64_t)min(f0 + 8 * m + g, a.f - 1) * a.d + piece;
-        wp[m][0] = (const T*)a.gate + (int64_t)e * a.gate_stride + at;
-        wp[m][1] = (const T*)a.up + (int64_t)e * a.up_stride + at;
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) xp[0][t] = (const T*)a.x + (int64_t)(s_pairs[min(8 * t + g, n - 1)] / a.k) * a.x_stride + piece;
-    float acc[MT][NT][4] = {};
-    Products<T, MT, NT, 1> p;
-    p.run(acc, wp, xp, warp * each * kChunk, min((warp + 1) * each * kChunk, a.d));
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) s_red[((warp * MT + m) * NT + t) * 32 + lane] = make_float4(acc[m][t][0], acc[m][t][1], acc[m][t][2], acc[m][t][3]);
-    __syncthreads();
-    for (int i = tid; i < MT * NT * 32; i += kMoeThreads) {
-        float4 s = s_red[i];
-#pragma unroll
-        for (int w = 1; w < kMoeWarps; ++w) {
-            const float4 v = s_red[w * MT * NT * 32 + i];
-            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+// the ring's barriers, and the plan behind the ring
+template <typename P>
+__device__ __forceinline__ void set_barriers(uint64_t* full, uint64_t* empty, int* s_fail) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < P::kDepth; ++i) {
+            tc::mb_init(full + i, 1 + 32 * P::kLoaders);
+            tc::mb_init(empty + i, kMoeWarps);
         }
-        const int f = f0 + i / (NT * 32) * 8 + lane / 4, col = i / 32 % NT * 8 + lane % 4 * 2;
-        const float h[2] = {s.x / (1.f + expf(-s.x)) * s.z, s.y / (1.f + expf(-s.y)) * s.w};
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (f < a.f && col + j < n) {
-                T* to = (T*)a.h + (int64_t)s_pairs[col + j] * a.f + f;
-                const T hi = (T)h[j];
-                to[0] = hi;
-                to[(int64_t)a.n_rows * a.k * a.f] = isfinite((float)hi) ? (T)(h[j] - (float)hi) : (T)0.f;
-            }
+        *s_fail = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
 }
 
-template <typename T, int MT>
-__global__ void __launch_bounds__(kMoeThreads, 2) moe_up_kernel(const __grid_constant__ MoeArgs a) {
-    extern __shared__ __align__(16) unsigned char s_plan[];
-    __shared__ int s_count[kMaxExperts], s_scan[kMoeWarps], s_pairs[kMaxGroup], s_n;
-    __shared__ float4 s_red[kMoeWarps * MT * (group_of(MT) / 8) * 32];
+template <typename T, int NT>
+__global__ void __launch_bounds__(Products<T, NT, true>::kThreads, Products<T, NT, true>::kCtas)
+    moe_up_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ CUtensorMap gate, const __grid_constant__ CUtensorMap up) {
+    using P = Products<T, NT, true>;
+    extern __shared__ unsigned char s_dyn[];
+    __shared__ float4 s_red[P::kSumBuffers * P::kSums];
+    __shared__ uint64_t full[P::kDepth], empty[P::kDepth];
+    __shared__ int s_scan[kMoeWarps], s_fail;
+    static_assert(sizeof(s_red) >= kMaxExperts * sizeof(int), "a count for each expert");
+    const uint32_t pad = (1024u - smem_u32(s_dyn) % 1024u) % 1024u;
+    set_barriers<P>(full, empty, &s_fail);
     pdl_wait();
     pdl_launch_dependents();  // (only here: the next kernel reads ids before it waits)
-    const Plan<group_of(MT)> p = make_plan<group_of(MT)>(a, s_plan, s_count, s_scan);
-    const int tiles = (a.f + 8 * MT - 1) / (8 * MT);
-    for (int i = blockIdx.x * kMoeThreads + threadIdx.x; i < (a.d + 15) / 16; i += gridDim.x * kMoeThreads) a.arrived[i] = 0u;
-    int last = -1;
-    for (int64_t u = blockIdx.x; u < (int64_t)p.n_groups * tiles; u += gridDim.x) {
-        const int group = (int)(u / tiles), f0 = (int)(u % tiles) * 8 * MT;
-        if (group != last) {
-            __syncthreads();
-            if (threadIdx.x < 32) find_pairs(p, a.n_rows * a.k, group, s_pairs, &s_n);
-            last = group;
-        }
-        __syncthreads();  // (the sums of the unit before are read, too)
-        const int e = p.expert[group], n = s_n;
-        if (MT == 1 || n <= 8) up_unit<T, MT, 1>(a, e, f0, n, s_pairs, s_red);
-        else if (n <= 16) up_unit<T, MT, MT == 1 ? 1 : 2>(a, e, f0, n, s_pairs, s_red);
-        else up_unit<T, MT, MT == 1 ? 1 : 4>(a, e, f0, n, s_pairs, s_red);
-    }
+    const Plan p = make_plan<P::kThreads>(a, P::kColumns, s_dyn + pad + a.up_depth * P::kSlot, reinterpret_cast<int*>(s_red), s_scan);
+    P::run(a, &gate, &up, p, smem_u32(s_dyn) + pad, s_red, full, empty, &s_fail);
 }
 
-// y = weights * (down h), h as two planes
-template <typename T, int MT, int NT>
-__device__ __forceinline__ void down_unit(const MoeArgs& a, int e, int d0, int n, const int* s_pairs, float4* s_red, bool& waited) {
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, piece = lane % 4 * 8;
-    const int chunks = (a.f + kChunk - 1) / kChunk, each = (chunks + kMoeWarps - 1) / kMoeWarps;
-    const T *wp[MT][2], *xp[2][NT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) wp[m][r] = (const T*)a.down + (int64_t)e * a.down_stride + (int64_t)min(d0 + 16 * m + 8 * r + g, a.d - 1) * a.f + piece;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        xp[0][t] = (const T*)a.h + (int64_t)s_pairs[min(8 * t + g, n - 1)] * a.f + piece;
-        xp[1][t] = xp[0][t] + (int64_t)a.n_rows * a.k * a.f;
-    }
-    float acc[MT][NT][4] = {};
-    Products<T, MT, NT, 2> p;
-    if (!waited) {
-        pdl_wait();
-        waited = true;
-    }
-    p.run(acc, wp, xp, warp * each * kChunk, min((warp + 1) * each * kChunk, a.f));
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) s_red[((warp * MT + m) * NT + t) * 32 + lane] = make_float4(acc[m][t][0], acc[m][t][1], acc[m][t][2], acc[m][t][3]);
-    __syncthreads();
-    for (int i = tid; i < MT * NT * 32; i += kMoeThreads) {
-        float4 s = s_red[i];
-#pragma unroll
-        for (int w = 1; w < kMoeWarps; ++w) {
-            const float4 v = s_red[w * MT * NT * 32 + i];
-            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-        }
-        const int dim = d0 + i / (NT * 32) * 16 + lane / 4, col = i / 32 % NT * 8 + lane % 4 * 2;
-        const float v[2][2] = {{s.x, s.y}, {s.z, s.w}};
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (col + j < n) {
-                const int pair = s_pairs[col + j];
-                const float w = __ldcg(a.weights + pair);
-                float* y = a.y + (int64_t)pair * a.d;
-                if (dim < a.d) y[dim] = w * v[0][j];
-                if (dim + 8 < a.d) y[dim + 8] = w * v[1][j];
-            }
-    }
-}
-
-// The CTA that writes the last part of a tile of y adds the rows' slots in order, whoever wrote them.
-template <typename T, int MT>
-__global__ void __launch_bounds__(kMoeThreads, 2) moe_down_kernel(const __grid_constant__ MoeArgs a) {
-    extern __shared__ __align__(16) unsigned char s_plan[];
-    __shared__ int s_count[kMaxExperts], s_scan[kMoeWarps], s_pairs[kMaxGroup], s_n, s_last;
-    __shared__ float4 s_red[kMoeWarps * MT * (group_of(MT) / 8) * 32];
+template <typename T, int NT>
+__global__ void __launch_bounds__(Products<T, NT, false>::kThreads, Products<T, NT, false>::kCtas) moe_down_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ CUtensorMap down) {
+    using P = Products<T, NT, false>;
+    extern __shared__ unsigned char s_dyn[];
+    __shared__ float4 s_red[P::kSumBuffers * P::kSums];
+    __shared__ uint64_t full[P::kDepth], empty[P::kDepth];
+    __shared__ int s_scan[kMoeWarps], s_fail;
+    const uint32_t pad = (1024u - smem_u32(s_dyn) % 1024u) % 1024u;
+    set_barriers<P>(full, empty, &s_fail);
     pdl_launch_dependents();
-    // ids were complete before the kernel before this one let it start
-    const Plan<group_of(MT)> p = make_plan<group_of(MT)>(a, s_plan, s_count, s_scan);
-    constexpr int kTile = 16 * MT;
-    const int tiles = (a.d + kTile - 1) / kTile, groups = max(p.n_groups, 1);
-    bool waited = false;
-    int last = -1;
-    for (int64_t u = blockIdx.x; u < (int64_t)groups * tiles; u += gridDim.x) {
-        const int group = (int)(u / tiles), tile = (int)(u % tiles), d0 = tile * kTile;
-        if (p.n_groups) {
-            if (group != last) {
-                __syncthreads();
-                if (threadIdx.x < 32) find_pairs(p, a.n_rows * a.k, group, s_pairs, &s_n);
-                last = group;
-            }
-            __syncthreads();
-            const int e = p.expert[group], n = s_n;
-            if (MT == 1 || n <= 8) down_unit<T, MT, 1>(a, e, d0, n, s_pairs, s_red, waited);
-            else if (n <= 16) down_unit<T, MT, MT == 1 ? 1 : 2>(a, e, d0, n, s_pairs, s_red, waited);
-            else down_unit<T, MT, MT == 1 ? 1 : 4>(a, e, d0, n, s_pairs, s_red, waited);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) s_last = atomicAdd(a.arrived + tile, 1u) == (unsigned)p.n_groups - 1u;
-            __syncthreads();
-            if (!s_last) continue;
-            __threadfence();
-        } else if (!waited) {
-            pdl_wait();
-            waited = true;
-        }
-        const int width = min(kTile, a.d - d0);
-        for (int i = threadIdx.x; i < a.n_rows * width; i += kMoeThreads) {
-            const int row = i / width, dim = d0 + i % width;
-            float s = a.residual ? (float)((const T*)a.residual)[(int64_t)row * a.residual_stride + dim] : 0.f;
-            float t = 0.f;
-            for (int j = 0; j < a.k; ++j)
-                if (p.of_pair[row * a.k + j] != 0xffff) t += __ldcg(a.y + ((int64_t)row * a.k + j) * a.d + dim);
-            ((T*)a.out)[(int64_t)row * a.out_stride + dim] = (T)(s + t);
-        }
-    }
-    if (!waited) pdl_wait();
+    // ids were complete before the kernel before this one let it start; weights need not wait for h, and the warps that multiply do
+    const Plan p = make_plan<P::kThreads>(a, P::kColumns, s_dyn + pad + a.down_depth * P::kSlot, reinterpret_cast<int*>(s_red), s_scan);
+    P::run(a, &down, nullptr, p, smem_u32(s_dyn) + pad, s_red, full, empty, &s_fail);
 }
 
-size_t plan_bytes(int n_pairs, int n_experts, int size) { return 2 * ((size_t)n_pairs + 2 * (size_t)max_groups(n_pairs, n_experts, size)); }
+// out = residual + the rows' slots and their parts, in order
+constexpr int kSumThreads = 128, kSumAhead = 8;
+template <typename T>
+__global__ void __launch_bounds__(kSumThreads) moe_sum_kernel(const __grid_constant__ MoeArgs a) {
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ bool s_has[kMaxSlots];
+    const int row = blockIdx.y, dim = (blockIdx.x * kSumThreads + threadIdx.x) * 4;
+    if (threadIdx.x < a.k) {
+        const int e = __ldcg(a.ids + (int64_t)row * a.k + threadIdx.x);
+        s_has[threadIdx.x] = e >= 0 && e < a.n_experts;
+    }
+    __syncthreads();
+    if (dim >= a.d) return;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int n = a.k * a.parts;
+    const float* y = a.y + (int64_t)row * n * a.d + dim;
+    for (int i = 0; i < n; i += kSumAhead) {
+        float4 v[kSumAhead];
+#pragma unroll
+        for (int j = 0; j < kSumAhead; ++j) {
+            v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i + j < n && s_has[(i + j) / a.parts]) v[j] = __ldcg(reinterpret_cast<const float4*>(y + (int64_t)(i + j) * a.d));
+        }
+#pragma unroll
+        for (int j = 0; j < kSumAhead; ++j) s.x += v[j].x, s.y += v[j].y, s.z += v[j].z, s.w += v[j].w;
+    }
+    uint2 r = make_uint2(0u, 0u);
+    if (a.residual) r = __ldcg(reinterpret_cast<const uint2*>((const T*)a.residual + (int64_t)row * a.residual_stride + dim));
+    const float2 r0 = unpack2(r.x, T()), r1 = unpack2(r.y, T());
+    *reinterpret_cast<uint2*>((T*)a.out + (int64_t)row * a.out_stride + dim) = make_uint2(pack2(r0.x + s.x, r0.y + s.y, T()), pack2(r1.x + s.z, r1.y + s.w, T()));
+}
+
+// ssd_debug_moe_stall, for one call
+std::mutex g_stall_mu;
+int g_stall = -1;
+double g_stall_wait_s = 0.0;
+
+size_t plan_bytes(int n_pairs, int n_experts, int size) { return 4 * ((size_t)max_groups(n_pairs, n_experts, size) + (size_t)n_pairs); }
+
+// parts of f: until there are units of down for two waves of CTAs and more (as many experts met as can be), four stages each at least
+int parts_of(const ssd_moe& m, int n_rows, int k) {
+    const int64_t tiles = (m.d + 31) / 32, met = std::min(m.n_experts, n_rows * k);
+    int parts = 1;
+    while (parts < 8 && met * tiles * parts < 2000 && m.f >= 8 * kStageK * parts) parts *= 2;
+    return parts;
+}
 
 struct Workspace {
-    size_t h, y, total;  // offsets behind the counters, bytes
+    size_t y, total;  // offset behind h, bytes
 };
 Workspace workspace_of(const ssd_moe& m, int n_rows, int k) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t pairs = (size_t)n_rows * k;
     Workspace w;
-    w.h = up(4 * (((size_t)m.d + 15) / 16));
-    w.y = w.h + up(2 * 2 * pairs * m.f);
-    w.total = w.y + up(4 * pairs * m.d);
+    w.y = up(2 * 2 * pairs * m.f);
+    w.total = w.y + up(4 * pairs * (size_t)parts_of(m, n_rows, k) * m.d);
     return w;
 }
 
@@ -505,29 +679,62 @@ int check_experts(const char* call, const ssd_moe* m, int n_rows, int k) {
     return SSD_OK;
 }
 
-template <typename T>
-int launch_moe(const char* call, const MoeArgs& a, void* stream) {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+constexpr int kMostShared = 209 * 1024;  // dynamic; 17 KB are static
+
+// the experts' matrices [expert][rows][width] as {width, rows, experts}, box 64 x box_rows
+int encode(const char* call, CUtensorMap* m, const void* base, int dtype, int width, int rows, int n_experts, int64_t stride, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)n_experts};
+    const cuuint64_t strides[2] = {(cuuint64_t)width * 2, (cuuint64_t)(n_experts > 1 ? stride : (int64_t)width * rows) * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    const CUresult r = g_encode(m, dtype == SSD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box,
+                                step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SSD_OK : refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+template <typename T, int NT>
+int launch_moe(const char* call, MoeArgs& a, const ssd_moe& m, int sms, void* stream) {
+    using U = Products<T, NT, true>;
+    using D = Products<T, NT, false>;
     static bool ready[64] = {};  // (set once a device and type; setting it twice is harmless)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && !(dev < 64 && ready[dev])) {
-        // (static and dynamic shared memory may pass 48 KB together)
-        const int most = (int)plan_bytes(kMaxMoeRows * kMaxSlots, kMaxExperts, kMaxGroup);
-        e = cudaFuncSetAttribute(moe_up_kernel<T, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<T, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+        e = cudaFuncSetAttribute(moe_up_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+        if (e == cudaSuccess && (!fn || found != cudaDriverEntryPointSuccess)) return refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled unavailable");
+        if (e == cudaSuccess) g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
         if (e == cudaSuccess && dev < 64) ready[dev] = true;
     }
     if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
-    const size_t smem = plan_bytes(a.n_rows * a.k, a.n_experts, a.n_rows <= 8 ? group_of(1) : group_of(2));
-    const dim3 grid((unsigned)(2 * sms));
-    // up to 8 rows an expert has one tile of columns at most: tiles of 16 weight rows, more chunks under way
-    if (a.n_rows <= 8) {
-        if (int rc = launch(call, moe_up_kernel<T, 1>, grid, kMoeThreads, smem, stream, a)) return rc;
-        return launch(call, moe_down_kernel<T, 1>, grid, kMoeThreads, smem, stream, a);
-    }
-    if (int rc = launch(call, moe_up_kernel<T, 2>, grid, kMoeThreads, smem, stream, a)) return rc;
-    return launch(call, moe_down_kernel<T, 2>, grid, kMoeThreads, smem, stream, a);
+    CUtensorMap gate, up, down;
+    if (int rc = encode(call, &gate, m.gate, m.dtype, m.d, m.f, m.n_experts, m.gate_stride, U::kWeightRows / 2)) return rc;
+    if (int rc = encode(call, &up, m.up, m.dtype, m.d, m.f, m.n_experts, m.up_stride, U::kWeightRows / 2)) return rc;
+    if (int rc = encode(call, &down, m.down, m.dtype, m.f, m.d, m.n_experts, m.down_stride, D::kWeightRows)) return rc;
+    const int more = 1024 + (int)plan_bytes(a.n_rows * a.k, a.n_experts, 8 * NT);
+    a.up_depth = std::min((int)U::kDepth, (kMostShared - more) / U::kSlot);
+    a.down_depth = std::min((int)D::kDepth, (kMostShared - more) / D::kSlot);
+    const dim3 grid((unsigned)(U::kCtas * sms));
+    if (int rc = launch(call, moe_up_kernel<T, NT>, grid, U::kThreads, (size_t)(a.up_depth * U::kSlot + more), stream, a, gate, up)) return rc;
+    if (int rc = launch(call, moe_down_kernel<T, NT>, grid, D::kThreads, (size_t)(a.down_depth * D::kSlot + more), stream, a, down)) return rc;
+    return launch(call, moe_sum_kernel<T>, dim3((unsigned)((a.d + 4 * kSumThreads - 1) / (4 * kSumThreads)), (unsigned)a.n_rows), kSumThreads, 0, stream, a);
+}
+
+template <typename T>
+int start_moe(const char* call, MoeArgs& a, const ssd_moe& m, void* stream) {
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
+    a.parts = parts_of(m, a.n_rows, a.k);
+    // rows of an expert that its weights are read for at once: as many as it has on average, or all of a few
+    const int64_t pairs = (int64_t)a.n_rows * a.k;
+    if (a.n_rows <= 8 || pairs <= 4 * (int64_t)a.n_experts) return launch_moe<T, 1>(call, a, m, sms, stream);
+    if (a.n_rows <= 16 || pairs <= 12 * (int64_t)a.n_experts) return launch_moe<T, 2>(call, a, m, sms, stream);
+    return launch_moe<T, 4>(call, a, m, sms, stream);
 }
 
 }  // namespace step
@@ -535,6 +742,12 @@ int launch_moe(const char* call, const MoeArgs& a, void* stream) {
 
 using namespace ssd;
 using namespace ssd::step;
+
+extern "C" void ssd_debug_moe_stall(int cta, double wait_limit_s) {
+    std::lock_guard<std::mutex> lock(g_stall_mu);
+    g_stall = cta >= 0 && wait_limit_s > 0.0 && wait_limit_s <= 10.0 ? cta : -1;
+    g_stall_wait_s = wait_limit_s;
+}
 
 extern "C" int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k, const void* x, int64_t x_stride, const void* w_router,
                              const float* favour, int score, int renorm, float scale, int32_t* ids, float* weights, void* cuda_stream) {
@@ -591,7 +804,7 @@ extern "C" int ssd_moe_workspace(const ssd_moe* experts, int n_rows, int k, size
 
 extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void* x, int64_t x_stride, const int32_t* ids,
                            const float* weights, const void* residual, int64_t residual_stride, void* out, int64_t out_stride,
-                           void* workspace, size_t workspace_bytes, void* cuda_stream) {
+                           void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream) {
     static const char call[] = "ssd_moe_mlp";
     if (int rc = check_experts(call, experts, n_rows, k)) return rc;
     const ssd_moe& m = *experts;
@@ -617,12 +830,6 @@ extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void
     if (workspace_bytes < w.total) return refuse(SSD_ERR_CAPACITY, call, "the workspace needs %zu bytes", w.total);
     if (int rc = check_device(call, x)) return rc;
     MoeArgs a{};
-    a.gate = m.gate;
-    a.up = m.up;
-    a.down = m.down;
-    a.gate_stride = m.gate_stride;
-    a.up_stride = m.up_stride;
-    a.down_stride = m.down_stride;
     a.x = x;
     a.x_stride = x_stride;
     a.residual = residual;
@@ -631,13 +838,23 @@ extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void
     a.out_stride = out_stride;
     a.ids = ids;
     a.weights = weights;
-    a.arrived = (unsigned*)workspace;
-    a.h = (char*)workspace + w.h;
+    a.h = workspace;
     a.y = (float*)((char*)workspace + w.y);
     a.n_rows = n_rows;
     a.k = k;
     a.n_experts = m.n_experts;
     a.d = m.d;
     a.f = m.f;
-    return m.dtype == SSD_F16 ? launch_moe<f16>(call, a, cuda_stream) : launch_moe<bf16>(call, a, cuda_stream);
+    a.status = status;
+    a.wait_clocks = (long long)(kWaitSeconds * kClocksPerSecond);
+    a.stall = -1;
+    {
+        std::lock_guard<std::mutex> lock(g_stall_mu);
+        if (g_stall >= 0) {
+            a.stall = g_stall;
+            a.wait_clocks = (long long)(g_stall_wait_s * kClocksPerSecond);
+            g_stall = -1;
+        }
+    }
+    return m.dtype == SSD_F16 ? start_moe<f16>(call, a, m, cuda_stream) : start_moe<bf16>(call, a, m, cuda_stream);
 }

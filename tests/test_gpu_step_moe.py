@@ -247,6 +247,24 @@ def test_layers_behind_one_another_and_replayed(ssd):
     assert all(torch.equal(a, b) for a, b in zip(bufs, want))
 
 
+def test_a_wait_that_gives_up_is_told(ssd):
+    x = Layer(ssd, 12, "bf16", 5, 512, 264, 6, 3)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ssd.ssd_debug_moe_stall(1, 0.01)
+    ssd.ssd_moe_mlp(x.experts, x.x, x.ids, x.weights, x.out[:, :512], x.ws, residual=x.residual, status=status, cuda_stream=stream())
+    torch.cuda.synchronize()
+    assert status.item() == ssd.SSD_STATUS_TIMEOUT
+    status.zero_()
+    ssd.ssd_debug_moe_stall(1, 0.01)
+    ssd.ssd_debug_moe_stall(-1)
+    ssd.ssd_moe_mlp(x.experts, x.x, x.ids, x.weights, x.out[:, :512], x.ws, residual=x.residual, status=status, cuda_stream=stream())
+    x.check()
+    assert status.item() == 0
+    for bad in (0.0, 11.0):
+        with pytest.raises(ssd.SSDError):
+            ssd.ssd_debug_moe_stall(0, bad)
+
+
 def test_the_binding_refuses(ssd):
     x = Layer(ssd, 1, "f16", 3, 64, 40, 4, 2)
     for bad in (dict(x=x.x[:, :56]), dict(x=x.x.bfloat16()), dict(ids=x.ids.long()), dict(ids=x.ids[:2]), dict(weights=x.weights.half()), dict(out=x.out), dict(ws=x.ws[:-1]),

@@ -182,7 +182,7 @@ def moe(ssd, **kw):
 
 
 def mlp(ssd, m=None, **kw):
-    f = dict(n_rows=3, k=2, x=P, xs=64, ids=P, weights=P, residual=None, rs=0, out=FAR, os=64, ws=2 * FAR, wb=1 << 20, stream=None)
+    f = dict(n_rows=3, k=2, x=P, xs=64, ids=P, weights=P, residual=None, rs=0, out=FAR, os=64, ws=2 * FAR, wb=1 << 20, status=None, stream=None)
     f.update(kw)
     return ssd.lib.ssd_moe_mlp(m or moe(ssd), *f.values())
 
