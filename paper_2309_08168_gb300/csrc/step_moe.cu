@@ -18,8 +18,8 @@ constexpr int kMaxExperts = 1024, kMaxSlots = 16, kMaxMoeRows = 1024;
 // ---------------------------------------------------------------------------
 // ssd_moe_route
 // ---------------------------------------------------------------------------
-constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32, kRouteSplit = 8;
-constexpr int kRouteShare = kMaxExperts / kRouteSplit;  // experts of a CTA at most
+constexpr int kRouteThreads = 512, kRouteWarps = kRouteThreads / 32, kRouteSplit = 8;  // CTAs of a row at most, 2 at least
+constexpr int kRouteShare = kMaxExperts / 2;  // experts of a CTA at most
 
 struct RouteArgs {
     const void *x, *w;
@@ -38,24 +38,31 @@ __device__ __forceinline__ uint64_t order_of(double v) {
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// A cluster of 8 CTAs takes a row, each an eighth of the experts.  Which of two experts comes first must not hang on the order of a sum,
+// s + c += q without loss but in c
+__device__ __forceinline__ void add_exactly(float& s, float& c, float q) {
+    const float t = __fadd_rn(s, q), b = __fsub_rn(t, s);
+    c = __fadd_rn(c, __fadd_rn(__fsub_rn(s, __fsub_rn(t, b)), __fsub_rn(q, b)));
+    s = t;
+}
+
+// A cluster of CTAs (8 to 2) takes a row, each a share of the experts.  Which of two experts comes first must not hang on the order of a sum,
 // so the products (exact in fp32: two values of 8 or 11 bits) are added without loss to a pair of floats, 6 additions each
-// (Knuth's two-sum), and pairs are joined in fp64.  fp64 sums would be slower by an order: the chip has two fp64 units an SM.
+// (Knuth's two-sum), over lanes too; fp64 sums would be slower by an order, with two fp64 units an SM.
 // Scores decide by z itself where that is the same order, in fp64 where something is added to them.  The rank of an
-// expert is the number of better ones, counted by the CTA that has it; the winners go to the first CTA.
+// expert is the number of better ones, counted by a warp of the CTA that has it; the winners go to the first CTA.
 template <typename T>
-__global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_constant__ RouteArgs a) {
-    __shared__ double s_part[kRouteWarps * kRouteShare];  // [warp of an expert][expert]
+__global__ void __launch_bounds__(kRouteThreads, 2) route_kernel(const __grid_constant__ RouteArgs a) {
+    __shared__ float2 s_part[kRouteShare];  // [warp of an expert][expert], with more than one warp for up to 8 experts
     __shared__ double s_z[kRouteShare];
     __shared__ uint64_t s_key[kRouteShare], s_all[kMaxExperts];
     __shared__ double s_top[kMaxSlots];  // the winners' z and expert, in the first CTA
     __shared__ uint64_t s_who[kMaxSlots], s_stat[kRouteSplit];
     pdl_launch_dependents();
     pdl_wait();
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = blockIdx.x, row = blockIdx.y;
-    const int share = (a.n_experts + kRouteSplit - 1) / kRouteSplit, e0 = min(rank * share, a.n_experts), mine = min(share, a.n_experts - e0);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = blockIdx.x, row = blockIdx.y, split = gridDim.x;
+    const int share = (a.n_experts + split - 1) / split, e0 = min(rank * share, a.n_experts), mine = min(share, a.n_experts - e0);
     // warps of an expert, each a part of d
-    const int per = share <= 1 ? 8 : share <= 2 ? 4 : share <= 4 ? 2 : 1, part = warp % per;
+    const int per = share <= 2 ? 8 : share <= 4 ? 4 : share <= 8 ? 2 : 1, part = warp % per;
     const int pieces = a.d / 8, p0 = (int)((int64_t)pieces * part / per), p1 = (int)((int64_t)pieces * (part + 1) / per);
     const uint4* x = reinterpret_cast<const uint4*>((const T*)a.x + (int64_t)row * a.x_stride);
     for (int e = warp / per; e < mine; e += kRouteWarps / per) {
@@ -75,23 +82,26 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
                 Vec<T>::get(u[i], f);
                 Vec<T>::get(v[i], g);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float q = __fmul_rn(f[j], g[j]), t = __fadd_rn(s, q), b = __fsub_rn(t, s);
-                    c = __fadd_rn(c, __fadd_rn(__fsub_rn(s, __fsub_rn(t, b)), __fsub_rn(q, b)));
-                    s = t;
-                }
+                for (int j = 0; j < 8; ++j) add_exactly(s, c, __fmul_rn(f[j], g[j]));
             }
         }
-        double z = isfinite(s) ? (double)s + (double)c : (double)s;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (lane == 0) s_part[part * kRouteShare + e] = z;
+        for (int o = 16; o > 0; o >>= 1) {
+            const float q = __shfl_xor_sync(0xffffffffu, s, o), r = __shfl_xor_sync(0xffffffffu, c, o);
+            add_exactly(s, c, q);
+            c = __fadd_rn(c, r);
+        }
+        if (lane == 0) s_part[part * share + e] = make_float2(s, c);
     }
     __syncthreads();
     for (int e = tid; e < mine; e += kRouteThreads) {
-        double z = 0.0;
-        for (int i = 0; i < per; ++i) z += s_part[i * kRouteShare + e];
-        s_z[e] = z;
+        float2 v = s_part[e];
+        for (int i = 1; i < per; ++i) {
+            const float2 o = s_part[i * share + e];
+            add_exactly(v.x, v.y, o.x);
+            v.y = __fadd_rn(v.y, o.y);
+        }
+        s_z[e] = isfinite(v.x) ? (double)v.x + (double)v.y : (double)v.x;
     }
     __syncthreads();
     // softmax over all experts where the scores or the weights need it: the row's maximum and sum
@@ -103,11 +113,11 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
             for (int e = lane; e < mine; e += 32) m = fmax(m, s_z[e]);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-            if (lane < kRouteSplit) peer_store(&s_stat[rank], lane, (uint64_t)__double_as_longlong(m));
+            if (lane < split) peer_store(&s_stat[rank], lane, (uint64_t)__double_as_longlong(m));
         }
         cluster_sync();
         m = -INFINITY;
-        for (int i = 0; i < kRouteSplit; ++i) m = fmax(m, __longlong_as_double((long long)s_stat[i]));
+        for (int i = 0; i < split; ++i) m = fmax(m, __longlong_as_double((long long)s_stat[i]));
         double sum = 0.0;
         if (warp == 0) {
             for (int e = lane; e < mine; e += 32) sum += exp(s_z[e] - m);
@@ -115,10 +125,10 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         }
         cluster_sync();  // (the maxima are read)
-        if (warp == 0 && lane < kRouteSplit) peer_store(&s_stat[rank], lane, (uint64_t)__double_as_longlong(sum));
+        if (warp == 0 && lane < split) peer_store(&s_stat[rank], lane, (uint64_t)__double_as_longlong(sum));
         cluster_sync();
         sum = 0.0;
-        for (int i = 0; i < kRouteSplit; ++i) sum += __longlong_as_double((long long)s_stat[i]);
+        for (int i = 0; i < split; ++i) sum += __longlong_as_double((long long)s_stat[i]);
         for (int e = tid; e < mine; e += kRouteThreads) {
             const double p = exp(s_z[e] - m) / sum;
             s_z[e] = p;  // (from here on the score)
@@ -133,11 +143,12 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
     cluster_sync();
     for (int e = tid; e < a.n_experts; e += kRouteThreads) s_all[e] = peer_load(&s_key[e % share], e / share);
     __syncthreads();
-    for (int e = tid; e < mine; e += kRouteThreads) {
+    for (int e = warp; e < mine; e += kRouteWarps) {
         const uint64_t key = s_key[e];
         int better = 0;
-        for (int i = 0; i < a.n_experts; ++i) better += s_all[i] > key || (s_all[i] == key && i < e0 + e);
-        if (better < a.k) {
+        for (int i = lane; i < a.n_experts; i += 32) better += s_all[i] > key || (s_all[i] == key && i < e0 + e);
+        better = __reduce_add_sync(0xffffffffu, better);
+        if (better < a.k && lane == 0) {
             peer_store(&s_top[better], 0, (uint64_t)__double_as_longlong(s_z[e]));
             peer_store(&s_who[better], 0, (uint64_t)(e0 + e));
         }
@@ -780,14 +791,17 @@ extern "C" int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k,
     a.renorm = renorm;
     a.scale = scale;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kRouteSplit, (unsigned)n_rows, 1);
+    // as many CTAs a row as are there at once, two an SM
+    unsigned split = kRouteSplit;
+    while (split > 2 && (long long)n_rows * split > 304) split /= 2;
+    cfg.gridDim = dim3(split, (unsigned)n_rows, 1);
     cfg.blockDim = dim3(kRouteThreads, 1, 1);
     cfg.stream = (cudaStream_t)cuda_stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kRouteSplit, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = split, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     const cudaError_t e = dtype == SSD_F16 ? cudaLaunchKernelEx(&cfg, route_kernel<f16>, a) : cudaLaunchKernelEx(&cfg, route_kernel<bf16>, a);
