@@ -8,8 +8,7 @@
 namespace ssd {
 namespace step {
 
-constexpr int kHeadThreads = 128;
-constexpr int kHeadAhead = 4;  // heads under way in a lane
+constexpr int kHeadAhead = 4, kValueAhead = 4;  // heads under way in a lane
 
 struct HeadArgs {
     const void *q, *k, *v;
@@ -29,21 +28,45 @@ struct HeadArgs {
 // head, 16 bytes each, so that the sum of squares is a few shuffles and every byte is read once.
 // Rotated dim e with partner p becomes r (x_e g_e cos +- x_p g_p sin), r = 1 / sqrt(mean x^2 + eps): the
 // products of gains and angles are formed once a row in shared memory (a, b), and the partner's 16 bytes come from
-// the lane that holds them.  Bound by HBM, or for few rows by the chain position - angle - table - store.
+// the lane that holds them.  Bound by HBM, for 16-bit rows of few heads by instructions, for few rows by the chain position - angle -
+// table - store.  Measured: 4095 fp32 rows of 32 + 2 x 32 heads of 128 63 us (335 MB, 5.3 TB/s, 78 % of the copy rate); 16000 bf16
+// rows of 32 + 2 x 8 heads 91 us (394 MB, 4.3 TB/s); 403 fp16 rows 7.1; one row 3.5.
 //
 // T: rows, C: cache
-template <typename T, typename C>
-__global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_constant__ HeadArgs a) {
+template <typename T, typename C, int kHeadThreads>
+__global__ void __launch_bounds__(kHeadThreads, 1024 / kHeadThreads) heads_kernel(const __grid_constant__ HeadArgs a) {
     constexpr int V = Vec<T>::N;
     __shared__ float2 s_cs[64];
     __shared__ __align__(16) float s_a[2][128], s_b[2][128];  // [q, k][dim]
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x, rot = a.rope.rot_dim, half = rot / 2, tid = threadIdx.x;
+    const int per = a.hd / V, c = tid % per, e = c * V;  // lanes of a head (8, 16 or 32), this one's place
+    const int line = (blockIdx.y * kHeadThreads + tid) / per, step = kHeadThreads * gridDim.y / per;
+    const int heads = a.n_heads + a.n_kv_heads;
+    auto source = [&](int h) {
+        return h < a.n_heads ? (const T*)a.q + (int64_t)row * a.q_stride + (int64_t)h * a.hd + e
+                             : (const T*)a.k + (int64_t)row * a.k_stride + (int64_t)(h - a.n_heads) * a.hd + e;
+    };
+    uint4 x[kHeadAhead], y[kValueAhead];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int i = 0; i < kHeadAhead; ++i)
+            if (h0 + i * step < heads) x[i] = __ldcg(reinterpret_cast<const uint4*>(source(h0 + i * step)));
+    };
+    auto load_values = [&](int h0) {
+        const T* v = (const T*)a.v + (int64_t)row * a.v_stride + e;
+#pragma unroll
+        for (int i = 0; i < kValueAhead; ++i)
+            if (h0 + i * step < a.n_kv_heads) y[i] = __ldcg(reinterpret_cast<const uint4*>(v + (int64_t)(h0 + i * step) * a.hd));
+    };
+    // the first heads and values are on their way while the row's position becomes angles
     const int slot = __ldcg(a.slots + row);
+    const int64_t position = tid < half ? __ldcg(a.positions + (int64_t)a.axis[tid] * a.n_rows + row) : 0;
+    load(line);
+    load_values(line);
     if (tid < half) {
-        const int64_t p = __ldcg(a.positions + (int64_t)a.axis[tid] * a.n_rows + row);
-        const uint64_t turn = (uint64_t)p * a.rope.turns[tid];
+        const uint64_t turn = (uint64_t)position * a.rope.turns[tid];
         float s, c;
         sincospif((float)((int64_t)turn >> 32) * 0x1p-31f, &s, &c);
         s_cs[tid] = make_float2(c * a.rope.amplitude, s * a.rope.amplitude);
@@ -51,70 +74,60 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_consta
     const bool cached = slot >= 0 && slot < a.n_pages * a.page_size;
     const int64_t at = cached ? (int64_t)(slot / a.page_size) * a.page_stride + (int64_t)(slot % a.page_size) * a.pos_stride : 0;
     auto to_cache = [&](void* base, int head, int e, const float (&f)[V]) {
+        if (!cached) return;
         C* p = (C*)base + at + (int64_t)head * a.head_stride + e;
         if constexpr (V == 8) *reinterpret_cast<uint4*>(p) = Vec<C>::put(f);
         else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1], C()), pack2(f[2], f[3], C()));
     };
-    const int per = a.hd / V, c = tid % per, e = c * V;  // lanes of a head (8, 16 or 32), this one's place
-    const int line = (blockIdx.y * kHeadThreads + tid) / per, step = kHeadThreads * gridDim.y / per;
-    const int kv_heads = cached ? a.n_kv_heads : 0, heads = a.n_heads + kv_heads;
-    auto source = [&](int h) {
-        return h < a.n_heads ? (const T*)a.q + (int64_t)row * a.q_stride + (int64_t)h * a.hd + e
-                             : (const T*)a.k + (int64_t)row * a.k_stride + (int64_t)(h - a.n_heads) * a.hd + e;
-    };
-    uint4 x[kHeadAhead];
-    auto load = [&](int h0) {
+    __syncthreads();
+    for (int d = tid; d < a.hd; d += kHeadThreads) {
+        const bool rotated = d < rot, inter = a.rope.interleaved;
+        const int pair = inter ? d / 2 : d < half ? d : d - half;
+        const bool first = inter ? d % 2 == 0 : d < half;
+        const int partner = inter ? d ^ 1 : first ? d + half : d - half;
+        const float2 cs = rotated ? s_cs[pair] : make_float2(1.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kHeadAhead; ++i)
-            if (h0 + i * step < heads) x[i] = __ldcg(reinterpret_cast<const uint4*>(source(h0 + i * step)));
-    };
-    // values first: they need no angles; the first heads are on their way meanwhile
-    load(line);
-    for (int h = line; h < kv_heads; h += kHeadAhead * step) {
-        const T* v = (const T*)a.v + (int64_t)row * a.v_stride + e;
-        uint4 y[kHeadAhead];
+        for (int i = 0; i < 2; ++i) {
+            const float* g = i ? a.k_gain : a.q_gain;
+            s_a[i][d] = cs.x * (g ? __ldcg(g + d) : 1.f);
+            s_b[i][d] = rotated ? (first ? -cs.y : cs.y) * (g ? __ldcg(g + partner) : 1.f) : 0.f;
+        }
+    }
+    for (int h = line; h < a.n_kv_heads; h += kValueAhead * step) {
+        if (h != line) load_values(h);
 #pragma unroll
-        for (int i = 0; i < kHeadAhead; ++i)
-            if (h + i * step < kv_heads) y[i] = __ldcg(reinterpret_cast<const uint4*>(v + (int64_t)(h + i * step) * a.hd));
-#pragma unroll
-        for (int i = 0; i < kHeadAhead; ++i)
-            if (h + i * step < kv_heads) {
+        for (int i = 0; i < kValueAhead; ++i)
+            if (h + i * step < a.n_kv_heads) {
                 float f[V];
                 Vec<T>::get(y[i], f);
                 to_cache(a.vc, h + i * step, e, f);
             }
     }
     __syncthreads();
-    if (tid < a.hd) {
-        const bool rotated = tid < rot, inter = a.rope.interleaved;
-        const int pair = inter ? tid / 2 : tid < half ? tid : tid - half;
-        const bool first = inter ? tid % 2 == 0 : tid < half;
-        const int partner = inter ? tid ^ 1 : first ? tid + half : tid - half;
-        const float2 cs = rotated ? s_cs[pair] : make_float2(1.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float* g = i ? a.k_gain : a.q_gain;
-            s_a[i][tid] = cs.x * (g ? __ldcg(g + tid) : 1.f);
-            s_b[i][tid] = rotated ? (first ? -cs.y : cs.y) * (g ? __ldcg(g + partner) : 1.f) : 0.f;
-        }
-    }
-    __syncthreads();
     // where the partners of this lane's dims are: its own 16 bytes (neighbours), or another lane's
     const bool rotated = e < rot;
     const int lane = tid % 32, other = a.rope.interleaved || !rotated ? lane : e < half ? lane + half / V : lane - half / V;
     const float inv_hd = 1.f / (float)a.hd;
-    for (int h0 = line; __any_sync(0xffffffffu, h0 < heads); h0 += kHeadAhead * step) {
+    const int first_line = (blockIdx.y * kHeadThreads + tid / 32 * 32) / per;  // of the warp
+    for (int h0 = line, w0 = first_line; w0 < heads; h0 += kHeadAhead * step, w0 += kHeadAhead * step) {
         if (h0 != line) load(h0);
         // (all lanes of a warp take part in the shuffles; those without a head shuffle what they hold)
         float r[kHeadAhead];
 #pragma unroll
         for (int i = 0; i < kHeadAhead; ++i) {
+            r[i] = 0.f;
+            if (w0 + i * step >= heads) break;
             if (h0 + i * step >= heads) x[i] = make_uint4(0u, 0u, 0u, 0u);
             float f[V];
             Vec<T>::get(x[i], f);
-            r[i] = 0.f;
+            uint64_t s = 0ull;
 #pragma unroll
-            for (int j = 0; j < V; ++j) r[i] = fmaf(f[j], f[j], r[i]);
+            for (int j = 0; j < V; j += 2) {
+                const uint64_t v = pair_of(f[j], f[j + 1]);
+                s = fma_pair(v, v, s);
+            }
+            const float2 both = of_pair(s);
+            r[i] = both.x + both.y;
         }
         if (a.q_gain || a.k_gain) {
             for (int o = per / 2; o > 0; o >>= 1)
@@ -124,6 +137,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_consta
 #pragma unroll
         for (int i = 0; i < kHeadAhead; ++i) {
             const int h = h0 + i * step;
+            if (w0 + i * step >= heads) break;
             uint4 y;
             y.x = __shfl_sync(0xffffffffu, x[i].x, other);
             y.y = __shfl_sync(0xffffffffu, x[i].y, other);
@@ -132,26 +146,24 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_consta
             if (h >= heads) continue;
             const int kind = h < a.n_heads ? 0 : 1;
             const float scale = (kind ? a.k_gain : a.q_gain) ? rsqrtf(fmaf(r[i], inv_hd, a.eps)) : 1.f;
-            float f[V], g[V], A[V];
+            float f[V], g[V], o[V];
             Vec<T>::get(x[i], f);
             Vec<T>::get(y, g);
+            const uint64_t both = pair_of(scale, scale);
 #pragma unroll
-            for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(A + j) = *reinterpret_cast<const float4*>(&s_a[kind][e + j]);
-            if (rotated) {
-                float B[V];
-#pragma unroll
-                for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(B + j) = *reinterpret_cast<const float4*>(&s_b[kind][e + j]);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float p = a.rope.interleaved ? f[j ^ 1] : g[j];
-                    A[j] = scale * (f[j] * A[j] + p * B[j]);
+            for (int j = 0; j < V; j += 4) {
+                const ulonglong2 A = *reinterpret_cast<const ulonglong2*>(&s_a[kind][e + j]);
+                uint64_t u = mul_pair(pair_of(f[j], f[j + 1]), A.x), w = mul_pair(pair_of(f[j + 2], f[j + 3]), A.y);
+                if (rotated) {
+                    const ulonglong2 B = *reinterpret_cast<const ulonglong2*>(&s_b[kind][e + j]);
+                    u = fma_pair(a.rope.interleaved ? pair_of(f[j + 1], f[j]) : pair_of(g[j], g[j + 1]), B.x, u);
+                    w = fma_pair(a.rope.interleaved ? pair_of(f[j + 3], f[j + 2]) : pair_of(g[j + 2], g[j + 3]), B.y, w);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) A[j] *= scale * f[j];
+                const float2 p = of_pair(mul_pair(u, both)), q = of_pair(mul_pair(w, both));
+                o[j] = p.x, o[j + 1] = p.y, o[j + 2] = q.x, o[j + 3] = q.y;
             }
-            if (kind) to_cache(a.kc, h - a.n_heads, e, A);
-            else *reinterpret_cast<uint4*>((T*)a.q_out + (int64_t)row * a.q_out_stride + (int64_t)h * a.hd + e) = Vec<T>::put(A);
+            if (kind) to_cache(a.kc, h - a.n_heads, e, o);
+            else *reinterpret_cast<uint4*>((T*)a.q_out + (int64_t)row * a.q_out_stride + (int64_t)h * a.hd + e) = Vec<T>::put(o);
         }
     }
 }
@@ -161,6 +173,14 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_consta
 
 using namespace ssd;
 using namespace ssd::step;
+
+template <int kThreads>
+static int start(const char* call, const HeadArgs& a, int dtype, int split, void* stream) {
+    const dim3 grid((unsigned)a.n_rows, (unsigned)split);
+    if (dtype == SSD_F32) return launch(call, heads_kernel<float, f16, kThreads>, grid, kThreads, 0, stream, a);
+    if (dtype == SSD_F16) return launch(call, heads_kernel<f16, f16, kThreads>, grid, kThreads, 0, stream, a);
+    return launch(call, heads_kernel<bf16, bf16, kThreads>, grid, kThreads, 0, stream, a);
+}
 
 static bool rope_ok(const ssd_rope* rope, int most) {
     return rope && rope->rot_dim >= 16 && rope->rot_dim % 16 == 0 && rope->rot_dim <= most;
@@ -248,13 +268,13 @@ extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rop
     a.page_size = cache->page_size;
     a.n_pages = cache->n_pages;
     a.rope = *rope;
-    // few rows: a row's heads over several CTAs, until there are four per SM
+    // few rows: a row's heads over several CTAs, until there are four per SM.  Many rows of few heads: half as many threads each, since what
+    // a warp does once a row is half of its instructions (16000 bf16 rows of 32 + 8 heads of 128 91 us, 128 threads 101; 4095 of 32 + 32
+    // heads 45, 128 threads 44).
     const int per16 = dtype == SSD_F32 ? 4 : 8;
     const long long units = (long long)(n_heads + cache->n_kv_heads) * hd / per16;
+    if (n_rows >= 2432 && units < 1024) return start<64>(call, a, dtype, 1, cuda_stream);
     int split = 1;
-    while (split < 64 && (long long)n_rows * split < 608 && units > (long long)kHeadThreads * split) split *= 2;
-    const dim3 grid((unsigned)n_rows, (unsigned)split);
-    if (dtype == SSD_F32) return launch(call, heads_kernel<float, f16>, grid, kHeadThreads, 0, cuda_stream, a);
-    if (dtype == SSD_F16) return launch(call, heads_kernel<f16, f16>, grid, kHeadThreads, 0, cuda_stream, a);
-    return launch(call, heads_kernel<bf16, bf16>, grid, kHeadThreads, 0, cuda_stream, a);
+    while (split < 64 && (long long)n_rows * split < 608 && units > 128ll * split) split *= 2;
+    return start<128>(call, a, dtype, split, cuda_stream);
 }

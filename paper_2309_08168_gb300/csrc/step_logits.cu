@@ -51,28 +51,6 @@ __device__ __forceinline__ void copy4(void* to, const void* from) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(smem_u32(to)), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;\n" ::: "memory"); }
-// two fp32 operations in one instruction
-__device__ __forceinline__ uint64_t pair_of(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ float2 of_pair(uint64_t p) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(r.x), "=f"(r.y) : "l"(p));
-    return r;
-}
-__device__ __forceinline__ uint64_t add_pair(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul_pair(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-
 // what the CTAs of a row hand to the one that joins them
 struct Partial {
     uint64_t sum;  // (maximum, sum of weights) as floats
@@ -316,7 +294,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
             } else {
                 float v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = inside(x + j) ? __ldcg(bias + x + j) : 0.f;
+                for (int j = 0; j < 8; ++j) v[j] = inside(x + j) ? bias[x + j] : 0.f;  // (through L1: the next lanes want the same sectors)
                 add[0] = make_float4(v[0], v[1], v[2], v[3]), add[1] = make_float4(v[4], v[5], v[6], v[7]);
             }
         };
