@@ -244,7 +244,13 @@ extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rop
     if (int rc = check_rows(call, "k", k, k_stride, dtype, (int64_t)cache->n_kv_heads * hd)) return rc;
     if (int rc = check_rows(call, "v", v, v_stride, dtype, (int64_t)cache->n_kv_heads * hd)) return rc;
     if (q == q_out && q_stride != q_out_stride) return refuse_arg(call, "q_out in q's place needs its stride");
-    if (q_out == k || q_out == v) return refuse_arg(call, "q_out must not be k or v");
+    const size_t row_bytes = dtype == SSD_F32 ? 4 : 2, n = 4 * (size_t)n_rows;
+    const Range o[1] = {{q_out, span(n_rows, q_out_stride, (int64_t)n_heads * hd, dtype)}};
+    const Range in[4] = {{positions, n * (axes ? axes->n_axes : 1)}, {slots, n}, {a.q_gain, 4 * (size_t)hd}, {a.k_gain, 4 * (size_t)hd}};
+    // (k and v may lie between the rows of q in one tensor: the first row tells)
+    if (meet(o, in) || meet(q_out, row_bytes * n_heads * hd, k, row_bytes * cache->n_kv_heads * hd) || meet(q_out, row_bytes * n_heads * hd, v, row_bytes * cache->n_kv_heads * hd) ||
+        (q_out != q && meet(q_out, row_bytes * n_heads * hd, q, row_bytes * n_heads * hd)))
+        return refuse_arg(call, "q_out must be q with its stride or overlap no input");
     if (int rc = check_device(call, cache->k)) return rc;
     a.q = q;
     a.k = k;

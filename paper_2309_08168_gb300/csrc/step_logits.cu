@@ -2,6 +2,7 @@
 // best tokens of every row (ssd_logits_adjust, ssd_logits_choose of ssd_step.h).
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 
 #include "step_ops.cuh"
 
@@ -566,16 +567,40 @@ int check_rules(const char* call, const ssd_logit_rules* r, int dtype, const voi
     return SSD_OK;
 }
 
+// whether a result lies where the rules are read
+bool meets_rules(const Range (&out)[1], const ssd_logit_rules& r) {
+    const size_t b = 4 * (size_t)r.n_requests, n = 4 * (size_t)r.n_rows, words = (size_t)(r.vocab + 31) / 32;
+    const Range in[14] = {{r.row_start, b + 4},
+                          {r.history, 4 * ((size_t)(r.n_requests - 1) * (size_t)r.history_stride + (size_t)r.max_history)},
+                          {r.history_len, b},
+                          {r.prompt_len, b},
+                          {r.tokens, n},
+                          {r.masks, 2 * n * (size_t)r.mask_words},
+                          {r.repetition, b},
+                          {r.presence, b},
+                          {r.frequency, b},
+                          {r.bias, r.bias ? 4 * ((size_t)(r.n_bias - 1) * (size_t)r.bias_stride + (size_t)r.vocab) : 0},
+                          {r.bias_of, b},
+                          {r.allowed, r.allowed ? 4 * ((size_t)(r.n_allowed - 1) * (size_t)r.allowed_stride + words) : 0},
+                          {r.allowed_of, n},
+                          {nullptr, 0}};
+    return meet(out, in);
+}
+
 int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* stream) {
     const ssd_logit_rules& r = a.r;
     int dev = 0;
     if (int rc = check_device(call, a.logits)) return rc;
-    if (cudaGetDevice(&dev) != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "no device");
-    static int ready[64][3] = {};  // (set once a device and type; setting it twice is harmless)
-    if (dev < 64 && !ready[dev][dtype]) {
-        const int e = dtype == SSD_F32 ? set_up<float>() : dtype == SSD_F16 ? set_up<f16>() : set_up<bf16>();
-        if (e) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString((cudaError_t)e));
-        ready[dev][dtype] = 1;
+    if (int rc = device_of(call, &dev)) return rc;
+    {
+        static std::mutex mu;
+        static bool ready[kMaxDevices][3] = {};
+        std::lock_guard<std::mutex> lock(mu);
+        if (!ready[dev][dtype]) {
+            const int e = dtype == SSD_F32 ? set_up<float>() : dtype == SSD_F16 ? set_up<f16>() : set_up<bf16>();
+            if (e) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString((cudaError_t)e));
+            ready[dev][dtype] = true;
+        }
     }
     a.counted = (r.repetition || r.presence || r.frequency) && (r.history || r.tokens);
     // slices
@@ -624,6 +649,8 @@ extern "C" int ssd_logits_adjust(const ssd_logit_rules* rules, int dtype, const 
         return refuse_arg(call, "out: rows must not overlap, aligned to their type");
     if (out == logits ? out_stride != stride : meet(out, span(rules->n_rows, out_stride, rules->vocab, dtype), logits, span(rules->n_rows, stride, rules->vocab, dtype)))
         return refuse_arg(call, "out must be the logits with their stride, or not overlap them");
+    const Range all[1] = {{out, span(rules->n_rows, out_stride, rules->vocab, dtype)}};
+    if (meets_rules(all, *rules)) return refuse_arg(call, "out must not overlap what the rules read");
     LogitArgs a{};
     a.r = *rules;
     a.logits = logits;
@@ -640,10 +667,11 @@ extern "C" int ssd_logits_choose(const ssd_logit_rules* rules, int dtype, const 
     if (k < 1 || k > kMaxBest) return refuse_arg(call, "need 1 <= k <= 16");
     if (rules->n_rows == 0) return SSD_OK;
     if (!tokens || !logprob) return refuse_arg(call, "NULL pointer");
-    const size_t n = 4 * (size_t)rules->n_rows, rows = span(rules->n_rows, stride, rules->vocab, dtype);
-    if (meet(tokens, n * k, logprob, n * k) || meet(tokens, n * k, total, n) || meet(logprob, n * k, total, n) || meet(tokens, n * k, logits, rows) ||
-        meet(logprob, n * k, logits, rows) || meet(total, n, logits, rows) || meet(tokens, n * k, rules->tokens, n))
-        return refuse_arg(call, "the results must overlap neither each other, nor the logits or the nodes' tokens");
+    const size_t n = 4 * (size_t)rules->n_rows;
+    const Range a1[1] = {{tokens, n * k}}, a2[1] = {{logprob, n * k}}, a3[1] = {{total, n}}, in[1] = {{logits, span(rules->n_rows, stride, rules->vocab, dtype)}};
+    if (meet(a1, a2) || meet(a1, a3) || meet(a2, a3) || meet(a1, in) || meet(a2, in) || meet(a3, in) || meets_rules(a1, *rules) || meets_rules(a2, *rules) ||
+        meets_rules(a3, *rules))
+        return refuse_arg(call, "the results must overlap neither each other, nor the logits or what the rules read");
     LogitArgs a{};
     a.r = *rules;
     a.logits = logits;

@@ -654,8 +654,8 @@ __global__ void __launch_bounds__(kSumThreads) moe_sum_kernel(const __grid_const
     *reinterpret_cast<uint2*>((T*)a.out + (int64_t)row * a.out_stride + dim) = make_uint2(pack2(r0.x + s.x, r0.y + s.y, T()), pack2(r1.x + s.z, r1.y + s.w, T()));
 }
 
+std::mutex g_mu;  // guards what follows, and what is set up
 // ssd_debug_moe_stall, for one call
-std::mutex g_stall_mu;
 int g_stall = -1;
 double g_stall_wait_s = 0.0;
 
@@ -707,20 +707,23 @@ template <typename T, int NT>
 int launch_moe(const char* call, MoeArgs& a, const ssd_moe& m, int sms, void* stream) {
     using U = Products<T, NT, true>;
     using D = Products<T, NT, false>;
-    static bool ready[64] = {};  // (set once a device and type; setting it twice is harmless)
     int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && !(dev < 64 && ready[dev])) {
-        e = cudaFuncSetAttribute(moe_up_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
-        if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-        if (e == cudaSuccess && (!fn || found != cudaDriverEntryPointSuccess)) return refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled unavailable");
-        if (e == cudaSuccess) g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
-        if (e == cudaSuccess && dev < 64) ready[dev] = true;
+    if (int rc = device_of(call, &dev)) return rc;
+    {
+        static bool ready[kMaxDevices] = {};
+        std::lock_guard<std::mutex> lock(g_mu);
+        if (!ready[dev]) {
+            cudaError_t e = cudaFuncSetAttribute(moe_up_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+            void* fn = nullptr;
+            cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+            if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+            if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "set-up: %s", cudaGetErrorString(e));
+            if (!fn || found != cudaDriverEntryPointSuccess) return refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled unavailable");
+            g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+            ready[dev] = true;
+        }
     }
-    if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
     CUtensorMap gate, up, down;
     if (int rc = encode(call, &gate, m.gate, m.dtype, m.d, m.f, m.n_experts, m.gate_stride, U::kWeightRows / 2)) return rc;
     if (int rc = encode(call, &up, m.up, m.dtype, m.d, m.f, m.n_experts, m.up_stride, U::kWeightRows / 2)) return rc;
@@ -755,7 +758,7 @@ using namespace ssd;
 using namespace ssd::step;
 
 extern "C" void ssd_debug_moe_stall(int cta, double wait_limit_s) {
-    std::lock_guard<std::mutex> lock(g_stall_mu);
+    std::lock_guard<std::mutex> lock(g_mu);
     g_stall = cta >= 0 && wait_limit_s > 0.0 && wait_limit_s <= 10.0 ? cta : -1;
     g_stall_wait_s = wait_limit_s;
 }
@@ -774,8 +777,9 @@ extern "C" int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k,
     if (int rc = check_rows(call, "x", x, x_stride, dtype, d)) return rc;
     if ((uintptr_t)w_router & 15u) return refuse_arg(call, "w_router must be 16-byte aligned");
     const size_t picked = 4 * (size_t)n_rows * k;
-    if (meet(ids, picked, weights, picked) || meet(ids, picked, x, span(n_rows, x_stride, d, dtype)) || meet(weights, picked, x, span(n_rows, x_stride, d, dtype)))
-        return refuse_arg(call, "ids and weights must overlap neither each other nor x");
+    const Range i1[1] = {{ids, picked}}, w1[1] = {{weights, picked}};
+    const Range in[3] = {{x, span(n_rows, x_stride, d, dtype)}, {w_router, 2 * (size_t)n_experts * d}, {favour, 4 * (size_t)n_experts}};
+    if (meet(i1, w1) || meet(i1, in) || meet(w1, in)) return refuse_arg(call, "ids and weights must overlap neither each other nor an input");
     if (int rc = check_device(call, x)) return rc;
     RouteArgs a{};
     a.x = x;
@@ -836,10 +840,11 @@ extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void
     if (residual == out && residual_stride != out_stride) return refuse_arg(call, "out in the residual's place needs its stride");
     const Workspace w = workspace_of(m, n_rows, k);
     const size_t picked = 4 * (size_t)n_rows * k, rows = span(n_rows, out_stride, m.d, m.dtype);
-    if (x == out || meet(out, rows, ids, picked) || meet(out, rows, weights, picked)) return refuse_arg(call, "out must not overlap x, ids or weights");
-    if (meet(workspace, w.total, out, rows) || meet(workspace, w.total, x, span(n_rows, x_stride, m.d, m.dtype)) || meet(workspace, w.total, ids, picked) ||
-        meet(workspace, w.total, weights, picked) || meet(workspace, w.total, residual, span(n_rows, residual_stride, m.d, m.dtype)))
-        return refuse_arg(call, "the workspace must not overlap other tensors");
+    const Range o[1] = {{out, rows}}, ws[1] = {{workspace, w.total}}, st[1] = {{status, 4}};
+    const Range in[3] = {{x, span(n_rows, x_stride, m.d, m.dtype)}, {ids, picked}, {weights, picked}}, re[1] = {{residual, residual ? span(n_rows, residual_stride, m.d, m.dtype) : 0}};
+    if (meet(o, in) || (out != residual && meet(o, re))) return refuse_arg(call, "out must be the residual with its stride or overlap no input");
+    if (meet(ws, o) || meet(ws, in) || meet(ws, re) || meet(st, o) || meet(st, ws) || meet(st, in) || meet(st, re))
+        return refuse_arg(call, "workspace and status must not overlap other tensors");
     if ((uintptr_t)workspace & 15u) return refuse_arg(call, "the workspace must be 16-byte aligned");
     if (workspace_bytes < w.total) return refuse(SSD_ERR_CAPACITY, call, "the workspace needs %zu bytes", w.total);
     if (int rc = check_device(call, x)) return rc;
@@ -863,7 +868,7 @@ extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void
     a.wait_clocks = (long long)(kWaitSeconds * kClocksPerSecond);
     a.stall = -1;
     {
-        std::lock_guard<std::mutex> lock(g_stall_mu);
+        std::lock_guard<std::mutex> lock(g_mu);
         if (g_stall >= 0) {
             a.stall = g_stall;
             a.wait_clocks = (long long)(g_stall_wait_s * kClocksPerSecond);

@@ -9,12 +9,34 @@ namespace step {
 using namespace tree;
 
 // whether two ranges of bytes meet; NULL meets nothing
+struct Range {
+    const void* p;
+    size_t n;
+};
 inline bool meet(const void* a, size_t na, const void* b, size_t nb) {
     return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+// whether some range of one list meets one of the other
+template <size_t N, size_t M>
+inline bool meet(const Range (&a)[N], const Range (&b)[M]) {
+    for (const Range& x : a)
+        for (const Range& y : b)
+            if (meet(x.p, x.n, y.p, y.n)) return true;
+    return false;
 }
 // bytes from the first row's start to the last row's end
 inline size_t span(int n_rows, int64_t stride, int64_t width, int dtype) {
     return ((size_t)(n_rows - 1) * (size_t)stride + (size_t)width) * (dtype == SSD_F32 ? 4 : 2);
+}
+
+// the current device
+constexpr int kMaxDevices = 64;
+inline int device_of(const char* call, int* dev) {
+    if (cudaGetDevice(dev) != cudaSuccess || *dev < 0 || *dev >= kMaxDevices) {
+        (void)cudaGetLastError();
+        return refuse(SSD_ERR_CUDA, call, "no usable current device");
+    }
+    return SSD_OK;
 }
 
 // ---------------------------------------------------------------------------

@@ -158,6 +158,26 @@ def test_rows_that_hold_infinities_do_not_reach_others(ssd):
     assert not diff.any()
 
 
+def test_rows_and_cache_beyond_32_bits(ssd):
+    """Rows 2^30 values apart, and a cache whose layers are."""
+    far = 1 << 30
+    a, b = (Case(ssd, 15, "bf16", 4, 2, 1, 64, 64, False, pairs=[12, 10, 10]) for _ in range(2))
+    big = torch.zeros(3 * far + 4 * 64, dtype=torch.bfloat16, device="cuda")
+    b.q, b.k, b.v = (torch.as_strided(big, (4, h, 64), (far, 64, 1), o) for h, o in ((2, 0), (1, 128), (1, 192)))
+    for x, y in ((b.q, a.q), (b.k, a.k), (b.v, a.v)):
+        x.copy_(y)
+    pages = a.kc.shape[1]
+    store = [torch.zeros(2 * far + pages * 1024, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    b.kc, b.vc = (torch.as_strided(s, (2, pages, 1, 16, 64), (2 * far, 1024, 1024, 64, 1)) for s in store)
+    b.kc.copy_(a.kc)
+    b.vc.copy_(a.vc)
+    b.kv = ssd.PagedKV(b.kc, b.vc)
+    a.run()
+    b.run()
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, b.out) and torch.equal(a.kc, b.kc) and torch.equal(a.vc, b.vc)
+
+
 def test_the_binding_refuses(ssd):
     x = Case(ssd, 1, "f16", 4, 4, 2, 64, 64, False, pairs=[16, 16])
     pos, slots = x.positions.cuda(), x.slots.cuda()

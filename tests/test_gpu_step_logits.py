@@ -257,6 +257,21 @@ def test_a_replay_reads_lengths_and_starts_anew(ssd):
     assert torch.equal(torch.nan_to_num(logits), torch.nan_to_num(torch.from_numpy(d.expected()).cuda()))
 
 
+def test_rows_beyond_32_bits(ssd):
+    far = (1 << 31) + 5
+    big = torch.zeros(2 * far + 3001, dtype=torch.float16, device="cuda")
+    c, d = (Case(31, "f16", 3001, [2, 1], hist=40, few=100, masks=4, bias=2) for _ in range(2))
+    d.logits = torch.as_strided(big, (3, 3001), (far, 1))
+    d.logits.copy_(c.logits)
+    for x, y in zip(check(ssd, c, 5), check(ssd, d, 5)):
+        assert torch.equal(x, y)
+    out = torch.empty_like(c.logits)
+    ssd.ssd_logits_adjust(c.rules(ssd), c.logits, out, stream())
+    ssd.ssd_logits_adjust(d.rules(ssd), d.logits, d.logits, stream())
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), d.logits.contiguous().view(torch.int16))
+
+
 def test_two_streams_at_once(ssd):
     cs = [Case(20 + i, "bf16", 20000, [9] * 12, hist=100, few=100, masks=4) for i in range(2)]
     rules = [c.rules(ssd) for c in cs]

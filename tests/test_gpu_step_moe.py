@@ -247,6 +247,51 @@ def test_layers_behind_one_another_and_replayed(ssd):
     assert all(torch.equal(a, b) for a, b in zip(bufs, want))
 
 
+def test_two_layers_on_two_streams(ssd):
+    xs = [Layer(ssd, 40 + i, "bf16", 9 + 20 * i, 512, 264, 16, 4) for i in range(2)]
+    for x in xs:
+        x.run()
+    torch.cuda.synchronize()
+    want = [x.out.clone() for x in xs]
+    outs = [[torch.zeros_like(x.out) for _ in range(8)] for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for x, o, s in zip(xs, outs, streams):
+            ssd.ssd_moe_mlp(x.experts, x.x, x.ids, x.weights, o[i][:, :512], x.ws, residual=x.residual, cuda_stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        assert all(torch.equal(w[:, :512], y[:, :512]) for y in o)
+
+
+def test_experts_beyond_32_bits(ssd):
+    """Experts and rows whose offsets pass 2^31 elements."""
+    d, f, e, n, far = 64, 40, 3, 3, (1 << 31) + 64
+    big = torch.zeros(2 * far + 4 * d * f, dtype=torch.bfloat16, device="cuda")
+    x = Layer(ssd, 50, "bf16", n, d, f, e, 3)
+    size = d * f
+    gate, up = (torch.as_strided(big, (e, f, d), (far, d, 1), i * size) for i in (0, 1))
+    down, rows = torch.as_strided(big, (e, d, f), (far, f, 1), 2 * size), torch.as_strided(big, (n, d), (far, 1), 3 * size)
+    for a, b in ((gate, x.gate), (up, x.up), (down, x.down), (rows, x.x)):
+        a.copy_(b)
+    x.run()
+    torch.cuda.synchronize()
+    want = x.out.clone()
+    x.gate, x.up, x.down, x.x = gate, up, down, rows
+    x.experts = ssd.MoeWeights(gate, up, down)
+    x.out.fill_(7.0)
+    x.run()
+    torch.cuda.synchronize()
+    assert torch.equal(x.out, want)
+    ids, weights = x.ids.clone(), x.weights.clone()
+    for r in (rows, rows.contiguous()):
+        ssd.ssd_moe_route(r, x.gate[0].contiguous(), ids, weights, cuda_stream=stream())
+        torch.cuda.synchronize()
+        if r is rows:
+            first = ids.clone(), weights.clone()
+    assert torch.equal(first[0], ids) and torch.equal(first[1], weights)
+
+
 def test_a_wait_that_gives_up_is_told(ssd):
     x = Layer(ssd, 12, "bf16", 5, 512, 264, 6, 3)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
