@@ -1,6 +1,7 @@
 // step_logits.cu - penalties, biases and masks on logits, and the choice of the
 // best tokens of every row (ssd_logits_adjust, ssd_logits_choose of ssd_step.h).
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <mutex>
 
@@ -170,6 +171,8 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
             const int s0 = __ldcg(a.r.row_start), s1 = __ldcg(a.r.row_start + a.r.n_requests);
             owner = s0 <= row && row < s1 ? 0 : a.r.n_requests;
             end = row + 1;
+        } else if (a.r.row_start && fresh && a.r.n_requests == a.r.n_rows && __ldcg(a.r.row_start + row) == row && __ldcg(a.r.row_start + row + 1) == row + 1) {
+            owner = start = row, end = row + 1;  // (a row a request: no search)
         } else if (a.r.row_start && fresh) {
             if (tid == 0) s_request = a.r.n_requests;
             __syncthreads();
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
             }
         };
         // choose: the largest logit of the thread, its chunk, and the sum of exp(logit - ref)
-        float best = -INFINITY, ref = -INFINITY, sum = 0.f;
+        float best = -INFINITY, ref = -FLT_MAX, sum = 0.f;
         int at = 0x7fffffff;
         Chunk<T> kept;
         T* out = kChoose ? nullptr : (T*)a.out + (int64_t)row * a.out_stride;
@@ -363,7 +366,6 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                         sum *= exp2_of((ref - up) * kLog2e);
                         ref = up;
                     }
-                    if (!(top > -INFINITY)) continue;
                     uint64_t e2 = 0ull;
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) {
@@ -405,7 +407,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
         } else {
             // the CTA's reference and sum of weights
             const float m_w = warp_max(ref);
-            const float s_w = warp_sum(ref > -INFINITY ? sum * weight(ref, m_w) : 0.f);
+            const float s_w = warp_sum(sum * weight(ref, m_w));
             if (lane == 0) s_m[warp] = m_w, s_s[warp] = s_w;
             // each warp's k best of its threads, largest first, of equal ones the lowest chunk
             uint32_t mine = best > -INFINITY ? order_of(best + 0.f) : 0u;
@@ -452,7 +454,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
             }
             if (warp == kLogitWarps - 1) {
                 const float m = lane < kLogitWarps ? s_m[lane] : -INFINITY, s = lane < kLogitWarps ? s_s[lane] : 0.f;
-                const float m_c = warp_max(m), s_c = warp_sum(m > -INFINITY ? s * weight(m, m_c) : 0.f);
+                const float m_c = warp_max(m), s_c = warp_sum(s * weight(m, m_c));
                 if (lane == 0) part.sum = (uint64_t)__float_as_uint(m_c) << 32 | __float_as_uint(s_c);
             }
             if (a.k > 1) {
@@ -499,7 +501,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                     m = __uint_as_float((uint32_t)(u >> 32)), s = __uint_as_float((uint32_t)u);
                 }
                 const float top = warp_max(m);
-                const float log_sum = logf(warp_sum(m > -INFINITY ? s * weight(m, top) : 0.f));
+                const float log_sum = logf(warp_sum(s * weight(m, top)));
                 asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kJoinWarps) : "memory");
                 for (int i = tid; i < n; i += 32 * kJoinWarps) {
                     const uint64_t key = all[i];
@@ -511,7 +513,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                         a.logprob[(int64_t)row * a.k + rank] = key ? (v == top ? 0.f : v - top) - log_sum : -INFINITY;
                     }
                 }
-                if (tid == 0 && a.total) a.total[row] = top > -INFINITY ? top + log_sum : -INFINITY;
+                if (tid == 0 && a.total) a.total[row] = top + log_sum;
             }
             __syncthreads();
         }
