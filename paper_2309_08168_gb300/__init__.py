@@ -504,9 +504,26 @@ def ssd_norm_rope_kv(cache: PagedKV, layer: int, rope: ssd_rope, q, k, v, positi
 
 def _matrix(t, what: str, device: int, dtype, rows: int, width: int):
     """(address, row stride) of rows of `width` adjacent values."""
-    if tuple(t.shape) != (rows, width) or t.dtype is not dtype or t.get_device() != device or (t.stride(1) != 1 and width > 1 and rows > 0):
-        _refuse(f"{what}: {dtype} of shape ({rows}, {width}) with adjacent values on CUDA device {device} is wanted, got {t.dtype}, {tuple(t.shape)} on {t.device}")
-    return (t.data_ptr(), t.stride(0) if rows > 1 else width) if rows else (None, width)
+    if t.shape != (rows, width) or t.dtype is not dtype or t.get_device() != device:
+        _refuse(f"{what}: {dtype} of shape ({rows}, {width}) on CUDA device {device} is wanted, got {t.dtype}, {tuple(t.shape)} on {t.device}")
+    if rows == 0:  # (strides of no rows mean nothing)
+        return None, width
+    stride = t.stride()
+    if stride[1] != 1 and width > 1:
+        _refuse(f"{what}: the values of a row must be adjacent")
+    return t.data_ptr(), stride[0] if rows > 1 else width
+
+
+def _half_type(t, what: str) -> int:
+    """Whether rows are fp16 or bf16."""
+    k = _ROW_TYPES.get(t.dtype)
+    if k is None:
+        k = _ROW_TYPES.get(str(t.dtype))
+        if k is not None:
+            _ROW_TYPES[t.dtype] = k
+    if k is None or k == SSD_F32:
+        _refuse(f"{what}: fp16 or bf16 rows are wanted")
+    return k
 
 
 class LogitRules:
@@ -609,11 +626,10 @@ def ssd_moe_route(x, w_router, ids, weights, score: int = SSD_MOE_SOFTMAX, favou
     favour fp32 [experts] (added to the scores that choose) or None."""
     if x.dim() != 2 or w_router.dim() != 2 or ids.dim() != 2 or not x.is_cuda:
         _refuse("x [row][d], w_router [expert][d] and ids [row][k] on a CUDA device are wanted")
-    if str(x.dtype) not in ("torch.float16", "torch.bfloat16"):
-        _refuse("x: fp16 or bf16 rows are wanted")
+    kind = _half_type(x, "x")
     (n, d), e, k, dev = x.shape, w_router.shape[0], ids.shape[1], x.get_device()
     f32 = _of_type(weights, "weights", "torch.float32")
-    _check(lib.ssd_moe_route(_ROW_TYPES[str(x.dtype)], n, d, e, k, *_matrix(x, "x", dev, x.dtype, n, d), _dev(w_router, "w_router", x.dtype, dev, e * d),
+    _check(lib.ssd_moe_route(kind, n, d, e, k, *_matrix(x, "x", dev, x.dtype, n, d), _dev(w_router, "w_router", x.dtype, dev, e * d),
                              _dev(favour, "favour", f32, dev, e), score, int(bool(renorm)), scale,
                              _dev(ids, "ids", _of_type(ids, "ids", "torch.int32"), dev, n * k), _dev(weights, "weights", f32, dev, n * k), cuda_stream))
 
