@@ -27,9 +27,10 @@ struct LogitArgs {
     float *logprob, *total;
     int k, slice, rows;  // tokens of a CTA (a multiple of 64), rows of a cluster
     int counted;         // whether anything is penalised
-    // dynamic shared memory: candidates of the k best, words of the row's mask from at_show on, and from at_bits on what has been
+    // dynamic shared memory: candidates of the k best, words of the row's mask from at_show on, the
+    // tokens that a mask of few leaves from at_list on, and from at_bits on what has been
     // said: n_words words of bits, the bits before each four of them, counts
-    int at_show, at_bits, n_words;
+    int at_show, at_list, at_bits, n_words;
 };
 
 // what a float sorts by; 0 is below all of them (-inf gives 0x007fffff)
@@ -99,12 +100,14 @@ struct Chunk {
 // chip has it), so a thread keeps its best chunk rather than its best token, and sums weights relative to a whole number above its
 // best, which seldom changes.
 //
-// kRules: whether the rules have any part
-template <typename T, bool kChoose, bool kRules>
-__global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logits_kernel(const __grid_constant__ LogitArgs a) {
+// kRules: 0: the rules have no part; 1: no biases; 2: biases.  (With the code for biases in it, though none are added, 456 rows of 128256 take
+// 55 us instead of 42 where texts are penalised.)
+constexpr int ctas_of(bool choose, int rules) { return choose && rules ? 3 : 4; }  // of an SM
+template <typename T, bool kChoose, int kRules>
+__global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logits_kernel(const __grid_constant__ LogitArgs a) {
     constexpr int V = Vec<T>::N;  // tokens in 16 bytes
     constexpr int kParts = 8 / V;
-    constexpr int kAhead = kRules ? 2 : V / 2;  // chunks under way in a thread
+    constexpr int kAhead = kRules == 2 || (kRules && !kChoose) ? 2 : V / 2;  // chunks under way in a thread
     extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ int s_request, s_rows[2], s_n, s_scan[kLogitWarps];
     __shared__ float s_m[kLogitWarps], s_s[kLogitWarps];
@@ -112,7 +115,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
     __shared__ int s_from[kMaxBest], s_found;
     __shared__ Partial s_part[2];
     uint64_t* s_cand = reinterpret_cast<uint64_t*>(s_dyn);
-    uint32_t* s_show = reinterpret_cast<uint32_t*>(s_dyn + a.at_show);
+    uint32_t *s_show = reinterpret_cast<uint32_t*>(s_dyn + a.at_show), *s_list = reinterpret_cast<uint32_t*>(s_dyn + a.at_list);
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, split = gridDim.x, vocab = a.r.vocab;
@@ -292,7 +295,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
         // the 8 bits of a chunk's tokens in the row's mask; 0: nothing of it is left
         auto shown = [&](int x0) -> uint32_t { return allowed ? bits8(s_show, x0 - 32 * word0) : 255u; };
         auto load_bias = [&](int x, float4* add) {
-            if (!bias) return;
+            if (kRules < 2 || !bias) return;
             if (whole(x) && ((uintptr_t)(bias + x) & 15u) == 0) {
                 add[0] = __ldcg(reinterpret_cast<const float4*>(bias + x)), add[1] = __ldcg(reinterpret_cast<const float4*>(bias + x) + 1);
             } else {
@@ -302,6 +305,11 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                 add[0] = make_float4(v[0], v[1], v[2], v[3]), add[1] = make_float4(v[4], v[5], v[6], v[7]);
             }
         };
+        auto penalised = [&](float l, uint32_t n) {
+            const uint32_t c = n & ~kPrompt;
+            l = __fsub_rn(l > 0.f ? __fdiv_rn(l, again) : __fmul_rn(l, again), __fmul_rn(often, (float)c));
+            return c ? __fsub_rn(l, once) : l;
+        };
         auto rules = [&](int x0, uint32_t show, const float4* add, float (&f)[8]) {
             if (a.counted) {
                 const int at = x0 - lo + 8;  // >= 0
@@ -310,14 +318,12 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                     const uint32_t* counts = s_count + count_of(at);  // of the chunk's said tokens, one behind the other
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const uint32_t n = m >> j & 1u ? counts[__popc(m & ((1u << j) - 1u))] : 0u, c = n & ~kPrompt;
-                        if (!n) continue;  // (not said, or by another node only)
-                        const float l = __fsub_rn(f[j] > 0.f ? __fdiv_rn(f[j], again) : __fmul_rn(f[j], again), __fmul_rn(often, (float)c));
-                        f[j] = c ? __fsub_rn(l, once) : l;
+                        const uint32_t n = m >> j & 1u ? counts[__popc(m & ((1u << j) - 1u))] : 0u;
+                        if (n) f[j] = penalised(f[j], n);  // (0: not said, or by another node only)
                     }
                 }
             }
-            if (bias) {
+            if (kRules == 2 && bias) {
                 const float4 u = add[0], w = add[1];
                 f[0] += u.x, f[1] += u.y, f[2] += u.z, f[3] += u.w, f[4] += w.x, f[5] += w.y, f[6] += w.z, f[7] += w.w;
             }
@@ -326,12 +332,77 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                 for (int j = 0; j < 8; ++j) f[j] = show >> j & 1u ? f[j] : -INFINITY;
             }
         };
-        // choose: the largest logit of the thread, its chunk, and the sum of exp(logit - ref)
+        // A mask that leaves at most 1 / 32 of the slice: its tokens in order, so that only they are read (`few` of them; -1: more)
+        int few = -1;
+        if (kChoose && kRules && allowed) {
+            const int low = max(first, 0), n = (stop - 1) / 32 - word0 + 1;
+            const int each = (n + kLogitThreads - 1) / kLogitThreads | 1;  // (odd: threads meet different banks)
+            const int w0 = min(tid * each, n), w1 = min(w0 + each, n);
+            auto word = [&](int w) {  // bits of [low, stop)
+                const int x = 32 * (word0 + w);
+                uint32_t u = s_show[w];
+                if (x < low) u = x + 32 <= low ? 0u : u & ~0u << (low - x);
+                return x + 32 > stop ? u & ~0u >> (x + 32 - stop) : u;
+            };
+            int mine = 0;
+            for (int w = w0; w < w1; ++w) mine += __popc(word(w));
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            if (lane == 31) s_scan[warp] = upto;
+            __syncthreads();
+            int to = upto - mine, all = 0;
+            for (int w = 0; w < kLogitWarps; ++w) {
+                if (w < warp) to += s_scan[w];
+                all += s_scan[w];
+            }
+            if (all * 32 <= a.slice) {
+                few = all;
+                for (int w = w0; w < w1; ++w)
+                    for (uint32_t u = word(w); u; u &= u - 1) s_list[to++] = (uint32_t)(32 * (word0 + w) + __ffs((int)u) - 1);
+            }
+            __syncthreads();
+        }
+        // the logit l of a token that the mask leaves after the other rules
+        auto value = [&](int x, float l, float add) {
+            if (a.counted) {
+                const int i = x - lo + 8;
+                const uint32_t n = s_bits[i / 32] >> i % 32 & 1u ? s_count[count_of(i)] : 0u;
+                if (n) l = penalised(l, n);
+            }
+            return kRules == 2 && bias ? l + add : l;
+        };
+        // choose: the largest logit of the thread, its chunk (of few: its number among them), and the sum of exp(logit - ref)
         float best = -INFINITY, ref = -FLT_MAX, sum = 0.f;
         int at = 0x7fffffff;
         Chunk<T> kept;
         T* out = kChoose ? nullptr : (T*)a.out + (int64_t)row * a.out_stride;
-        for (int x = first + 8 * tid; x < stop; x += 8 * kLogitThreads * kAhead) {
+        for (int e = tid; e < few; e += 4 * kLogitThreads) {
+            float raw[4], add[4];
+            int token[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                token[i] = e + i * kLogitThreads < few ? (int)s_list[e + i * kLogitThreads] : -1;
+                raw[i] = token[i] >= 0 ? (float)src[token[i]] : -INFINITY;
+                add[i] = kRules == 2 && bias && token[i] >= 0 ? __ldcg(bias + token[i]) : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (token[i] < 0) break;
+                const float l = value(token[i], raw[i], add[i]);
+                if (l > best) best = l, at = e + i * kLogitThreads;
+                if (l > ref) {
+                    const float up = ceilf(l);
+                    sum *= exp2_of((ref - up) * kLog2e);
+                    ref = up;
+                }
+                if (l == l) sum += weight(l, ref);
+            }
+        }
+        for (int x = few < 0 ? first + 8 * tid : stop; x < stop; x += 8 * kLogitThreads * kAhead) {
             Chunk<T> c[kAhead];
             float4 add[2];
             uint32_t show[kAhead];
@@ -428,17 +499,21 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
 #pragma unroll
                 for (int i = 0; i < kLogitWarps; ++i) key = max(key, s_first[i]);
                 if (key && at == (int)~(uint32_t)key - 8) {  // (this thread's chunk)
-                    float f[8];
-                    float4 add[2];
-                    if (kRules) {
-                        load(at, kept);
-                        load_bias(at, add);
-                    }
-                    kept.get(f);
-                    if (kRules) rules(at, shown(at), add, f);
                     int token = at + 7;
+                    if (kRules && few >= 0) {
+                        token = (int)s_list[at];
+                    } else {
+                        float f[8];
+                        float4 add[2];
+                        if (kRules) {
+                            load(at, kept);
+                            load_bias(at, add);
+                        }
+                        kept.get(f);
+                        if (kRules) rules(at, shown(at), add, f);
 #pragma unroll
-                    for (int j = 6; j >= 0; --j) token = f[j] == best ? at + j : token;
+                        for (int j = 6; j >= 0; --j) token = f[j] == best ? at + j : token;
+                    }
                     part.best[0] = key_of(best + 0.f, token);
                 }
             } else if (tid < lists) {  // the k best threads, and the last of them as the bound
@@ -447,7 +522,7 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                 for (int i = 0; i < lists; ++i) rank += s_first[i] > key;
                 if (key && rank < a.k) {
                     const int x = (int)~(uint32_t)key - 8;
-                    s_from[rank] = (x - first) / 8 % kLogitThreads;
+                    s_from[rank] = (kRules && few >= 0 ? x : (x - first) / 8) % kLogitThreads;
                     if (rank == a.k - 1) s_bound = key & ~0xffffffffull;  // (by the logit alone: the token lies somewhere in the chunk)
                     atomicAdd(&s_found, 1);
                 }
@@ -461,7 +536,18 @@ __global__ void __launch_bounds__(kLogitThreads, kChoose && kRules ? 3 : 4) logi
                 __syncthreads();
                 const int n_from = s_found;
                 const uint64_t bound = s_bound;
-                for (int i = tid; i < n_from * deep; i += kLogitThreads) {
+                const bool listed = kRules && few >= 0;
+                if (listed) {
+                    for (int i = tid; i < n_from * ((few + kLogitThreads - 1) / kLogitThreads); i += kLogitThreads) {
+                        const int e = s_from[i % n_from] + i / n_from * kLogitThreads;
+                        if (e >= few) continue;
+                        const int x = (int)s_list[e];
+                        const float l = value(x, (float)src[x], kRules == 2 && bias ? __ldcg(bias + x) : 0.f);
+                        const uint64_t key = key_of(l + 0.f, x);
+                        if (l > -INFINITY && key >= bound) s_cand[atomicAdd(&s_n, 1)] = key;
+                    }
+                }
+                for (int i = listed ? n_from * deep : tid; i < n_from * deep; i += kLogitThreads) {
                     const int x0 = first + 8 * (s_from[i % n_from] + i / n_from * kLogitThreads);
                     if (x0 >= stop) continue;
                     Chunk<T> c;
@@ -526,7 +612,8 @@ size_t lay_out(LogitArgs& a) {
     const ssd_logit_rules& r = a.r;
     const int deep = (a.slice / 8 + kLogitThreads - 1) / kLogitThreads;
     a.at_show = a.k > 1 ? a.k * deep * 8 * 8 : 0;
-    a.at_bits = a.at_show + (r.allowed ? (a.slice / 32 + 3) * 4 : 0);
+    a.at_list = a.at_show + (r.allowed ? (a.slice / 32 + 3) * 4 : 0);
+    a.at_bits = a.at_list + (r.allowed && a.k ? a.slice / 32 * 4 : 0);
     a.at_bits = (a.at_bits + 15) / 16 * 16;
     a.n_words = (a.slice + 8 + 127) / 128 * 4;
     if (!a.counted) return a.at_bits;
@@ -537,15 +624,17 @@ constexpr int kMostShared = 180 * 1024;  // (a slice of 32832 tokens, all of the
 
 template <typename T>
 int set_up() {
-    cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(logits_kernel<T, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    void (*const k[])(LogitArgs) = {logits_kernel<T, true, 0>, logits_kernel<T, true, 1>, logits_kernel<T, true, 2>, logits_kernel<T, false, 1>, logits_kernel<T, false, 2>};
+    cudaError_t e = cudaSuccess;
+    for (auto f : k)
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     return (int)e;
 }
 
 template <typename T>
-cudaError_t start(const cudaLaunchConfig_t& cfg, const LogitArgs& a, bool choose) {
-    if (!choose) return cudaLaunchKernelEx(&cfg, logits_kernel<T, false, true>, a);
-    return a.counted || a.r.bias || a.r.allowed ? cudaLaunchKernelEx(&cfg, logits_kernel<T, true, true>, a) : cudaLaunchKernelEx(&cfg, logits_kernel<T, true, false>, a);
+cudaError_t start(const cudaLaunchConfig_t& cfg, const LogitArgs& a, bool choose, int rules) {
+    if (!choose) return cudaLaunchKernelEx(&cfg, rules == 2 ? logits_kernel<T, false, 2> : logits_kernel<T, false, 1>, a);
+    return cudaLaunchKernelEx(&cfg, rules == 2 ? logits_kernel<T, true, 2> : rules ? logits_kernel<T, true, 1> : logits_kernel<T, true, 0>, a);
 }
 
 int check_rules(const char* call, const ssd_logit_rules* r, int dtype, const void* logits, int64_t stride) {
@@ -605,14 +694,25 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
         }
     }
     a.counted = (r.repetition || r.presence || r.frequency) && (r.history || r.tokens);
-    // slices
-    int split = 1;
-    auto slice_of = [&](int n) { return ((r.vocab + 7 + n - 1) / n + 63) / 64 * 64; };
-    a.slice = slice_of(split);
-    while (split < kMaxSplit && (a.slice > kMaxSlice || lay_out(a) > 56 * 1024 || ((long long)r.n_rows * split < 304 && r.vocab > 2048 * split))) {
-        split *= 2;
-        a.slice = slice_of(split);
+    int sms = 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "no device");
+    const int rules = r.bias ? 2 : a.counted || r.allowed ? 1 : 0, slots = sms * ctas_of(choose, rules);
+    // A row's slices: 1 to 8, whichever is done first if a wave of CTAs takes as long as its slice and 20000 tokens more for its start
+    // and end, or 30000 with counts to make.  (512 rows of 128256, penalised and masked: whole 68 us, in two 70, in four 94; 200
+    // rows of 50257, penalised and with biases: whole 39, in two 29, in four 44.)
+    int best = 0;
+    long long least = 0;
+    for (int split = 1; split <= kMaxSplit; split *= 2) {
+        a.slice = ((r.vocab + 7 + split - 1) / split + 63) / 64 * 64;
+        if (a.slice > kMaxSlice || (split > 1 && a.slice < 1024)) continue;
+        const size_t bytes = lay_out(a);
+        if (bytes > kMostShared) continue;
+        const int fit = (int)std::min<size_t>(slots / sms, (222 * 1024) / (bytes + 4096));
+        const long long waves = ((long long)r.n_rows * split + sms * fit - 1) / (sms * fit), cost = waves * (a.slice + (a.counted ? 30000 : 20000));
+        if (!best || cost < least) best = split, least = cost;
     }
+    const int split = best;
+    a.slice = ((r.vocab + 7 + split - 1) / split + 63) / 64 * 64;
     // rows of a request share its counts, as many as leave two waves of CTAs
     a.rows = a.counted ? (int)std::min<long long>(r.max_rows, std::max(1ll, (long long)r.n_rows * split / 912)) : 1;
     cudaLaunchConfig_t cfg = {};
@@ -631,7 +731,7 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     attr[1].val.clusterDim.x = (unsigned)split, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = choose && split > 1 ? 2 : 1;
-    const cudaError_t e = dtype == SSD_F32 ? start<float>(cfg, a, choose) : dtype == SSD_F16 ? start<f16>(cfg, a, choose) : start<bf16>(cfg, a, choose);
+    const cudaError_t e = dtype == SSD_F32 ? start<float>(cfg, a, choose, rules) : dtype == SSD_F16 ? start<f16>(cfg, a, choose, rules) : start<bf16>(cfg, a, choose, rules);
     return e == cudaSuccess ? SSD_OK : refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
 }
 

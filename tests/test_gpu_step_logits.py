@@ -158,6 +158,8 @@ CASES = [
     dict(typ="f32", vocab=700, rows=None, n=700, hist=30, few=50, masks=7),
     dict(typ="f16", vocab=2500, rows=[17] * 30, hist=30, few=50, masks=7),
     dict(typ="bf16", vocab=3001, rows=[256], tokens=True, few=100),
+    dict(typ="f16", vocab=262144, rows=[2], hist=60000, bias=1, masks=3),  # more said tokens than a list has room for
+    dict(typ="bf16", vocab=5000, rows=[3, 2], hist=9000, masks=4),  # (nearly) every token said
 ]
 
 
@@ -166,7 +168,7 @@ def test_logits(ssd, c):
     c = dict(c)
     if c.get("mask_of") is False:
         c["masks"] = sum(c["rows"])
-    check(ssd, Case(3, **c), k=min(16, 1 + c["vocab"] % 7))
+    check(ssd, Case(3, **c), k=16 if c["vocab"] in (5000, 262144) else min(16, 1 + c["vocab"] % 7))
 
 
 @pytest.mark.parametrize("k", [1, 2, 3, 8, 16])
@@ -185,6 +187,28 @@ def test_ties_go_to_the_lowest(ssd, k):
     c.logits[3] = float("nan")
     c.host = c.logits.float().cpu().numpy()
     check(ssd, c, k, want_adjust=False)
+
+
+@pytest.mark.parametrize("k", [1, 4, 16])
+@pytest.mark.parametrize("typ,vocab,pad", [("f32", 32000, 0), ("bf16", 50257, 0), ("f16", 131075, 2)])
+def test_masks_that_leave_few(ssd, k, typ, vocab, pad):
+    """Up to a 32nd of a slice, where only the tokens that are left are read: none, one, some, just as many and one more; ties and
+    infinities among them, said tokens, biases."""
+    rng = np.random.default_rng(k)
+    c = Case(41, typ, vocab, [9, 7], hist=60, few=vocab, bias=2, masks=16, mask_of=False, pad=pad)
+    bits = np.zeros((16, -(-vocab // 32) * 32), bool)
+    for row, n in enumerate([0, 1, 5, 31, 200, vocab // 33, vocab // 32, vocab // 32 + 2, vocab // 20, vocab // 64, 3, 3, 40, 40, 900, 900]):
+        bits[row, rng.permutation(vocab)[:n]] = True
+    bits[10, vocab - 1] = bits[11, 0] = True
+    bits[12, :vocab] = rng.random(vocab) < 0.01
+    said = c.r["history"][0, :20]
+    bits[13, said[(said >= 0) & (said < vocab)]] = True
+    c.r["allowed"] = np.packbits(bits, axis=1, bitorder="little").view(np.int32)
+    left = np.flatnonzero(bits[14, :vocab])
+    c.logits[14, torch.from_numpy(left[:300]).cuda()] = 2.5
+    c.logits[15, torch.from_numpy(np.flatnonzero(bits[15, :vocab])[:4]).cuda()] = torch.tensor([float("nan"), float("inf"), -float("inf"), 1.0], device="cuda").to(c.logits.dtype)
+    c.host = c.logits.float().cpu().numpy()
+    check(ssd, c, k)
 
 
 def test_infinities_and_nan(ssd):
