@@ -698,7 +698,7 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "no device");
     const int rules = r.bias ? 2 : a.counted || r.allowed ? 1 : 0, slots = sms * ctas_of(choose, rules);
     // A row's slices: 1 to 8, whichever is done first if a wave of CTAs takes as long as its slice and 20000 tokens more for its start
-    // and end, or 30000 with counts to make.  (512 rows of 128256, penalised and masked: whole 68 us, in two 70, in four 94; 200
+    // and end, or 30000 with counts to make.  (512 rows of 128256, penalised and masked: whole 68 us, in two 70, in four 94; 207
     // rows of 50257, penalised and with biases: whole 39, in two 29, in four 44.)
     int best = 0;
     long long least = 0;
