@@ -141,9 +141,8 @@ typedef enum { SSD_MOE_SOFTMAX = 0, SSD_MOE_SIGMOID = 1 } ssd_moe_score;
 /* The experts of each row: the k with the largest p + favour[e] (favour fp32 [n_experts], NULL: 0), largest first, of equal ones the
  * lowest first:  ids[row][j] = e,  weights[row][j] = scale p  (renorm = 1: divided by the sum of the row's k p's).
  * x: [row][d], rows x_stride elements apart, and w_router [n_experts][d], of dtype SSD_F16 or SSD_BF16, 16-byte aligned, d and
- * x_stride multiples of 8.  1 <= k <= 16, k <= n_experts <= 1024; d <= 65536.  Products are summed exactly enough (48 bits) and scored in fp64, so
- * that scores differ in order from exact ones only if they differ by less than 1e-11 of the row's largest.  NaN counts as the
- * lowest score.
+ * x_stride multiples of 8.  1 <= k <= 16, k <= n_experts <= 1024; d <= 65536.  Products are summed to about 48 bits and scored in fp64: two experts come in their exact
+ * order unless their sums are within some 1e-11 of the sum of their products' absolute values.  NaN counts as the lowest score.
  * Errors: INVALID_ARG, CUDA. */
 int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k, const void* x, int64_t x_stride, const void* w_router,
                   const float* favour, int score, int renorm, float scale, int32_t* ids, float* weights, void* cuda_stream);
@@ -161,7 +160,7 @@ typedef struct {
 
 /* out[row] = residual[row] + sum_j weights[row][j] * down[e] (silu(gate[e] x[row]) * (up[e] x[row])),  e = ids[row][j],
  * silu(a) = a / (1 + exp(-a)); a slot with ids outside [0, n_experts) adds nothing (experts that are elsewhere).  Made for the rows of a
- * decoding or verification step: every expert that some row goes to is read once for up to 32 of its rows.
+ * decoding or verification step: an expert that some row goes to is read once for up to 8, 16 or 32 of its rows, by how many go to one on average.
  * x, residual and out: [row][d] of the experts' dtype, 16-byte aligned, rows *_stride elements apart, multiples of 8; residual may be
  * NULL; out may be residual with its stride, and overlaps nothing else.  n_rows <= 1024, 1 <= k <= 16.
  * Sums in fp32, slots in order; silu(..) * (..) enters the product with down as a pair of values of the type (16 bits
