@@ -155,16 +155,30 @@ __global__ void __launch_bounds__(kRouteThreads, 2) route_kernel(const __grid_co
     }
     cluster_sync();
     if (rank || warp) return;
-    // weights of the winners, a lane each
+    // Weights of the winners, a lane each.  Renormalised ones are formed relative to the largest, so that scores below fp32 (sigmoids far below
+    // 0, or experts that favour alone puts first) keep their ratios.
+    auto exp_of = [](double z) {  // (what rounding the exponent to fp32 leaves is a factor)
+        const float near = (float)z, rest = (float)(z - (double)near);
+        return expf(near) * (1.f + (isfinite(near) ? rest : 0.f));
+    };
+    double v = lane < a.k ? s_top[lane] : -INFINITY;
+    const float lead = warp_max((float)v);
     float p = 0.f;
-    if (lane < a.k) {
-        // (what rounding the exponent to fp32 leaves is a factor)
-        const double z = a.score == SSD_MOE_SIGMOID ? -s_top[lane] : s_top[lane] - s_top[0];
-        const float near = (float)z, rest = (float)(z - (double)near), e = expf(near) * (1.f + (isfinite(near) ? rest : 0.f));
-        if (whole) p = (float)s_top[lane];
-        else if (a.score == SSD_MOE_SIGMOID) p = 1.f / (1.f + e);
-        else p = e;  // (renormalised below)
+    if (whole) {
+        if (a.renorm && lead < 0x1p-100f) {
+            double m = v;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
+            v /= m;
+        }
+        p = (float)v;
+    } else if (a.score == SSD_MOE_SIGMOID) {
+        const float shift = a.renorm ? fminf(lead, 0.f) : 0.f;
+        p = (v > 0.0 ? 1.f : exp_of(v - (double)shift)) / (1.f + exp_of(-fabs(v)));
+    } else {
+        p = exp_of(v - s_top[0]);
     }
+    if (lane >= a.k) p = 0.f;
     if (a.renorm) p /= warp_sum(p);
     if (lane < a.k) {
         a.ids[(int64_t)row * a.k + lane] = (int)s_who[lane];
@@ -841,7 +855,8 @@ extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void
     const Workspace w = workspace_of(m, n_rows, k);
     const size_t picked = 4 * (size_t)n_rows * k, rows = span(n_rows, out_stride, m.d, m.dtype);
     const Range o[1] = {{out, rows}}, ws[1] = {{workspace, w.total}}, st[1] = {{status, 4}};
-    const Range in[3] = {{x, span(n_rows, x_stride, m.d, m.dtype)}, {ids, picked}, {weights, picked}}, re[1] = {{residual, residual ? span(n_rows, residual_stride, m.d, m.dtype) : 0}};
+    auto matrices = [&](int64_t stride) { return 2 * ((size_t)(m.n_experts - 1) * (size_t)(m.n_experts > 1 ? stride : 0) + (size_t)size); };
+    const Range in[6] = {{x, span(n_rows, x_stride, m.d, m.dtype)}, {ids, picked}, {weights, picked}, {m.gate, matrices(m.gate_stride)}, {m.up, matrices(m.up_stride)}, {m.down, matrices(m.down_stride)}}, re[1] = {{residual, residual ? span(n_rows, residual_stride, m.d, m.dtype) : 0}};
     if (meet(o, in) || (out != residual && meet(o, re))) return refuse_arg(call, "out must be the residual with its stride or overlap no input");
     if (meet(ws, o) || meet(ws, in) || meet(ws, re) || meet(st, o) || meet(st, ws) || meet(st, in) || meet(st, re))
         return refuse_arg(call, "workspace and status must not overlap other tensors");

@@ -74,6 +74,28 @@ def test_route_with_nan_and_infinities(ssd):
     assert abs(p[0] - 1) < 1e-7 and p[1] == p[2] == 0.5 and p[3] == 0.0 and p[4] != p[4]
 
 
+@pytest.mark.parametrize("score,favour", [(0, True), (1, False), (1, True)])
+def test_route_of_scores_below_fp32(ssd, score, favour):
+    """Products from -400 to 0: renormalised weights are ratios, however small the scores.  (Sums of few powers of two: the products are exact.)"""
+    n, e, k = 6, 24, 4
+    x, w = torch.zeros(n, 8, dtype=torch.bfloat16), torch.zeros(e, 8, dtype=torch.bfloat16)
+    x[:, 0], x[:, 1] = 1.0, torch.tensor([0.0, -8.0, -20.0, -40.0, -50.0, 1.0])
+    w[:, 0], w[:, 1] = -torch.arange(e) / 4.0, 8.0
+    w[0] = 0.0
+    bias = torch.zeros(e)
+    bias[5:12] = torch.arange(7) * 0.25 + 2.0  # (these come first)
+    if not favour:
+        w[0, 0], w[0, 1] = -3.0, 8.0
+    x, w, bias = x.cuda(), w.cuda(), bias.cuda() if favour else None
+    ids, weights = torch.empty(n, k, dtype=torch.int32, device="cuda"), torch.empty(n, k, device="cuda")
+    for renorm in (True, False):
+        ssd.ssd_moe_route(x, w, ids, weights, score=score, favour=bias, renorm=renorm, cuda_stream=stream())
+        torch.cuda.synchronize()
+        want, p = ref.routed(f64(x), f64(w), k, None if bias is None else bias.cpu().numpy(), score == 1, renorm, 1.0)
+        assert np.array_equal(ids.cpu().numpy(), want)
+        np.testing.assert_allclose(f64(weights), p, rtol=16 * 2.0**-24, atol=2.0**-140)
+
+
 # -- products ---------------------------------------------------------------------
 
 class Layer:

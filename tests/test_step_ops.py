@@ -200,6 +200,12 @@ def test_mlp_refuses(ssd, bad):
     refused(ssd, mlp(ssd, **bad), "ssd_moe_mlp")
 
 
+@pytest.mark.parametrize("bad", [dict(out=3 * FAR - 16), dict(ws=3 * FAR + 2 * 64 * 48 - 16), dict(status=3 * FAR + 2 * 64 * 48 * 8 - 4)], ids=str)
+@pytest.mark.parametrize("which", ["gate", "up", "down"])
+def test_mlp_refuses_results_in_its_matrices(ssd, which, bad):
+    refused(ssd, mlp(ssd, moe(ssd, **{which: 3 * FAR}), **bad), "ssd_moe_mlp")
+
+
 def test_mlp_says_when_the_workspace_is_short(ssd):
     n = ctypes.c_size_t()
     assert ssd.lib.ssd_moe_workspace(moe(ssd), 3, 2, n) == ssd.SSD_OK and n.value >= 2 * 2 * 6 * 48 + 4 * 6 * 64
