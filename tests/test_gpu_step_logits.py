@@ -223,6 +223,39 @@ def test_infinities_and_nan(ssd):
     check(ssd, c, 6)
 
 
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_rows_of_the_lowest_value(ssd, typ):
+    """Masks that were made with the type's lowest value instead of -inf: tokens like any other."""
+    c = Case(5, typ, 5003, [4], hist=0, tokens=False)
+    c.logits[:] = torch.finfo(TYPES[typ]).min
+    c.logits[1, 4000] = -1.0
+    c.logits[2, ::2] = -float("inf")
+    c.logits[3, 1:] = -float("inf")
+    c.host = c.logits.float().cpu().numpy()
+    for k in (1, 3):
+        check(ssd, c, k, want_adjust=False)
+
+
+def test_more_rows_than_a_grid_axis_has(ssd):
+    n, vocab = 70001, 37
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(n, vocab, device="cuda", generator=g)
+    bias = torch.randn(2, vocab, device="cuda", generator=g)
+    rules = ssd.LogitRules(vocab, n, bias=bias, bias_of=(torch.arange(n, device="cuda") % 2).int())
+    tokens, logprob, total, out = torch.empty(n, 2, dtype=torch.int32, device="cuda"), torch.empty(n, 2, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x)
+    ssd.ssd_logits_choose(rules, x, tokens, logprob, total, stream())
+    ssd.ssd_logits_adjust(rules, x, out, stream())
+    torch.cuda.synchronize()
+    want = x + bias[torch.arange(n, device="cuda") % 2]
+    assert torch.equal(out, want)
+    top = torch.sort(want, dim=-1, descending=True, stable=True)
+    assert torch.equal(tokens, top[1][:, :2].int())
+    sums = torch.logsumexp(want.double(), -1)
+    # (logits under 16, sums of 37 weights: 64 roundings of values under 16)
+    assert float((total.double() - sums).abs().max()) < 64 * 16 * 2.0**-24
+    assert float((logprob.double() - (top[0][:, :2].double() - sums[:, None])).abs().max()) < 64 * 16 * 2.0**-24
+
+
 def test_an_ascending_row(ssd):
     """The best are all of one thread's chunk, and the last thread's best is the row's worst."""
     c = Case(3, "f32", 30000, [3], tokens=False)
