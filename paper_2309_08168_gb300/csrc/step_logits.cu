@@ -4,6 +4,7 @@
 #include <cfloat>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "step_ops.cuh"
 
@@ -100,14 +101,15 @@ struct Chunk {
 // chip has it), so a thread keeps its best chunk rather than its best token, and sums weights relative to a whole number above its
 // best, which seldom changes.
 //
-// kRules: 0: the rules have no part; 1: no biases; 2: biases.  (With the code for biases in it, though none are added, 456 rows of 128256 take
-// 55 us instead of 42 where texts are penalised.)
+// kRules: 0: the rules have no part; 1: no biases; 2: biases; 3: biases that do not lie on 16 bytes where the logits do.  (With the code for biases in it, though none are added, 456 rows of 128256 take
+// 55 us instead of 42 where texts are penalised.  207 bf16 rows of 50257 with biases, eight best: 28.0 us; biases as eight floats each through L1
+// 29.0; in 3 with two chunks under way, which spills, 30.0.)
 constexpr int ctas_of(bool choose, int rules) { return choose && rules ? 3 : 4; }  // of an SM
 template <typename T, bool kChoose, int kRules>
 __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logits_kernel(const __grid_constant__ LogitArgs a) {
     constexpr int V = Vec<T>::N;  // tokens in 16 bytes
-    constexpr int kParts = 8 / V;
-    constexpr int kAhead = kRules == 2 || (kRules && !kChoose) ? 2 : V / 2;  // chunks under way in a thread
+    constexpr int kParts = 8 / V, kAdds = kRules == 3 ? 3 : 2;
+    constexpr int kAhead = kRules == 3 ? 1 : kRules >= 2 || (kRules && !kChoose) ? 2 : V / 2;  // chunks under way in a thread
     extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ int s_request, s_rows[2], s_n, s_scan[kLogitWarps];
     __shared__ float s_m[kLogitWarps], s_s[kLogitWarps];
@@ -294,15 +296,22 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
         };
         // the 8 bits of a chunk's tokens in the row's mask; 0: nothing of it is left
         auto shown = [&](int x0) -> uint32_t { return allowed ? bits8(s_show, x0 - 32 * word0) : 255u; };
-        auto load_bias = [&](int x, float4* add) {
+        // A chunk's biases are the 8 floats from number `shift` on of the 12 in add (rules 3: aligned loads, and the same shift for all of the row)
+        const int shift = kRules == 3 && bias ? (int)(((uintptr_t)bias / 4 + (uintptr_t)(intptr_t)first) & 3u) : 0;
+        auto load_bias = [&](int x, float4 (&add)[kAdds]) {
             if (kRules < 2 || !bias) return;
-            if (whole(x) && ((uintptr_t)(bias + x) & 15u) == 0) {
-                add[0] = __ldcg(reinterpret_cast<const float4*>(bias + x)), add[1] = __ldcg(reinterpret_cast<const float4*>(bias + x) + 1);
-            } else {
-                float v[8];
+            if (kRules == 2 ? whole(x) && ((uintptr_t)(bias + x) & 15u) == 0 : x >= shift && x - shift + 12 <= vocab) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = inside(x + j) ? bias[x + j] : 0.f;  // (through L1: the next lanes want the same sectors)
-                add[0] = make_float4(v[0], v[1], v[2], v[3]), add[1] = make_float4(v[4], v[5], v[6], v[7]);
+                for (int i = 0; i < kAdds; ++i) add[i] = __ldcg(reinterpret_cast<const float4*>(bias + x - shift) + i);
+            } else {
+                float v[4 * kAdds];
+#pragma unroll
+                for (int j = 0; j < 4 * kAdds; ++j) {
+                    const bool there = j >= shift && j < shift + 8 && inside(x + j - shift);
+                    v[j] = there ? bias[x + j - shift] : 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < kAdds; ++i) add[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             }
         };
         auto penalised = [&](float l, uint32_t n) {
@@ -310,7 +319,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
             l = __fsub_rn(l > 0.f ? __fdiv_rn(l, again) : __fmul_rn(l, again), __fmul_rn(often, (float)c));
             return c ? __fsub_rn(l, once) : l;
         };
-        auto rules = [&](int x0, uint32_t show, const float4* add, float (&f)[8]) {
+        auto rules = [&](int x0, uint32_t show, const float4 (&add)[kAdds], float (&f)[8]) {
             if (a.counted) {
                 const int at = x0 - lo + 8;  // >= 0
                 const uint32_t m = bits8(s_bits, at);
@@ -323,16 +332,26 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                     }
                 }
             }
-            if (kRules == 2 && bias) {
-                const float4 u = add[0], w = add[1];
-                f[0] += u.x, f[1] += u.y, f[2] += u.z, f[3] += u.w, f[4] += w.x, f[5] += w.y, f[6] += w.z, f[7] += w.w;
+            if (kRules >= 2 && bias) {
+                float v[4 * kAdds];
+#pragma unroll
+                for (int i = 0; i < kAdds; ++i) v[4 * i] = add[i].x, v[4 * i + 1] = add[i].y, v[4 * i + 2] = add[i].z, v[4 * i + 3] = add[i].w;
+                auto plus = [&](auto from) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] += v[(j + decltype(from)::value) % (4 * kAdds)];
+                };
+                if (kRules == 2 || shift == 0) plus(std::integral_constant<int, 0>());
+                else if (shift == 1) plus(std::integral_constant<int, 1>());
+                else if (shift == 2) plus(std::integral_constant<int, 2>());
+                else plus(std::integral_constant<int, 3>());
             }
             if (show != 255u) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = show >> j & 1u ? f[j] : -INFINITY;
             }
         };
-        // A mask that leaves at most 1 / 32 of the slice: its tokens in order, so that only they are read (`few` of them; -1: more)
+        // A mask that leaves at most 1 / 16 of the slice: its tokens in order, so that only they are read (`few` of them; -1: more).  (512 rows of 128256,
+        // 64 masks: 92 us; at 1 / 32 95, at 1 / 8 95: the list takes a CTA's place.)
         int few = -1;
         if (kChoose && kRules && allowed) {
             const int low = max(first, 0), n = (stop - 1) / 32 - word0 + 1;
@@ -359,7 +378,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                 if (w < warp) to += s_scan[w];
                 all += s_scan[w];
             }
-            if (all * 32 <= a.slice) {
+            if (all * 16 <= a.slice) {
                 few = all;
                 for (int w = w0; w < w1; ++w)
                     for (uint32_t u = word(w); u; u &= u - 1) s_list[to++] = (uint32_t)(32 * (word0 + w) + __ffs((int)u) - 1);
@@ -373,7 +392,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                 const uint32_t n = s_bits[i / 32] >> i % 32 & 1u ? s_count[count_of(i)] : 0u;
                 if (n) l = penalised(l, n);
             }
-            return kRules == 2 && bias ? l + add : l;
+            return kRules >= 2 && bias ? l + add : l;
         };
         // choose: the largest logit of the thread, its chunk (of few: its number among them), and the sum of exp(logit - ref)
         float best = -INFINITY, ref = -FLT_MAX, sum = 0.f;
@@ -387,7 +406,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
             for (int i = 0; i < 4; ++i) {
                 token[i] = e + i * kLogitThreads < few ? (int)s_list[e + i * kLogitThreads] : -1;
                 raw[i] = token[i] >= 0 ? (float)src[token[i]] : -INFINITY;
-                add[i] = kRules == 2 && bias && token[i] >= 0 ? __ldcg(bias + token[i]) : 0.f;
+                add[i] = kRules >= 2 && bias && token[i] >= 0 ? __ldcg(bias + token[i]) : 0.f;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -404,7 +423,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
         }
         for (int x = few < 0 ? first + 8 * tid : stop; x < stop; x += 8 * kLogitThreads * kAhead) {
             Chunk<T> c[kAhead];
-            float4 add[2];
+            float4 add[kAdds];
             uint32_t show[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -504,7 +523,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                         token = (int)s_list[at];
                     } else {
                         float f[8];
-                        float4 add[2];
+                        float4 add[kAdds];
                         if (kRules) {
                             load(at, kept);
                             load_bias(at, add);
@@ -542,7 +561,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                         const int e = s_from[i % n_from] + i / n_from * kLogitThreads;
                         if (e >= few) continue;
                         const int x = (int)s_list[e];
-                        const float l = value(x, (float)src[x], kRules == 2 && bias ? __ldcg(bias + x) : 0.f);
+                        const float l = value(x, (float)src[x], kRules >= 2 && bias ? __ldcg(bias + x) : 0.f);
                         const uint64_t key = key_of(l + 0.f, x);
                         if (l > -INFINITY && key >= bound) s_cand[atomicAdd(&s_n, 1)] = key;
                     }
@@ -552,7 +571,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                     if (x0 >= stop) continue;
                     Chunk<T> c;
                     float f[8];
-                    float4 add[2];
+                    float4 add[kAdds];
                     load(x0, c);
                     if (kRules) load_bias(x0, add);
                     c.get(f);
@@ -613,7 +632,7 @@ size_t lay_out(LogitArgs& a) {
     const int deep = (a.slice / 8 + kLogitThreads - 1) / kLogitThreads;
     a.at_show = a.k > 1 ? a.k * deep * 8 * 8 : 0;
     a.at_list = a.at_show + (r.allowed ? (a.slice / 32 + 3) * 4 : 0);
-    a.at_bits = a.at_list + (r.allowed && a.k ? a.slice / 32 * 4 : 0);
+    a.at_bits = a.at_list + (r.allowed && a.k ? a.slice / 16 * 4 : 0);
     a.at_bits = (a.at_bits + 15) / 16 * 16;
     a.n_words = (a.slice + 8 + 127) / 128 * 4;
     if (!a.counted) return a.at_bits;
@@ -624,7 +643,8 @@ constexpr int kMostShared = 180 * 1024;  // (a slice of 32832 tokens, all of the
 
 template <typename T>
 int set_up() {
-    void (*const k[])(LogitArgs) = {logits_kernel<T, true, 0>, logits_kernel<T, true, 1>, logits_kernel<T, true, 2>, logits_kernel<T, false, 1>, logits_kernel<T, false, 2>};
+    void (*const k[])(LogitArgs) = {logits_kernel<T, true, 0>, logits_kernel<T, true, 1>, logits_kernel<T, true, 2>, logits_kernel<T, true, 3>, logits_kernel<T, false, 1>, logits_kernel<T, false, 2>,
+                                      logits_kernel<T, false, 3>};
     cudaError_t e = cudaSuccess;
     for (auto f : k)
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
@@ -633,8 +653,8 @@ int set_up() {
 
 template <typename T>
 cudaError_t start(const cudaLaunchConfig_t& cfg, const LogitArgs& a, bool choose, int rules) {
-    if (!choose) return cudaLaunchKernelEx(&cfg, rules == 2 ? logits_kernel<T, false, 2> : logits_kernel<T, false, 1>, a);
-    return cudaLaunchKernelEx(&cfg, rules == 2 ? logits_kernel<T, true, 2> : rules ? logits_kernel<T, true, 1> : logits_kernel<T, true, 0>, a);
+    if (!choose) return cudaLaunchKernelEx(&cfg, rules == 3 ? logits_kernel<T, false, 3> : rules == 2 ? logits_kernel<T, false, 2> : logits_kernel<T, false, 1>, a);
+    return cudaLaunchKernelEx(&cfg, rules == 3 ? logits_kernel<T, true, 3> : rules == 2 ? logits_kernel<T, true, 2> : rules ? logits_kernel<T, true, 1> : logits_kernel<T, true, 0>, a);
 }
 
 int check_rules(const char* call, const ssd_logit_rules* r, int dtype, const void* logits, int64_t stride) {
@@ -696,7 +716,10 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     a.counted = (r.repetition || r.presence || r.frequency) && (r.history || r.tokens);
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "no device");
-    const int rules = r.bias ? 2 : a.counted || r.allowed ? 1 : 0, slots = sms * ctas_of(choose, rules);
+    // (chunks start on 16 bytes of the logits: those of the biases too in every row and set, or not)
+    const size_t size = dtype == SSD_F32 ? 4 : 2;
+    const bool even = ((uintptr_t)r.bias & 15u) == 0 && r.bias_stride % 4 == 0 && (uintptr_t)a.logits % (4 * size) == 0 && a.stride % 4 == 0;
+    const int rules = r.bias ? even ? 2 : 3 : a.counted || r.allowed ? 1 : 0, slots = sms * ctas_of(choose, rules);
     // A row's slices: 1 to 8, whichever is done first if a wave of CTAs takes as long as its slice and 20000 tokens more for its start
     // and end, or 30000 with counts to make.  (512 rows of 128256, penalised and masked: whole 68 us, in two 70, in four 94; 207
     // rows of 50257, penalised and with biases: whole 39, in two 29, in four 44.)
