@@ -14,6 +14,8 @@ namespace step {
 constexpr int kLogitThreads = 256, kLogitWarps = kLogitThreads / 32;
 constexpr int kMaxVocab = 262144;
 constexpr int kMaxSlice = 131136;  // tokens of a CTA: at most 17 chunks of 8 in each of its threads
+constexpr int kFew = 8;            // a mask that leaves one token of so many is taken as a list
+constexpr int kMaxListed = 65472;  // tokens of a CTA whose places a list can hold in 16 bits
 constexpr int kMaxSplit = 8;      // CTAs of a row: one portable cluster
 constexpr int kMaxBest = 16;
 constexpr int kJoinWarps = kMaxSplit * kMaxBest / 32;
@@ -117,7 +119,8 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
     __shared__ int s_from[kMaxBest], s_found;
     __shared__ Partial s_part[2];
     uint64_t* s_cand = reinterpret_cast<uint64_t*>(s_dyn);
-    uint32_t *s_show = reinterpret_cast<uint32_t*>(s_dyn + a.at_show), *s_list = reinterpret_cast<uint32_t*>(s_dyn + a.at_list);
+    uint32_t* s_show = reinterpret_cast<uint32_t*>(s_dyn + a.at_show);
+    uint16_t* s_list = reinterpret_cast<uint16_t*>(s_dyn + a.at_list);
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, split = gridDim.x, vocab = a.r.vocab;
@@ -350,8 +353,8 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                 for (int j = 0; j < 8; ++j) f[j] = show >> j & 1u ? f[j] : -INFINITY;
             }
         };
-        // A mask that leaves at most 1 / 16 of the slice: its tokens in order, so that only they are read (`few` of them; -1: more).  (512 rows of 128256,
-        // 64 masks: 92 us; at 1 / 32 95, at 1 / 8 95: the list takes a CTA's place.)
+        // A mask that leaves at most 1 / kFew of the slice: its tokens in order, so that only they are read (`few` of them; -1: more).  512 rows
+        // of 128256 with penalties and biases, 64 masks, one of ten in [1/16, 1/8]: 90.0 us; at 1/16 93.8, at 1/4 97.7, for five best 130 (a list of 32 KB takes a CTA's place).
         int few = -1;
         if (kChoose && kRules && allowed) {
             const int low = max(first, 0), n = (stop - 1) / 32 - word0 + 1;
@@ -378,10 +381,10 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                 if (w < warp) to += s_scan[w];
                 all += s_scan[w];
             }
-            if (all * 16 <= a.slice) {
+            if (all * kFew <= a.slice) {
                 few = all;
                 for (int w = w0; w < w1; ++w)
-                    for (uint32_t u = word(w); u; u &= u - 1) s_list[to++] = (uint32_t)(32 * (word0 + w) + __ffs((int)u) - 1);
+                    for (uint32_t u = word(w); u; u &= u - 1) s_list[to++] = (uint16_t)(32 * (word0 + w) + __ffs((int)u) - 1 - (lo - 8));
             }
             __syncthreads();
         }
@@ -399,27 +402,62 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
         int at = 0x7fffffff;
         Chunk<T> kept;
         T* out = kChoose ? nullptr : (T*)a.out + (int64_t)row * a.out_stride;
-        for (int e = tid; e < few; e += 4 * kLogitThreads) {
-            float raw[4], add[4];
-            int token[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                token[i] = e + i * kLogitThreads < few ? (int)s_list[e + i * kLogitThreads] : -1;
-                raw[i] = token[i] >= 0 ? (float)src[token[i]] : -INFINITY;
-                add[i] = kRules >= 2 && bias && token[i] >= 0 ? __ldcg(bias + token[i]) : 0.f;
+        // sum and reference with 8 more logits, the largest of them top
+        auto weigh = [&](const float (&f)[8], float top) {
+            if (top > ref) {
+                const float up = ceilf(top);
+                sum *= exp2_of((ref - up) * kLog2e);
+                ref = up;
             }
+            uint64_t e2 = 0ull;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (token[i] < 0) break;
-                const float l = value(token[i], raw[i], add[i]);
-                if (l > best) best = l, at = e + i * kLogitThreads;
-                if (l > ref) {
-                    const float up = ceilf(l);
-                    sum *= exp2_of((ref - up) * kLog2e);
-                    ref = up;
+            for (int j = 0; j < 8; j += 2) {
+                const float2 d = of_pair(mul_pair(add_pair(pair_of(f[j], f[j + 1]), pair_of(-ref, -ref)), pair_of(kLog2e, kLog2e)));
+                e2 = add_pair(e2, pair_of(exp2_of(d.x), exp2_of(d.y)));
+            }
+            const float2 e = of_pair(e2);
+            float s = e.x + e.y;
+            if (!(s < 16.f)) {  // (infinite or NaN among them)
+                s = 0.f;
+                for (int j = 0; j < 8; ++j)
+                    if (f[j] == f[j]) s += weight(f[j], ref);
+            }
+            sum += s;
+        };
+        // (fmaxf passes NaN over)
+        auto largest = [](const float (&f)[8]) { return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7]))); };
+        for (int e = tid; kChoose && kRules && e < few; e += 8 * kLogitThreads) {
+            int x[8];  // places
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = e + i * kLogitThreads < few ? (int)s_list[e + i * kLogitThreads] : -1;
+                f[i] = x[i] >= 0 ? (float)src[lo - 8 + x[i]] : -INFINITY;
+            }
+            if (a.counted) {
+                uint32_t m = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (x[i] >= 0) m |= (s_bits[x[i] / 32] >> x[i] % 32 & 1u) << i;
+                if (m) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t n = m >> i & 1u ? s_count[count_of(x[i])] : 0u;
+                        if (n) f[i] = penalised(f[i], n);
+                    }
                 }
-                if (l == l) sum += weight(l, ref);
             }
+            if (kRules >= 2 && bias) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] += x[i] >= 0 ? __ldcg(bias + lo - 8 + x[i]) : 0.f;  // (asked for with the logits: registers, the same time)
+            }
+            const float top = largest(f);
+            if (top > best) {
+                best = top;
+#pragma unroll
+                for (int i = 7; i >= 0; --i) at = f[i] == top ? e + i * kLogitThreads : at;
+            }
+            weigh(f, top);
         }
         for (int x = few < 0 ? first + 8 * tid : stop; x < stop; x += 8 * kLogitThreads * kAhead) {
             Chunk<T> c[kAhead];
@@ -445,31 +483,12 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                     }
                     if (kRules && i + 1 < kAhead && show[(i + 1) % kAhead]) load_bias(x0 + 8 * kLogitThreads, add);
                     if (!show[i]) continue;
-                    // (fmaxf passes NaN over)
-                    const float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+                    const float top = largest(f);
                     if (top > best) {
                         best = top, at = x0;
                         if (!kRules) kept = c[i];
                     }
-                    if (top > ref) {
-                        const float up = ceilf(top);
-                        sum *= exp2_of((ref - up) * kLog2e);
-                        ref = up;
-                    }
-                    uint64_t e2 = 0ull;
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const float2 d = of_pair(mul_pair(add_pair(pair_of(f[j], f[j + 1]), pair_of(-ref, -ref)), pair_of(kLog2e, kLog2e)));
-                        e2 = add_pair(e2, pair_of(exp2_of(d.x), exp2_of(d.y)));
-                    }
-                    const float2 e = of_pair(e2);
-                    float s = e.x + e.y;
-                    if (!(s < 16.f)) {  // (infinite or NaN among them)
-                        s = 0.f;
-                        for (int j = 0; j < 8; ++j)
-                            if (f[j] == f[j]) s += weight(f[j], ref);
-                    }
-                    sum += s;
+                    weigh(f, top);
                 } else {
                     if (x0 >= stop) break;
                     if (show[i]) {
@@ -520,7 +539,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                 if (key && at == (int)~(uint32_t)key - 8) {  // (this thread's chunk)
                     int token = at + 7;
                     if (kRules && few >= 0) {
-                        token = (int)s_list[at];
+                        token = lo - 8 + (int)s_list[at];
                     } else {
                         float f[8];
                         float4 add[kAdds];
@@ -560,7 +579,7 @@ __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logit
                     for (int i = tid; i < n_from * ((few + kLogitThreads - 1) / kLogitThreads); i += kLogitThreads) {
                         const int e = s_from[i % n_from] + i / n_from * kLogitThreads;
                         if (e >= few) continue;
-                        const int x = (int)s_list[e];
+                        const int x = lo - 8 + (int)s_list[e];
                         const float l = value(x, (float)src[x], kRules >= 2 && bias ? __ldcg(bias + x) : 0.f);
                         const uint64_t key = key_of(l + 0.f, x);
                         if (l > -INFINITY && key >= bound) s_cand[atomicAdd(&s_n, 1)] = key;
@@ -632,7 +651,7 @@ size_t lay_out(LogitArgs& a) {
     const int deep = (a.slice / 8 + kLogitThreads - 1) / kLogitThreads;
     a.at_show = a.k > 1 ? a.k * deep * 8 * 8 : 0;
     a.at_list = a.at_show + (r.allowed ? (a.slice / 32 + 3) * 4 : 0);
-    a.at_bits = a.at_list + (r.allowed && a.k ? a.slice / 16 * 4 : 0);
+    a.at_bits = a.at_list + (r.allowed && a.k ? (a.slice / kFew + 1) / 2 * 4 : 0);
     a.at_bits = (a.at_bits + 15) / 16 * 16;
     a.n_words = (a.slice + 8 + 127) / 128 * 4;
     if (!a.counted) return a.at_bits;
@@ -727,7 +746,7 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     long long least = 0;
     for (int split = 1; split <= kMaxSplit; split *= 2) {
         a.slice = ((r.vocab + 7 + split - 1) / split + 63) / 64 * 64;
-        if (a.slice > kMaxSlice || (split > 1 && a.slice < 1024)) continue;
+        if (a.slice > (choose && r.allowed ? kMaxListed : kMaxSlice) || (split > 1 && a.slice < 1024)) continue;
         const size_t bytes = lay_out(a);
         if (bytes > kMostShared) continue;
         const int fit = (int)std::min<size_t>(slots / sms, (222 * 1024) / (bytes + 4096));

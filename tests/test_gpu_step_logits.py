@@ -211,6 +211,21 @@ def test_masks_that_leave_few(ssd, k, typ, vocab, pad):
     check(ssd, c, k)
 
 
+@pytest.mark.parametrize("k", [1, 5])
+@pytest.mark.parametrize("typ,vocab,n", [("f16", 262144, 8), ("bf16", 66001, 320), ("f32", 9001, 16)])
+def test_masks_that_leave_an_eighth(ssd, k, typ, vocab, n):
+    """As many tokens as are taken as a list, some fewer and more; slices as large as lists can be."""
+    rng = np.random.default_rng(n)
+    c = Case(43, typ, vocab, None, n=n, hist=90, few=vocab, tokens=False, bias=2, masks=8)
+    bits = np.zeros((8, -(-vocab // 32) * 32), bool)
+    for i, step in enumerate((7, 8, 9)):
+        bits[i, i:vocab:step] = True
+    for i, share in enumerate((0.1, 0.124, 0.126, 0.3, 0.06)):
+        bits[3 + i, :vocab] = rng.random(vocab) < share
+    c.r["allowed"] = np.packbits(bits, axis=1, bitorder="little").view(np.int32)
+    check(ssd, c, k, want_adjust=False)
+
+
 def test_infinities_and_nan(ssd):
     c = Case(2, "f32", 3333, [5], hist=40, few=20, masks=3)
     c.r["allowed_of"][:] = -1
