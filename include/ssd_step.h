@@ -22,7 +22,7 @@
  * other as long as they share no output and no workspace.
  *
  * Return value: SSD_OK or a negative SSD_ERR_* code of ssd.h, with the message
- * in ssd_last_error().  The first use of a call on a device sets its kernels up;
+ * in ssd_last_error().  Tensors are aligned to their type at least (refused if not).  The first use of a call on a device sets its kernels up;
  * make it before any stream capture.  Host-side errors are found before anything
  * is launched.  What only the device can see is kept inside the tensors' bounds:
  * rows outside [0, n_rows), slots outside the cache, tokens outside [0, vocab),

@@ -238,6 +238,7 @@ extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rop
     if (n_rows < 0 || n_heads < 1 || n_heads > 65536) return refuse_arg(call, "need n_rows >= 0 and 1 <= n_heads <= 65536");
     if (n_rows == 0) return SSD_OK;
     if (!q || !k || !v || !positions || !slots || !q_out) return refuse_arg(call, "NULL pointer");
+    if (!aligned(4, {positions, slots})) return refuse_arg(call, "positions and slots must be aligned to their type");
     const int hd = cache->head_dim;
     if (int rc = check_rows(call, "q", q, q_stride, dtype, (int64_t)n_heads * hd)) return rc;
     if (int rc = check_rows(call, "q_out", q_out, q_out_stride, dtype, (int64_t)n_heads * hd)) return rc;

@@ -684,6 +684,9 @@ int check_rules(const char* call, const ssd_logit_rules* r, int dtype, const voi
     if (r->n_rows == 0) return SSD_OK;
     if (r->row_start ? r->n_requests < 1 || r->n_requests > kMaxRequests : r->n_requests != r->n_rows)
         return refuse_arg(call, "need 1 <= n_requests <= 4096, or without row_start n_requests = n_rows");
+    if (!aligned(4, {r->row_start, r->history, r->history_len, r->prompt_len, r->tokens, r->repetition, r->presence, r->frequency, r->bias, r->bias_of, r->allowed, r->allowed_of}) ||
+        !aligned(8, {r->masks}))
+        return refuse_arg(call, "what the rules read must be aligned to its type");
     const int64_t most = int64_t(1) << 37;
     if (!logits) return refuse_arg(call, "NULL logits");
     if (stride < r->vocab || stride > most || (uintptr_t)logits % (dtype == SSD_F32 ? 4 : 2)) return refuse_arg(call, "logits: rows must not overlap, aligned to their type");
@@ -811,6 +814,7 @@ extern "C" int ssd_logits_choose(const ssd_logit_rules* rules, int dtype, const 
     if (k < 1 || k > kMaxBest) return refuse_arg(call, "need 1 <= k <= 16");
     if (rules->n_rows == 0) return SSD_OK;
     if (!tokens || !logprob) return refuse_arg(call, "NULL pointer");
+    if (!aligned(4, {tokens, logprob, total})) return refuse_arg(call, "the results must be aligned to their type");
     const size_t n = 4 * (size_t)rules->n_rows;
     const Range a1[1] = {{tokens, n * k}}, a2[1] = {{logprob, n * k}}, a3[1] = {{total, n}}, in[1] = {{logits, span(rules->n_rows, stride, rules->vocab, dtype)}};
     if (meet(a1, a2) || meet(a1, a3) || meet(a2, a3) || meet(a1, in) || meet(a2, in) || meet(a3, in) || meets_rules(a1, *rules) || meets_rules(a2, *rules) ||

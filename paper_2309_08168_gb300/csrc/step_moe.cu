@@ -790,6 +790,7 @@ extern "C" int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k,
     if (!x || !w_router || !ids || !weights) return refuse_arg(call, "NULL pointer");
     if (int rc = check_rows(call, "x", x, x_stride, dtype, d)) return rc;
     if ((uintptr_t)w_router & 15u) return refuse_arg(call, "w_router must be 16-byte aligned");
+    if (!aligned(4, {favour, ids, weights})) return refuse_arg(call, "favour, ids and weights must be aligned to their type");
     const size_t picked = 4 * (size_t)n_rows * k;
     const Range i1[1] = {{ids, picked}}, w1[1] = {{weights, picked}};
     const Range in[3] = {{x, span(n_rows, x_stride, d, dtype)}, {w_router, 2 * (size_t)n_experts * d}, {favour, 4 * (size_t)n_experts}};
@@ -851,6 +852,7 @@ extern "C" int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void
     if (int rc = check_rows(call, "out", out, out_stride, m.dtype, m.d)) return rc;
     if (residual)
         if (int rc = check_rows(call, "residual", residual, residual_stride, m.dtype, m.d)) return rc;
+    if (!aligned(4, {ids, weights, status})) return refuse_arg(call, "ids, weights and status must be aligned to their type");
     if (residual == out && residual_stride != out_stride) return refuse_arg(call, "out in the residual's place needs its stride");
     const Workspace w = workspace_of(m, n_rows, k);
     const size_t picked = 4 * (size_t)n_rows * k, rows = span(n_rows, out_stride, m.d, m.dtype);

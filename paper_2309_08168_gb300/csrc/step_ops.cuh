@@ -1,6 +1,8 @@
 // step_ops.cuh - what the operators of ssd_step.h share.
 #pragma once
 
+#include <initializer_list>
+
 #include "ssd_step.h"
 #include "tree_ops.cuh"
 
@@ -27,6 +29,13 @@ inline bool meet(const Range (&a)[N], const Range (&b)[M]) {
 // bytes from the first row's start to the last row's end
 inline size_t span(int n_rows, int64_t stride, int64_t width, int dtype) {
     return ((size_t)(n_rows - 1) * (size_t)stride + (size_t)width) * (dtype == SSD_F32 ? 4 : 2);
+}
+
+// whether all of these addresses are multiples of `to` bytes
+inline bool aligned(size_t to, std::initializer_list<const void*> all) {
+    uintptr_t bits = 0;
+    for (const void* p : all) bits |= (uintptr_t)p;
+    return bits % to == 0;
 }
 
 // the current device

@@ -220,6 +220,40 @@ def test_empty_layers_need_no_device(ssd):
     assert mlp(ssd, n_rows=0, x=None, ws=None, wb=0) == ssd.SSD_OK
 
 
+# -- addresses that the types do not have ------------------------------------------
+
+@pytest.mark.parametrize("name", ["row_start", "history", "history_len", "prompt_len", "tokens", "masks", "repetition", "presence", "frequency", "bias", "bias_of", "allowed", "allowed_of"])
+def test_unaligned_rules_are_refused(ssd, name):
+    off = 4 if name == "masks" else 2
+    for call in (adjust, choose):
+        refused(ssd, call(ssd, rules(ssd, **{name: P + off})), "ssd_logits_adjust" if call is adjust else "ssd_logits_choose")
+        assert b"aligned" in ssd.lib.ssd_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(pos=P + 2), dict(slots=P + 1)], ids=str)
+def test_unaligned_heads_are_refused(ssd, bad):
+    refused(ssd, heads(ssd, **bad), "ssd_norm_rope_kv")
+    assert b"aligned" in ssd.lib.ssd_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(tokens=FAR + 2), dict(logprob=2 * FAR + 1), dict(total=3 * FAR + 2)], ids=str)
+def test_unaligned_choices_are_refused(ssd, bad):
+    refused(ssd, choose(ssd, **bad), "ssd_logits_choose")
+    assert b"aligned" in ssd.lib.ssd_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(ids=FAR + 2), dict(weights=2 * FAR + 2), dict(favour=P + 1)], ids=str)
+def test_unaligned_routes_are_refused(ssd, bad):
+    refused(ssd, route(ssd, **bad), "ssd_moe_route")
+    assert b"aligned" in ssd.lib.ssd_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(ids=P + 2), dict(weights=P + 2), dict(status=3 * FAR + 2)], ids=str)
+def test_unaligned_layers_are_refused(ssd, bad):
+    refused(ssd, mlp(ssd, **bad), "ssd_moe_mlp")
+    assert b"aligned" in ssd.lib.ssd_last_error()
+
+
 # -- what dependent launches keep to (a stale value or a hang otherwise) -------------
 
 def source(name):
