@@ -27,16 +27,16 @@ struct HeadArgs {
 // A CTA takes a row (blockIdx.x), or with gridDim.y > 1 a share of its heads; hd / V lanes hold a
 // head, 16 bytes each, so that the sum of squares is a few shuffles and every byte is read once.
 // Rotated dim e with partner p becomes r (x_e g_e cos +- x_p g_p sin), r = 1 / sqrt(mean x^2 + eps): the
-// products of gains and angles are formed once a row in shared memory (a, b), and the partner's 16 bytes come from
-// the lane that holds them.  Bound by HBM, for 16-bit rows of few heads by instructions, for few rows by the chain position - angle -
-// table - store.  Measured: 4095 fp32 rows of 32 + 2 x 32 heads of 128 63 us (335 MB, 5.3 TB/s, 78 % of the copy rate); 16000 bf16
-// rows of 32 + 2 x 8 heads 91 us (394 MB, 4.3 TB/s); 403 fp16 rows 7.1; one row 3.5.
+// products of gains and angles are formed once a row in shared memory (a, b; pair p's by thread p, so that one barrier does), and the
+// partner's 16 bytes come from the lane that holds them.  Bound by HBM, for 16-bit rows of few heads by instructions, for few rows by the chain
+// position - angle - table - store.  Measured: 4095 fp32 rows of 32 + 2 x 32 heads of 128 60.7 us (335 MB, 5.5 TB/s, 82 % of the copy rate); 16000 fp16
+// rows of 32 + 2 x 8 heads 84.4 us (394 MB, 4.7 TB/s); 403 fp16 rows 6.0; one row 2.8.  (Angles first, then each dim's products behind a second
+// barrier: 63.8, 90.0, 7.1, 3.5.  CTAs that stay for several rows, the next one's table and loads under way: 77, 106.)
 //
 // T: rows, C: cache
 template <typename T, typename C, int kHeadThreads>
 __global__ void __launch_bounds__(kHeadThreads, 1024 / kHeadThreads) heads_kernel(const __grid_constant__ HeadArgs a) {
     constexpr int V = Vec<T>::N;
-    __shared__ float2 s_cs[64];
     __shared__ __align__(16) float s_a[2][128], s_b[2][128];  // [q, k][dim]
     pdl_launch_dependents();
     pdl_wait();
@@ -65,11 +65,28 @@ __global__ void __launch_bounds__(kHeadThreads, 1024 / kHeadThreads) heads_kerne
     const int64_t position = tid < half ? __ldcg(a.positions + (int64_t)a.axis[tid] * a.n_rows + row) : 0;
     load(line);
     load_values(line);
+    // thread p has pair p, in both of its dims
     if (tid < half) {
+        const int d0 = a.rope.interleaved ? 2 * tid : tid, d1 = a.rope.interleaved ? 2 * tid + 1 : tid + half;
+        float g[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float* gain = i ? a.k_gain : a.q_gain;
+            g[i][0] = gain ? __ldcg(gain + d0) : 1.f, g[i][1] = gain ? __ldcg(gain + d1) : 1.f;
+        }
         const uint64_t turn = (uint64_t)position * a.rope.turns[tid];
         float s, c;
         sincospif((float)((int64_t)turn >> 32) * 0x1p-31f, &s, &c);
-        s_cs[tid] = make_float2(c * a.rope.amplitude, s * a.rope.amplitude);
+        s *= a.rope.amplitude, c *= a.rope.amplitude;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s_a[i][d0] = c * g[i][0], s_a[i][d1] = c * g[i][1];
+            s_b[i][d0] = -s * g[i][1], s_b[i][d1] = s * g[i][0];
+        }
+    }
+    for (int d = rot + (kHeadThreads - 1 - tid); d < a.hd; d += kHeadThreads) {
+        s_a[0][d] = a.q_gain ? __ldcg(a.q_gain + d) : 1.f, s_a[1][d] = a.k_gain ? __ldcg(a.k_gain + d) : 1.f;
+        s_b[0][d] = s_b[1][d] = 0.f;
     }
     const bool cached = slot >= 0 && slot < a.n_pages * a.page_size;
     const int64_t at = cached ? (int64_t)(slot / a.page_size) * a.page_stride + (int64_t)(slot % a.page_size) * a.pos_stride : 0;
@@ -79,20 +96,6 @@ __global__ void __launch_bounds__(kHeadThreads, 1024 / kHeadThreads) heads_kerne
         if constexpr (V == 8) *reinterpret_cast<uint4*>(p) = Vec<C>::put(f);
         else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1], C()), pack2(f[2], f[3], C()));
     };
-    __syncthreads();
-    for (int d = tid; d < a.hd; d += kHeadThreads) {
-        const bool rotated = d < rot, inter = a.rope.interleaved;
-        const int pair = inter ? d / 2 : d < half ? d : d - half;
-        const bool first = inter ? d % 2 == 0 : d < half;
-        const int partner = inter ? d ^ 1 : first ? d + half : d - half;
-        const float2 cs = rotated ? s_cs[pair] : make_float2(1.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float* g = i ? a.k_gain : a.q_gain;
-            s_a[i][d] = cs.x * (g ? __ldcg(g + d) : 1.f);
-            s_b[i][d] = rotated ? (first ? -cs.y : cs.y) * (g ? __ldcg(g + partner) : 1.f) : 0.f;
-        }
-    }
     for (int h = line; h < a.n_kv_heads; h += kValueAhead * step) {
         if (h != line) load_values(h);
 #pragma unroll
@@ -276,8 +279,8 @@ extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rop
     a.n_pages = cache->n_pages;
     a.rope = *rope;
     // few rows: a row's heads over several CTAs, until there are four per SM.  Many rows of few heads: half as many threads each, since what
-    // a warp does once a row is half of its instructions (16000 bf16 rows of 32 + 8 heads of 128 91 us, 128 threads 101; 4095 of 32 + 32
-    // heads 45, 128 threads 44).
+    // a warp does once a row is half of its instructions (with a longer start of a row 16000 bf16 rows of 32 + 8 heads of 128 took 91 us, 128 threads 101;
+    // 4095 of 32 + 32 heads 42, 128 threads 41).
     const int per16 = dtype == SSD_F32 ? 4 : 8;
     const long long units = (long long)(n_heads + cache->n_kv_heads) * hd / per16;
     if (n_rows >= 2432 && units < 1024) return start<64>(call, a, dtype, 1, cuda_stream);
