@@ -67,7 +67,7 @@ typedef struct {
 /* ssd_rope_kv (ssd_ops.h: its tensors, strides and slots) with norms before the rotation and
  * positions on several axes.
  * norm = NULL: no norms.  axes = NULL: one axis.  positions: [n_axes][n_rows], any
- * int32.  Values are copied.  Angles are exact to 2^-24 of a turn at any position; squares, sums and products in
+ * int32.  Of two rows with the same slot either may stay, K and V and each head by itself.  Values are copied.  Angles are exact to 2^-24 of a turn at any position; squares, sums and products in
  * fp32, one rounding to the rows' and the cache's type.
  * Errors: INVALID_ARG, CUDA. */
 int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rope* rope, const ssd_rope_axes* axes,
