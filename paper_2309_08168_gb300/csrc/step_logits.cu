@@ -111,7 +111,9 @@ template <typename T, bool kChoose, int kRules>
 __global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logits_kernel(const __grid_constant__ LogitArgs a) {
     constexpr int V = Vec<T>::N;  // tokens in 16 bytes
     constexpr int kParts = 8 / V, kAdds = kRules == 3 ? 3 : 2;
-    constexpr int kAhead = kRules == 3 ? 1 : kRules >= 2 || (kRules && !kChoose) ? 2 : V / 2;  // chunks under way in a thread
+    // chunks under way in a thread, as many as registers hold (adjusting 294 bf16 rows of 151936, penalised and masked: 2 43.0 us, 3 41.0, 4 41.5; fp32 rows
+    // 59.7, 61.5, 64.1; with biases 51.7, 51.8, 55.7)
+    constexpr int kAhead = kRules == 3 ? 1 : kRules == 2 ? 2 : kRules && !kChoose ? V == 8 ? 3 : 2 : V / 2;
     extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ int s_request, s_rows[2], s_n, s_scan[kLogitWarps];
     __shared__ float s_m[kLogitWarps], s_s[kLogitWarps];
