@@ -106,14 +106,17 @@ struct Chunk {
 // kRules: 0: the rules have no part; 1: no biases; 2: biases; 3: biases that do not lie on 16 bytes where the logits do.  (With the code for biases in it, though none are added, 456 rows of 128256 take
 // 55 us instead of 42 where texts are penalised.  207 bf16 rows of 50257 with biases, eight best: 28.0 us; biases as eight floats each through L1
 // 29.0; in 3 with two chunks under way, which spills, 30.0.)
-constexpr int ctas_of(bool choose, int rules) { return choose && rules ? 3 : 4; }  // of an SM
-template <typename T, bool kChoose, int kRules>
-__global__ void __launch_bounds__(kLogitThreads, ctas_of(kChoose, kRules)) logits_kernel(const __grid_constant__ LogitArgs a) {
+//
+// kCtas of an SM at most.  With biases three of them leave 80 registers, which spills; where two are enough for all of the work, they are faster
+// (64 rows of 128256, all rules: 28.5 us, two 21.6; 512 rows 90, two 92; 200 rows 47, two 56).
+constexpr int ctas_of(bool choose, int rules) { return choose && rules ? 3 : 4; }
+template <typename T, bool kChoose, int kRules, int kCtas = ctas_of(kChoose, kRules)>
+__global__ void __launch_bounds__(kLogitThreads, kCtas) logits_kernel(const __grid_constant__ LogitArgs a) {
     constexpr int V = Vec<T>::N;  // tokens in 16 bytes
     constexpr int kParts = 8 / V, kAdds = kRules == 3 ? 3 : 2;
     // chunks under way in a thread, as many as registers hold (adjusting 294 bf16 rows of 151936, penalised and masked: 2 43.0 us, 3 41.0, 4 41.5; fp32 rows
     // 59.7, 61.5, 64.1; with biases 51.7, 51.8, 55.7)
-    constexpr int kAhead = kRules == 3 ? 1 : kRules == 2 ? 2 : kRules && !kChoose ? V == 8 ? 3 : 2 : V / 2;
+    constexpr int kAhead = kRules == 3 && kCtas > 2 ? 1 : kRules >= 2 ? 2 : kRules && !kChoose ? V == 8 ? 3 : 2 : V / 2;
     extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ int s_request, s_rows[2], s_n, s_scan[kLogitWarps];
     __shared__ float s_m[kLogitWarps], s_s[kLogitWarps];
@@ -664,7 +667,7 @@ constexpr int kMostShared = 180 * 1024;  // (a slice of 32832 tokens, all of the
 
 template <typename T>
 int set_up() {
-    void (*const k[])(LogitArgs) = {logits_kernel<T, true, 0>, logits_kernel<T, true, 1>, logits_kernel<T, true, 2>, logits_kernel<T, true, 3>, logits_kernel<T, false, 1>, logits_kernel<T, false, 2>,
+    void (*const k[])(LogitArgs) = {logits_kernel<T, true, 0>, logits_kernel<T, true, 1>, logits_kernel<T, true, 2>, logits_kernel<T, true, 3>, logits_kernel<T, true, 2, 2>, logits_kernel<T, true, 3, 2>, logits_kernel<T, false, 1>, logits_kernel<T, false, 2>,
                                       logits_kernel<T, false, 3>};
     cudaError_t e = cudaSuccess;
     for (auto f : k)
@@ -673,7 +676,8 @@ int set_up() {
 }
 
 template <typename T>
-cudaError_t start(const cudaLaunchConfig_t& cfg, const LogitArgs& a, bool choose, int rules) {
+cudaError_t start(const cudaLaunchConfig_t& cfg, const LogitArgs& a, bool choose, int rules, int ctas) {
+    if (choose && ctas == 2) return cudaLaunchKernelEx(&cfg, rules == 3 ? logits_kernel<T, true, 3, 2> : logits_kernel<T, true, 2, 2>, a);
     if (!choose) return cudaLaunchKernelEx(&cfg, rules == 3 ? logits_kernel<T, false, 3> : rules == 2 ? logits_kernel<T, false, 2> : logits_kernel<T, false, 1>, a);
     return cudaLaunchKernelEx(&cfg, rules == 3 ? logits_kernel<T, true, 3> : rules == 2 ? logits_kernel<T, true, 2> : rules ? logits_kernel<T, true, 1> : logits_kernel<T, true, 0>, a);
 }
@@ -743,22 +747,24 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     // (chunks start on 16 bytes of the logits: those of the biases too in every row and set, or not)
     const size_t size = dtype == SSD_F32 ? 4 : 2;
     const bool even = ((uintptr_t)r.bias & 15u) == 0 && r.bias_stride % 4 == 0 && (uintptr_t)a.logits % (4 * size) == 0 && a.stride % 4 == 0;
-    const int rules = r.bias ? even ? 2 : 3 : a.counted || r.allowed ? 1 : 0, slots = sms * ctas_of(choose, rules);
+    const int rules = r.bias ? even ? 2 : 3 : a.counted || r.allowed ? 1 : 0;
     // A row's slices: 1 to 8, whichever is done first if a wave of CTAs takes as long as its slice and 20000 tokens more for its start
     // and end, or 30000 with counts to make.  (512 rows of 128256, penalised and masked: whole 68 us, in two 70, in four 94; 207
     // rows of 50257, penalised and with biases: whole 39, in two 29, in four 44.)
-    int best = 0;
+    // With biases two CTAs an SM are taken to need three quarters of the time of three.
+    int split = 0, ctas = 0;
     long long least = 0;
-    for (int split = 1; split <= kMaxSplit; split *= 2) {
-        a.slice = ((r.vocab + 7 + split - 1) / split + 63) / 64 * 64;
-        if (a.slice > (choose && r.allowed ? kMaxListed : kMaxSlice) || (split > 1 && a.slice < 1024)) continue;
-        const size_t bytes = lay_out(a);
-        if (bytes > kMostShared) continue;
-        const int fit = (int)std::min<size_t>(slots / sms, (222 * 1024) / (bytes + 4096));
-        const long long waves = ((long long)r.n_rows * split + sms * fit - 1) / (sms * fit), cost = waves * (a.slice + (a.counted ? 30000 : 20000));
-        if (!best || cost < least) best = split, least = cost;
-    }
-    const int split = best;
+    for (int n = ctas_of(choose, rules); n >= (choose && rules >= 2 ? 2 : ctas_of(choose, rules)); --n)
+        for (int parts = 1; parts <= kMaxSplit; parts *= 2) {
+            a.slice = ((r.vocab + 7 + parts - 1) / parts + 63) / 64 * 64;
+            if (a.slice > (choose && r.allowed ? kMaxListed : kMaxSlice) || (parts > 1 && a.slice < 1024)) continue;
+            const size_t bytes = lay_out(a);
+            if (bytes > kMostShared) continue;
+            const int fit = (int)std::min<size_t>(n, (222 * 1024) / (bytes + 4096));
+            const long long waves = ((long long)r.n_rows * parts + sms * fit - 1) / (sms * fit);
+            const long long cost = waves * (a.slice + (a.counted ? 30000 : 20000)) * (n == 2 ? 3 : 4);
+            if (!split || cost < least) split = parts, ctas = n, least = cost;
+        }
     a.slice = ((r.vocab + 7 + split - 1) / split + 63) / 64 * 64;
     // rows of a request share its counts, as many as leave two waves of CTAs
     a.rows = a.counted ? (int)std::min<long long>(r.max_rows, std::max(1ll, (long long)r.n_rows * split / 912)) : 1;
@@ -778,7 +784,7 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     attr[1].val.clusterDim.x = (unsigned)split, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = choose && split > 1 ? 2 : 1;
-    const cudaError_t e = dtype == SSD_F32 ? start<float>(cfg, a, choose, rules) : dtype == SSD_F16 ? start<f16>(cfg, a, choose, rules) : start<bf16>(cfg, a, choose, rules);
+    const cudaError_t e = dtype == SSD_F32 ? start<float>(cfg, a, choose, rules, ctas) : dtype == SSD_F16 ? start<f16>(cfg, a, choose, rules, ctas) : start<bf16>(cfg, a, choose, rules, ctas);
     return e == cudaSuccess ? SSD_OK : refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
 }
 
