@@ -163,8 +163,8 @@ typedef struct {
  * decoding or verification step: an expert that some row goes to is read once for up to 8, 16 or 32 of its rows, by how many go to one on average.
  * x, residual and out: [row][d] of the experts' dtype, 16-byte aligned, rows *_stride elements apart, multiples of 8; residual may be
  * NULL; out may be residual with its stride, and overlaps nothing else.  n_rows <= 1024, 1 <= k <= 16.
- * Sums in fp32, slots in order; silu(..) * (..) enters the product with down as a pair of values of the type (16 bits
- * of mantissa in bf16, 22 in fp16, where it is infinite beyond 65504).  The same inputs give the same bits.
+ * Sums in fp32, slots in order; silu(..) * (..) enters the product with down in all bits of fp32 (bf16), or off by 2^-22 of it and 2^-36 at most
+ * (fp16, where it is infinite beyond 65504).  The same inputs give the same bits.
  * A wait inside the call that has not ended after two seconds gives up (SSD_STATUS_TIMEOUT in `status`, which may be NULL): the call ends,
  * and without `status` no one can tell that its output is not valid.
  * workspace: ssd_moe_workspace() bytes, 16-byte aligned; its contents mean nothing between calls.

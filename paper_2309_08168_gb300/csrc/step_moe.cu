@@ -201,7 +201,7 @@ struct MoeArgs {
     const int32_t* ids;
     const float* weights;
     int64_t x_stride, residual_stride, out_stride;
-    void* h;   // [2][pair][f]: silu(gate x) * (up x) as hi + lo
+    void* h;   // [kPlanes][pair][f]: silu(gate x) * (up x) in values of the type
     float* y;  // [pair][part][d]: weights * down h over a part of f
     int n_rows, k, n_experts, d, f;
     int parts;  // of f, each summed by a unit of its own
@@ -221,6 +221,17 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// silu(..) * (..) goes to the second product as a sum of values of the type, each what the ones before leave of it: three of bf16, the 24 bits of
+// fp32, or two of fp16, the second times 2^11, which are off by 2^-22 of it or by 2^-36 (without the factor by 2^-25: nothing is left of small ones).
+template <typename T>
+constexpr int kPlanes = 2;
+template <>
+constexpr int kPlanes<bf16> = 3;
+template <typename T>
+constexpr float kRestScale = 1.f;
+template <>
+constexpr float kRestScale<f16> = 0x1p11f;
+
 __device__ __forceinline__ uint4 load_shared(uint32_t at) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
@@ -346,15 +357,18 @@ __device__ __forceinline__ Plan make_plan(const MoeArgs& a, int size, unsigned c
 // stage ahead is too late (64 rows, 8 an expert: 1215 us, copied 990).  The k that
 // a lane holds go to the matrix instruction in an order of their own, the same for both operands, so that every operand is 16 bytes
 // in a row; lane group g has row (g / 2) + 4 (g mod 2) of 8, so that the 8 lanes that shared memory serves at once meet
-// different banks.  Bound by HBM: two CTAs have 192 KB of weights under way on an SM.
+// different banks.  The matrix instructions cut off what is below their sum, so a stage's products are summed from 0, the smallest plane first, and added to the
+// sums before them with a rounding.  (With two planes of bf16 and one sum for all stages 26 of 24576 results of a layer of 4096 x 11008, two experts of 8, were
+// neighbours of the nearest value, now 4 are, and 4 of fp32 products; its one row took 102.9 us instead of 106.8, 64 rows of 5120 x 13824 1010
+// instead of 1063: with three planes the ring has three stages instead of four.)  Bound by HBM: two CTAs have 192 KB of weights under way on an SM.
 //
 // kUp: h = silu(gate x) * (up x); a tile of 16 weight rows is 8 of gate and the same 8 of up, so that both sums of an output are in
-// one lane.  Else y = weights * (down h), h as two planes.
+// one lane.  Else y = weights * (down h), h in kPlanes planes.
 template <typename T, int NT, bool kUp>
 struct Products {
     static constexpr int kTiles = NT == 1 ? 2 : 4, kWeightRows = 16 * kTiles;
     static constexpr int kBox = kWeightRows * 128, kStage = kStageK / 64 * kBox;  // 64 k of them; 16 or 32 KB
-    static constexpr int PL = kUp ? 1 : 2, kRows = kWeightRows / (kUp ? 2 : 1);   // output rows of a unit
+    static constexpr int PL = kUp ? 1 : kPlanes<T>, kRows = kWeightRows / (kUp ? 2 : 1);   // output rows of a unit
     static constexpr int kColumns = 8 * NT, kCtas = NT == 1 ? 2 : 1;              // of an SM
     static constexpr bool kCopied = NT > 1;                                       // columns
     static constexpr int kLoaders = kCopied ? 3 : 0, kThreads = kMoeSums + 32 + 32 * kLoaders;
@@ -481,7 +495,7 @@ struct Products {
         int u = blockIdx.x, stage = begin_of(u), end = end_of(u), slot = 0;
         unsigned phase = 0;
         int buffer = 0, turn = 0;
-        float acc[kTiles][NT][4] = {};
+        float acc[NT][kTiles][4] = {};
         // one stage: columns x, and those of the next one asked for; false after the last
         auto one = [&](uint4 (&x)[PL][NT], uint4 (&next)[PL][NT]) {
             load_columns(next);
@@ -498,18 +512,30 @@ struct Products {
 #pragma unroll
                         for (int t = 0; t < NT; ++t) x[l][t] = load_shared(columns + slot * kSlot + l * (kStageK / 64 * kColumnBox) + t * 1024);
                 }
+                auto multiply = [&](float (&sum)[kTiles][4], const uint4& v) {
 #pragma unroll
-                for (int l = 0; l < PL; ++l)
+                    for (int m = 0; m < kTiles; ++m) mma(sum[m], w[m][0].x, w[m][1].x, w[m][0].y, w[m][1].y, v.x, v.y, T());
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                    for (int m = 0; m < kTiles; ++m) mma(sum[m], w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w, v.z, v.w, T());
+                };
 #pragma unroll
-                        for (int m = 0; m < kTiles; ++m) mma(acc[m][t], w[m][0].x, w[m][1].x, w[m][0].y, w[m][1].y, x[l][t].x, x[l][t].y, T());
+                for (int t = 0; t < NT; ++t) {
+                    float sum[kTiles][4] = {};
 #pragma unroll
-                for (int l = 0; l < PL; ++l)
+                    for (int l = PL - 1; l >= 0; --l) {
+                        if (l + 1 < PL && kRestScale<T> != 1.f) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                            for (int m = 0; m < kTiles; ++m)
 #pragma unroll
-                        for (int m = 0; m < kTiles; ++m) mma(acc[m][t], w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w, x[l][t].z, x[l][t].w, T());
+                                for (int i = 0; i < 4; ++i) sum[m][i] *= 1.f / kRestScale<T>;
+                        }
+                        multiply(sum, x[l][t]);
+                    }
+#pragma unroll
+                    for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][m][i] += sum[m][i];
+                }
             }
             __syncwarp();
             if (lane == 0) arrive(empty + slot);
@@ -523,7 +549,7 @@ struct Products {
             for (int t = 0; t < NT; ++t) {
                 float4* red = s_red + buffer * kSums;
 #pragma unroll
-                for (int m = 0; m < kTiles; ++m) red[(warp * kTiles + m) * 32 + lane] = make_float4(acc[m][t][0], acc[m][t][1], acc[m][t][2], acc[m][t][3]);
+                for (int m = 0; m < kTiles; ++m) red[(warp * kTiles + m) * 32 + lane] = make_float4(acc[t][m][0], acc[t][m][1], acc[t][m][2], acc[t][m][3]);
                 sums_sync();
                 const int m = (warp + turn) % kMoeWarps;  // (tiles go to other warps from unit to unit)
                 if (m < kTiles) {
@@ -539,7 +565,7 @@ struct Products {
                 else buffer ^= 1;
                 turn += kTiles;
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i) acc[i][t][0] = acc[i][t][1] = acc[i][t][2] = acc[i][t][3] = 0.f;
+                for (int i = 0; i < kTiles; ++i) acc[t][i][0] = acc[t][i][1] = acc[t][i][2] = acc[t][i][3] = 0.f;
             }
             u += gridDim.x;
             if (u >= units) return false;
@@ -570,9 +596,13 @@ struct Products {
             for (int j = 0; j < 2; ++j)
                 if (row < rows && col + j * kNext < q.n) {
                     T* to = (T*)a.h + (int64_t)p.pairs[q.first + col + j * kNext] * a.f + row;
-                    const T hi = (T)h[j];
-                    to[0] = hi;
-                    to[plane] = isfinite((float)hi) ? (T)(h[j] - (float)hi) : (T)0.f;
+                    float left = h[j];
+#pragma unroll
+                    for (int l = 0; l < kPlanes<T>; ++l) {
+                        const T v = (T)left;
+                        to[l * plane] = v;
+                        left = isfinite((float)v) ? (left - (float)v) * kRestScale<T> : 0.f;
+                    }
                 }
         } else {
             const float y[2][2] = {{v.x, v.y}, {v.z, v.w}};
@@ -690,7 +720,7 @@ Workspace workspace_of(const ssd_moe& m, int n_rows, int k) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t pairs = (size_t)n_rows * k;
     Workspace w;
-    w.y = up(2 * 2 * pairs * m.f);
+    w.y = up(2 * (size_t)(m.dtype == SSD_BF16 ? kPlanes<bf16> : kPlanes<f16>) * pairs * m.f);
     w.total = w.y + up(4 * pairs * (size_t)parts_of(m, n_rows, k) * m.d);
     return w;
 }

@@ -1,0 +1,60 @@
+"""ssd_moe_route and ssd_moe_mlp on the GPU: how exact the activations are.  Plain numpy in 64 bits."""
+import numpy as np
+import pytest
+
+import test_gpu_step_moe as moe
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ssd():
+    import paper_2309_08168_gb300 as m
+    return m
+
+
+def differences(ssd, typ, n, scale, gain):
+    """The activations of expert 0's units 2i and 2i + 1 are nearly alike, and output i is gain times their difference: what is
+    lost of an activation on its way to the second product shows.  Returns (outputs, wanted ones, limits)."""
+    t, half, d, f = moe.TYPES[typ], moe.HALF[typ], 64, 128
+    g = torch.Generator().manual_seed(n)
+    a = (0.5 + 3.0 * torch.rand(d, generator=g)).to(t).double()
+    delta = (a * 2.0**-12 * torch.rand(d, generator=g).double()).to(t).double()
+    x, gate, up, down = torch.zeros(n, d), torch.zeros(1, f, d), torch.zeros(1, f, d), torch.zeros(1, d, f)
+    x[:, 0] = x[:, 1] = 2.0 ** -(torch.arange(n) % 2).float()
+    gate[0, 0::2, 0], gate[0, 1::2, 0], gate[0, 1::2, 1] = a.float(), a.float(), delta.float()
+    up[0, :, 0] = scale
+    i = torch.arange(d)
+    down[0, i, 2 * i], down[0, i, 2 * i + 1] = gain, -gain
+    dev = [v.to(t).cuda() for v in (x, gate, up, down)]
+    experts, out = ssd.MoeWeights(*dev[1:]), torch.empty(n, d, dtype=t, device="cuda")
+    ids, weights = torch.zeros(n, 1, dtype=torch.int32, device="cuda"), torch.ones(n, 1, device="cuda")
+    ws = torch.empty(ssd.ssd_moe_workspace(experts, n, 1), dtype=torch.uint8, device="cuda")
+    ssd.ssd_moe_mlp(experts, dev[0], ids, weights, out, ws, cuda_stream=moe.stream())
+    torch.cuda.synchronize()
+    c = x[:, :1].double().numpy()
+    h = [(lambda v: v / (1 + np.exp(-v)) * scale * c)(c * v.numpy()) for v in (a, a + delta)]
+    want = gain * (h[0] - h[1])
+    # an activation: products of few bits, exact; exp 2^-22 (two steps), 1 + exp, the division, the product with up and the weight 2^-24 each,
+    # its values of the type 2^-22, and two sums of the matrix instructions, which cut off, 2^-22 each
+    lim = 5 * 2.0**-22 * gain * (np.abs(h[0]) + np.abs(h[1])) + half * np.abs(want)
+    return moe.f64(out), want, lim
+
+
+@pytest.mark.parametrize("n", [1, 12, 40])
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_activations_keep_their_bits(ssd, typ, n):
+    got, want, lim = differences(ssd, typ, n, 1.0, 1.0)
+    assert (np.abs(got - want) <= lim + 2.0**-25).all(), (np.abs(got - want) / lim).max()
+
+
+@pytest.mark.parametrize("n", [1, 12, 40])
+@pytest.mark.parametrize("scale", [2.0**-12, 2.0**-16])
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_small_activations_keep_their_bits(ssd, typ, scale, n):
+    """Activations near and below the lowest normal number of fp16, brought back by large weights: off by 2^-36 where that is more than
+    2^-22 of them."""
+    gain = 2.0**12
+    got, want, lim = differences(ssd, typ, n, scale, gain)
+    assert (np.abs(got - want) <= lim + 2 * gain * 2.0**-36 + 2.0**-25).all(), (np.abs(got - want) / lim).max()
