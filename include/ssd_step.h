@@ -178,7 +178,7 @@ int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void* x, int64_
  * calls after it are not affected.  cta < 0 disarms. */
 void ssd_debug_moe_stall(int cta, double wait_limit_s);
 
-/* Bytes of workspace for this many rows and slots.  Errors: INVALID_ARG. */
+/* Bytes of workspace for this many rows and slots; never fewer than for fewer rows or slots.  Errors: INVALID_ARG. */
 int ssd_moe_workspace(const ssd_moe* experts, int n_rows, int k, size_t* bytes);
 
 #ifdef __cplusplus

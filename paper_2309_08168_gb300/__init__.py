@@ -635,7 +635,7 @@ def ssd_moe_route(x, w_router, ids, weights, score: int = SSD_MOE_SOFTMAX, favou
 
 
 def ssd_moe_workspace(experts: MoeWeights, n_rows: int, k: int) -> int:
-    """Bytes of workspace that ssd_moe_mlp wants for this many rows and slots."""
+    """Bytes of workspace that ssd_moe_mlp wants for this many rows and slots (never fewer than for fewer of them)."""
     n = ctypes.c_size_t()
     _check(lib.ssd_moe_workspace(experts.struct, n_rows, k, n))
     return n.value

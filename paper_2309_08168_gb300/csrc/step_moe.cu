@@ -706,11 +706,23 @@ double g_stall_wait_s = 0.0;
 size_t plan_bytes(int n_pairs, int n_experts, int size) { return 4 * ((size_t)max_groups(n_pairs, n_experts, size) + (size_t)n_pairs); }
 
 // parts of f: until there are units of down for two waves of CTAs and more (as many experts met as can be), four stages each at least
-int parts_of(const ssd_moe& m, int n_rows, int k) {
-    const int64_t tiles = (m.d + 31) / 32, met = std::min(m.n_experts, n_rows * k);
+constexpr int kMaxParts = 8, kDownUnits = 2000;
+int parts_of(const ssd_moe& m, int64_t pairs) {
+    const int64_t tiles = (m.d + 31) / 32, met = std::min<int64_t>(m.n_experts, pairs);
     int parts = 1;
-    while (parts < 8 && met * tiles * parts < 2000 && m.f >= 8 * kStageK * parts) parts *= 2;
+    while (parts < kMaxParts && met * tiles * parts < kDownUnits && m.f >= 8 * kStageK * parts) parts *= 2;
     return parts;
+}
+// The most that pairs * parts comes to for up to this many pairs.  (More pairs have fewer parts, so that few of them can need
+// more than many do; a workspace for the largest round is enough for all.)
+int64_t most_sums(const ssd_moe& m, int64_t pairs) {
+    const int64_t tiles = (m.d + 31) / 32;
+    int64_t most = pairs;
+    for (int parts = 2; parts <= kMaxParts && m.f >= 8 * kStageK * (parts / 2); parts *= 2) {
+        const int64_t met = (kDownUnits - 1) / (tiles * (parts / 2));  // as many experts at most have so many parts
+        most = std::max(most, parts * (m.n_experts <= met ? pairs : std::min(pairs, met)));
+    }
+    return most;
 }
 
 struct Workspace {
@@ -721,7 +733,7 @@ Workspace workspace_of(const ssd_moe& m, int n_rows, int k) {
     const size_t pairs = (size_t)n_rows * k;
     Workspace w;
     w.y = up(2 * (size_t)(m.dtype == SSD_BF16 ? kPlanes<bf16> : kPlanes<f16>) * pairs * m.f);
-    w.total = w.y + up(4 * pairs * (size_t)parts_of(m, n_rows, k) * m.d);
+    w.total = w.y + up(4 * (size_t)most_sums(m, (int64_t)pairs) * m.d);
     return w;
 }
 
@@ -787,7 +799,7 @@ int start_moe(const char* call, MoeArgs& a, const ssd_moe& m, void* stream) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString(e));
-    a.parts = parts_of(m, a.n_rows, a.k);
+    a.parts = parts_of(m, (int64_t)a.n_rows * a.k);
     // rows of an expert that its weights are read for at once: as many as it has on average, or all of a few
     const int64_t pairs = (int64_t)a.n_rows * a.k;
     if (a.n_rows <= 8 || pairs <= 4 * (int64_t)a.n_experts) return launch_moe<T, 1>(call, a, m, sms, stream);

@@ -1,4 +1,4 @@
-"""ssd_moe_route and ssd_moe_mlp on the GPU: how exact the activations are.  Plain numpy in 64 bits."""
+"""ssd_moe_route and ssd_moe_mlp on the GPU: how exact the activations are, and workspaces.  Plain numpy in 64 bits."""
 import numpy as np
 import pytest
 
@@ -58,3 +58,15 @@ def test_small_activations_keep_their_bits(ssd, typ, scale, n):
     gain = 2.0**12
     got, want, lim = differences(ssd, typ, n, scale, gain)
     assert (np.abs(got - want) <= lim + 2 * gain * 2.0**-36 + 2.0**-25).all(), (np.abs(got - want) / lim).max()
+
+
+def test_a_workspace_for_the_largest_round(ssd):
+    """Seven rows have their sums over f in two parts, eight in one: the buffer for eight does for seven, and nothing behind it is written."""
+    layers = [moe.Layer(ssd, 60, "bf16", n, 8192, 2048, 8, 1) for n in (8, 7)]
+    size = ssd.ssd_moe_workspace(layers[0].experts, 8, 1)
+    ws = torch.full((size + 4096,), 201, dtype=torch.uint8, device="cuda")
+    for x in layers:
+        x.ws = ws[:size]
+        x.run()
+        x.check([0, 6])
+    assert (ws[size:] == 201).all()
