@@ -165,8 +165,8 @@ typedef struct {
  * NULL; out may be residual with its stride, and overlaps nothing else.  n_rows <= 1024, 1 <= k <= 16.
  * Sums in fp32, slots in order; silu(..) * (..) enters the product with down in all bits of fp32 (bf16), or off by 2^-22 of it and 2^-36 at most
  * (fp16, where it is infinite beyond 65504).  The same inputs give the same bits.
- * A wait inside the call that has not ended after two seconds gives up (SSD_STATUS_TIMEOUT in `status`, which may be NULL): the call ends,
- * and without `status` no one can tell that its output is not valid.
+ * A wait inside the call that has not ended after two seconds gives up: the call ends with SSD_STATUS_TIMEOUT in `status` (which may be NULL),
+ * and results that miss something are NaN.
  * workspace: ssd_moe_workspace() bytes, 16-byte aligned; its contents mean nothing between calls.
  * Errors: INVALID_ARG, CAPACITY (workspace too small), CUDA. */
 int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void* x, int64_t x_stride, const int32_t* ids,
@@ -174,7 +174,7 @@ int ssd_moe_mlp(const ssd_moe* experts, int n_rows, int k, const void* x, int64_
                 void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream);
 
 /* Test hook for the bounded waits of ssd_moe_mlp: in the next call of the process CTA `cta` never asks for its weights, and waits give
- * up after wait_limit_s (0 < wait_limit_s <= 10; else 2 s).  The call ends with SSD_STATUS_TIMEOUT, its output is not valid, and the
+ * up after wait_limit_s (0 < wait_limit_s <= 10; else 2 s).  The call ends with SSD_STATUS_TIMEOUT, the rows that the CTA had a part in are NaN, and the
  * calls after it are not affected.  cta < 0 disarms. */
 void ssd_debug_moe_stall(int cta, double wait_limit_s);
 

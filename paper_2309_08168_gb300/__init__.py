@@ -643,7 +643,7 @@ def ssd_moe_workspace(experts: MoeWeights, n_rows: int, k: int) -> int:
 
 def ssd_moe_mlp(experts: MoeWeights, x, ids, weights, out, workspace, residual=None, status=None, cuda_stream: int | None = None) -> None:
     """out [n][d] = residual + the rows x [n][d] through their experts ids int32 [n][k], by weights fp32 [n][k].
-    workspace: a contiguous uint8 tensor.  A wait that gave up is told by status int32 [1] alone, set to 0 before."""
+    workspace: a contiguous uint8 tensor.  A wait that gave up leaves NaN in out; status int32 [1], set to 0 before, tells the reason."""
     if x.dim() != 2 or ids.dim() != 2:
         _refuse("x [row][d] and ids [row][k] are wanted")
     n, k, d, t = x.shape[0], ids.shape[1], experts.device, experts.dtype

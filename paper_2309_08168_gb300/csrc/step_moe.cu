@@ -359,8 +359,8 @@ __device__ __forceinline__ Plan make_plan(const MoeArgs& a, int size, unsigned c
 // in a row; lane group g has row (g / 2) + 4 (g mod 2) of 8, so that the 8 lanes that shared memory serves at once meet
 // different banks.  The matrix instructions cut off what is below their sum, so a stage's products are summed from 0, the smallest plane first, and added to the
 // sums before them with a rounding.  (With two planes of bf16 and one sum for all stages 26 of 24576 results of a layer of 4096 x 11008, two experts of 8, were
-// neighbours of the nearest value, now 4 are, and 4 of fp32 products; its one row took 102.9 us instead of 106.8, 64 rows of 5120 x 13824 1010
-// instead of 1063: with three planes the ring has three stages instead of four.)  Bound by HBM: two CTAs have 192 KB of weights under way on an SM.
+// neighbours of the nearest value, now 4 are, and 4 of fp32 products; its one row took 102.9 us instead of 106.5, 64 rows of 5120 x 13824 1010
+// instead of 1065, with rings of their own for weights and columns, four and three stages, 1074.)  Bound by HBM: two CTAs have 192 KB of weights under way on an SM.
 //
 // kUp: h = silu(gate x) * (up x); a tile of 16 weight rows is 8 of gate and the same 8 of up, so that both sums of an output are in
 // one lane.  Else y = weights * (down h), h in kPlanes planes.
@@ -545,11 +545,12 @@ struct Products {
             // so that the warps that do not add go on (what they write next is read by then: there is a barrier in between).
             const int part = u % parts, rest = u / parts, row0 = rest % tiles * kRows;
             const Group q = p[rest / tiles];
+            const float lost = ok ? 0.f : __int_as_float(0x7fffffff);  // (what misses something is NaN, so that it is seen without `status`, too)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 float4* red = s_red + buffer * kSums;
 #pragma unroll
-                for (int m = 0; m < kTiles; ++m) red[(warp * kTiles + m) * 32 + lane] = make_float4(acc[t][m][0], acc[t][m][1], acc[t][m][2], acc[t][m][3]);
+                for (int m = 0; m < kTiles; ++m) red[(warp * kTiles + m) * 32 + lane] = make_float4(acc[t][m][0] + lost, acc[t][m][1] + lost, acc[t][m][2] + lost, acc[t][m][3] + lost);
                 sums_sync();
                 const int m = (warp + turn) % kMoeWarps;  // (tiles go to other warps from unit to unit)
                 if (m < kTiles) {

@@ -70,3 +70,19 @@ def test_a_workspace_for_the_largest_round(ssd):
         x.run()
         x.check([0, 6])
     assert (ws[size:] == 201).all()
+
+
+@pytest.mark.parametrize("n,k,e", [(5, 3, 6), (20, 2, 4), (70, 1, 2)])
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_a_wait_that_gives_up_leaves_nan(ssd, typ, n, k, e):
+    """Without `status` too: a row is NaN where it misses something, or right; and the call after it is right."""
+    x = moe.Layer(ssd, 12, typ, n, 512, 264, e, k)
+    ssd.ssd_debug_moe_stall(1, 0.01)
+    x.run()
+    torch.cuda.synchronize()
+    bad = torch.isnan(x.out[:, :512])
+    rows = bad.any(1)
+    assert rows.any() and torch.equal(bad.all(1), rows)  # (the second product's sums run over all that the first missed)
+    x.check([r for r in range(n) if not rows[r]])
+    x.run()
+    x.check(range(0, n, 7))
