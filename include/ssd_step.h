@@ -142,7 +142,9 @@ typedef enum { SSD_MOE_SOFTMAX = 0, SSD_MOE_SIGMOID = 1 } ssd_moe_score;
  * lowest first:  ids[row][j] = e,  weights[row][j] = scale p  (renorm = 1: divided by the sum of the row's k p's).
  * x: [row][d], rows x_stride elements apart, and w_router [n_experts][d], of dtype SSD_F16 or SSD_BF16, 16-byte aligned, d and
  * x_stride multiples of 8.  1 <= k <= 16, k <= n_experts <= 1024; d <= 65536.  Products are summed to about 48 bits and scored in fp64: two experts come in their exact
- * order unless their sums are within some 1e-11 of the sum of their products' absolute values.  NaN counts as the lowest score.
+ * order unless their sums are within some 1e-11 of the sum of their products' absolute values.  An expert whose score is NaN comes after all others; one
+ * whose product is NaN has no part in the sums, and weight NaN where it is among the k all the same.  +inf takes all of the softmax, shared with others of +inf.
+ * Without favour the order is that of the products.
  * Errors: INVALID_ARG, CUDA. */
 int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k, const void* x, int64_t x_stride, const void* w_router,
                   const float* favour, int score, int renorm, float scale, int32_t* ids, float* weights, void* cuda_stream);

@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kRouteThreads, 2) route_kernel(const __grid_co
         s_z[e] = isfinite(v.x) ? (double)v.x + (double)v.y : (double)v.x;
     }
     __syncthreads();
-    // softmax over all experts where the scores or the weights need it: the row's maximum and sum
+    // softmax over all experts where the scores or the weights need it: the row's maximum and sum (without NaN; of +inf each has the same share)
     const bool whole = a.score == SSD_MOE_SOFTMAX && (a.favour || !a.renorm);
     if (whole) {
         cluster_sync();  // (every CTA has started)
@@ -118,9 +118,10 @@ __global__ void __launch_bounds__(kRouteThreads, 2) route_kernel(const __grid_co
         cluster_sync();
         m = -INFINITY;
         for (int i = 0; i < split; ++i) m = fmax(m, __longlong_as_double((long long)s_stat[i]));
+        auto above = [&](double z) { return z == m ? 1.0 : exp(z - m); };
         double sum = 0.0;
         if (warp == 0) {
-            for (int e = lane; e < mine; e += 32) sum += exp(s_z[e] - m);
+            for (int e = lane; e < mine; e += 32) sum += s_z[e] == s_z[e] ? above(s_z[e]) : 0.0;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         }
@@ -130,9 +131,9 @@ __global__ void __launch_bounds__(kRouteThreads, 2) route_kernel(const __grid_co
         sum = 0.0;
         for (int i = 0; i < split; ++i) sum += __longlong_as_double((long long)s_stat[i]);
         for (int e = tid; e < mine; e += kRouteThreads) {
-            const double p = exp(s_z[e] - m) / sum;
+            const double p = above(s_z[e]) / sum;
+            s_key[e] = order_of(a.favour ? p + (double)__ldcg(a.favour + e0 + e) : s_z[e]);
             s_z[e] = p;  // (from here on the score)
-            s_key[e] = order_of(a.favour ? p + (double)__ldcg(a.favour + e0 + e) : p);
         }
     } else {
         for (int e = tid; e < mine; e += kRouteThreads) {
@@ -176,10 +177,10 @@ __global__ void __launch_bounds__(kRouteThreads, 2) route_kernel(const __grid_co
         const float shift = a.renorm ? fminf(lead, 0.f) : 0.f;
         p = (v > 0.0 ? 1.f : exp_of(v - (double)shift)) / (1.f + exp_of(-fabs(v)));
     } else {
-        p = exp_of(v - s_top[0]);
+        p = v == s_top[0] ? 1.f : exp_of(v - s_top[0]);
     }
     if (lane >= a.k) p = 0.f;
-    if (a.renorm) p /= warp_sum(p);
+    if (a.renorm) p /= warp_sum(p == p ? p : 0.f);
     if (lane < a.k) {
         a.ids[(int64_t)row * a.k + lane] = (int)s_who[lane];
         a.weights[(int64_t)row * a.k + lane] = p * a.scale;

@@ -1,4 +1,4 @@
-"""ssd_moe_route and ssd_moe_mlp on the GPU: how exact the activations are, and workspaces.  Plain numpy in 64 bits."""
+"""ssd_moe_route and ssd_moe_mlp on the GPU: how exact the activations are, workspaces, waits that give up, NaN and infinities.  Plain numpy in 64 bits."""
 import numpy as np
 import pytest
 
@@ -86,3 +86,44 @@ def test_a_wait_that_gives_up_leaves_nan(ssd, typ, n, k, e):
     x.check([r for r in range(n) if not rows[r]])
     x.run()
     x.check(range(0, n, 7))
+
+
+def routed(z, k, favour, sigmoid, renorm):
+    """(ids, weights) of one row's products z: NaN comes last and has no part in sums, +inf takes all of a softmax."""
+    with np.errstate(all="ignore"):
+        if sigmoid:
+            p = 1.0 / (1.0 + np.exp(-z))
+        else:
+            p = np.where(z == np.nanmax(z), 1.0, np.exp(z - np.nanmax(z)))
+            p = p / np.nansum(p)
+        score = z if favour is None else p + favour  # (without favour the order of p is that of z)
+        ids = sorted(range(len(z)), key=lambda e: (bool(np.isnan(score[e])), -score[e] if score[e] == score[e] else 0.0, e))[:k]
+        q = p[ids]
+        return ids, q / np.nansum(q) if renorm else q
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("favour", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("k,e", [(1, 9), (3, 9), (8, 9), (9, 9), (4, 300)])
+def test_route_has_one_rule_for_nan_and_infinities(ssd, typ, score, favour, renorm, k, e):
+    nan, inf = float("nan"), float("inf")
+    head = [[0.5, nan, -1.5, 2.0, -0.25, 1.0, 0.5, nan, -2.0],       # NaN among ordinary products
+            [0.5, inf, -1.5, 2.0, -0.25, inf, 0.5, nan, -inf],       # both infinities
+            [-inf, -1.0, nan, -inf, 0.75, 3.0, -0.5, 0.0, 1.0],
+            [nan, nan, nan, nan, nan, nan, nan, 1.0, nan]]           # one that is left
+    z = torch.full((len(head), e), -6.0)
+    z[:, :9] = torch.tensor(head)
+    x, w = torch.zeros(len(head), 8 * len(head)), torch.zeros(len(head), e, 8 * len(head))
+    f = torch.arange(e).float() % 7 / 16 if favour else None
+    for r in range(len(head)):
+        x[r, 8 * r] = 1.0
+        w[r, :, 8 * r] = z[r]
+        ids, weights = torch.full((1, k), -7, dtype=torch.int32, device="cuda"), torch.zeros(1, k, device="cuda")
+        ssd.ssd_moe_route(x[r:r + 1].to(moe.TYPES[typ]).cuda(), w[r].to(moe.TYPES[typ]).cuda(), ids, weights, score=score, favour=None if f is None else f.cuda(), renorm=renorm,
+                          cuda_stream=moe.stream())
+        torch.cuda.synchronize()
+        want, p = routed(z[r].double().numpy(), k, None if f is None else f.double().numpy(), score == 1, renorm)
+        assert ids[0].tolist() == want, r
+        np.testing.assert_allclose(moe.f64(weights)[0], p, rtol=16 * 2.0**-24, atol=2.0**-140, equal_nan=True)
