@@ -256,6 +256,9 @@ extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rop
         (q_out != q && meet(q_out, row_bytes * n_heads * hd, q, row_bytes * n_heads * hd)))
         return refuse_arg(call, "q_out must be q with its stride or overlap no input");
     if (int rc = check_device(call, cache->k)) return rc;
+    if (int rc = set_up_once<heads_kernel<float, f16, 64>, heads_kernel<f16, f16, 64>, heads_kernel<bf16, bf16, 64>, heads_kernel<float, f16, 128>, heads_kernel<f16, f16, 128>,
+                             heads_kernel<bf16, bf16, 128>>(call))
+        return rc;
     a.q = q;
     a.k = k;
     a.v = v;

@@ -733,12 +733,14 @@ int launch_logits(const char* call, LogitArgs& a, int dtype, bool choose, void* 
     if (int rc = device_of(call, &dev)) return rc;
     {
         static std::mutex mu;
-        static bool ready[kMaxDevices][3] = {};
+        static bool ready[kMaxDevices] = {};
         std::lock_guard<std::mutex> lock(mu);
-        if (!ready[dev][dtype]) {
-            const int e = dtype == SSD_F32 ? set_up<float>() : dtype == SSD_F16 ? set_up<f16>() : set_up<bf16>();
+        if (!ready[dev]) {  // (for all types, so that a first use with one of them prepares captures with any)
+            int e = set_up<float>();
+            if (!e) e = set_up<f16>();
+            if (!e) e = set_up<bf16>();
             if (e) return refuse(SSD_ERR_CUDA, call, "%s", cudaGetErrorString((cudaError_t)e));
-            ready[dev][dtype] = true;
+            ready[dev] = true;
         }
     }
     a.counted = (r.repetition || r.presence || r.frequency) && (r.history || r.tokens);

@@ -761,27 +761,41 @@ int encode(const char* call, CUtensorMap* m, const void* base, int dtype, int wi
     return r == CUDA_SUCCESS ? SSD_OK : refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
+// all kernels of the call, so that a first use with one row prepares captures with any
+template <typename T, int NT>
+cudaError_t set_up_moe() {
+    const cudaError_t e = cudaFuncSetAttribute(moe_up_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    return e == cudaSuccess ? cudaFuncSetAttribute(moe_down_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) : e;
+}
+template <typename T>
+cudaError_t set_up_moe() {
+    cudaError_t e = set_up_moe<T, 1>();
+    if (e == cudaSuccess) e = set_up_moe<T, 2>();
+    if (e == cudaSuccess) e = set_up_moe<T, 4>();
+    return e == cudaSuccess ? loaded({(const void*)moe_sum_kernel<T>}) : e;
+}
+int set_up_moe(const char* call) {
+    static bool ready[kMaxDevices] = {};
+    int dev = 0;
+    if (int rc = device_of(call, &dev)) return rc;
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (ready[dev]) return SSD_OK;
+    cudaError_t e = set_up_moe<f16>();
+    if (e == cudaSuccess) e = set_up_moe<bf16>();
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "set-up: %s", cudaGetErrorString(e));
+    if (!fn || found != cudaDriverEntryPointSuccess) return refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled unavailable");
+    g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+    ready[dev] = true;
+    return SSD_OK;
+}
+
 template <typename T, int NT>
 int launch_moe(const char* call, MoeArgs& a, const ssd_moe& m, int sms, void* stream) {
     using U = Products<T, NT, true>;
     using D = Products<T, NT, false>;
-    int dev = 0;
-    if (int rc = device_of(call, &dev)) return rc;
-    {
-        static bool ready[kMaxDevices] = {};
-        std::lock_guard<std::mutex> lock(g_mu);
-        if (!ready[dev]) {
-            cudaError_t e = cudaFuncSetAttribute(moe_up_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(moe_down_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-            void* fn = nullptr;
-            cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
-            if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-            if (e != cudaSuccess) return refuse(SSD_ERR_CUDA, call, "set-up: %s", cudaGetErrorString(e));
-            if (!fn || found != cudaDriverEntryPointSuccess) return refuse(SSD_ERR_CUDA, call, "cuTensorMapEncodeTiled unavailable");
-            g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
-            ready[dev] = true;
-        }
-    }
     CUtensorMap gate, up, down;
     if (int rc = encode(call, &gate, m.gate, m.dtype, m.d, m.f, m.n_experts, m.gate_stride, U::kWeightRows / 2)) return rc;
     if (int rc = encode(call, &up, m.up, m.dtype, m.d, m.f, m.n_experts, m.up_stride, U::kWeightRows / 2)) return rc;
@@ -797,6 +811,7 @@ int launch_moe(const char* call, MoeArgs& a, const ssd_moe& m, int sms, void* st
 
 template <typename T>
 int start_moe(const char* call, MoeArgs& a, const ssd_moe& m, void* stream) {
+    if (int rc = set_up_moe(call)) return rc;
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -840,6 +855,7 @@ extern "C" int ssd_moe_route(int dtype, int n_rows, int d, int n_experts, int k,
     const Range in[3] = {{x, span(n_rows, x_stride, d, dtype)}, {w_router, 2 * (size_t)n_experts * d}, {favour, 4 * (size_t)n_experts}};
     if (meet(i1, w1) || meet(i1, in) || meet(w1, in)) return refuse_arg(call, "ids and weights must overlap neither each other nor an input");
     if (int rc = check_device(call, x)) return rc;
+    if (int rc = set_up_once<route_kernel<f16>, route_kernel<bf16>>(call)) return rc;
     RouteArgs a{};
     a.x = x;
     a.w = w_router;

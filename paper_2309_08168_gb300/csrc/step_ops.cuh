@@ -2,6 +2,7 @@
 #pragma once
 
 #include <initializer_list>
+#include <mutex>
 
 #include "ssd_step.h"
 #include "tree_ops.cuh"
@@ -45,6 +46,28 @@ inline int device_of(const char* call, int* dev) {
         (void)cudaGetLastError();
         return refuse(SSD_ERR_CUDA, call, "no usable current device");
     }
+    return SSD_OK;
+}
+
+// Loads kernels that need no other set-up.  (Left to a first launch, it may come inside a stream capture.)
+inline cudaError_t loaded(std::initializer_list<const void*> kernels) {
+    cudaFuncAttributes at;
+    cudaError_t e = cudaSuccess;
+    for (const void* k : kernels)
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, k);
+    return e;
+}
+// ... once a device
+template <auto... kKernels>
+inline int set_up_once(const char* call) {
+    static std::mutex mu;
+    static bool ready[kMaxDevices] = {};
+    int dev = 0;
+    if (int rc = device_of(call, &dev)) return rc;
+    std::lock_guard<std::mutex> lock(mu);
+    if (ready[dev]) return SSD_OK;
+    if (const cudaError_t e = loaded({(const void*)kKernels...})) return refuse(SSD_ERR_CUDA, call, "set-up: %s", cudaGetErrorString(e));
+    ready[dev] = true;
     return SSD_OK;
 }
 
