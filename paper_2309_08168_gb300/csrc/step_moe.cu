@@ -361,7 +361,7 @@ __device__ __forceinline__ Plan make_plan(const MoeArgs& a, int size, unsigned c
 // different banks.  The matrix instructions cut off what is below their sum, so a stage's products are summed from 0, the smallest plane first, and added to the
 // sums before them with a rounding.  (With two planes of bf16 and one sum for all stages 26 of 24576 results of a layer of 4096 x 11008, two experts of 8, were
 // neighbours of the nearest value, now 4 are, and 4 of fp32 products; its one row took 102.9 us instead of 106.5, 64 rows of 5120 x 13824 1010
-// instead of 1065, with rings of their own for weights and columns, four and three stages, 1074.)  Bound by HBM: two CTAs have 192 KB of weights under way on an SM.
+// instead of 1065, with rings of their own for weights and columns, four and three stages, 1074.)  Bound by HBM: two CTAs have 160 KB of weights under way on an SM.
 //
 // kUp: h = silu(gate x) * (up x); a tile of 16 weight rows is 8 of gate and the same 8 of up, so that both sums of an output are in
 // one lane.  Else y = weights * (down h), h in kPlanes planes.
@@ -749,7 +749,9 @@ int check_experts(const char* call, const ssd_moe* m, int n_rows, int k) {
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
-constexpr int kMostShared = 209 * 1024;  // dynamic; 17 KB are static
+// dynamic shared memory of a CTA, and of one of two on an SM (of 228 KB each has 17 KB static and 1 KB for the system.  With
+// more of it for the pairs of 512 rows, 8 of 1024 experts, one CTA an SM had to end before the next began)
+constexpr int kMostShared = 209 * 1024, kMostOfTwo = 96 * 1024;
 
 // the experts' matrices [expert][rows][width] as {width, rows, experts}, box 64 x box_rows
 int encode(const char* call, CUtensorMap* m, const void* base, int dtype, int width, int rows, int n_experts, int64_t stride, int box_rows) {
@@ -801,8 +803,9 @@ int launch_moe(const char* call, MoeArgs& a, const ssd_moe& m, int sms, void* st
     if (int rc = encode(call, &up, m.up, m.dtype, m.d, m.f, m.n_experts, m.up_stride, U::kWeightRows / 2)) return rc;
     if (int rc = encode(call, &down, m.down, m.dtype, m.f, m.d, m.n_experts, m.down_stride, D::kWeightRows)) return rc;
     const int more = 1024 + (int)plan_bytes(a.n_rows * a.k, a.n_experts, 8 * NT);
-    a.up_depth = std::min((int)U::kDepth, (kMostShared - more) / U::kSlot);
-    a.down_depth = std::min((int)D::kDepth, (kMostShared - more) / D::kSlot);
+    constexpr int kRoom = U::kCtas == 2 ? kMostOfTwo : kMostShared;
+    a.up_depth = std::min((int)U::kDepth, (kRoom - more) / U::kSlot);
+    a.down_depth = std::min((int)D::kDepth, (kRoom - more) / D::kSlot);
     const dim3 grid((unsigned)(U::kCtas * sms));
     if (int rc = launch(call, moe_up_kernel<T, NT>, grid, U::kThreads, (size_t)(a.up_depth * U::kSlot + more), stream, a, gate, up)) return rc;
     if (int rc = launch(call, moe_down_kernel<T, NT>, grid, D::kThreads, (size_t)(a.down_depth * D::kSlot + more), stream, a, down)) return rc;

@@ -127,3 +127,11 @@ def test_route_has_one_rule_for_nan_and_infinities(ssd, typ, score, favour, reno
         want, p = routed(z[r].double().numpy(), k, None if f is None else f.double().numpy(), score == 1, renorm)
         assert ids[0].tolist() == want, r
         np.testing.assert_allclose(moe.f64(weights)[0], p, rtol=16 * 2.0**-24, atol=2.0**-140, equal_nan=True)
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_as_many_pairs_as_columns_in_registers_take(ssd, typ):
+    """512 rows, 8 of 1024 experts each: the longest lists of pairs that go with eight columns a group."""
+    x = moe.Layer(ssd, 61, typ, 512, 64, 520, 1024, 8)
+    x.run()
+    x.check([0, 1, 255, 511])
