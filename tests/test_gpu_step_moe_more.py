@@ -135,3 +135,12 @@ def test_as_many_pairs_as_columns_in_registers_take(ssd, typ):
     x = moe.Layer(ssd, 61, typ, 512, 64, 520, 1024, 8)
     x.run()
     x.check([0, 1, 255, 511])
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [20, 40, 100])
+def test_copied_columns_with_f_in_parts(ssd, typ, n):
+    """16 and 32 columns a group, and sums over f in two parts."""
+    x = moe.Layer(ssd, 62, typ, n, 64, 4104, 4, 2)
+    x.run()
+    x.check(range(0, n, 9))
