@@ -28,8 +28,8 @@ struct HeadArgs {
 // head, 16 bytes each, so that the sum of squares is a few shuffles and every byte is read once.
 // Rotated dim e with partner p becomes r (x_e g_e cos +- x_p g_p sin), r = 1 / sqrt(mean x^2 + eps): the
 // products of gains and angles are formed once a row in shared memory (a, b; pair p's by thread p, so that one barrier does), and the
-// partner's 16 bytes come from the lane that holds them.  Bound by HBM, for 16-bit rows of few heads by instructions, for few rows by the chain
-// position - angle - table - store.  Measured: 4095 fp32 rows of 32 + 2 x 32 heads of 128 60.7 us (335 MB, 5.5 TB/s, 82 % of the copy rate); 16000 fp16
+// partner's 16 bytes come from the lane that holds them.  Bound by HBM, for 16-bit rows of few heads by instructions (16000 fp16 rows: issue slots 73 %, then the table's
+// reads from shared memory), for few rows by the chain position - angle - table - store.  Measured: 4095 fp32 rows of 32 + 2 x 32 heads of 128 60.7 us (335 MB, 5.5 TB/s, 82 % of the copy rate); 16000 fp16
 // rows of 32 + 2 x 8 heads 84.4 us (394 MB, 4.7 TB/s); 403 fp16 rows 6.0; one row 2.8.  (Angles first, then each dim's products behind a second
 // barrier: 63.8, 90.0, 7.1, 3.5.  CTAs that stay for several rows, the next one's table and loads under way: 77, 106.)
 //
@@ -282,8 +282,8 @@ extern "C" int ssd_norm_rope_kv(const ssd_pages* cache, int layer, const ssd_rop
     a.n_pages = cache->n_pages;
     a.rope = *rope;
     // few rows: a row's heads over several CTAs, until there are four per SM.  Many rows of few heads: half as many threads each, since what
-    // a warp does once a row is half of its instructions (with a longer start of a row 16000 bf16 rows of 32 + 8 heads of 128 took 91 us, 128 threads 101;
-    // 4095 of 32 + 32 heads 42, 128 threads 41).
+    // a warp does once a row is half of its instructions (16000 bf16 rows of 32 + 8 heads of 128 84.5 us, 128 threads 96; 4095 of them 26.3,
+    // 128 threads 28.7; of 32 + 32 heads, with a longer start of a row, 42, 128 threads 41).
     const int per16 = dtype == SSD_F32 ? 4 : 8;
     const long long units = (long long)(n_heads + cache->n_kv_heads) * hd / per16;
     if (n_rows >= 2432 && units < 1024) return start<64>(call, a, dtype, 1, cuda_stream);

@@ -13,7 +13,7 @@ namespace step {
 
 constexpr int kLogitThreads = 256, kLogitWarps = kLogitThreads / 32;
 constexpr int kMaxVocab = 262144;
-constexpr int kMaxSlice = 131136;  // tokens of a CTA: at most 17 chunks of 8 in each of its threads
+constexpr int kMaxSlice = 131136;  // tokens of a CTA: at most 65 chunks of 8 in each of its threads
 constexpr int kFew = 8;            // a mask that leaves one token of so many is taken as a list
 constexpr int kMaxListed = 65472;  // tokens of a CTA whose places a list can hold in 16 bits
 constexpr int kMaxSplit = 8;      // CTAs of a row: one portable cluster

@@ -355,13 +355,14 @@ __device__ __forceinline__ Plan make_plan(const MoeArgs& a, int size, unsigned c
 // the units: while the 8 warps of a CTA join their sums, the next unit's weights are on their way.  A warp multiplies its 32 k of
 // a stage.  Columns (PL planes each): up to 8 come from L2 straight to a warp's registers, a stage ahead, over the units' ends
 // too; more of them (64 weight rows then, so that they are read half as often) are copied into the ring by three warps, since a
-// stage ahead is too late (64 rows, 8 an expert: 1215 us, copied 990).  The k that
+// stage ahead is too late (64 rows, 8 an expert, h in two planes: 1215 us, copied 990).  The k that
 // a lane holds go to the matrix instruction in an order of their own, the same for both operands, so that every operand is 16 bytes
 // in a row; lane group g has row (g / 2) + 4 (g mod 2) of 8, so that the 8 lanes that shared memory serves at once meet
 // different banks.  The matrix instructions cut off what is below their sum, so a stage's products are summed from 0, the smallest plane first, and added to the
 // sums before them with a rounding.  (With two planes of bf16 and one sum for all stages 26 of 24576 results of a layer of 4096 x 11008, two experts of 8, were
 // neighbours of the nearest value, now 4 are, and 4 of fp32 products; its one row took 102.9 us instead of 106.5, 64 rows of 5120 x 13824 1010
-// instead of 1065, with rings of their own for weights and columns, four and three stages, 1074.)  Bound by HBM: two CTAs have 160 KB of weights under way on an SM.
+// instead of 1065, with rings of their own for weights and columns, four and three stages, 1074; the third plane loaded and not
+// multiplied 103.4 and 1037.)  Bound by HBM: two CTAs have 160 KB of weights under way on an SM.
 //
 // kUp: h = silu(gate x) * (up x); a tile of 16 weight rows is 8 of gate and the same 8 of up, so that both sums of an output are in
 // one lane.  Else y = weights * (down h), h in kPlanes planes.
