@@ -141,8 +141,8 @@ int ssd_rope_init(int rot_dim, int interleaved, int scaling, double theta, doubl
  * [row][n_kv_heads][head_dim] to positions[row] >= 0; writes the queries to q_out
  * (which may be q; else it overlaps no input) and the keys and the values v [row][n_kv_heads][head_dim] to rows
  * slots[row] of the cache's layer.  A row whose slot is negative or outside the cache
- * leaves the cache alone.  Slots are distinct: of two rows with the same slot either may
- * stay, K and V and each head by itself.  Rows are q_stride, k_stride, v_stride and q_out_stride elements
+ * leaves the cache alone.  Slots are distinct: of rows with the same slot the last stays in calls
+ * of up to 129 rows; in larger ones any may, K and V and each head by itself.  Rows are q_stride, k_stride, v_stride and q_out_stride elements
  * apart (so q, k and v may be parts of one projection's output), heads
  * head_dim; pointers 16-byte aligned, strides multiples of 16 bytes.  rot_dim <= head_dim.
  * Angles are exact to 2^-24 of a turn at any position; sums in fp32, one rounding.

@@ -66,7 +66,7 @@ typedef struct {
 
 /* ssd_rope_kv (ssd_ops.h: its tensors, strides and slots) with norms before the rotation and
  * positions on several axes.  Without both it gives what ssd_rope_kv gives, up to the last place, and that call is the faster one but for
- * many rows of 16 bits (403 rows of 32 + 16 heads 4.2 against 6.5 us, 4095 of 32 + 64 52 against 57).
+ * many rows of 16 bits (403 rows of 32 + 16 heads 4.2 against 6.5 us, 4095 of 32 + 64 51 against 57).
  * norm = NULL: no norms.  axes = NULL: one axis.  positions: [n_axes][n_rows], any
  * int32.  Of two rows with the same slot either may stay, K and V and each head by itself.  Values are copied.  Angles are exact to 2^-24 of a turn at any position; squares, sums and products in
  * fp32, one rounding to the rows' and the cache's type.
